@@ -18,7 +18,7 @@
  *   - Every function returning int returns LPQ_OK (0) or an error code below; on
  *     error no output buffer has been written by the failing call and
  *     lpq_last_error() describes the failure.  No C++ exception crosses the ABI.
- *   - The library owns only its two opaque handle types.  A handle may be used from
+ *   - The library owns only its opaque handle types.  A handle may be used from
  *     one thread at a time.
  *   - Item ids are 0-based row numbers in the order the items were added.
  */
@@ -34,6 +34,7 @@ extern "C" {
 
 typedef struct lpq_quantizer lpq_quantizer;
 typedef struct lpq_index lpq_index;
+typedef struct lpq_kv lpq_kv;
 
 enum {
     LPQ_OK = 0,
@@ -229,6 +230,98 @@ int lpq_gather_dist_i8(const lpq_index *idx, const int8_t *qcodes_dev, int64_t n
 int lpq_rerank_f32(const float *x_dev, int64_t n, int64_t ldx, const float *q_dev, int64_t nq,
                    int64_t ldq, int d, const int32_t *cand_ids_dev, int kc, int k, int metric,
                    int32_t *ids_dev, float *dist_dev, void *stream);
+
+/* ------------------------------------------------------------- key-value cache ---- */
+
+/* The maximum-inner-product search a language model makes for every token it generates, over keys that
+ * grow by one per step: keys and values of the tokens so far, held as codes of Equation 1 in pages of a
+ * pool, and the attention that reads them.  One lpq_kv is the cache of one layer: `heads` key-value heads
+ * of D = d / heads features (feature h D + i of the quantizers is feature i of head h).
+ *
+ * Storage is the caller's device memory, 256-byte aligned, and must outlive the handle:
+ *   k_dev, v_dev  [pages][heads][page][row bytes] codes: one byte each, rows padded to 64, 128, 192 or 256
+ *                 features with code 0; packed: two 4-bit codes per byte as in lpq_index_create_packed
+ *                 (stored + 8, feature 2j in the low half of byte j, +8 stored as 7)
+ *   bounds_dev    [pages][heads][2][padded features] int8: the smallest and the largest key code of each feature
+ *                 over the page's tokens
+ * It need not be cleared.  A sequence's token at position p lies in row p % page of page table[p / page] of
+ * its row of a table (int32, device, ld_table apart, table_pages columns).  Every call checks table entries:
+ * one outside [0, pages) means that there is no page there (what would go there is dropped, what would be
+ * read there does not exist).  A position at or beyond table_pages * page has no page.
+ *
+ * A code c reads back as x^ = k + (c + 1/2) s with s = fl32(1 / m), each operation rounded to binary32 (a
+ * feature without a range reads back as k).  Types of rows and queries: */
+enum { LPQ_TYPE_F32 = 0, LPQ_TYPE_F16 = 1, LPQ_TYPE_BF16 = 2 };
+
+/* Bytes of k_dev and of v_dev (each) and of bounds_dev; *row_features receives the padded features of a row.
+ * Any output may be null.  head_dim 1..256; page 16, 32, 64, 128 or 256 tokens.
+ * LPQ_EINVAL: heads, head_dim or pages < 1, another page size; LPQ_ERANGE: head_dim > 256, pages >= 2^31. */
+int lpq_kv_storage_bytes(int heads, int head_dim, int page, int64_t pages, int packed, size_t *codes, size_t *bounds,
+                         int *row_features);
+
+/* The cache of the quantizers' constants (copied; both of the same d, a multiple of heads; packed: of at most
+ * 4 bits).  Synchronises the device.  Errors as above; LPQ_ESTATE: a quantizer without constants. */
+int lpq_kv_create(lpq_kv **out, const lpq_quantizer *keys, const lpq_quantizer *values, int heads, int page,
+                  int64_t pages, int packed, void *k_dev, void *v_dev, void *bounds_dev);
+void lpq_kv_destroy(lpq_kv *kv);
+
+/* Encodes n new rows of keys and values, k_dev / v_dev [n][heads][D] of `type` (strides in elements, the features
+ * of a head contiguous), and stores them: row starts_dev[b] + i goes to position first_dev[b] + i of sequence b
+ * (starts_dev int32 [nseq + 1], ascending from 0 to n; null: one row per sequence, n = nseq).  Rows at negative
+ * positions are dropped.  Bounds of the pages touched become those of their tokens up to the last one written,
+ * so that a sequence may be cut back and written on.  No page may be touched twice by one call.
+ * Asynchronous on stream.  n = 0 is a no-op.
+ * LPQ_EINVAL: null argument, n or nseq < 0, strides that overlap, unknown type, starts_dev null and n != nseq;
+ * LPQ_ERANGE: nseq * heads or table_pages * page too large. */
+int lpq_kv_write(const lpq_kv *kv, const void *k_dev, int64_t ldk_token, int64_t ldk_head, const void *v_dev,
+                 int64_t ldv_token, int64_t ldv_head, int type, int64_t n, int64_t nseq, const int32_t *first_dev,
+                 const int32_t *starts_dev, const int32_t *table_dev, int64_t ld_table, int64_t table_pages,
+                 void *stream);
+
+/* The way back: rows of the same numbering receive x^ of their position, rounded to `type`; positions without a
+ * page give zeros.  Errors as above. */
+int lpq_kv_read(const lpq_kv *kv, void *k_dev, int64_t ldk_token, int64_t ldk_head, void *v_dev, int64_t ldv_token,
+                int64_t ldv_head, int type, int64_t n, int64_t nseq, const int32_t *first_dev,
+                const int32_t *starts_dev, const int32_t *table_dev, int64_t ld_table, int64_t table_pages,
+                void *stream);
+
+/* Queries of the calls below: q_dev [nseq][new_tokens][q_heads][D] of `type`, strides in elements; q_heads a multiple
+ * of heads, query heads h G .. h G + G - 1 share key-value head h (G = q_heads / heads).  lengths_dev int32 [nseq]:
+ * tokens of each sequence, the new ones included: new token i sees positions <= length - new_tokens + i.
+ *
+ * Which pages can hold large inner products.  Over the R = new_tokens * G rows of a key-value head, in binary32:
+ * q' = q s, A = max |q'|, z = rint(q' * (127 / A)) (what is not finite counts as 0; A <= 1e-30: all 0);
+ *   score(page) = sum_i [ (sum_r max(z_ri, 0)) hi_i + (sum_r min(z_ri, 0)) lo_i ],
+ * an upper bound, summed over the rows, of the integer product with any token of the page.  pages_dev
+ * [nseq][heads][n_select] receives the numbers (columns of the table) of the first keep_first and the last keep_last of
+ * a sequence's pages and of those with the largest scores, ties to the lower number, ascending; -1 behind them where
+ * there are fewer.  Integers throughout: the result is unique.  Workspace: 256-byte aligned.
+ * LPQ_EINVAL: null argument, n_select < 1, keep_first or keep_last < 0 or more than n_select together, q_heads not a
+ * multiple of heads; LPQ_ERANGE: new_tokens * G > 128, workspace too small, sizes as above. */
+size_t lpq_kv_select_workspace_bytes(const lpq_kv *kv, int64_t nseq, int64_t table_pages);
+int lpq_kv_select(const lpq_kv *kv, const void *q_dev, int64_t ldq_seq, int64_t ldq_token, int64_t ldq_head, int type,
+                  int64_t nseq, int new_tokens, int q_heads, const int32_t *lengths_dev, const int32_t *table_dev,
+                  int64_t ld_table, int64_t table_pages, int n_select, int keep_first, int keep_last, int32_t *pages_dev,
+                  void *workspace_dev, size_t workspace_bytes, void *stream);
+
+/* Attention: out_dev (as q_dev, strides of its own) = sum_j p_j y^_j over the tokens j a row sees, p = softmax(scale
+ * q . x^_j), x^ and y^ keys and values as they read back.  chosen_dev null: all pages (n_select is not used); else
+ * int32 [nseq][heads][n_select] pages as lpq_kv_select gives them, in any order (an entry outside [0, table_pages) is
+ * none; a page named twice counts twice).  lse_dev: null, or float [nseq][new_tokens][q_heads], the logarithm of the sum of
+ * exp(scale q . x^_j), with which attention over other tokens can be joined.  A row that sees no token gives
+ * zeros and -inf; a row of queries that holds a NaN or an infinity gives NaN.  Scores are exact sums of a query rounded
+ * to 15 bits (float32: 22) of its largest q s; weights are rounded to fp16 (float32: to 22 bits); sums are in 32 bits.
+ * The order of all sums is fixed: equal calls give equal bits.
+ * The workspace (256-byte aligned) holds the parts a long sequence is split into.
+ * LPQ_EINVAL: null argument, new_tokens < 1, q_heads not a multiple of heads, strides that overlap, unknown type,
+ * n_select < 1 with chosen_dev, scale not finite; LPQ_ERANGE: workspace too small, sizes as above. */
+size_t lpq_kv_attend_workspace_bytes(const lpq_kv *kv, int64_t nseq, int new_tokens, int q_heads, int64_t table_pages,
+                                     int n_select);
+int lpq_kv_attend(const lpq_kv *kv, const void *q_dev, int64_t ldq_seq, int64_t ldq_token, int64_t ldq_head, int type,
+                  int64_t nseq, int new_tokens, int q_heads, float scale, const int32_t *lengths_dev,
+                  const int32_t *table_dev, int64_t ld_table, int64_t table_pages, const int32_t *chosen_dev,
+                  int n_select, void *out_dev, int64_t ldo_seq, int64_t ldo_token, int64_t ldo_head, float *lse_dev,
+                  void *workspace_dev, size_t workspace_bytes, void *stream);
 
 /* ---------------------------------------------------------------- diagnostics ---- */
 

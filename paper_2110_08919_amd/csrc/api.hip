@@ -26,6 +26,11 @@ static int fail(int code, const char *fmt, ...)
     return code;
 }
 
+int lpq::set_error(int code, const char *message)
+{
+    return fail(code, "%s", message);
+}
+
 #define HIP_TRY(expr)                                                                        \
     do {                                                                                     \
         hipError_t e_ = (expr);                                                              \
@@ -199,6 +204,12 @@ static QuantParams view(const float *params, int d, int bits)
     qp.k = params; qp.sb = params + d; qp.se = params + 2 * d; qp.m = params + 3 * d;
     qp.d = d; qp.bits = bits;
     return qp;
+}
+
+bool lpq::quantizer_constants(const lpq_quantizer *q, QuantParams *out)
+{
+    *out = view(q->params, q->d, q->bits);
+    return q->ready;
 }
 
 extern "C" void lpq_quantizer_destroy(lpq_quantizer *q)

@@ -1,0 +1,166 @@
+// Declarations shared by the key-value cache kernels (kv_cache.hip, kv_select.hip, kv_attend.hip) and their C entry
+// points (kv_api.hip).  gfx950 only.
+#pragma once
+
+#include "lpq_internal.h"
+
+namespace lpq {
+
+enum { KV_MAX_DIM = 256, KV_MIN_PAGE = 16, KV_MAX_PAGE = 256,
+       KV_MAX_SELECT_ROWS = 128,      // query rows per key-value head whose summed codes fit two 7-bit digits
+       KV_MAX_BLOCKS = 1 << 23 };     // workgroups of a launch: 256 threads each stay below 2^32
+
+// Constants of Equation 1 and the step s = 1 / m, five arrays of [heads][dpad] floats on the device.  Features without
+// a range (S_e <= S_b) and padding hold S_b = -inf, S_e = inf, m = s = 0: they encode to 0 and read back as k (padding: 0).
+struct KvConstants {
+    const float *k, *sb, *se, *m, *s;
+    int bits;
+};
+
+// One layer's cache.  Codes [pages][heads][page][row_bytes], bounds [pages][heads][2][dpad] (smallest, largest key code).
+struct KvView {
+    uint8_t *k, *v;
+    int8_t *bounds;
+    KvConstants key, value;
+    int64_t pages;
+    int heads, dim, dpad, page, page_shift;
+    bool packed;
+    __host__ __device__ int row_bytes() const { return packed ? dpad >> 1 : dpad; }
+};
+
+// Rows [n][heads][dim] of a model's type, strides in elements.
+struct KvRows {
+    void *p;
+    int64_t ld_token, ld_head;
+    int type;
+    bool vec;    // every run of 8 features that starts at a multiple of 8 is aligned to its load
+};
+
+// Which rows belong to which sequence and where their pages are.
+struct KvPlaces {
+    const int32_t *first, *starts;   // starts null: one row per sequence
+    const int32_t *table;
+    int64_t ld_table, n;
+    int nseq, table_pages;
+};
+
+struct KvQueries {
+    const void *p;
+    int64_t ld_seq, ld_token, ld_head;
+    int type, new_tokens, group;     // group: query heads per key-value head
+    bool vec;
+};
+
+hipError_t launch_kv_constants(const QuantParams &q, int heads, int dim, int dpad, float *out, hipStream_t st);
+hipError_t launch_kv_write(const KvView &kv, const KvRows &k, const KvRows &v, const KvPlaces &pl, hipStream_t st);
+hipError_t launch_kv_read(const KvView &kv, const KvRows &k, const KvRows &v, const KvPlaces &pl, hipStream_t st);
+
+struct KvSelect {
+    const int32_t *lengths, *table;
+    int64_t ld_table;
+    int nseq, table_pages, n_select, keep_first, keep_last;
+    int32_t *pages;                  // [nseq][heads][n_select]
+    int32_t *scores;                 // workspace [nseq][heads][table_pages]
+};
+hipError_t launch_kv_select(const KvView &kv, const KvQueries &q, const KvSelect &s, hipStream_t st);
+
+struct KvAttend {
+    const int32_t *lengths, *table;
+    int64_t ld_table;
+    int nseq, table_pages;
+    const int32_t *chosen;           // null: all pages; else [nseq][heads][n_select]
+    int n_select;
+    float scale;
+    void *out;
+    int64_t ldo_seq, ldo_token, ldo_head;
+    bool vec_out;
+    float *lse;                      // null or [nseq][new_tokens][heads * group]
+    float *part;                     // workspace of kv_attend_plan
+};
+// How a call is shared out: blocks of `rows` query rows, `splits` parts of a sequence at most.
+struct KvAttendPlan {
+    int row_tiles, rows, splits;     // row_tiles blocks of `rows` rows each cover the rows of a key-value head
+    size_t bytes;                    // of workspace
+};
+KvAttendPlan kv_attend_plan(const KvView &kv, int64_t nseq, int new_tokens, int group, int64_t tokens);
+hipError_t launch_kv_attend(const KvView &kv, const KvQueries &q, const KvAttend &a, const KvAttendPlan &plan, hipStream_t st);
+
+#if defined(__HIPCC__)
+// 8 consecutive features as floats; those at or past `left` are 0.
+__device__ __forceinline__ void kv_load8(const void *base, int type, int64_t at, int left, bool vec, float *v)
+{
+    if (type == LPQ_TYPE_F32) {
+        const float *p = static_cast<const float *>(base) + at;
+        if (vec && left >= 8) {
+            const float4 a = *reinterpret_cast<const float4 *>(p), b = *reinterpret_cast<const float4 *>(p + 4);
+            v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+            v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = e < left ? p[e] : 0.0f;
+        }
+        return;
+    }
+    const uint16_t *p = static_cast<const uint16_t *>(base) + at;
+    uint16_t h[8];
+    if (vec && left >= 8) {
+        const uint4 w = *reinterpret_cast<const uint4 *>(p);
+        __builtin_memcpy(h, &w, 16);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) h[e] = e < left ? p[e] : (uint16_t)0;
+    }
+    if (type == LPQ_TYPE_BF16) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = __builtin_bit_cast(float, (uint32_t)h[e] << 16);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = (float)__builtin_bit_cast(_Float16, h[e]);
+    }
+}
+
+// 16-bit image of v in a 16-bit type, rounded to nearest even.
+__device__ __forceinline__ uint16_t kv_to16(float v, int type)
+{
+    return type == LPQ_TYPE_BF16 ? __builtin_bit_cast(uint16_t, (__bf16)v) : __builtin_bit_cast(uint16_t, (_Float16)v);
+}
+
+// N (4 or 8) consecutive features out; those at or past `left` are not written.
+template <int N>
+__device__ __forceinline__ void kv_store(void *base, int type, int64_t at, int left, bool vec, const float *v)
+{
+    if (type == LPQ_TYPE_F32) {
+        float *p = static_cast<float *>(base) + at;
+        if (vec && left >= N) {
+#pragma unroll
+            for (int e = 0; e < N; e += 4) *reinterpret_cast<float4 *>(p + e) = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < N; ++e)
+                if (e < left) p[e] = v[e];
+        }
+        return;
+    }
+    uint16_t *p = static_cast<uint16_t *>(base) + at;
+    uint16_t h[N];
+#pragma unroll
+    for (int e = 0; e < N; ++e) h[e] = kv_to16(v[e], type);
+    if (vec && left >= N) {
+        if (N == 8) {
+            uint4 w;
+            __builtin_memcpy(&w, h, 16);
+            *reinterpret_cast<uint4 *>(p) = w;
+        } else {
+            uint2 w;
+            __builtin_memcpy(&w, h, 8);
+            *reinterpret_cast<uint2 *>(p) = w;
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+            if (e < left) p[e] = h[e];
+    }
+}
+#endif
+
+}  // namespace lpq

@@ -89,6 +89,11 @@ struct QuantParams {
     int d, bits;
 };
 
+// For entry points outside api.hip: the message of lpq_last_error (returns code), and the constants of a quantizer
+// (false: it has none yet; d and bits are set all the same).
+int set_error(int code, const char *message);
+bool quantizer_constants(const lpq_quantizer *q, QuantParams *out);
+
 // ---- quantizer kernels (quant_kernels.hip) ---------------------------------------
 // Calibration scratch layout is private to quant_kernels.hip; the API allocates
 // calib_scratch_bytes(d) bytes.

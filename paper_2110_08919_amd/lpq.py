@@ -79,6 +79,17 @@ def lib() -> C.CDLL:
             "lpq_probe_mfma_i8": (i32, [vp, C.c_size_t, i32, C.POINTER(C.c_double), vp]),
             "lpq_probe_scan_core": (i32, [vp, C.c_size_t, i32, C.POINTER(C.c_double), vp]),
             "lpq_probe_stream": (i32, [vp, C.c_size_t, i32, i32, C.POINTER(C.c_double), vp]),
+            "lpq_kv_storage_bytes": (i32, [i32, i32, i32, i64, i32, C.POINTER(C.c_size_t), C.POINTER(C.c_size_t), C.POINTER(i32)]),
+            "lpq_kv_create": (i32, [C.POINTER(vp), vp, vp, i32, i32, i64, i32, vp, vp, vp]),
+            "lpq_kv_destroy": (None, [vp]),
+            "lpq_kv_write": (i32, [vp, vp, i64, i64, vp, i64, i64, i32, i64, i64, vp, vp, vp, i64, i64, vp]),
+            "lpq_kv_read": (i32, [vp, vp, i64, i64, vp, i64, i64, i32, i64, i64, vp, vp, vp, i64, i64, vp]),
+            "lpq_kv_select_workspace_bytes": (C.c_size_t, [vp, i64, i64]),
+            "lpq_kv_select": (i32, [vp, vp, i64, i64, i64, i32, i64, i32, i32, vp, vp, i64, i64, i32, i32, i32, vp, vp,
+                                    C.c_size_t, vp]),
+            "lpq_kv_attend_workspace_bytes": (C.c_size_t, [vp, i64, i32, i32, i64, i32]),
+            "lpq_kv_attend": (i32, [vp, vp, i64, i64, i64, i32, i64, i32, i32, f32, vp, vp, i64, i64, vp, i32, vp, i64, i64,
+                                    i64, vp, vp, C.c_size_t, vp]),
             "lpq_last_error": (C.c_char_p, []),
         }
         for name, (res, args) in sig.items():
@@ -329,6 +340,127 @@ class Index:
 
 
 STATIC_WORKSPACE_BYTES = 64 << 20
+
+TYPE_F32, TYPE_F16, TYPE_BF16 = 0, 1, 2
+_TYPE = {torch.float32: TYPE_F32, torch.float16: TYPE_F16, torch.bfloat16: TYPE_BF16}
+
+
+def _dev_ints(t: torch.Tensor, n: int):
+    assert t.is_cuda and t.dtype == torch.int32 and t.is_contiguous() and t.dim() == 1 and t.numel() == n, \
+        f"need {n} contiguous int32 values on the device"
+    return t.data_ptr()
+
+
+class KVCache:
+    """lpq_kv_*: keys and values of one layer as codes in pages, and the attention that reads them.
+
+    The quantizers hold the constants of the heads' features one after the other (d = heads * features of a head).
+    Storage is three tensors of this object: `k` and `v` [pages, heads, page, row bytes] and the pages' bounds.
+    Which pages a sequence has is the caller's to say: `table` int32 [sequences, columns], page numbers in order of
+    position, -1 (or anything outside the pool) where there is none."""
+
+    def __init__(self, keys: Quantizer, values: Quantizer, heads: int, page: int, pages: int, packed: bool = False,
+                 device="cuda"):
+        assert heads >= 1 and keys.d % heads == 0, "d of the quantizers must be a multiple of heads"
+        row = C.c_int()
+        self.heads, self.dim, self.page, self.pages, self.packed = heads, keys.d // heads, page, pages, packed
+        _check(lib().lpq_kv_storage_bytes(heads, self.dim, page, pages, 1 if packed else 0, None, None, C.byref(row)))
+        shape = (pages, heads, page, row.value // 2 if packed else row.value)
+        kind = torch.uint8 if packed else torch.int8
+        self.k, self.v = (torch.zeros(shape, dtype=kind, device=device) for _ in range(2))
+        self._bounds = torch.zeros((pages, heads, 2, row.value), dtype=torch.int8, device=device)
+        if self.k.is_cuda:
+            torch.cuda.current_stream().synchronize()       # calls on any stream find it cleared
+        h = C.c_void_p()
+        _check(lib().lpq_kv_create(C.byref(h), keys._h, values._h, heads, page, pages, 1 if packed else 0, self.k.data_ptr(),
+                                   self.v.data_ptr(), self._bounds.data_ptr()))
+        self._h = h
+
+    def __del__(self):
+        if getattr(self, "_h", None) and _lib is not None:
+            _lib.lpq_kv_destroy(self._h)
+            self._h = None
+
+    @property
+    def bounds(self) -> torch.Tensor:
+        """int8 [pages, heads, 2, features]: smallest and largest key code of each page."""
+        return self._bounds[..., :self.dim]
+
+    def _table(self, table: torch.Tensor):
+        p, nseq, ld = _dev_matrix(table, torch.int32)
+        return nseq, (p, ld, table.shape[1])
+
+    def _rows(self, t: torch.Tensor, dtype, n: int):
+        assert t.is_cuda and t.dtype == dtype and t.shape == (n, self.heads, self.dim) and (t.stride(2) == 1 or self.dim == 1), \
+            f"need device rows [{n}, {self.heads}, {self.dim}] of {dtype}, features contiguous"
+        return t.data_ptr(), t.stride(0), t.stride(1)
+
+    def write(self, k: torch.Tensor, v: torch.Tensor, first: torch.Tensor, table: torch.Tensor, starts: torch.Tensor = None):
+        """New rows [n, heads, features] (float32, float16 or bfloat16): rows starts[b] .. starts[b + 1] go to positions
+        first[b] on of sequence b; without starts one row per sequence."""
+        nseq, tab = self._table(table)
+        n = k.shape[0]
+        _check(lib().lpq_kv_write(self._h, *self._rows(k, k.dtype, n), *self._rows(v, k.dtype, n), _TYPE[k.dtype], n, nseq,
+                                  _dev_ints(first, nseq), None if starts is None else _dev_ints(starts, nseq + 1), *tab,
+                                  _stream()))
+
+    def read(self, first: torch.Tensor, table: torch.Tensor, starts: torch.Tensor = None, rows: int = None,
+             dtype=torch.float32, out=None):
+        """Keys and values [rows, heads, features] as they read back, numbered as in write()."""
+        nseq, tab = self._table(table)
+        n = nseq if starts is None else rows
+        assert n is not None, "with starts, say how many rows"
+        k, v = out if out is not None else (
+            torch.empty((n, self.heads, self.dim), dtype=dtype, device=table.device),
+            torch.empty((n, self.heads, self.dim), dtype=dtype, device=table.device))
+        _check(lib().lpq_kv_read(self._h, *self._rows(k, k.dtype, n), *self._rows(v, k.dtype, n), _TYPE[k.dtype], n, nseq,
+                                 _dev_ints(first, nseq), None if starts is None else _dev_ints(starts, nseq + 1), *tab,
+                                 _stream()))
+        return k, v
+
+    def _queries(self, q: torch.Tensor, nseq: int):
+        assert q.is_cuda and q.dtype in _TYPE and q.dim() == 4 and q.shape[0] == nseq and q.shape[3] == self.dim and (
+            q.stride(3) == 1 or self.dim == 1), "need device queries [sequences, new tokens, query heads, features], features contiguous"
+        return q.data_ptr(), q.stride(0), q.stride(1), q.stride(2)
+
+    def select(self, q: torch.Tensor, lengths: torch.Tensor, table: torch.Tensor, n_select: int, keep_first: int = 0,
+               keep_last: int = 1, out: torch.Tensor = None, workspace: torch.Tensor = None) -> torch.Tensor:
+        """int32 [sequences, heads, n_select]: the pages with the largest bounds of the queries' integer products,
+        ascending, -1 at the end."""
+        nseq, tab = self._table(table)
+        if out is None:
+            out = torch.empty((nseq, self.heads, n_select), dtype=torch.int32, device=q.device)
+        assert out.is_cuda and out.dtype == torch.int32 and out.is_contiguous() and out.shape == (nseq, self.heads, n_select)
+        if workspace is None:
+            need = lib().lpq_kv_select_workspace_bytes(self._h, nseq, table.shape[1])
+            workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+        _check(lib().lpq_kv_select(self._h, *self._queries(q, nseq), _TYPE[q.dtype], nseq, q.shape[1], q.shape[2],
+                                   _dev_ints(lengths, nseq), *tab, n_select, keep_first, keep_last, out.data_ptr(),
+                                   workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream()))
+        return out
+
+    def attend(self, q: torch.Tensor, lengths: torch.Tensor, table: torch.Tensor, pages: torch.Tensor = None,
+               scale: float = None, out: torch.Tensor = None, return_lse: bool = False, workspace: torch.Tensor = None):
+        """Attention of q [sequences, new tokens, query heads, features] over the cache (the last new_tokens positions of
+        each length are the queries' own), or over the `pages` that select() names; scale 1 / sqrt(features) by default."""
+        nseq, tab = self._table(table)
+        if out is None:
+            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        assert out.shape == q.shape and out.dtype == q.dtype
+        lse = torch.empty(q.shape[:3], dtype=torch.float32, device=q.device) if return_lse else None
+        n_select = 0
+        if pages is not None:
+            n_select = pages.shape[-1]
+            assert pages.is_cuda and pages.dtype == torch.int32 and pages.is_contiguous() and pages.shape == (nseq, self.heads, n_select), \
+                "need contiguous int32 pages [sequences, heads, pages]"
+        if workspace is None:
+            need = lib().lpq_kv_attend_workspace_bytes(self._h, nseq, q.shape[1], q.shape[2], table.shape[1], n_select)
+            workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+        _check(lib().lpq_kv_attend(self._h, *self._queries(q, nseq), _TYPE[q.dtype], nseq, q.shape[1], q.shape[2],
+                                   self.dim ** -0.5 if scale is None else scale, _dev_ints(lengths, nseq), *tab, _ptr(pages),
+                                   n_select, *self._queries(out, nseq), _ptr(lse), workspace.data_ptr(),
+                                   workspace.numel() * workspace.element_size(), _stream()))
+        return (out, lse) if return_lse else out
 
 
 def rerank_f32(x: torch.Tensor, q: torch.Tensor, cand_ids: torch.Tensor, k: int, metric="l2sq"):
