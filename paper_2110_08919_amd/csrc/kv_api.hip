@@ -260,7 +260,11 @@ extern "C" size_t lpq_kv_attend_workspace_bytes(const lpq_kv *kv, int64_t nseq, 
 {
     if (!kv || nseq < 1 || new_tokens < 1 || q_heads < kv->view.heads || q_heads % kv->view.heads || table_pages < 1 || n_select < 0) return 0;
     const int64_t pages = n_select ? n_select : table_pages;
-    return kv_attend_plan(kv->view, nseq, new_tokens, q_heads / kv->view.heads, pages * kv->view.page).bytes;
+    // enough for queries of any type
+    size_t most = 0;
+    for (const bool wide : {false, true})
+        most = std::max(most, kv_attend_plan(kv->view, nseq, new_tokens, q_heads / kv->view.heads, pages * kv->view.page, wide).bytes);
+    return most;
 }
 
 extern "C" int lpq_kv_attend(const lpq_kv *kv, const void *q_dev, int64_t ldq_seq, int64_t ldq_token, int64_t ldq_head,
@@ -285,7 +289,7 @@ extern "C" int lpq_kv_attend(const lpq_kv *kv, const void *q_dev, int64_t ldq_se
     if (!disjoint(dim, {{{ldo_seq, nseq}, {ldo_token, new_tokens}, {ldo_head, q_heads}}}))
         return kv_fail(LPQ_EINVAL, "strides %lld, %lld, %lld of the output overlap", (long long)ldo_seq, (long long)ldo_token, (long long)ldo_head);
     const int64_t pages = chosen_dev ? n_select : table_pages;
-    const KvAttendPlan plan = kv_attend_plan(kv->view, nseq, new_tokens, q.group, pages * kv->view.page);
+    const KvAttendPlan plan = kv_attend_plan(kv->view, nseq, new_tokens, q.group, pages * kv->view.page, type == LPQ_TYPE_F32);
     if (plan.bytes && (!workspace_dev || (uintptr_t)workspace_dev % 256)) return kv_fail(LPQ_EINVAL, "workspace null or not 256-byte aligned");
     if (workspace_bytes < plan.bytes) return kv_fail(LPQ_ERANGE, "workspace of %zu bytes, %zu needed", workspace_bytes, plan.bytes);
     const KvAttend a = {lengths_dev, table_dev, ld_table, (int)nseq, (int)table_pages, chosen_dev, n_select, scale, out_dev, ldo_seq,

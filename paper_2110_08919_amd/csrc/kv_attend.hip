@@ -19,7 +19,7 @@
 // (n, g) holds query row n and token 4 g + j of its group of 16, and the second product takes its 8 tokens per lane as
 // 4 g .. 4 g + 3 of two groups.  A lane owns dpad / 16 neighbouring features of the values: it loads them from the rows
 // of its 8 tokens and gathers the operand of each with byte permutes.  Nothing goes through LDS until the end.  Each wave
-// walks its own tiles of 64 (or 32) tokens with the next tile's loads in flight.
+// walks its own tiles of 32 or 64 tokens with the next tile's loads in flight.
 #include "kv_internal.h"
 
 namespace lpq {
@@ -36,35 +36,90 @@ constexpr float NEG = -INFINITY;
 constexpr float HEADROOM = 8.0f;     // how far scores may pass the maximum before it moves (powers of two)
 constexpr float LIFT = 6.0f;         // weights are exp2(t - m + LIFT): at most 2^14, and small ones stay normal fp16
 
-// Tiles of a sequence's tokens, and how they are dealt to the parts of a call.
-struct Deal {
-    int64_t tokens;
-    int tiles, per, used;      // per part; parts that have any
-};
-__device__ __forceinline__ Deal deal(int64_t tokens, int tile, int splits)
+// Memory that no kernel of the call writes, read at addresses all lanes share: scalar loads.
+typedef const __attribute__((address_space(4))) int32_t *Uniform;
+__device__ __forceinline__ Uniform uniform(const int32_t *p) { return (Uniform)(uintptr_t)p; }
+
+// Tokens a wave has in registers: 64 where a row of codes has at
+// most 64 bytes, else 32.
+__host__ __device__ constexpr int tile_tokens(int dpad, bool packed) { return (packed ? dpad / 2 : dpad) <= 64 ? 64 : 32; }
+// Workgroups of four waves that a CU's registers hold.
+__host__ __device__ constexpr int blocks_per_cu(int dpad, bool packed, int rt, bool wide)
 {
-    Deal d;
-    d.tokens = tokens;
-    d.tiles = (int)((tokens + tile - 1) / tile);
-    const int even = (d.tiles + splits - 1) / splits;
-    d.per = even > WAVES ? even : WAVES;
-    d.used = (d.tiles + d.per - 1) / d.per;
-    return d;
+    if (dpad > 128) return rt == 1 ? 2 : 1;
+    if (rt > 1 && wide && packed && dpad > 64) return 1;
+    if (rt > 1 || (wide && dpad > 64)) return 2;
+    return wide || (packed && dpad > 64) ? 3 : 4;
 }
 
-template <int DP>
-constexpr int tile_tokens() { return DP <= 128 ? 64 : 32; }
-
-__device__ __forceinline__ int64_t call_tokens(const KvView &kv, const KvAttend &a, int b)
+// Positions of sequence b that exist, and tiles of tokens a call goes through for it: at least one, so that a sequence
+// without tokens has its zeros written too.
+__device__ __forceinline__ int64_t length_of(const KvView &kv, const KvAttend &a, int b)
 {
-    int64_t len = a.lengths[b];
-    const int64_t room = (int64_t)a.table_pages << kv.page_shift;
-    len = len < 0 ? 0 : (len > room ? room : len);
-    if (a.chosen && len > 0) {
-        const int64_t listed = (int64_t)a.n_select << kv.page_shift;
-        return listed;
+    const int64_t len = uniform(a.lengths)[b], room = (int64_t)a.table_pages << kv.page_shift;
+    return len < 0 ? 0 : (len > room ? room : len);
+}
+__device__ __forceinline__ int tiles_of(const KvView &kv, const KvAttend &a, int b, int tile)
+{
+    int64_t len = length_of(kv, a, b);
+    if (a.chosen && len > 0) len = (int64_t)a.n_select << kv.page_shift;
+    const int64_t tiles = (len + tile - 1) / tile;
+    return tiles < 1 ? 1 : (int)tiles;
+}
+
+// The tiles of all (sequence, head, row tile) one behind the other are dealt to the workgroups in equal runs.  A run ends
+// where it ends: what a workgroup has of a pair that began before its run or goes on after it is a part, at most two
+// per workgroup, and kv_join_kernel joins a pair's parts.
+struct Place {
+    int b, pair, tile, tiles;      // sequence, (head, row tile) of it, tile of that, tiles of the sequence
+    int64_t run;                   // tiles per workgroup
+};
+// Where a pair's parts are: part 0 in slot 2 first + 1, part u > 0 in slot 2 (first + u).
+struct Parts {
+    int first, count;
+};
+__device__ __forceinline__ bool first_place(const KvView &kv, const KvAttend &a, int pairs, int tile, int least, int64_t *scan, Place *shared,
+                                            Place &out)
+{
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int per = (a.nseq + THREADS - 1) / THREADS, b0 = tid * per, b1 = b0 + per < a.nseq ? b0 + per : a.nseq;
+    int64_t mine = 0;
+    for (int b = b0; b < b1; ++b) mine += (int64_t)tiles_of(kv, a, b, tile) * pairs;
+    int64_t upto = mine;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const int64_t t = __shfl_up(upto, o, 64);
+        if (lane >= o) upto += t;
     }
-    return len;
+    if (lane == 63) scan[wave] = upto;
+    __syncthreads();
+    int64_t total = 0;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+        if (w < wave) upto += scan[w];
+        total += scan[w];
+    }
+    int64_t run = (total + gridDim.x - 1) / gridDim.x;
+    if (run < least) run = least;
+    const int64_t from = run * blockIdx.x;
+    if (from >= total) return false;
+    if (from >= upto - mine && from < upto) {       // one thread
+        int64_t left = from - (upto - mine);
+        int b = b0, tiles = 1;
+        for (; b < b1; ++b) {
+            tiles = tiles_of(kv, a, b, tile);
+            if (left < (int64_t)tiles * pairs) break;
+            left -= (int64_t)tiles * pairs;
+        }
+        shared->b = b;
+        shared->pair = (int)(left / tiles);
+        shared->tile = (int)(left % tiles);
+        shared->tiles = tiles;
+    }
+    __syncthreads();
+    out = *shared;
+    out.run = run;
+    return true;
 }
 
 // Bytes of a lane's share of a value row.
@@ -91,14 +146,13 @@ __device__ __forceinline__ void load_share(const uint8_t *p, uint32_t *w)
     }
 }
 
-// One tile in registers.
+// One tile of tokens in registers: the keys, and the values of a lane's features.
 template <int DP, bool PACKED>
 struct Tile {
-    static constexpr int TG = tile_tokens<DP>() / 16, NS = DP / 64, NT = DP / 16;
+    static constexpr int TG = tile_tokens(DP, PACKED) / 16, NS = DP / 64, NT = DP / 16;
     static constexpr int VB = PACKED ? NT / 2 : NT, VW = (VB + 3) / 4;
     uint32_t k[TG][NS][PACKED ? 2 : 4];
     uint32_t v[TG / 2][8][VW];
-    int pos[TG];          // position of a group's first token; INT32_MAX: the group does not count
 };
 
 // Halves [features t of token e | of token e + 1] as fp16, from the two tokens' shares of a row.
@@ -123,412 +177,474 @@ __device__ __forceinline__ uint32_t value_pair(uint32_t w0, uint32_t w1, int t)
     }
 }
 
+// Workspace: sums [2 grid][rows of a tile][DP], then maximum and sum of weights [2 grid][rows of a tile][2], then Parts per pair.
+struct Workspace {
+    float *sums, *ml;
+    Parts *parts;
+};
+__host__ __device__ __forceinline__ Workspace workspace(float *p, int64_t slots, int tile_rows, int dpad)
+{
+    Workspace w;
+    w.sums = p;
+    w.ml = p + slots * tile_rows * dpad;
+    w.parts = reinterpret_cast<Parts *>(w.ml + slots * tile_rows * 2);
+    return w;
+}
+
 template <int DP, bool PACKED, int RT, bool WIDE>
-__global__ __launch_bounds__(THREADS) void kv_attend_kernel(KvView kv, KvQueries q, KvAttend a, int row_tiles, int splits)
+__global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, WIDE)) void kv_attend_kernel(KvView kv, KvQueries q, KvAttend a, int row_tiles,
+                                                                                       int least)
 {
     typedef Tile<DP, PACKED> T;
     constexpr int TG = T::TG, NS = T::NS, NT = T::NT, VB = T::VB, TOK = 16 * TG;
     constexpr int ND = WIDE ? 3 : 2, NP = WIDE ? 2 : 1, RB = PACKED ? DP / 2 : DP;
     constexpr float QMAX = WIDE ? 2088895.0f : 16319.0f;
     __shared__ float red_m[WAVES][16 * RT], red_l[WAVES][16 * RT];
-    __shared__ float sums[WAVES][16][DP + 4];
+    __shared__ __align__(16) float sums[WAVES][16][DP + 4];
+    __shared__ __align__(16) int8_t digits[ND][16 * RT][DP + 16];
+    __shared__ float row_scale[16 * RT], row_shift[16 * RT];
+    __shared__ int row_sum[ND][16 * RT];
+    __shared__ int64_t scan[WAVES];
+    __shared__ Place shared;
 
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, g = lane >> 4;
-    int id = blockIdx.x;
-    const int h = id % kv.heads;
-    id /= kv.heads;
-    const int row_tile = id % row_tiles;
-    id /= row_tiles;
-    const int b = id % a.nseq, split = id / a.nseq;
-    const int rows = q.new_tokens * q.group, row0 = row_tile * 16 * RT;
-    int64_t len = a.lengths[b];
-    {
-        const int64_t room = (int64_t)a.table_pages << kv.page_shift;
-        len = len < 0 ? 0 : (len > room ? room : len);
-    }
-    const Deal d = deal(call_tokens(kv, a, b), TOK, splits);
-    if (split > 0 && split >= d.used) return;
-
-    // ---- queries: steps folded in, digits; lane (n, g) holds features 64 st + 16 g .. + 15 of row n
-    v4i qd[RT][ND][NS];
-    v4i q0[RT][ND];          // packed keys hold c + 8: what that adds to each sum is taken off at its start
-    float rs[RT], shift[RT], m[RT], l[RT];
-    int last[RT];            // last position a row sees
-#pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-        const int r = row0 + rt * 16 + n;
-        const bool on = r < rows;
-        const int64_t at = (int64_t)b * q.ld_seq + (int64_t)(r / q.group) * q.ld_token + (int64_t)(h * q.group + r % q.group) * q.ld_head;
-        float x[NS][16];
-        float most = 0.0f, offset = 0.0f;
-        bool bad = false;
-#pragma unroll
-        for (int st = 0; st < NS; ++st)
-#pragma unroll
-            for (int e0 = 0; e0 < 16; e0 += 8) {
-                const int c0 = 64 * st + 16 * g + e0;
-                float *v = &x[st][e0];
-                kv_load8(q.p, q.type, on ? at + c0 : 0, on ? kv.dim - c0 : 0, q.vec, v);
-                const float *step = kv.key.s + h * DP + c0, *k = kv.key.k + h * DP + c0;
-                if (a.lse) {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) offset += v[e] * (k[e] + 0.5f * step[e]);
-                }
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    v[e] *= step[e];
-                    most = fmaxf(most, fabsf(v[e]));
-                    bad |= !(fabsf(v[e]) <= 3.402823466e38f);
-                }
-            }
-        most = fmaxf(most, __shfl_xor(most, 16, 64));
-        most = fmaxf(most, __shfl_xor(most, 32, 64));
-        offset += __shfl_xor(offset, 16, 64);
-        offset += __shfl_xor(offset, 32, 64);
-        int any = bad;
-        any |= __shfl_xor(any, 16, 64);
-        any |= __shfl_xor(any, 32, 64);
-        const bool use = !any && most > 1e-30f;      // below that QMAX / most leaves the range of binary32, and scores are 0
-        const float f = use ? QMAX / most : 0.0f;
-        rs[rt] = any ? NAN : (use ? most / QMAX * a.scale * 1.44269504088896f : 0.0f);
-        shift[rt] = offset * a.scale;
-        int dsum[ND];
-#pragma unroll
-        for (int dd = 0; dd < ND; ++dd) dsum[dd] = 0;
-#pragma unroll
-        for (int st = 0; st < NS; ++st) {
-            int8_t digit[ND][16];
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                // packed: low nibbles (even features) first, then the high ones
-                const int src = PACKED ? (e < 8 ? 2 * e : 2 * (e - 8) + 1) : e;
-                int v = use ? (int)rintf(x[st][src] * f) : 0;
-#pragma unroll
-                for (int dd = ND - 1; dd > 0; --dd) {
-                    const int up = (v + 64) >> 7, low = v - (up << 7);       // low in -64 .. 63
-                    digit[dd][e] = (int8_t)low;
-                    dsum[dd] += low;
-                    v = up;
-                }
-                digit[0][e] = (int8_t)v;
-                dsum[0] += v;
-            }
-#pragma unroll
-            for (int dd = 0; dd < ND; ++dd) __builtin_memcpy(&qd[rt][dd][st], digit[dd], 16);
-        }
-#pragma unroll
-        for (int dd = 0; dd < ND; ++dd) {
-            int v = 0;
-            if (PACKED) {
-                v = dsum[dd];
-                v += __shfl_xor(v, 16, 64);
-                v += __shfl_xor(v, 32, 64);
-                v *= -8;
-            }
-            q0[rt][dd] = v4i{v, v, v, v};
-        }
-        m[rt] = NEG;
-        l[rt] = 0.0f;
-        const int64_t see = len - q.new_tokens + r / q.group;
-        last[rt] = on ? (int)(see < -1 ? -1 : see) : -1;
-    }
-    const int64_t least64 = len - q.new_tokens;      // a tile that ends at or before this position is seen by every row
-    const int least = (int)(least64 < -1 ? -1 : least64);
-
-    v4f acc[RT][NT];
-#pragma unroll
-    for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-        for (int t = 0; t < NT; ++t) acc[rt][t] = v4f{0.f, 0.f, 0.f, 0.f};
-
-    const int32_t *table = a.table + (int64_t)b * a.ld_table;
-    const int32_t *chosen = a.chosen ? a.chosen + ((int64_t)b * kv.heads + h) * a.n_select : nullptr;
+    const int lane0 = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int pairs = kv.heads * row_tiles, rows = q.new_tokens * q.group;
     const int64_t head_bytes = (int64_t)kv.page * RB;
+    const Workspace ws = workspace(a.part, 2 * (int64_t)gridDim.x, 16 * RT, DP);
+    Place at;
+    if (least == 0) {            // a workgroup per pair
+        at.b = blockIdx.x / pairs;
+        at.pair = blockIdx.x % pairs;
+        at.tile = 0;
+        at.tiles = tiles_of(kv, a, at.b, TOK);
+        at.run = at.tiles;
+    } else if (!first_place(kv, a, pairs, TOK, least, scan, &shared, at)) {
+        return;
+    }
+    const int64_t run = at.run;
+    int64_t left = run;
+    int b = __builtin_amdgcn_readfirstlane(at.b), pair = __builtin_amdgcn_readfirstlane(at.pair);
+    int start = __builtin_amdgcn_readfirstlane(at.tile), tiles = __builtin_amdgcn_readfirstlane(at.tiles);
 
-    // Page of the pool and position of group `grp` of the call's tokens; page -1 where there is none.
-    auto place = [&](int64_t grp, int &page, int &pos) {
-        const int64_t at = grp * 16;
-        int column = (int)(at >> kv.page_shift);
-        const int inside = (int)at & (kv.page - 1);
-        page = -1;
-        pos = INT32_MAX;
-        if (chosen) {
-            if (column >= a.n_select) return;
-            column = chosen[column];
-            if (column < 0 || column >= a.table_pages) return;
-        }
-        const int64_t p = ((int64_t)column << kv.page_shift) + inside;
-        if (p >= len) return;
-        const int id_ = table[column];
-        if (id_ < 0 || id_ >= kv.pages) return;
-        page = id_;
-        pos = (int)p;
-    };
-    struct Ids { int page[TG], pos[TG]; };
-    auto find = [&](int tile, Ids &i) {
-#pragma unroll
-        for (int tg = 0; tg < TG; ++tg) place((int64_t)tile * TG + tg, i.page[tg], i.pos[tg]);
-    };
-    auto load = [&](const Ids &i, T &t) {
-#pragma unroll
-        for (int tg = 0; tg < TG; ++tg) {
-            const int page = i.page[tg] < 0 ? 0 : i.page[tg];
-            const int row = i.page[tg] < 0 ? 0 : i.pos[tg] & (kv.page - 1);
-            t.pos[tg] = i.pos[tg];
-            const int64_t at = ((int64_t)page * kv.heads + h) * head_bytes + (int64_t)row * RB;
-            const uint8_t *kp = kv.k + at + n * RB + g * (PACKED ? 8 : 16);
-#pragma unroll
-            for (int st = 0; st < NS; ++st) {
-                if constexpr (PACKED) {
-                    const uint2 w = *reinterpret_cast<const uint2 *>(kp + 32 * st);
-                    t.k[tg][st][0] = w.x; t.k[tg][st][1] = w.y;
-                } else {
-                    const uint4 w = *reinterpret_cast<const uint4 *>(kp + 64 * st);
-                    t.k[tg][st][0] = w.x; t.k[tg][st][1] = w.y; t.k[tg][st][2] = w.z; t.k[tg][st][3] = w.w;
-                }
+    for (;;) {
+        // ---- tiles [start, end) of a pair
+        const int h = pair / row_tiles, row0 = (pair % row_tiles) * 16 * RT;
+        const int end = left < tiles - start ? start + (int)left : tiles;
+        const int64_t len = length_of(kv, a, b);
+        const Uniform table = uniform(a.table + (int64_t)b * a.ld_table);
+        const Uniform chosen = uniform(a.chosen + ((int64_t)b * kv.heads + h) * a.n_select);
+        int lane = lane0, tid = threadIdx.x;
+        asm volatile("" : "+v"(lane), "+v"(tid));      // nothing that depends on it is worth registers over all of a run
+        const int n = lane & 15, g = lane >> 4;
+
+        // Page of the pool and position of group `grp` of the call's tokens; position INT32_MAX where there is none.
+        const int columns = a.chosen ? a.n_select : a.table_pages;
+        auto place = [&](int64_t grp, int &page, int &pos) {
+            const int64_t token = grp * 16;
+            const int want = (int)(token >> kv.page_shift), inside = (int)token & (kv.page - 1);
+            bool there = want < columns;
+            int column = there ? want : columns - 1;
+            if (a.chosen) {
+                column = __builtin_amdgcn_readfirstlane(chosen[column]);
+                there = there && column >= 0 && column < a.table_pages;
+                column = there ? column : 0;
             }
-            const uint8_t *vp = kv.v + at + (4 * g) * RB + n * VB;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) load_share<VB>(vp + j * RB, t.v[tg >> 1][(tg & 1) * 4 + j]);
-        }
-    };
-    auto compute = [&](const T &t) {
-        bool part = false;
-#pragma unroll
-        for (int tg = 0; tg < TG; ++tg) part |= t.pos[tg] > least - 15;     // also where a group does not count
-        v8h w[RT][NP][TG / 2];
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt) {
-            float s[TG][4];
+            const int64_t p = ((int64_t)column << kv.page_shift) + inside;
+            const int id = __builtin_amdgcn_readfirstlane(table[column]);
+            there = there && p < len && id >= 0 && id < kv.pages;
+            page = there ? id : 0;
+            pos = there ? (int)p : INT32_MAX;
+        };
+        struct Where { int64_t base[TG]; int pos[TG]; };
+        auto find = [&](int tile, Where &w) {
 #pragma unroll
             for (int tg = 0; tg < TG; ++tg) {
-                v4i sum[ND];
+                int page;
+                place((int64_t)tile * TG + tg, page, w.pos[tg]);
+                const int row = w.pos[tg] & (kv.page - 1) & ~15;       // of page 0 where there is none
+                w.base[tg] = ((int64_t)page * kv.heads + h) * head_bytes + (int64_t)row * RB;
+            }
+        };
+        T t;
+        const unsigned ko = n * RB + g * (PACKED ? 8 : 16), vo = 4 * g * RB + n * VB;
+        auto load_keys = [&](const Where &w) {
 #pragma unroll
-                for (int dd = 0; dd < ND; ++dd) sum[dd] = q0[rt][dd];
+            for (int tg = 0; tg < TG; ++tg) {
+                const uint8_t *p = kv.k + w.base[tg];
 #pragma unroll
                 for (int st = 0; st < NS; ++st) {
-                    v4i kf;
                     if constexpr (PACKED) {
-                        const uint32_t x = t.k[tg][st][0], y = t.k[tg][st][1];
-                        kf = v4i{(int)(x & 0x0f0f0f0fu), (int)(y & 0x0f0f0f0fu), (int)((x >> 4) & 0x0f0f0f0fu), (int)((y >> 4) & 0x0f0f0f0fu)};
+                        const uint2 x = *reinterpret_cast<const uint2 *>(p + ko + 32 * st);
+                        t.k[tg][st][0] = x.x; t.k[tg][st][1] = x.y;
                     } else {
-                        kf = v4i{(int)t.k[tg][st][0], (int)t.k[tg][st][1], (int)t.k[tg][st][2], (int)t.k[tg][st][3]};
+                        const uint4 x = *reinterpret_cast<const uint4 *>(p + ko + 64 * st);
+                        t.k[tg][st][0] = x.x; t.k[tg][st][1] = x.y; t.k[tg][st][2] = x.z; t.k[tg][st][3] = x.w;
                     }
-#pragma unroll
-                    for (int dd = 0; dd < ND; ++dd) sum[dd] = __builtin_amdgcn_mfma_i32_16x16x64_i8(kf, qd[rt][dd][st], sum[dd], 0, 0, 0);
-                }
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    if constexpr (WIDE) s[tg][j] = ((float)sum[0][j] * 16384.0f + (float)(sum[1][j] * 128 + sum[2][j])) * rs[rt];
-                    else s[tg][j] = (float)(sum[0][j] * 128 + sum[1][j]) * rs[rt];
                 }
             }
-            if (part) {
+        };
+        auto load_values = [&](const Where &w) {
+#pragma unroll
+            for (int tg = 0; tg < TG; ++tg) {
+                const uint8_t *p = kv.v + w.base[tg];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) load_share<VB>(p + vo + j * RB, t.v[tg >> 1][(tg & 1) * 4 + j]);
+            }
+        };
+
+        // The first tile's loads are under way while the queries are made ready.
+        int tile = start + wave;
+        Where now, next;
+        find(tile, now);
+        next = now;
+        if (tile < end) {
+            load_keys(now);
+            load_values(now);
+        }
+
+        // ---- queries: steps folded in, digits; LR lanes per row, 8 features each
+        constexpr int LR = DP <= 64 ? 8 : DP <= 128 ? 16 : 32;
+#pragma unroll
+        for (int r0 = 0; r0 < 16 * RT; r0 += THREADS / LR) {
+            const int r16 = r0 + tid / LR, r = row0 + r16, c = tid % LR, c0 = 8 * c;
+            if (r0 + THREADS / LR > 16 * RT && r16 >= 16 * RT) break;        // (whole waves)
+            const bool on = r < rows && c0 < DP;
+            const int64_t qat = (int64_t)b * q.ld_seq + (int64_t)(r / q.group) * q.ld_token + (int64_t)(h * q.group + r % q.group) * q.ld_head;
+            float v[8], offset = 0.0f, most = 0.0f;
+            kv_load8(q.p, q.type, on ? qat + c0 : 0, on ? kv.dim - c0 : 0, q.vec, v);
+            const float *step = kv.key.s + h * DP + (c0 < DP ? c0 : 0), *k = kv.key.k + h * DP + (c0 < DP ? c0 : 0);
+            if (a.lse) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) offset += v[e] * (k[e] + 0.5f * step[e]);
+            }
+            int bad = 0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                v[e] *= step[e];
+                most = fmaxf(most, fabsf(v[e]));
+                bad |= !(fabsf(v[e]) <= 3.402823466e38f);
+            }
+#pragma unroll
+            for (int o = 1; o < LR; o <<= 1) {
+                most = fmaxf(most, __shfl_xor(most, o, 64));
+                offset += __shfl_xor(offset, o, 64);
+                bad |= __shfl_xor(bad, o, 64);
+            }
+            const bool use = !bad && most > 1e-30f;      // below that QMAX / most leaves the range of binary32, and scores are 0
+            const float f = use ? QMAX / most : 0.0f;
+            int8_t d[ND][8];
+            int dsum[ND];
+#pragma unroll
+            for (int dd = 0; dd < ND; ++dd) dsum[dd] = 0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                // packed rows have the even features of 16 first (low nibbles of 8 bytes), then the odd ones
+                const int to = PACKED ? (e >> 1) + 4 * (e & 1) : e;
+                int x = use ? (int)rintf(v[e] * f) : 0;
+#pragma unroll
+                for (int dd = ND - 1; dd > 0; --dd) {
+                    const int up = (x + 64) >> 7, low = x - (up << 7);       // low in -64 .. 63
+                    d[dd][to] = (int8_t)low;
+                    dsum[dd] += low;
+                    x = up;
+                }
+                d[0][to] = (int8_t)x;
+                dsum[0] += x;
+            }
+#pragma unroll
+            for (int dd = 0; dd < ND; ++dd) {
+                uint32_t w[2];
+                __builtin_memcpy(w, d[dd], 8);
+                if (c0 < DP) {
+                    int8_t *row = digits[dd][r16];
+                    if (PACKED) {
+                        *reinterpret_cast<uint32_t *>(row + 16 * (c >> 1) + 4 * (c & 1)) = w[0];
+                        *reinterpret_cast<uint32_t *>(row + 16 * (c >> 1) + 8 + 4 * (c & 1)) = w[1];
+                    } else {
+                        *reinterpret_cast<uint2 *>(row + c0) = make_uint2(w[0], w[1]);
+                    }
+                }
+                if (PACKED) {
+#pragma unroll
+                    for (int o = 1; o < LR; o <<= 1) dsum[dd] += __shfl_xor(dsum[dd], o, 64);
+                    if (c == 0) row_sum[dd][r16] = dsum[dd];
+                }
+            }
+            if (c == 0) {
+                row_scale[r16] = bad ? NAN : (use ? most / QMAX * a.scale * 1.44269504088896f : 0.0f);
+                row_shift[r16] = offset * a.scale;
+            }
+        }
+        __syncthreads();
+        v4i qd[RT][ND][NS];      // lane (n, g): features 64 st + 16 g .. + 15 of row n
+        int q0[RT][ND];          // packed keys hold c + 8: what that adds to each sum is taken off at its start
+        float rs[RT], m[RT], l[RT];
+        int last[RT];            // last position a row sees
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+#pragma unroll
+            for (int dd = 0; dd < ND; ++dd) {
+#pragma unroll
+                for (int st = 0; st < NS; ++st) qd[rt][dd][st] = *reinterpret_cast<const v4i *>(&digits[dd][rt * 16 + n][64 * st + 16 * g]);
+                q0[rt][dd] = PACKED ? -8 * row_sum[dd][rt * 16 + n] : 0;
+            }
+            rs[rt] = row_scale[rt * 16 + n];
+            m[rt] = NEG;
+            l[rt] = 0.0f;
+            const int r = row0 + rt * 16 + n;
+            const int64_t see = len - q.new_tokens + r / q.group;
+            last[rt] = r < rows ? (int)(see < -1 ? -1 : see) : -1;
+        }
+        const int64_t least_seen = len - q.new_tokens;       // a tile that ends at or before this position is seen by every row
+        const int seen = (int)(least_seen < -1 ? -1 : least_seen);
+
+        v4f acc[RT][NT];
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+            for (int t = 0; t < NT; ++t) acc[rt][t] = v4f{0.f, 0.f, 0.f, 0.f};
+
+        // ---- the wave's tiles: the next tile's keys are asked for as soon as this one's are used up, its values likewise
+        for (; tile < end; tile += WAVES) {
+            const bool more = tile + WAVES < end;
+            if (more) find(tile + WAVES, next);
+            bool part = false;
+#pragma unroll
+            for (int tg = 0; tg < TG; ++tg) part |= now.pos[tg] > seen - 15;     // also where a group does not count
+            float s[RT][TG][4];
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                for (int tg = 0; tg < TG; ++tg) {
+                    v4i sum[ND];
+#pragma unroll
+                    for (int dd = 0; dd < ND; ++dd) sum[dd] = v4i{q0[rt][dd], q0[rt][dd], q0[rt][dd], q0[rt][dd]};
+#pragma unroll
+                    for (int st = 0; st < NS; ++st) {
+                        v4i kf;
+                        if constexpr (PACKED) {
+                            const uint32_t x = t.k[tg][st][0], y = t.k[tg][st][1];
+                            kf = v4i{(int)(x & 0x0f0f0f0fu), (int)(y & 0x0f0f0f0fu), (int)((x >> 4) & 0x0f0f0f0fu), (int)((y >> 4) & 0x0f0f0f0fu)};
+                        } else {
+                            kf = v4i{(int)t.k[tg][st][0], (int)t.k[tg][st][1], (int)t.k[tg][st][2], (int)t.k[tg][st][3]};
+                        }
+#pragma unroll
+                        for (int dd = 0; dd < ND; ++dd) sum[dd] = __builtin_amdgcn_mfma_i32_16x16x64_i8(kf, qd[rt][dd][st], sum[dd], 0, 0, 0);
+                    }
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        if constexpr (WIDE) s[rt][tg][j] = ((float)sum[0][j] * 16384.0f + (float)(sum[1][j] * 128 + sum[2][j])) * rs[rt];
+                        else s[rt][tg][j] = (float)(sum[0][j] * 128 + sum[1][j]) * rs[rt];
+                    }
+                }
+            if (more) load_keys(next);
+            v8h w[RT][NP][TG / 2];
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) {
+                if (part) {
+#pragma unroll
+                    for (int tg = 0; tg < TG; ++tg)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+                            if (now.pos[tg] > last[rt] - (4 * g + j)) s[rt][tg][j] = NEG;
+                }
+                float top = s[rt][0][0];
 #pragma unroll
                 for (int tg = 0; tg < TG; ++tg)
 #pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        if (t.pos[tg] > last[rt] - (4 * g + j)) s[tg][j] = NEG;
-            }
-            float top = s[0][0];
+                    for (int j = 0; j < 4; ++j) top = fmaxf(top, s[rt][tg][j]);
+                if (__any(top > m[rt] + HEADROOM)) {
+                    top = fmaxf(top, __shfl_xor(top, 16, 64));
+                    top = fmaxf(top, __shfl_xor(top, 32, 64));
+                    const float next = fmaxf(m[rt], top);
+                    const float f = next == NEG ? 1.0f : __builtin_amdgcn_exp2f(m[rt] - next);
+                    m[rt] = next;
+                    l[rt] *= f;
 #pragma unroll
-            for (int tg = 0; tg < TG; ++tg)
+                    for (int t_ = 0; t_ < NT; ++t_)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) top = fmaxf(top, s[tg][j]);
-            if (__any(top > m[rt] + HEADROOM)) {
-                top = fmaxf(top, __shfl_xor(top, 16, 64));
-                top = fmaxf(top, __shfl_xor(top, 32, 64));
-                const float next = fmaxf(m[rt], top);
-                const float f = next == NEG ? 1.0f : __builtin_amdgcn_exp2f(m[rt] - next);
-                m[rt] = next;
-                l[rt] *= f;
+                        for (int j = 0; j < 4; ++j) acc[rt][t_][j] *= f;
+                }
+                const float base = (m[rt] == NEG ? 0.0f : m[rt]) - LIFT;
+                float add = 0.0f;
 #pragma unroll
-                for (int t_ = 0; t_ < NT; ++t_)
+                for (int tg = 0; tg < TG; ++tg)
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) acc[rt][t_][j] *= f;
-            }
-            const float base = (m[rt] == NEG ? 0.0f : m[rt]) - LIFT;
-            float add = 0.0f;
-#pragma unroll
-            for (int tg = 0; tg < TG; ++tg)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const float p = __builtin_amdgcn_exp2f(s[tg][j] - base);
-                    const _Float16 p0 = (_Float16)p;
-                    w[rt][0][tg >> 1][(tg & 1) * 4 + j] = p0;
-                    add += (float)p0;
-                    if constexpr (WIDE) {
-                        const _Float16 p1 = (_Float16)(p - (float)p0);
-                        w[rt][1][tg >> 1][(tg & 1) * 4 + j] = p1;
-                        add += (float)p1;
+                    for (int j = 0; j < 4; ++j) {
+                        const float p = __builtin_amdgcn_exp2f(s[rt][tg][j] - base);
+                        const _Float16 p0 = (_Float16)p;
+                        w[rt][0][tg >> 1][(tg & 1) * 4 + j] = p0;
+                        add += (float)p0;
+                        if constexpr (WIDE) {
+                            const _Float16 p1 = (_Float16)(p - (float)p0);
+                            w[rt][1][tg >> 1][(tg & 1) * 4 + j] = p1;
+                            add += (float)p1;
+                        }
                     }
+                l[rt] += add;
+            }
+#pragma unroll
+            for (int half = 0; half < TG / 2; ++half)
+#pragma unroll
+                for (int f = 0; f < NT; ++f) {
+                    const int word = PACKED ? f >> 3 : f >> 2;
+                    uint32_t two[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) two[e] = value_pair<PACKED>(t.v[half][2 * e][word], t.v[half][2 * e + 1][word], f);
+                    v8h vf;
+                    __builtin_memcpy(&vf, two, 16);
+#pragma unroll
+                    for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                        for (int p = 0; p < NP; ++p)
+                            acc[rt][f] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, w[rt][p][half], acc[rt][f], 0, 0, 0);
                 }
-            l[rt] += add;
+            if (more) load_values(next);
+            now = next;
         }
-#pragma unroll
-        for (int half = 0; half < TG / 2; ++half)
-#pragma unroll
-            for (int f = 0; f < NT; ++f) {
-                const int word = PACKED ? f >> 3 : f >> 2;
-                uint32_t pair[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) pair[e] = value_pair<PACKED>(t.v[half][2 * e][word], t.v[half][2 * e + 1][word], f);
-                v8h vf;
-                __builtin_memcpy(&vf, pair, 16);
-#pragma unroll
-                for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-                    for (int p = 0; p < NP; ++p)
-                        acc[rt][f] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, w[rt][p][half], acc[rt][f], 0, 0, 0);
-            }
-    };
+        asm volatile("s_nop 15");      // the last matrix results are read in other blocks of code
 
-    // ---- the wave's tiles, one ahead in registers, places of the one after that known
-    const int end = (split + 1) * d.per < d.tiles ? (split + 1) * d.per : d.tiles;
-    int tile = split * d.per + __builtin_amdgcn_readfirstlane(wave);
-    if (tile < end) {
-        Ids ids;
-        T t0, t1;
-        find(tile, ids);
-        load(ids, t0);
-        if (tile + WAVES < end) find(tile + WAVES, ids);
-        for (;;) {
-            if (tile + WAVES < end) {
-                load(ids, t1);
-                if (tile + 2 * WAVES < end) find(tile + 2 * WAVES, ids);
+        // ---- the waves' parts joined
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+            l[rt] += __shfl_xor(l[rt], 16, 64);
+            l[rt] += __shfl_xor(l[rt], 32, 64);
+            if (g == 0) {
+                red_m[wave][rt * 16 + n] = m[rt];
+                red_l[wave][rt * 16 + n] = l[rt];
             }
-            compute(t0);
-            tile += WAVES;
-            if (tile >= end) break;
-            if (tile + WAVES < end) {
-                load(ids, t0);
-                if (tile + 2 * WAVES < end) find(tile + 2 * WAVES, ids);
-            }
-            compute(t1);
-            tile += WAVES;
-            if (tile >= end) break;
         }
-    }
-    asm volatile("s_nop 15");      // the last matrix results are read in other blocks of code
-
-    // ---- the waves' parts joined
-#pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-        l[rt] += __shfl_xor(l[rt], 16, 64);
-        l[rt] += __shfl_xor(l[rt], 32, 64);
-        if (g == 0) {
-            red_m[wave][rt * 16 + n] = m[rt];
-            red_l[wave][rt * 16 + n] = l[rt];
-        }
-    }
-    __syncthreads();
-    const bool whole = d.used <= 1;
-    float *part = a.part;
-    const int all_rows = row_tiles * 16 * RT;
-    const int64_t part_at = (((int64_t)b * kv.heads + h) * splits + split) * all_rows + row0;     // row of the partial results
-    float *part_ml = part + (int64_t)a.nseq * kv.heads * splits * all_rows * DP;
-#pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-        float top = NEG;
-#pragma unroll
-        for (int w = 0; w < WAVES; ++w) top = fmaxf(top, red_m[w][rt * 16 + n]);
-        const float f = top == NEG ? 1.0f : __builtin_amdgcn_exp2f(m[rt] - top);
-        if (rt) __syncthreads();
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-#pragma unroll
-            for (int t = 0; t < NT; ++t) sums[wave][n][(4 * g + j) * NT + t] = acc[rt][t][j] * f;
         __syncthreads();
-        const int r16 = threadIdx.x >> 4, r = row0 + rt * 16 + r16;
-        if (r < rows) {
-            float mm = NEG, ll = 0.0f;
+        const bool whole = start == 0 && end == tiles;
+        const int64_t slot = 2 * (int64_t)blockIdx.x + (start == 0 ? 1 : 0);
+        if (least != 0 && start == 0 && threadIdx.x == 0)
+            ws.parts[(int64_t)b * pairs + pair] = {(int)blockIdx.x, 1 + (int)((tiles - end + run - 1) / run)};
 #pragma unroll
-            for (int w = 0; w < WAVES; ++w) mm = fmaxf(mm, red_m[w][rt * 16 + r16]);
+        for (int rt = 0; rt < RT; ++rt) {
+            float top = NEG;
 #pragma unroll
-            for (int w = 0; w < WAVES; ++w)
-                ll += red_l[w][rt * 16 + r16] * (mm == NEG ? 1.0f : __builtin_amdgcn_exp2f(red_m[w][rt * 16 + r16] - mm));
-            const float inv = ll == 0.0f ? 0.0f : 1.0f / ll;
-            const int64_t out_row = (int64_t)b * a.ldo_seq + (int64_t)(r / q.group) * a.ldo_token + (int64_t)(h * q.group + r % q.group) * a.ldo_head;
+            for (int w = 0; w < WAVES; ++w) top = fmaxf(top, red_m[w][rt * 16 + n]);
+            const float f = top == NEG ? 1.0f : __builtin_amdgcn_exp2f(m[rt] - top);
+            if (rt) __syncthreads();
 #pragma unroll
-            for (int i = 0; i < NS; ++i) {
-                const int c0 = 4 * ((threadIdx.x & 15) + 16 * i);
-                float x[4];
+            for (int j = 0; j < 4; ++j)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) x[e] = 0.0f;
+                for (int t = 0; t < NT; ++t) sums[wave][n][(4 * g + j) * NT + t] = acc[rt][t][j] * f;
+            if (a.lse && start == 0 && wave == 0 && g == 0) {      // of several parts: what every token has, the rest is added when they are joined
+                const int r = row0 + rt * 16 + n;
+                if (r < rows) {
+                    float sum = 0.0f;
 #pragma unroll
-                for (int w = 0; w < WAVES; ++w) {
-                    const float4 y = *reinterpret_cast<const float4 *>(&sums[w][r16][c0]);
-                    x[0] += y.x; x[1] += y.y; x[2] += y.z; x[3] += y.w;
-                }
-                if (whole) {
-                    const float *vs = kv.value.s + h * DP + c0, *vk = kv.value.k + h * DP + c0;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) x[e] = ll == 0.0f ? 0.0f : (x[e] * inv + 0.5f) * vs[e] + vk[e];
-                    kv_store<4>(a.out, q.type, out_row + c0, kv.dim - c0, a.vec_out, x);
-                } else {
-                    *reinterpret_cast<float4 *>(part + (part_at + rt * 16 + r16) * DP + c0) = make_float4(x[0], x[1], x[2], x[3]);
+                    for (int w = 0; w < WAVES; ++w)
+                        sum += red_l[w][rt * 16 + n] * (top == NEG ? 1.0f : __builtin_amdgcn_exp2f(red_m[w][rt * 16 + n] - top));
+                    const int64_t lat = ((int64_t)b * q.new_tokens + r / q.group) * ((int64_t)kv.heads * q.group) + h * q.group + r % q.group;
+                    a.lse[lat] = !whole ? row_shift[rt * 16 + n] : sum == 0.0f ? NEG : (top - LIFT + __log2f(sum)) * 0.69314718055994531f + row_shift[rt * 16 + n];
                 }
             }
-            if ((threadIdx.x & 15) == 0 && !whole) {
-                float *ml = part_ml + (part_at + rt * 16 + r16) * 2;
-                ml[0] = mm;
-                ml[1] = ll;
-            }
-        }
-        if (whole && a.lse && wave == 0 && g == 0) {
-            const int rr = row0 + rt * 16 + n;
-            if (rr < rows) {
-                float ll = 0.0f;
+            __syncthreads();
+            const int r16 = tid >> 4, r = row0 + rt * 16 + r16;
+            if (r < rows) {
+                float mm = NEG, ll = 0.0f;
+#pragma unroll
+                for (int w = 0; w < WAVES; ++w) mm = fmaxf(mm, red_m[w][rt * 16 + r16]);
 #pragma unroll
                 for (int w = 0; w < WAVES; ++w)
-                    ll += red_l[w][rt * 16 + n] * (top == NEG ? 1.0f : __builtin_amdgcn_exp2f(red_m[w][rt * 16 + n] - top));
-                const int64_t at = ((int64_t)b * q.new_tokens + rr / q.group) * ((int64_t)kv.heads * q.group) + h * q.group + rr % q.group;
-                a.lse[at] = ll == 0.0f ? NEG : (top - LIFT + __log2f(ll)) * 0.69314718055994531f + shift[rt];
+                    ll += red_l[w][rt * 16 + r16] * (mm == NEG ? 1.0f : __builtin_amdgcn_exp2f(red_m[w][rt * 16 + r16] - mm));
+                const float inv = ll == 0.0f ? 0.0f : 1.0f / ll;
+                const int64_t row = slot * (16 * RT) + rt * 16 + r16;
+                const int64_t out_row = (int64_t)b * a.ldo_seq + (int64_t)(r / q.group) * a.ldo_token + (int64_t)(h * q.group + r % q.group) * a.ldo_head;
+#pragma unroll
+                for (int i = 0; i < NS; ++i) {
+                    const int c0 = 4 * ((tid & 15) + 16 * i);
+                    float x[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                    for (int w = 0; w < WAVES; ++w) {
+                        const float4 y = *reinterpret_cast<const float4 *>(&sums[w][r16][c0]);
+                        x[0] += y.x; x[1] += y.y; x[2] += y.z; x[3] += y.w;
+                    }
+                    if (whole) {
+                        const float *vs = kv.value.s + h * DP + c0, *vk = kv.value.k + h * DP + c0;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) x[e] = ll == 0.0f ? 0.0f : (x[e] * inv + 0.5f) * vs[e] + vk[e];
+                        kv_store<4>(a.out, q.type, out_row + c0, kv.dim - c0, a.vec_out, x);
+                    } else {
+                        *reinterpret_cast<float4 *>(ws.sums + row * DP + c0) = make_float4(x[0], x[1], x[2], x[3]);
+                    }
+                }
+                if ((tid & 15) == 0 && !whole) {
+                    ws.ml[row * 2] = mm;
+                    ws.ml[row * 2 + 1] = ll;
+                }
             }
         }
-        if (!whole && a.lse && split == 0 && wave == 0 && g == 0) {      // the joining kernel adds what every token has
-            const int rr = row0 + rt * 16 + n;
-            if (rr < rows) {
-                const int64_t at = ((int64_t)b * q.new_tokens + rr / q.group) * ((int64_t)kv.heads * q.group) + h * q.group + rr % q.group;
-                a.lse[at] = shift[rt];
-            }
+
+        // ---- on to what follows in the workgroup's run
+        left -= end - start;
+        if (left <= 0) return;
+        if (end == tiles && ++pair == pairs) {
+            pair = 0;
+            if (++b >= a.nseq) return;
+            tiles = __builtin_amdgcn_readfirstlane(tiles_of(kv, a, b, TOK));
         }
+        start = 0;
+        __syncthreads();               // LDS is used again
     }
 }
 
 // Parts of a row joined: a workgroup per row, dpad / 4 threads side by side per part.
-__global__ __launch_bounds__(THREADS) void kv_join_kernel(KvView kv, KvQueries q, KvAttend a, int all_rows, int splits, int tile)
+__global__ __launch_bounds__(THREADS) void kv_join_kernel(KvView kv, KvQueries q, KvAttend a, int row_tiles, int tile_rows, int grid)
 {
     __shared__ float4 sums[THREADS];
-    __shared__ float lsum[THREADS];
+    __shared__ float weight[KV_ATTEND_GRID];
+    __shared__ float red[WAVES], redl[WAVES];
     const int rows = q.new_tokens * q.group;
-    const int r = blockIdx.x % rows, pair = blockIdx.x / rows, h = pair % kv.heads, b = pair / kv.heads;
-    const Deal d = deal(call_tokens(kv, a, b), tile, splits);
-    if (d.used <= 1) return;
-    const int64_t at = (int64_t)pair * splits * all_rows + r;
-    const float *part = a.part, *ml = a.part + (int64_t)a.nseq * kv.heads * splits * all_rows * kv.dpad;
-    const int cols = kv.dpad >> 2, groups = THREADS / cols, col = threadIdx.x % cols, grp = threadIdx.x / cols;
+    const int r = blockIdx.x % rows, bh = blockIdx.x / rows, h = bh % kv.heads, b = bh / kv.heads;
+    const Workspace ws = workspace(a.part, 2 * (int64_t)grid, tile_rows, kv.dpad);
+    const Parts parts = ws.parts[(int64_t)bh * row_tiles + r / tile_rows];
+    if (parts.count <= 1) return;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, inside = r % tile_rows;
+    auto row_of = [&](int u) { return (2 * ((int64_t)parts.first + u) + (u == 0 ? 1 : 0)) * tile_rows + inside; };
     float top = NEG;
-    for (int u = 0; u < d.used; ++u) top = fmaxf(top, ml[(at + (int64_t)u * all_rows) * 2]);
-    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int u = tid; u < parts.count; u += THREADS) {
+        const float m = ws.ml[row_of(u) * 2];
+        weight[u] = m;
+        top = fmaxf(top, m);
+    }
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
+    if (lane == 0) red[wave] = top;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) top = fmaxf(top, red[w]);
     float l = 0.0f;
+    for (int u = tid; u < parts.count; u += THREADS) {
+        const float f = top == NEG ? 1.0f : __builtin_amdgcn_exp2f(weight[u] - top);
+        weight[u] = f;
+        l += ws.ml[row_of(u) * 2 + 1] * f;
+    }
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) l += __shfl_xor(l, o, 64);
+    if (lane == 0) redl[wave] = l;
+    __syncthreads();
+    l = 0.0f;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) l += redl[w];
+    const int cols = kv.dpad >> 2, groups = THREADS / cols, col = tid % cols, grp = tid / cols;
+    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
     if (grp < groups) {
-        for (int u = grp; u < d.used; u += groups) {
-            const int64_t row = at + (int64_t)u * all_rows;
-            const float f = top == NEG ? 1.0f : __builtin_amdgcn_exp2f(ml[row * 2] - top);
-            const float4 y = *reinterpret_cast<const float4 *>(part + row * kv.dpad + 4 * col);
+#pragma unroll 4
+        for (int u = grp; u < parts.count; u += groups) {
+            const float f = weight[u];
+            const float4 y = *reinterpret_cast<const float4 *>(ws.sums + row_of(u) * kv.dpad + 4 * col);
             x.x += y.x * f; x.y += y.y * f; x.z += y.z * f; x.w += y.w * f;
-            l += ml[row * 2 + 1] * f;
         }
-        sums[threadIdx.x] = x;
-        lsum[threadIdx.x] = l;
+        sums[tid] = x;
     }
     __syncthreads();
     if (grp) return;
     for (int o = 1; o < groups; ++o) {
         const float4 y = sums[o * cols + col];
         x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w;
-        l += lsum[o * cols + col];
     }
     const int c0 = 4 * col;
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
@@ -545,65 +661,61 @@ __global__ __launch_bounds__(THREADS) void kv_join_kernel(KvView kv, KvQueries q
 }
 
 template <int DP, bool PACKED>
-void launch_rows(const KvView &kv, const KvQueries &q, const KvAttend &a, const KvAttendPlan &p, unsigned blocks, hipStream_t st)
+void launch_rows(const KvView &kv, const KvQueries &q, const KvAttend &a, const KvAttendPlan &p, hipStream_t st)
 {
     const bool wide = q.type == LPQ_TYPE_F32;
     if (p.rows == 16) {
-        if (wide) kv_attend_kernel<DP, PACKED, 1, true><<<blocks, THREADS, 0, st>>>(kv, q, a, p.row_tiles, p.splits);
-        else kv_attend_kernel<DP, PACKED, 1, false><<<blocks, THREADS, 0, st>>>(kv, q, a, p.row_tiles, p.splits);
+        if (wide) kv_attend_kernel<DP, PACKED, 1, true><<<p.grid, THREADS, 0, st>>>(kv, q, a, p.row_tiles, p.least);
+        else kv_attend_kernel<DP, PACKED, 1, false><<<p.grid, THREADS, 0, st>>>(kv, q, a, p.row_tiles, p.least);
     } else {
-        if (wide) kv_attend_kernel<DP, PACKED, 2, true><<<blocks, THREADS, 0, st>>>(kv, q, a, p.row_tiles, p.splits);
-        else kv_attend_kernel<DP, PACKED, 2, false><<<blocks, THREADS, 0, st>>>(kv, q, a, p.row_tiles, p.splits);
+        if (wide) kv_attend_kernel<DP, PACKED, 2, true><<<p.grid, THREADS, 0, st>>>(kv, q, a, p.row_tiles, p.least);
+        else kv_attend_kernel<DP, PACKED, 2, false><<<p.grid, THREADS, 0, st>>>(kv, q, a, p.row_tiles, p.least);
     }
 }
 
 template <int DP>
-void launch_dim(const KvView &kv, const KvQueries &q, const KvAttend &a, const KvAttendPlan &p, unsigned blocks, hipStream_t st)
+void launch_dim(const KvView &kv, const KvQueries &q, const KvAttend &a, const KvAttendPlan &p, hipStream_t st)
 {
-    if (kv.packed) launch_rows<DP, true>(kv, q, a, p, blocks, st);
-    else launch_rows<DP, false>(kv, q, a, p, blocks, st);
+    if (kv.packed) launch_rows<DP, true>(kv, q, a, p, st);
+    else launch_rows<DP, false>(kv, q, a, p, st);
 }
-
-int plan_tile(int dpad) { return dpad <= 128 ? 64 : 32; }
 
 }  // namespace
 
-// Parts of a sequence: enough workgroups for two per CU, of no fewer than a tile per wave, and none longer than 4096 tokens,
-// so that sequences of very different lengths end at about the same time.
-KvAttendPlan kv_attend_plan(const KvView &kv, int64_t nseq, int new_tokens, int group, int64_t tokens)
+// Sequences of up to 1024 tokens get a workgroup per (sequence, head, row tile): joining parts would cost more than it
+// gives.  Otherwise as many workgroups as the chip holds at once, and no fewer than 8 tiles each.
+KvAttendPlan kv_attend_plan(const KvView &kv, int64_t nseq, int new_tokens, int group, int64_t tokens, bool wide)
 {
     KvAttendPlan p;
     const int64_t rows = (int64_t)new_tokens * group;
     p.rows = rows <= 16 ? 16 : 32;
     p.row_tiles = (int)ceil_div(rows, (int64_t)p.rows);
-    const int64_t base = nseq * kv.heads * p.row_tiles, tile = plan_tile(kv.dpad);
-    const int64_t most = ceil_div(tokens, tile * WAVES);
-    int64_t s = ceil_div(int64_t(512), base > 0 ? base : 1);
-    const int64_t longest = ceil_div(tokens, int64_t(4096));
-    if (s < longest) s = longest;
-    if (s > most) s = most;
-    if (base > 0 && s > KV_MAX_BLOCKS / base) s = KV_MAX_BLOCKS / base;
-    if (s > 1024) s = 1024;
-    p.splits = (int)(s < 1 ? 1 : s);
-    const int64_t all = nseq * kv.heads * p.splits * p.row_tiles * p.rows;
-    p.bytes = p.splits > 1 ? (size_t)all * (kv.dpad + 2) * sizeof(float) : 0;
+    const int64_t pairs = nseq * kv.heads * p.row_tiles, tile = tile_tokens(kv.dpad, kv.packed);
+    p.least = 0;
+    p.grid = (unsigned)pairs;
+    p.bytes = 0;
+    if (tokens > 1024) {
+        p.least = 8;
+        const int64_t most = ceil_div(ceil_div(tokens, tile), (int64_t)p.least) * pairs, room = 256 * blocks_per_cu(kv.dpad, kv.packed, p.rows / 16, wide);
+        p.grid = (unsigned)(most < room ? most : room);
+        p.bytes = ((size_t)2 * p.grid * p.rows * (kv.dpad + 2) + (size_t)2 * pairs) * sizeof(float);
+    }
     return p;
 }
 
 hipError_t launch_kv_attend(const KvView &kv, const KvQueries &q, const KvAttend &a, const KvAttendPlan &p, hipStream_t st)
 {
     if (a.nseq <= 0) return hipSuccess;
-    const unsigned blocks = (unsigned)((int64_t)a.nseq * kv.heads * p.row_tiles * p.splits);
     switch (kv.dpad) {
-    case 64: launch_dim<64>(kv, q, a, p, blocks, st); break;
-    case 128: launch_dim<128>(kv, q, a, p, blocks, st); break;
-    case 192: launch_dim<192>(kv, q, a, p, blocks, st); break;
-    default: launch_dim<256>(kv, q, a, p, blocks, st); break;
+    case 64: launch_dim<64>(kv, q, a, p, st); break;
+    case 128: launch_dim<128>(kv, q, a, p, st); break;
+    case 192: launch_dim<192>(kv, q, a, p, st); break;
+    default: launch_dim<256>(kv, q, a, p, st); break;
     }
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess || p.splits <= 1) return e;
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || p.least == 0) return e;
     const unsigned rows = (unsigned)((int64_t)a.nseq * kv.heads * q.new_tokens * q.group);
-    kv_join_kernel<<<rows, THREADS, 0, st>>>(kv, q, a, p.row_tiles * p.rows, p.splits, plan_tile(kv.dpad));
+    kv_join_kernel<<<rows, THREADS, 0, st>>>(kv, q, a, p.row_tiles, p.rows, (int)p.grid);
     return hipGetLastError();
 }
 

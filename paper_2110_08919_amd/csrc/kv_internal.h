@@ -8,6 +8,7 @@ namespace lpq {
 
 enum { KV_MAX_DIM = 256, KV_MIN_PAGE = 16, KV_MAX_PAGE = 256,
        KV_MAX_SELECT_ROWS = 128,      // query rows per key-value head whose summed codes fit two 7-bit digits
+       KV_ATTEND_GRID = 1024,         // most workgroups that share out an attention call: four per CU
        KV_MAX_BLOCKS = 1 << 23 };     // workgroups of a launch: 256 threads each stay below 2^32
 
 // Constants of Equation 1 and the step s = 1 / m, five arrays of [heads][dpad] floats on the device.  Features without
@@ -77,12 +78,14 @@ struct KvAttend {
     float *lse;                      // null or [nseq][new_tokens][heads * group]
     float *part;                     // workspace of kv_attend_plan
 };
-// How a call is shared out: blocks of `rows` query rows, `splits` parts of a sequence at most.
+// How a call is shared out: `row_tiles` tiles of `rows` query rows cover a key-value head's; `grid` workgroups take equal
+// runs of all tiles of tokens, at least `least` each, or (least = 0) one (sequence, head, row tile) each.
 struct KvAttendPlan {
-    int row_tiles, rows, splits;     // row_tiles blocks of `rows` rows each cover the rows of a key-value head
+    int row_tiles, rows, least;
+    unsigned grid;
     size_t bytes;                    // of workspace
 };
-KvAttendPlan kv_attend_plan(const KvView &kv, int64_t nseq, int new_tokens, int group, int64_t tokens);
+KvAttendPlan kv_attend_plan(const KvView &kv, int64_t nseq, int new_tokens, int group, int64_t tokens, bool wide);
 hipError_t launch_kv_attend(const KvView &kv, const KvQueries &q, const KvAttend &a, const KvAttendPlan &plan, hipStream_t st);
 
 #if defined(__HIPCC__)
