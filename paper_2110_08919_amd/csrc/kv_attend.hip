@@ -20,7 +20,10 @@
 // 4 g .. 4 g + 3 of two groups.  A lane owns dpad / 16 neighbouring features of the values: it loads them from the rows
 // of its 8 tokens and gathers the operand of each with byte permutes.  Nothing goes through LDS until the end.  Each wave
 // walks its own tiles of 32 or 64 tokens with the next tile's loads in flight.
+#include <type_traits>
+
 #include "kv_internal.h"
+#include "wave_ops.h"
 
 namespace lpq {
 
@@ -48,77 +51,74 @@ __host__ __device__ constexpr int blocks_per_cu(int dpad, bool packed, int rt, b
 {
     if (dpad > 128) return rt == 1 ? 2 : 1;
     if (rt > 1 && wide && packed && dpad > 64) return 1;
-    if (rt > 1 || (wide && dpad > 64)) return 2;
+    if (rt > 1) return 2;
     return wide || (packed && dpad > 64) ? 3 : 4;
 }
 
 // Positions of sequence b that exist, and tiles of tokens a call goes through for it: at least one, so that a sequence
 // without tokens has its zeros written too.
-__device__ __forceinline__ int64_t length_of(const KvView &kv, const KvAttend &a, int b)
+__device__ __forceinline__ int length_of(const KvView &kv, const KvAttend &a, int len)
 {
-    const int64_t len = uniform(a.lengths)[b], room = (int64_t)a.table_pages << kv.page_shift;
+    const int room = a.table_pages << kv.page_shift;       // below 2^31
     return len < 0 ? 0 : (len > room ? room : len);
 }
-__device__ __forceinline__ int tiles_of(const KvView &kv, const KvAttend &a, int b, int tile)
+__device__ __forceinline__ int tiles_of(const KvView &kv, const KvAttend &a, int given, int tile)
 {
-    int64_t len = length_of(kv, a, b);
-    if (a.chosen && len > 0) len = (int64_t)a.n_select << kv.page_shift;
-    const int64_t tiles = (len + tile - 1) / tile;
-    return tiles < 1 ? 1 : (int)tiles;
+    int len = length_of(kv, a, given);
+    if (a.chosen && len > 0) len = a.n_select << kv.page_shift;
+    const int tiles = (int)(((unsigned)len + tile - 1) / tile);
+    return tiles < 1 ? 1 : tiles;
 }
 
 // The tiles of all (sequence, head, row tile) one behind the other are dealt to the workgroups in equal runs.  A run ends
 // where it ends: what a workgroup has of a pair that began before its run or goes on after it is a part, at most two
-// per workgroup, and kv_join_kernel joins a pair's parts.
+// per workgroup, and kv_join_kernel joins a pair's parts.  Fewer than 2^31 tiles (kv_attend_plan).
 struct Place {
     int b, pair, tile, tiles;      // sequence, (head, row tile) of it, tile of that, tiles of the sequence
-    int64_t run;                   // tiles per workgroup
+    int run;                       // tiles per workgroup
 };
 // Where a pair's parts are: part 0 in slot 2 first + 1, part u > 0 in slot 2 (first + u).
 struct Parts {
     int first, count;
 };
-__device__ __forceinline__ bool first_place(const KvView &kv, const KvAttend &a, int pairs, int tile, int least, int64_t *scan, Place *shared,
-                                            Place &out)
+// Every wave for itself: a lane adds up some neighbouring sequences, the lanes' sums are scanned, the lane whose sequences
+// hold the run's first tile finds it.
+__device__ __forceinline__ bool first_place(const KvView &kv, const KvAttend &a, int pairs, int tile, int least, Place &out)
 {
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int per = (a.nseq + THREADS - 1) / THREADS, b0 = tid * per, b1 = b0 + per < a.nseq ? b0 + per : a.nseq;
-    int64_t mine = 0;
-    for (int b = b0; b < b1; ++b) mine += (int64_t)tiles_of(kv, a, b, tile) * pairs;
-    int64_t upto = mine;
+    const int lane = threadIdx.x & 63;
+    const int per = (a.nseq + 63) / 64, b0 = lane * per, b1 = b0 + per < a.nseq ? b0 + per : a.nseq;
+    unsigned mine = 0;
+#pragma unroll 4
+    for (int b = b0; b < b1; ++b) mine += (unsigned)tiles_of(kv, a, a.lengths[b], tile);
+    unsigned upto = mine;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
-        const int64_t t = __shfl_up(upto, o, 64);
+        const unsigned t = __shfl_up(upto, o, 64);
         if (lane >= o) upto += t;
     }
-    if (lane == 63) scan[wave] = upto;
-    __syncthreads();
-    int64_t total = 0;
-#pragma unroll
-    for (int w = 0; w < WAVES; ++w) {
-        if (w < wave) upto += scan[w];
-        total += scan[w];
-    }
-    int64_t run = (total + gridDim.x - 1) / gridDim.x;
-    if (run < least) run = least;
-    const int64_t from = run * blockIdx.x;
-    if (from >= total) return false;
-    if (from >= upto - mine && from < upto) {       // one thread
-        int64_t left = from - (upto - mine);
-        int b = b0, tiles = 1;
+    const unsigned total = (unsigned)__builtin_amdgcn_readlane((int)upto, 63) * pairs;
+    unsigned run = __builtin_amdgcn_readfirstlane((int)((total + gridDim.x - 1) / gridDim.x));
+    if (run < (unsigned)least) run = least;
+    const uint64_t from64 = (uint64_t)run * blockIdx.x;
+    if (from64 >= total) return false;
+    const unsigned from = (unsigned)from64;
+    const int who = __ffsll((unsigned long long)__ballot(from < upto * pairs)) - 1;      // the first lane that reaches beyond it
+    unsigned left = from - (upto - mine) * pairs;
+    int b = b0, tiles = 1;
+    if (lane == who) {
         for (; b < b1; ++b) {
-            tiles = tiles_of(kv, a, b, tile);
-            if (left < (int64_t)tiles * pairs) break;
-            left -= (int64_t)tiles * pairs;
+            tiles = tiles_of(kv, a, a.lengths[b], tile);
+            if (left < (unsigned)tiles * pairs) break;
+            left -= (unsigned)tiles * pairs;
         }
-        shared->b = b;
-        shared->pair = (int)(left / tiles);
-        shared->tile = (int)(left % tiles);
-        shared->tiles = tiles;
     }
-    __syncthreads();
-    out = *shared;
-    out.run = run;
+    out.b = __builtin_amdgcn_readlane(b, who);
+    out.tiles = __builtin_amdgcn_readlane(tiles, who);
+    left = __builtin_amdgcn_readlane((int)left, who);
+    // (divisions leave their results in vector registers)
+    out.pair = __builtin_amdgcn_readfirstlane((int)(left / (unsigned)out.tiles));
+    out.tile = (int)left - out.pair * out.tiles;
+    out.run = (int)run;
     return true;
 }
 
@@ -191,6 +191,29 @@ __host__ __device__ __forceinline__ Workspace workspace(float *p, int64_t slots,
     return w;
 }
 
+// Over the 8, 16 or 32 neighbouring lanes of a row, in all of them.
+template <int LR>
+__device__ __forceinline__ float row_max(float v)
+{
+    auto with = [&](int t) { v = fmaxf(v, __builtin_bit_cast(float, t)); };
+    with(dpp_move<DPP_XOR1>(__builtin_bit_cast(int, v)));
+    with(dpp_move<DPP_XOR2>(__builtin_bit_cast(int, v)));
+    with(dpp_move<DPP_HALF_MIRROR>(__builtin_bit_cast(int, v)));
+    if (LR >= 16) with(dpp_move<DPP_ROW_MIRROR>(__builtin_bit_cast(int, v)));
+    if (LR >= 32) v = fmaxf(v, __shfl_xor(v, 16, 64));
+    return v;
+}
+template <int LR>
+__device__ __forceinline__ int row_sum_of(int v)
+{
+    v += dpp_move<DPP_XOR1>(v);
+    v += dpp_move<DPP_XOR2>(v);
+    v += dpp_move<DPP_HALF_MIRROR>(v);
+    if (LR >= 16) v += dpp_move<DPP_ROW_MIRROR>(v);
+    if (LR >= 32) v += __shfl_xor(v, 16, 64);
+    return v;
+}
+
 template <int DP, bool PACKED, int RT, bool WIDE>
 __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, WIDE)) void kv_attend_kernel(KvView kv, KvQueries q, KvAttend a, int row_tiles,
                                                                                        int least)
@@ -204,8 +227,6 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, WIDE)) void 
     __shared__ __align__(16) int8_t digits[ND][16 * RT][DP + 16];
     __shared__ float row_scale[16 * RT], row_shift[16 * RT];
     __shared__ int row_sum[ND][16 * RT];
-    __shared__ int64_t scan[WAVES];
-    __shared__ Place shared;
 
     const int lane0 = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int pairs = kv.heads * row_tiles, rows = q.new_tokens * q.group;
@@ -213,24 +234,27 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, WIDE)) void 
     const Workspace ws = workspace(a.part, 2 * (int64_t)gridDim.x, 16 * RT, DP);
     Place at;
     if (least == 0) {            // a workgroup per pair
-        at.b = blockIdx.x / pairs;
-        at.pair = blockIdx.x % pairs;
+        at.b = __builtin_amdgcn_readfirstlane(blockIdx.x / pairs);
+        at.pair = blockIdx.x - at.b * pairs;
         at.tile = 0;
-        at.tiles = tiles_of(kv, a, at.b, TOK);
+        at.tiles = tiles_of(kv, a, uniform(a.lengths)[at.b], TOK);
         at.run = at.tiles;
-    } else if (!first_place(kv, a, pairs, TOK, least, scan, &shared, at)) {
+    } else if (!first_place(kv, a, pairs, TOK, least, at)) {
         return;
     }
-    const int64_t run = at.run;
-    int64_t left = run;
-    int b = __builtin_amdgcn_readfirstlane(at.b), pair = __builtin_amdgcn_readfirstlane(at.pair);
-    int start = __builtin_amdgcn_readfirstlane(at.tile), tiles = __builtin_amdgcn_readfirstlane(at.tiles);
+    const int run = at.run;
+    int left = run, b = at.b, pair = at.pair, start = at.tile, tiles = at.tiles;
 
     for (;;) {
-        // ---- tiles [start, end) of a pair
-        const int h = pair / row_tiles, row0 = (pair % row_tiles) * 16 * RT;
-        const int end = left < tiles - start ? start + (int)left : tiles;
-        const int64_t len = length_of(kv, a, b);
+        // ---- tiles [start, end) of a pair; all lanes have the same, and scalar registers hold it
+        b = __builtin_amdgcn_readfirstlane(b);
+        pair = __builtin_amdgcn_readfirstlane(pair);
+        start = __builtin_amdgcn_readfirstlane(start);
+        tiles = __builtin_amdgcn_readfirstlane(tiles);
+        left = __builtin_amdgcn_readfirstlane(left);
+        const int h = __builtin_amdgcn_readfirstlane(pair / row_tiles), row0 = (pair - h * row_tiles) * 16 * RT;
+        const int end = left < tiles - start ? start + left : tiles;
+        const int len = length_of(kv, a, uniform(a.lengths)[b]);
         const Uniform table = uniform(a.table + (int64_t)b * a.ld_table);
         const Uniform chosen = uniform(a.chosen + ((int64_t)b * kv.heads + h) * a.n_select);
         int lane = lane0, tid = threadIdx.x;
@@ -238,29 +262,28 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, WIDE)) void 
         const int n = lane & 15, g = lane >> 4;
 
         // Page of the pool and position of group `grp` of the call's tokens; position INT32_MAX where there is none.
-        const int columns = a.chosen ? a.n_select : a.table_pages;
-        auto place = [&](int64_t grp, int &page, int &pos) {
-            const int64_t token = grp * 16;
+        const int columns = a.chosen ? a.n_select : a.table_pages, pool_pages = (int)kv.pages;      // below 2^31
+        auto place = [&](int grp, int &page, int &pos) {
+            const unsigned token = 16u * grp;
             const int want = (int)(token >> kv.page_shift), inside = (int)token & (kv.page - 1);
             bool there = want < columns;
             int column = there ? want : columns - 1;
             if (a.chosen) {
-                column = __builtin_amdgcn_readfirstlane(chosen[column]);
-                there = there && column >= 0 && column < a.table_pages;
+                column = chosen[column];
+                there = there && (unsigned)column < (unsigned)a.table_pages;
                 column = there ? column : 0;
             }
-            const int64_t p = ((int64_t)column << kv.page_shift) + inside;
-            const int id = __builtin_amdgcn_readfirstlane(table[column]);
-            there = there && p < len && id >= 0 && id < kv.pages;
+            const int p = (column << kv.page_shift) + inside, id = table[column];
+            there = there && p < len && (unsigned)id < (unsigned)pool_pages;
             page = there ? id : 0;
-            pos = there ? (int)p : INT32_MAX;
+            pos = there ? p : INT32_MAX;
         };
         struct Where { int64_t base[TG]; int pos[TG]; };
         auto find = [&](int tile, Where &w) {
 #pragma unroll
             for (int tg = 0; tg < TG; ++tg) {
                 int page;
-                place((int64_t)tile * TG + tg, page, w.pos[tg]);
+                place(tile * TG + tg, page, w.pos[tg]);
                 const int row = w.pos[tg] & (kv.page - 1) & ~15;       // of page 0 where there is none
                 w.base[tg] = ((int64_t)page * kv.heads + h) * head_bytes + (int64_t)row * RB;
             }
@@ -292,7 +315,17 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, WIDE)) void 
             }
         };
 
-        // The first tile's loads are under way while the queries are made ready.
+        // ---- what memory has to bring, all of it asked for before any is used: queries (LR lanes per row, 8 features each), the
+        // wave's first tile
+        constexpr int LR = DP <= 64 ? 8 : DP <= 128 ? 16 : 32, PASS = THREADS / LR, PASSES = (16 * RT + PASS - 1) / PASS;
+        Raw8 raw[PASSES];
+#pragma unroll
+        for (int i = 0; i < PASSES; ++i) {
+            const int r16 = i * PASS + tid / LR, r = row0 + r16, c0 = 8 * (tid % LR);
+            const bool on = r16 < 16 * RT && r < rows && c0 < DP;
+            const int64_t qat = (int64_t)b * q.ld_seq + (int64_t)(r / q.group) * q.ld_token + (int64_t)(h * q.group + r % q.group) * q.ld_head;
+            raw[i] = kv_load8_raw(q.p, q.type, on ? qat + c0 : 0, on ? kv.dim - c0 : 0, q.vec);
+        }
         int tile = start + wave;
         Where now, next;
         find(tile, now);
@@ -302,35 +335,32 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, WIDE)) void 
             load_values(now);
         }
 
-        // ---- queries: steps folded in, digits; LR lanes per row, 8 features each
-        constexpr int LR = DP <= 64 ? 8 : DP <= 128 ? 16 : 32;
+        // ---- queries: steps folded in, digits
+        const int qc = tid % LR, qc0 = 8 * qc < DP ? 8 * qc : 0;
+        float step[8];
+        kv_load_floats8(kv.key.s + h * DP + qc0, step);
 #pragma unroll
-        for (int r0 = 0; r0 < 16 * RT; r0 += THREADS / LR) {
-            const int r16 = r0 + tid / LR, r = row0 + r16, c = tid % LR, c0 = 8 * c;
-            if (r0 + THREADS / LR > 16 * RT && r16 >= 16 * RT) break;        // (whole waves)
-            const bool on = r < rows && c0 < DP;
-            const int64_t qat = (int64_t)b * q.ld_seq + (int64_t)(r / q.group) * q.ld_token + (int64_t)(h * q.group + r % q.group) * q.ld_head;
-            float v[8], offset = 0.0f, most = 0.0f;
-            kv_load8(q.p, q.type, on ? qat + c0 : 0, on ? kv.dim - c0 : 0, q.vec, v);
-            const float *step = kv.key.s + h * DP + (c0 < DP ? c0 : 0), *k = kv.key.k + h * DP + (c0 < DP ? c0 : 0);
+        for (int i = 0; i < PASSES; ++i) {
+            const int r16 = i * PASS + tid / LR;
+            float v[8], most = 0.0f;
+            kv_floats8(raw[i], q.type, v);
             if (a.lse) {
+                float offset = 0.0f;
+                const float *k = kv.key.k + h * DP + qc0;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) offset += v[e] * (k[e] + 0.5f * step[e]);
+#pragma unroll
+                for (int o = 1; o < LR; o <<= 1) offset += __shfl_xor(offset, o, 64);
+                if (qc == 0 && r16 < 16 * RT) row_shift[r16] = offset * a.scale;
             }
-            int bad = 0;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 v[e] *= step[e];
-                most = fmaxf(most, fabsf(v[e]));
-                bad |= !(fabsf(v[e]) <= 3.402823466e38f);
+                const float x = fabsf(v[e]);
+                most = fmaxf(most, x <= 3.402823466e38f ? x : INFINITY);     // a NaN counts as infinite
             }
-#pragma unroll
-            for (int o = 1; o < LR; o <<= 1) {
-                most = fmaxf(most, __shfl_xor(most, o, 64));
-                offset += __shfl_xor(offset, o, 64);
-                bad |= __shfl_xor(bad, o, 64);
-            }
-            const bool use = !bad && most > 1e-30f;      // below that QMAX / most leaves the range of binary32, and scores are 0
+            most = row_max<LR>(most);
+            const bool bad = most == INFINITY, use = !bad && most > 1e-30f;  // below that QMAX / most leaves the range of binary32, and scores are 0
             const float f = use ? QMAX / most : 0.0f;
             int8_t d[ND][8];
             int dsum[ND];
@@ -355,25 +385,21 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, WIDE)) void 
             for (int dd = 0; dd < ND; ++dd) {
                 uint32_t w[2];
                 __builtin_memcpy(w, d[dd], 8);
-                if (c0 < DP) {
+                if (8 * qc < DP && r16 < 16 * RT) {
                     int8_t *row = digits[dd][r16];
                     if (PACKED) {
-                        *reinterpret_cast<uint32_t *>(row + 16 * (c >> 1) + 4 * (c & 1)) = w[0];
-                        *reinterpret_cast<uint32_t *>(row + 16 * (c >> 1) + 8 + 4 * (c & 1)) = w[1];
+                        *reinterpret_cast<uint32_t *>(row + 16 * (qc >> 1) + 4 * (qc & 1)) = w[0];
+                        *reinterpret_cast<uint32_t *>(row + 16 * (qc >> 1) + 8 + 4 * (qc & 1)) = w[1];
                     } else {
-                        *reinterpret_cast<uint2 *>(row + c0) = make_uint2(w[0], w[1]);
+                        *reinterpret_cast<uint2 *>(row + 8 * qc) = make_uint2(w[0], w[1]);
                     }
                 }
                 if (PACKED) {
-#pragma unroll
-                    for (int o = 1; o < LR; o <<= 1) dsum[dd] += __shfl_xor(dsum[dd], o, 64);
-                    if (c == 0) row_sum[dd][r16] = dsum[dd];
+                    const int all = row_sum_of<LR>(dsum[dd]);
+                    if (qc == 0 && r16 < 16 * RT) row_sum[dd][r16] = all;
                 }
             }
-            if (c == 0) {
-                row_scale[r16] = bad ? NAN : (use ? most / QMAX * a.scale * 1.44269504088896f : 0.0f);
-                row_shift[r16] = offset * a.scale;
-            }
+            if (qc == 0 && r16 < 16 * RT) row_scale[r16] = bad ? NAN : (use ? most / QMAX * a.scale * 1.44269504088896f : 0.0f);
         }
         __syncthreads();
         v4i qd[RT][ND][NS];      // lane (n, g): features 64 st + 16 g .. + 15 of row n
@@ -392,11 +418,10 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, WIDE)) void 
             m[rt] = NEG;
             l[rt] = 0.0f;
             const int r = row0 + rt * 16 + n;
-            const int64_t see = len - q.new_tokens + r / q.group;
-            last[rt] = r < rows ? (int)(see < -1 ? -1 : see) : -1;
+            const int see = len - q.new_tokens + r / q.group;
+            last[rt] = r < rows ? (see < -1 ? -1 : see) : -1;
         }
-        const int64_t least_seen = len - q.new_tokens;       // a tile that ends at or before this position is seen by every row
-        const int seen = (int)(least_seen < -1 ? -1 : least_seen);
+        const int seen = len - q.new_tokens;       // a tile that ends at or before this position is seen by every row
 
         v4f acc[RT][NT];
 #pragma unroll
@@ -405,9 +430,10 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, WIDE)) void 
             for (int t = 0; t < NT; ++t) acc[rt][t] = v4f{0.f, 0.f, 0.f, 0.f};
 
         // ---- the wave's tiles: the next tile's keys are asked for as soon as this one's are used up, its values likewise
-        for (; tile < end; tile += WAVES) {
-            const bool more = tile + WAVES < end;
-            if (more) find(tile + WAVES, next);
+        // (the last one apart: loads that every turn of the loop makes are waited for one kind at a time)
+        auto step_through = [&](auto more_) {
+            constexpr bool more = decltype(more_)::value;
+            if constexpr (more) find(tile + WAVES, next);
             bool part = false;
 #pragma unroll
             for (int tg = 0; tg < TG; ++tg) part |= now.pos[tg] > seen - 15;     // also where a group does not count
@@ -437,7 +463,7 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, WIDE)) void 
                         else s[rt][tg][j] = (float)(sum[0][j] * 128 + sum[1][j]) * rs[rt];
                     }
                 }
-            if (more) load_keys(next);
+            if constexpr (more) load_keys(next);
             v8h w[RT][NP][TG / 2];
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt) {
@@ -499,8 +525,14 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, WIDE)) void 
                         for (int p = 0; p < NP; ++p)
                             acc[rt][f] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, w[rt][p][half], acc[rt][f], 0, 0, 0);
                 }
-            if (more) load_values(next);
-            now = next;
+            if constexpr (more) {
+                load_values(next);
+                now = next;
+            }
+        };
+        if (tile < end) {
+            for (; tile + WAVES < end; tile += WAVES) step_through(std::true_type());
+            step_through(std::false_type());
         }
         asm volatile("s_nop 15");      // the last matrix results are read in other blocks of code
 
@@ -518,7 +550,7 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, WIDE)) void 
         const bool whole = start == 0 && end == tiles;
         const int64_t slot = 2 * (int64_t)blockIdx.x + (start == 0 ? 1 : 0);
         if (least != 0 && start == 0 && threadIdx.x == 0)
-            ws.parts[(int64_t)b * pairs + pair] = {(int)blockIdx.x, 1 + (int)((tiles - end + run - 1) / run)};
+            ws.parts[(int64_t)b * pairs + pair] = {(int)blockIdx.x, 1 + (int)(((unsigned)(tiles - end) + run - 1) / run)};
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
             float top = NEG;
@@ -584,7 +616,7 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, WIDE)) void 
         if (end == tiles && ++pair == pairs) {
             pair = 0;
             if (++b >= a.nseq) return;
-            tiles = __builtin_amdgcn_readfirstlane(tiles_of(kv, a, b, TOK));
+            tiles = tiles_of(kv, a, uniform(a.lengths)[b], TOK);
         }
         start = 0;
         __syncthreads();               // LDS is used again
@@ -694,9 +726,10 @@ KvAttendPlan kv_attend_plan(const KvView &kv, int64_t nseq, int new_tokens, int 
     p.least = 0;
     p.grid = (unsigned)pairs;
     p.bytes = 0;
-    if (tokens > 1024) {
+    const int64_t tiles = ceil_div(tokens, tile);
+    if (tokens > 1024 && pairs * tiles < (int64_t(1) << 31)) {      // (beyond that there are pairs enough)
         p.least = 8;
-        const int64_t most = ceil_div(ceil_div(tokens, tile), (int64_t)p.least) * pairs, room = 256 * blocks_per_cu(kv.dpad, kv.packed, p.rows / 16, wide);
+        const int64_t most = ceil_div(tiles, (int64_t)p.least) * pairs, room = 256 * blocks_per_cu(kv.dpad, kv.packed, p.rows / 16, wide);
         p.grid = (unsigned)(most < room ? most : room);
         p.bytes = ((size_t)2 * p.grid * p.rows * (kv.dpad + 2) + (size_t)2 * pairs) * sizeof(float);
     }

@@ -89,37 +89,65 @@ KvAttendPlan kv_attend_plan(const KvView &kv, int64_t nseq, int new_tokens, int 
 hipError_t launch_kv_attend(const KvView &kv, const KvQueries &q, const KvAttend &a, const KvAttendPlan &plan, hipStream_t st);
 
 #if defined(__HIPCC__)
-// 8 consecutive features as floats; those at or past `left` are 0.
+// 8 consecutive features as they lie in memory, to be converted once they are there; those at or past `left` are 0.
+struct Raw8 {
+    uint4 a, b;      // a 16-bit type: the first four words
+};
+__device__ __forceinline__ Raw8 kv_load8_raw(const void *base, int type, int64_t at, int left, bool vec)
+{
+    Raw8 r = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
+    if (type == LPQ_TYPE_F32) {
+        const uint32_t *p = static_cast<const uint32_t *>(base) + at;
+        if (vec && left >= 8) {
+            r.a = *reinterpret_cast<const uint4 *>(p);
+            r.b = *reinterpret_cast<const uint4 *>(p + 4);
+        } else {
+            auto word = [&](int e) { return e < left ? p[e] : 0u; };
+            r.a = make_uint4(word(0), word(1), word(2), word(3));
+            r.b = make_uint4(word(4), word(5), word(6), word(7));
+        }
+    } else {
+        const uint16_t *p = static_cast<const uint16_t *>(base) + at;
+        if (vec && left >= 8) {
+            r.a = *reinterpret_cast<const uint4 *>(p);
+        } else {
+            auto word = [&](int e) {
+                return (e < left ? (uint32_t)p[e] : 0u) | (e + 1 < left ? (uint32_t)p[e + 1] << 16 : 0u);
+            };
+            r.a = make_uint4(word(0), word(2), word(4), word(6));
+        }
+    }
+    return r;
+}
+__device__ __forceinline__ void kv_floats8(const Raw8 &r, int type, float *v)
+{
+    const uint32_t w[8] = {r.a.x, r.a.y, r.a.z, r.a.w, r.b.x, r.b.y, r.b.z, r.b.w};
+    if (type == LPQ_TYPE_F32) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = __builtin_bit_cast(float, w[e]);
+    } else if (type == LPQ_TYPE_BF16) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            v[2 * e] = __builtin_bit_cast(float, w[e] << 16);
+            v[2 * e + 1] = __builtin_bit_cast(float, w[e] & 0xffff0000u);
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            v[2 * e] = (float)__builtin_bit_cast(_Float16, (uint16_t)w[e]);
+            v[2 * e + 1] = (float)__builtin_bit_cast(_Float16, (uint16_t)(w[e] >> 16));
+        }
+    }
+}
 __device__ __forceinline__ void kv_load8(const void *base, int type, int64_t at, int left, bool vec, float *v)
 {
-    if (type == LPQ_TYPE_F32) {
-        const float *p = static_cast<const float *>(base) + at;
-        if (vec && left >= 8) {
-            const float4 a = *reinterpret_cast<const float4 *>(p), b = *reinterpret_cast<const float4 *>(p + 4);
-            v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
-            v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-        } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = e < left ? p[e] : 0.0f;
-        }
-        return;
-    }
-    const uint16_t *p = static_cast<const uint16_t *>(base) + at;
-    uint16_t h[8];
-    if (vec && left >= 8) {
-        const uint4 w = *reinterpret_cast<const uint4 *>(p);
-        __builtin_memcpy(h, &w, 16);
-    } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) h[e] = e < left ? p[e] : (uint16_t)0;
-    }
-    if (type == LPQ_TYPE_BF16) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = __builtin_bit_cast(float, (uint32_t)h[e] << 16);
-    } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = (float)__builtin_bit_cast(_Float16, h[e]);
-    }
+    kv_floats8(kv_load8_raw(base, type, at, left, vec), type, v);
+}
+__device__ __forceinline__ void kv_load_floats8(const float *p, float *v)
+{
+    const float4 a = *reinterpret_cast<const float4 *>(p), b = *reinterpret_cast<const float4 *>(p + 4);
+    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+    v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
 }
 
 // 16-bit image of v in a 16-bit type, rounded to nearest even.
