@@ -120,13 +120,6 @@ static int check_places(const lpq_kv *kv, int64_t nseq, const int32_t *table_dev
 
 static int element_bytes(int type) { return type == LPQ_TYPE_F32 ? 4 : type == LPQ_TYPE_F16 || type == LPQ_TYPE_BF16 ? 2 : 0; }
 
-// Whether 8 features starting at any multiple of 8 are aligned to 16 bytes for all rows.
-static bool aligned(const void *p, int type, int64_t a, int64_t b, int64_t c)
-{
-    const int64_t unit = 16 / element_bytes(type);
-    return (uintptr_t)p % 16 == 0 && a % unit == 0 && b % unit == 0 && c % unit == 0;
-}
-
 constexpr int64_t MAX_STRIDE = int64_t(1) << 40;
 
 // Whether runs of `dim` elements, three axes of them, lie apart from each other, whichever axis is the outer one.
@@ -165,8 +158,8 @@ static int kv_rows(const lpq_kv *kv, const void *k, int64_t ldk_token, int64_t l
         if (n > 0 && !disjoint(dim, {{{s[0], n}, {s[1], heads}, {0, 1}}}))
             return kv_fail(LPQ_EINVAL, "strides %lld, %lld of rows [n][heads][%lld] overlap", (long long)s[0], (long long)s[1], (long long)dim);
     }
-    *kr = {const_cast<void *>(k), strides[0][0], strides[0][1], type, aligned(k, type, strides[0][0], strides[0][1], 0)};
-    *vr = {const_cast<void *>(v), strides[1][0], strides[1][1], type, aligned(v, type, strides[1][0], strides[1][1], 0)};
+    *kr = {const_cast<void *>(k), strides[0][0], strides[0][1], type};
+    *vr = {const_cast<void *>(v), strides[1][0], strides[1][1], type};
     *pl = {first, starts, table, ld_table, n, (int)nseq, (int)table_pages};
     return LPQ_OK;
 }
@@ -219,7 +212,7 @@ static int kv_queries(const lpq_kv *kv, const void *q, int64_t ld_seq, int64_t l
     if (nseq <= 1) ld_seq = 0;             // a stride over one element means nothing
     if (new_tokens == 1) ld_token = 0;
     if (q_heads == 1) ld_head = 0;
-    *out = {q, ld_seq, ld_token, ld_head, type, new_tokens, q_heads / heads, aligned(q, type, ld_seq, ld_token, ld_head)};
+    *out = {q, ld_seq, ld_token, ld_head, type, new_tokens, q_heads / heads};
     return LPQ_OK;
 }
 
@@ -293,8 +286,7 @@ extern "C" int lpq_kv_attend(const lpq_kv *kv, const void *q_dev, int64_t ldq_se
     if (plan.bytes && (!workspace_dev || (uintptr_t)workspace_dev % 256)) return kv_fail(LPQ_EINVAL, "workspace null or not 256-byte aligned");
     if (workspace_bytes < plan.bytes) return kv_fail(LPQ_ERANGE, "workspace of %zu bytes, %zu needed", workspace_bytes, plan.bytes);
     const KvAttend a = {lengths_dev, table_dev, ld_table, (int)nseq, (int)table_pages, chosen_dev, n_select, scale, out_dev, ldo_seq,
-                        ldo_token, ldo_head, aligned(out_dev, type, ldo_seq, ldo_token, ldo_head), lse_dev,
-                        static_cast<float *>(workspace_dev)};
+                        ldo_token, ldo_head, lse_dev, static_cast<float *>(workspace_dev)};
     const hipError_t e = launch_kv_attend(kv->view, q, a, plan, (hipStream_t)stream);
     return e == hipSuccess ? LPQ_OK : hip_fail(e, "lpq_kv_attend");
 }

@@ -20,8 +20,6 @@
 // 4 g .. 4 g + 3 of two groups.  A lane owns dpad / 16 neighbouring features of the values: it loads them from the rows
 // of its 8 tokens and gathers the operand of each with byte permutes.  Nothing goes through LDS until the end.  Each wave
 // walks its own tiles of 32 or 64 tokens with the next tile's loads in flight.
-#include <type_traits>
-
 #include "kv_internal.h"
 #include "wave_ops.h"
 
@@ -122,27 +120,47 @@ __device__ __forceinline__ bool first_place(const KvView &kv, const KvAttend &a,
     return true;
 }
 
-// Bytes of a lane's share of a value row.
-template <int BYTES>
-__device__ __forceinline__ void load_share(const uint8_t *p, uint32_t *w)
+// A stretch of memory: what lies beyond its end reads as 0 and is not fetched.
+typedef __amdgpu_buffer_rsrc_t Stretch;
+__device__ __forceinline__ Stretch stretch(const uint8_t *p, int bytes)
 {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(p), 0, bytes, 0x00027000);
+}
+
+typedef uint32_t v2u __attribute__((ext_vector_type(2)));
+typedef uint32_t v3u __attribute__((ext_vector_type(3)));
+typedef uint32_t v4u __attribute__((ext_vector_type(4)));
+
+// Feature number f (0 .. dpad / 16 - 1) of a lane's share of a value row: neighbours, or, where that would be 6 bytes, 8 (4 bytes)
+// from the first 128 features and 4 (2 bytes) from the others.
+template <int DP, bool PACKED>
+__device__ __forceinline__ constexpr int feature_of(int lane16, int f)
+{
+    constexpr int NT = DP / 16;
+    if (PACKED && NT == 12) return f < 8 ? lane16 * 8 + f : 128 + lane16 * 4 + f - 8;
+    return lane16 * NT + f;
+}
+// Bytes of that share, of the row that begins at `at` of the stretch.
+template <int DP, bool PACKED>
+__device__ __forceinline__ void load_share(Stretch s, unsigned at, int lane16, uint32_t *w)
+{
+    constexpr int BYTES = PACKED ? DP / 32 : DP / 16;
     if constexpr (BYTES == 16) {
-        const uint4 t = *reinterpret_cast<const uint4 *>(p);
+        const v4u t = __builtin_amdgcn_raw_buffer_load_b128(s, at + lane16 * 16, 0, 0);
         w[0] = t.x; w[1] = t.y; w[2] = t.z; w[3] = t.w;
     } else if constexpr (BYTES == 12) {
-        const uint3 t = *reinterpret_cast<const uint3 *>(p);
+        const v3u t = __builtin_amdgcn_raw_buffer_load_b96(s, at + lane16 * 12, 0, 0);
         w[0] = t.x; w[1] = t.y; w[2] = t.z;
     } else if constexpr (BYTES == 8) {
-        const uint2 t = *reinterpret_cast<const uint2 *>(p);
+        const v2u t = __builtin_amdgcn_raw_buffer_load_b64(s, at + lane16 * 8, 0, 0);
         w[0] = t.x; w[1] = t.y;
     } else if constexpr (BYTES == 6) {
-        const uint16_t *t = reinterpret_cast<const uint16_t *>(p);
-        w[0] = (uint32_t)t[0] | (uint32_t)t[1] << 16;
-        w[1] = t[2];
+        w[0] = __builtin_amdgcn_raw_buffer_load_b32(s, at + lane16 * 4, 0, 0);
+        w[1] = __builtin_amdgcn_raw_buffer_load_b16(s, at + 64 + lane16 * 2, 0, 0);
     } else if constexpr (BYTES == 4) {
-        w[0] = *reinterpret_cast<const uint32_t *>(p);
+        w[0] = __builtin_amdgcn_raw_buffer_load_b32(s, at + lane16 * 4, 0, 0);
     } else {
-        w[0] = *reinterpret_cast<const uint16_t *>(p);
+        w[0] = __builtin_amdgcn_raw_buffer_load_b16(s, at + lane16 * 2, 0, 0);
     }
 }
 
@@ -150,7 +168,7 @@ __device__ __forceinline__ void load_share(const uint8_t *p, uint32_t *w)
 template <int DP, bool PACKED>
 struct Tile {
     static constexpr int TG = tile_tokens(DP, PACKED) / 16, NS = DP / 64, NT = DP / 16;
-    static constexpr int VB = PACKED ? NT / 2 : NT, VW = (VB + 3) / 4;
+    static constexpr int VW = ((PACKED ? NT / 2 : NT) + 3) / 4;
     uint32_t k[TG][NS][PACKED ? 2 : 4];
     uint32_t v[TG / 2][8][VW];
 };
@@ -219,14 +237,13 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, WIDE)) void 
                                                                                        int least)
 {
     typedef Tile<DP, PACKED> T;
-    constexpr int TG = T::TG, NS = T::NS, NT = T::NT, VB = T::VB, TOK = 16 * TG;
+    constexpr int TG = T::TG, NS = T::NS, NT = T::NT, TOK = 16 * TG;
     constexpr int ND = WIDE ? 3 : 2, NP = WIDE ? 2 : 1, RB = PACKED ? DP / 2 : DP;
     constexpr float QMAX = WIDE ? 2088895.0f : 16319.0f;
     __shared__ float red_m[WAVES][16 * RT], red_l[WAVES][16 * RT];
     __shared__ __align__(16) float sums[WAVES][16][DP + 4];
     __shared__ __align__(16) int8_t digits[ND][16 * RT][DP + 16];
     __shared__ float row_scale[16 * RT], row_shift[16 * RT];
-    __shared__ int row_sum[ND][16 * RT];
 
     const int lane0 = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int pairs = kv.heads * row_tiles, rows = q.new_tokens * q.group;
@@ -255,16 +272,19 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, WIDE)) void 
         const int h = __builtin_amdgcn_readfirstlane(pair / row_tiles), row0 = (pair - h * row_tiles) * 16 * RT;
         const int end = left < tiles - start ? start + left : tiles;
         const int len = length_of(kv, a, uniform(a.lengths)[b]);
-        const Uniform table = uniform(a.table + (int64_t)b * a.ld_table);
-        const Uniform chosen = uniform(a.chosen + ((int64_t)b * kv.heads + h) * a.n_select);
+        const int32_t *table = a.table + (int64_t)b * a.ld_table, *chosen = a.chosen + ((int64_t)b * kv.heads + h) * a.n_select;
         int lane = lane0, tid = threadIdx.x;
         asm volatile("" : "+v"(lane), "+v"(tid));      // nothing that depends on it is worth registers over all of a run
         const int n = lane & 15, g = lane >> 4;
 
-        // Page of the pool and position of group `grp` of the call's tokens; position INT32_MAX where there is none.
+        // Pages.  A lane looks up the page of the pool and the position of one group of 16 tokens, those of the wave's next
+        // PER tiles at once, and again while these are gone through; a tile's come out by lane number.  Position INT32_MAX:
+        // there is none.
+        constexpr int PER = 64 / TG;
         const int columns = a.chosen ? a.n_select : a.table_pages, pool_pages = (int)kv.pages;      // below 2^31
-        auto place = [&](int grp, int &page, int &pos) {
-            const unsigned token = 16u * grp;
+        const int first_tile = start + wave;
+        auto look_up = [&](int turn, int &page, int &pos) {
+            const unsigned token = 16u * ((first_tile + (turn + lane / TG) * WAVES) * TG + lane % TG);
             const int want = (int)(token >> kv.page_shift), inside = (int)token & (kv.page - 1);
             bool there = want < columns;
             int column = there ? want : columns - 1;
@@ -278,29 +298,29 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, WIDE)) void 
             page = there ? id : 0;
             pos = there ? p : INT32_MAX;
         };
+        const int turns = first_tile < end ? (end - first_tile + WAVES - 1) / WAVES : 0;
+        int page_now, pos_now, page_then = 0, pos_then = INT32_MAX;
         struct Where { int64_t base[TG]; int pos[TG]; };
-        auto find = [&](int tile, Where &w) {
+        auto find = [&](int turn, Where &w) {
 #pragma unroll
             for (int tg = 0; tg < TG; ++tg) {
-                int page;
-                place(tile * TG + tg, page, w.pos[tg]);
-                const int row = w.pos[tg] & (kv.page - 1) & ~15;       // of page 0 where there is none
-                w.base[tg] = ((int64_t)page * kv.heads + h) * head_bytes + (int64_t)row * RB;
+                const int from = (turn % PER) * TG + tg, page = __builtin_amdgcn_readlane(page_now, from), pos = __builtin_amdgcn_readlane(pos_now, from);
+                w.pos[tg] = turn < turns ? pos : INT32_MAX;
+                w.base[tg] = ((int64_t)page * kv.heads + h) * head_bytes + (int64_t)((pos & (kv.page - 1) & ~15) * RB);
             }
         };
         T t;
-        const unsigned ko = n * RB + g * (PACKED ? 8 : 16), vo = 4 * g * RB + n * VB;
         auto load_keys = [&](const Where &w) {
 #pragma unroll
             for (int tg = 0; tg < TG; ++tg) {
-                const uint8_t *p = kv.k + w.base[tg];
+                const Stretch rows16 = stretch(kv.k + w.base[tg], w.pos[tg] == INT32_MAX ? 0 : 16 * RB);
 #pragma unroll
                 for (int st = 0; st < NS; ++st) {
                     if constexpr (PACKED) {
-                        const uint2 x = *reinterpret_cast<const uint2 *>(p + ko + 32 * st);
+                        const v2u x = __builtin_amdgcn_raw_buffer_load_b64(rows16, n * RB + g * 8 + 32 * st, 0, 0);
                         t.k[tg][st][0] = x.x; t.k[tg][st][1] = x.y;
                     } else {
-                        const uint4 x = *reinterpret_cast<const uint4 *>(p + ko + 64 * st);
+                        const v4u x = __builtin_amdgcn_raw_buffer_load_b128(rows16, n * RB + g * 16 + 64 * st, 0, 0);
                         t.k[tg][st][0] = x.x; t.k[tg][st][1] = x.y; t.k[tg][st][2] = x.z; t.k[tg][st][3] = x.w;
                     }
                 }
@@ -309,41 +329,39 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, WIDE)) void 
         auto load_values = [&](const Where &w) {
 #pragma unroll
             for (int tg = 0; tg < TG; ++tg) {
-                const uint8_t *p = kv.v + w.base[tg];
+                const Stretch rows16 = stretch(kv.v + w.base[tg], w.pos[tg] == INT32_MAX ? 0 : 16 * RB);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) load_share<VB>(p + vo + j * RB, t.v[tg >> 1][(tg & 1) * 4 + j]);
+                for (int j = 0; j < 4; ++j) load_share<DP, PACKED>(rows16, (4 * g + j) * RB, n, t.v[tg >> 1][(tg & 1) * 4 + j]);
             }
         };
 
-        // ---- what memory has to bring, all of it asked for before any is used: queries (LR lanes per row, 8 features each), the
-        // wave's first tile
+        // ---- what memory has to bring, asked for before any of it is used: queries (LR lanes per row, 8 features each), the wave's
+        // first tile
         constexpr int LR = DP <= 64 ? 8 : DP <= 128 ? 16 : 32, PASS = THREADS / LR, PASSES = (16 * RT + PASS - 1) / PASS;
-        Raw8 raw[PASSES];
-#pragma unroll
-        for (int i = 0; i < PASSES; ++i) {
-            const int r16 = i * PASS + tid / LR, r = row0 + r16, c0 = 8 * (tid % LR);
-            const bool on = r16 < 16 * RT && r < rows && c0 < DP;
-            const int64_t qat = (int64_t)b * q.ld_seq + (int64_t)(r / q.group) * q.ld_token + (int64_t)(h * q.group + r % q.group) * q.ld_head;
-            raw[i] = kv_load8_raw(q.p, q.type, on ? qat + c0 : 0, on ? kv.dim - c0 : 0, q.vec);
-        }
-        int tile = start + wave;
-        Where now, next;
-        find(tile, now);
-        next = now;
-        if (tile < end) {
-            load_keys(now);
-            load_values(now);
-        }
-
-        // ---- queries: steps folded in, digits
         const int qc = tid % LR, qc0 = 8 * qc < DP ? 8 * qc : 0;
+        auto load_queries = [&](int i) {
+            const int r16 = i * PASS + tid / LR, r = row0 + r16;
+            const bool on = r16 < 16 * RT && r < rows && 8 * qc < DP;
+            const int64_t qat = (int64_t)b * q.ld_seq + (int64_t)(r / q.group) * q.ld_token + (int64_t)(h * q.group + r % q.group) * q.ld_head;
+            return kv_load8_raw(q.p, q.type, on ? qat + qc0 : 0, on ? kv.dim - qc0 : 0);
+        };
+        Raw8 raw = load_queries(0);
         float step[8];
         kv_load_floats8(kv.key.s + h * DP + qc0, step);
-#pragma unroll
+        Where now, next;
+        look_up(0, page_now, pos_now);
+        if (turns > PER) look_up(PER, page_then, pos_then);
+        find(0, now);
+        load_keys(now);
+        load_values(now);
+
+        // ---- queries: steps folded in, digits (a loop: what runs once per call costs its fetch from memory, not its instructions)
+#pragma unroll 1
         for (int i = 0; i < PASSES; ++i) {
             const int r16 = i * PASS + tid / LR;
             float v[8], most = 0.0f;
-            kv_floats8(raw[i], q.type, v);
+            kv_floats8(raw, q.type, v);
+            if (i + 1 < PASSES) raw = load_queries(i + 1);
             if (a.lse) {
                 float offset = 0.0f;
                 const float *k = kv.key.k + h * DP + qc0;
@@ -363,9 +381,6 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, WIDE)) void 
             const bool bad = most == INFINITY, use = !bad && most > 1e-30f;  // below that QMAX / most leaves the range of binary32, and scores are 0
             const float f = use ? QMAX / most : 0.0f;
             int8_t d[ND][8];
-            int dsum[ND];
-#pragma unroll
-            for (int dd = 0; dd < ND; ++dd) dsum[dd] = 0;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 // packed rows have the even features of 16 first (low nibbles of 8 bytes), then the odd ones
@@ -373,19 +388,17 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, WIDE)) void 
                 int x = use ? (int)rintf(v[e] * f) : 0;
 #pragma unroll
                 for (int dd = ND - 1; dd > 0; --dd) {
-                    const int up = (x + 64) >> 7, low = x - (up << 7);       // low in -64 .. 63
-                    d[dd][to] = (int8_t)low;
-                    dsum[dd] += low;
+                    const int up = (x + 64) >> 7;
+                    d[dd][to] = (int8_t)(x - (up << 7));                     // -64 .. 63
                     x = up;
                 }
                 d[0][to] = (int8_t)x;
-                dsum[0] += x;
             }
+            if (8 * qc < DP && r16 < 16 * RT) {
 #pragma unroll
-            for (int dd = 0; dd < ND; ++dd) {
-                uint32_t w[2];
-                __builtin_memcpy(w, d[dd], 8);
-                if (8 * qc < DP && r16 < 16 * RT) {
+                for (int dd = 0; dd < ND; ++dd) {
+                    uint32_t w[2];
+                    __builtin_memcpy(w, d[dd], 8);
                     int8_t *row = digits[dd][r16];
                     if (PACKED) {
                         *reinterpret_cast<uint32_t *>(row + 16 * (qc >> 1) + 4 * (qc & 1)) = w[0];
@@ -394,16 +407,11 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, WIDE)) void 
                         *reinterpret_cast<uint2 *>(row + 8 * qc) = make_uint2(w[0], w[1]);
                     }
                 }
-                if (PACKED) {
-                    const int all = row_sum_of<LR>(dsum[dd]);
-                    if (qc == 0 && r16 < 16 * RT) row_sum[dd][r16] = all;
-                }
+                if (qc == 0) row_scale[r16] = bad ? NAN : (use ? most / QMAX * a.scale * (PACKED ? 1.44269504088896f / 16.0f : 1.44269504088896f) : 0.0f);
             }
-            if (qc == 0 && r16 < 16 * RT) row_scale[r16] = bad ? NAN : (use ? most / QMAX * a.scale * 1.44269504088896f : 0.0f);
         }
         __syncthreads();
         v4i qd[RT][ND][NS];      // lane (n, g): features 64 st + 16 g .. + 15 of row n
-        int q0[RT][ND];          // packed keys hold c + 8: what that adds to each sum is taken off at its start
         float rs[RT], m[RT], l[RT];
         int last[RT];            // last position a row sees
 #pragma unroll
@@ -412,7 +420,6 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, WIDE)) void 
             for (int dd = 0; dd < ND; ++dd) {
 #pragma unroll
                 for (int st = 0; st < NS; ++st) qd[rt][dd][st] = *reinterpret_cast<const v4i *>(&digits[dd][rt * 16 + n][64 * st + 16 * g]);
-                q0[rt][dd] = PACKED ? -8 * row_sum[dd][rt * 16 + n] : 0;
             }
             rs[rt] = row_scale[rt * 16 + n];
             m[rt] = NEG;
@@ -430,10 +437,14 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, WIDE)) void 
             for (int t = 0; t < NT; ++t) acc[rt][t] = v4f{0.f, 0.f, 0.f, 0.f};
 
         // ---- the wave's tiles: the next tile's keys are asked for as soon as this one's are used up, its values likewise
-        // (the last one apart: loads that every turn of the loop makes are waited for one kind at a time)
-        auto step_through = [&](auto more_) {
-            constexpr bool more = decltype(more_)::value;
-            if constexpr (more) find(tile + WAVES, next);
+        // (behind the last tile as well, with nothing to fetch: loads that every turn makes are waited for one kind at a time)
+        for (int turn = 0; turn < turns; ++turn) {
+            if ((turn + 1) % PER == 0) {
+                page_now = page_then;
+                pos_now = pos_then;
+                if (turns > turn + 1 + PER) look_up(turn + 1 + PER, page_then, pos_then);
+            }
+            find(turn + 1, next);
             bool part = false;
 #pragma unroll
             for (int tg = 0; tg < TG; ++tg) part |= now.pos[tg] > seen - 15;     // also where a group does not count
@@ -444,13 +455,14 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, WIDE)) void 
                 for (int tg = 0; tg < TG; ++tg) {
                     v4i sum[ND];
 #pragma unroll
-                    for (int dd = 0; dd < ND; ++dd) sum[dd] = v4i{q0[rt][dd], q0[rt][dd], q0[rt][dd], q0[rt][dd]};
+                    for (int dd = 0; dd < ND; ++dd) sum[dd] = v4i{0, 0, 0, 0};
 #pragma unroll
                     for (int st = 0; st < NS; ++st) {
                         v4i kf;
                         if constexpr (PACKED) {
-                            const uint32_t x = t.k[tg][st][0], y = t.k[tg][st][1];
-                            kf = v4i{(int)(x & 0x0f0f0f0fu), (int)(y & 0x0f0f0f0fu), (int)((x >> 4) & 0x0f0f0f0fu), (int)((y >> 4) & 0x0f0f0f0fu)};
+                            // nibbles c + 8 -> bytes 16 c
+                            const uint32_t x = t.k[tg][st][0] ^ 0x88888888u, y = t.k[tg][st][1] ^ 0x88888888u;
+                            kf = v4i{(int)((x << 4) & 0xf0f0f0f0u), (int)((y << 4) & 0xf0f0f0f0u), (int)(x & 0xf0f0f0f0u), (int)(y & 0xf0f0f0f0u)};
                         } else {
                             kf = v4i{(int)t.k[tg][st][0], (int)t.k[tg][st][1], (int)t.k[tg][st][2], (int)t.k[tg][st][3]};
                         }
@@ -463,7 +475,7 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, WIDE)) void 
                         else s[rt][tg][j] = (float)(sum[0][j] * 128 + sum[1][j]) * rs[rt];
                     }
                 }
-            if constexpr (more) load_keys(next);
+            load_keys(next);
             v8h w[RT][NP][TG / 2];
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt) {
@@ -525,14 +537,8 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, WIDE)) void 
                         for (int p = 0; p < NP; ++p)
                             acc[rt][f] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, w[rt][p][half], acc[rt][f], 0, 0, 0);
                 }
-            if constexpr (more) {
-                load_values(next);
-                now = next;
-            }
-        };
-        if (tile < end) {
-            for (; tile + WAVES < end; tile += WAVES) step_through(std::true_type());
-            step_through(std::false_type());
+            load_values(next);
+            now = next;
         }
         asm volatile("s_nop 15");      // the last matrix results are read in other blocks of code
 
@@ -551,17 +557,21 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, WIDE)) void 
         const int64_t slot = 2 * (int64_t)blockIdx.x + (start == 0 ? 1 : 0);
         if (least != 0 && start == 0 && threadIdx.x == 0)
             ws.parts[(int64_t)b * pairs + pair] = {(int)blockIdx.x, 1 + (int)(((unsigned)(tiles - end) + run - 1) / run)};
-#pragma unroll
+#pragma unroll 1
         for (int rt = 0; rt < RT; ++rt) {
             float top = NEG;
 #pragma unroll
             for (int w = 0; w < WAVES; ++w) top = fmaxf(top, red_m[w][rt * 16 + n]);
-            const float f = top == NEG ? 1.0f : __builtin_amdgcn_exp2f(m[rt] - top);
+            const float f = top == NEG ? 1.0f : __builtin_amdgcn_exp2f(red_m[wave][rt * 16 + n] - top);
             if (rt) __syncthreads();
+            auto put = [&](const v4f *x) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
+                for (int j = 0; j < 4; ++j)
 #pragma unroll
-                for (int t = 0; t < NT; ++t) sums[wave][n][(4 * g + j) * NT + t] = acc[rt][t][j] * f;
+                    for (int t_ = 0; t_ < NT; ++t_) sums[wave][n][feature_of<DP, PACKED>(4 * g + j, t_)] = x[t_][j] * f;
+            };
+            if (RT == 1 || rt == 0) put(acc[0]);
+            else put(acc[RT - 1]);
             if (a.lse && start == 0 && wave == 0 && g == 0) {      // of several parts: what every token has, the rest is added when they are joined
                 const int r = row0 + rt * 16 + n;
                 if (r < rows) {
@@ -585,7 +595,7 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, WIDE)) void 
                 const float inv = ll == 0.0f ? 0.0f : 1.0f / ll;
                 const int64_t row = slot * (16 * RT) + rt * 16 + r16;
                 const int64_t out_row = (int64_t)b * a.ldo_seq + (int64_t)(r / q.group) * a.ldo_token + (int64_t)(h * q.group + r % q.group) * a.ldo_head;
-#pragma unroll
+#pragma unroll 1
                 for (int i = 0; i < NS; ++i) {
                     const int c0 = 4 * ((tid & 15) + 16 * i);
                     float x[4] = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -598,7 +608,7 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, WIDE)) void 
                         const float *vs = kv.value.s + h * DP + c0, *vk = kv.value.k + h * DP + c0;
 #pragma unroll
                         for (int e = 0; e < 4; ++e) x[e] = ll == 0.0f ? 0.0f : (x[e] * inv + 0.5f) * vs[e] + vk[e];
-                        kv_store<4>(a.out, q.type, out_row + c0, kv.dim - c0, a.vec_out, x);
+                        kv_store<4>(a.out, q.type, out_row + c0, kv.dim - c0, x);
                     } else {
                         *reinterpret_cast<float4 *>(ws.sums + row * DP + c0) = make_float4(x[0], x[1], x[2], x[3]);
                     }
@@ -685,7 +695,7 @@ __global__ __launch_bounds__(THREADS) void kv_join_kernel(KvView kv, KvQueries q
 #pragma unroll
     for (int e = 0; e < 4; ++e) v[e] = l == 0.0f ? 0.0f : (v[e] * inv + 0.5f) * vs[e] + vk[e];
     const int64_t out_row = (int64_t)b * a.ldo_seq + (int64_t)(r / q.group) * a.ldo_token + (int64_t)(h * q.group + r % q.group) * a.ldo_head;
-    kv_store<4>(a.out, q.type, out_row + c0, kv.dim - c0, a.vec_out, v);
+    kv_store<4>(a.out, q.type, out_row + c0, kv.dim - c0, v);
     if (a.lse && col == 0) {
         const int64_t lat = ((int64_t)b * q.new_tokens + r / q.group) * ((int64_t)kv.heads * q.group) + h * q.group + r % q.group;
         a.lse[lat] = l == 0.0f ? NEG : (top - LIFT + __log2f(l)) * 0.69314718055994531f + a.lse[lat];

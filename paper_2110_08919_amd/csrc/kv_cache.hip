@@ -165,7 +165,7 @@ __global__ __launch_bounds__(KV_THREADS) void kv_write_kernel(KvView kv, KvRows 
 #pragma unroll
                 for (int u = 0; u < KV_ROWS; ++u) {
                     const int t = t0 + u * lanes;
-                    if (t < p.hi) kv_load8(kr.p, kr.type, (p.source + t - p.lo) * kr.ld_token + h * kr.ld_head + c0, left, kr.vec, x[u]);
+                    if (t < p.hi) kv_load8(kr.p, kr.type, (p.source + t - p.lo) * kr.ld_token + h * kr.ld_head + c0, left, x[u]);
                 }
 #pragma unroll
                 for (int u = 0; u < KV_ROWS; ++u) {
@@ -216,7 +216,7 @@ __global__ __launch_bounds__(KV_THREADS) void kv_write_kernel(KvView kv, KvRows 
 #pragma unroll
                 for (int u = 0; u < KV_ROWS; ++u) {
                     const int t = t0 + u * lanes;
-                    if (t < p.hi) kv_load8(vr.p, vr.type, (p.source + t - p.lo) * vr.ld_token + h * vr.ld_head + c0, left, vr.vec, x[u]);
+                    if (t < p.hi) kv_load8(vr.p, vr.type, (p.source + t - p.lo) * vr.ld_token + h * vr.ld_head + c0, left, x[u]);
                 }
 #pragma unroll
                 for (int u = 0; u < KV_ROWS; ++u) {
@@ -276,7 +276,7 @@ __global__ __launch_bounds__(KV_THREADS) void kv_read_kernel(KvView kv, KvRows k
                     for (int e = 0; e < 8; ++e)
                         x[e] = p.page >= 0 ? __fadd_rn(__fmul_rn((float)q[w][u][e] + 0.5f, s[w][e]), k[w][e]) : 0.0f;
                     const KvRows &out = w ? vr : kr;
-                    kv_store<8>(out.p, out.type, row * out.ld_token + h * out.ld_head + c0, left, out.vec, x);
+                    kv_store<8>(out.p, out.type, row * out.ld_token + h * out.ld_head + c0, left, x);
                 }
             }
         }

@@ -34,7 +34,6 @@ struct KvRows {
     void *p;
     int64_t ld_token, ld_head;
     int type;
-    bool vec;    // every run of 8 features that starts at a multiple of 8 is aligned to its load
 };
 
 // Which rows belong to which sequence and where their pages are.
@@ -49,7 +48,6 @@ struct KvQueries {
     const void *p;
     int64_t ld_seq, ld_token, ld_head;
     int type, new_tokens, group;     // group: query heads per key-value head
-    bool vec;
 };
 
 hipError_t launch_kv_constants(const QuantParams &q, int heads, int dim, int dpad, float *out, hipStream_t st);
@@ -74,7 +72,6 @@ struct KvAttend {
     float scale;
     void *out;
     int64_t ldo_seq, ldo_token, ldo_head;
-    bool vec_out;
     float *lse;                      // null or [nseq][new_tokens][heads * group]
     float *part;                     // workspace of kv_attend_plan
 };
@@ -89,27 +86,27 @@ KvAttendPlan kv_attend_plan(const KvView &kv, int64_t nseq, int new_tokens, int 
 hipError_t launch_kv_attend(const KvView &kv, const KvQueries &q, const KvAttend &a, const KvAttendPlan &plan, hipStream_t st);
 
 #if defined(__HIPCC__)
-// 8 consecutive features as they lie in memory, to be converted once they are there; those at or past `left` are 0.
+// 8 consecutive features as they lie in memory, to be converted once they are there; those at or past `left` are 0.  Wide
+// loads whatever the alignment: the hardware takes them at any address of its elements.
 struct Raw8 {
     uint4 a, b;      // a 16-bit type: the first four words
 };
-__device__ __forceinline__ Raw8 kv_load8_raw(const void *base, int type, int64_t at, int left, bool vec)
+__device__ __forceinline__ Raw8 kv_load8_raw(const void *base, int type, int64_t at, int left)
 {
     Raw8 r = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
     if (type == LPQ_TYPE_F32) {
         const uint32_t *p = static_cast<const uint32_t *>(base) + at;
-        if (vec && left >= 8) {
-            r.a = *reinterpret_cast<const uint4 *>(p);
-            r.b = *reinterpret_cast<const uint4 *>(p + 4);
+        if (left >= 8) {
+            __builtin_memcpy(&r, p, 32);
         } else {
             auto word = [&](int e) { return e < left ? p[e] : 0u; };
             r.a = make_uint4(word(0), word(1), word(2), word(3));
-            r.b = make_uint4(word(4), word(5), word(6), word(7));
+            r.b = make_uint4(word(4), word(5), word(6), 0u);
         }
     } else {
         const uint16_t *p = static_cast<const uint16_t *>(base) + at;
-        if (vec && left >= 8) {
-            r.a = *reinterpret_cast<const uint4 *>(p);
+        if (left >= 8) {
+            __builtin_memcpy(&r.a, p, 16);
         } else {
             auto word = [&](int e) {
                 return (e < left ? (uint32_t)p[e] : 0u) | (e + 1 < left ? (uint32_t)p[e + 1] << 16 : 0u);
@@ -139,9 +136,9 @@ __device__ __forceinline__ void kv_floats8(const Raw8 &r, int type, float *v)
         }
     }
 }
-__device__ __forceinline__ void kv_load8(const void *base, int type, int64_t at, int left, bool vec, float *v)
+__device__ __forceinline__ void kv_load8(const void *base, int type, int64_t at, int left, float *v)
 {
-    kv_floats8(kv_load8_raw(base, type, at, left, vec), type, v);
+    kv_floats8(kv_load8_raw(base, type, at, left), type, v);
 }
 __device__ __forceinline__ void kv_load_floats8(const float *p, float *v)
 {
@@ -158,16 +155,15 @@ __device__ __forceinline__ uint16_t kv_to16(float v, int type)
 
 // N (4 or 8) consecutive features out; those at or past `left` are not written.
 template <int N>
-__device__ __forceinline__ void kv_store(void *base, int type, int64_t at, int left, bool vec, const float *v)
+__device__ __forceinline__ void kv_store(void *base, int type, int64_t at, int left, const float *v)
 {
     if (type == LPQ_TYPE_F32) {
         float *p = static_cast<float *>(base) + at;
-        if (vec && left >= N) {
-#pragma unroll
-            for (int e = 0; e < N; e += 4) *reinterpret_cast<float4 *>(p + e) = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
+        if (left >= N) {
+            __builtin_memcpy(p, v, 4 * N);
         } else {
 #pragma unroll
-            for (int e = 0; e < N; ++e)
+            for (int e = 0; e < N - 1; ++e)
                 if (e < left) p[e] = v[e];
         }
         return;
@@ -176,19 +172,11 @@ __device__ __forceinline__ void kv_store(void *base, int type, int64_t at, int l
     uint16_t h[N];
 #pragma unroll
     for (int e = 0; e < N; ++e) h[e] = kv_to16(v[e], type);
-    if (vec && left >= N) {
-        if (N == 8) {
-            uint4 w;
-            __builtin_memcpy(&w, h, 16);
-            *reinterpret_cast<uint4 *>(p) = w;
-        } else {
-            uint2 w;
-            __builtin_memcpy(&w, h, 8);
-            *reinterpret_cast<uint2 *>(p) = w;
-        }
+    if (left >= N) {
+        __builtin_memcpy(p, h, 2 * N);
     } else {
 #pragma unroll
-        for (int e = 0; e < N; ++e)
+        for (int e = 0; e < N - 1; ++e)
             if (e < left) p[e] = h[e];
     }
 }
