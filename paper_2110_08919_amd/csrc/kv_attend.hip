@@ -20,6 +20,8 @@
 // 4 g .. 4 g + 3 of two groups.  A lane owns dpad / 16 neighbouring features of the values: it loads them from the rows
 // of its 8 tokens and gathers the operand of each with byte permutes.  Nothing goes through LDS until the end.  Each wave
 // walks its own tiles of 32 or 64 tokens with the next tile's loads in flight.
+#include <type_traits>
+
 #include "kv_internal.h"
 #include "wave_ops.h"
 
@@ -68,19 +70,36 @@ __device__ __forceinline__ int tiles_of(const KvView &kv, const KvAttend &a, int
     return tiles < 1 ? 1 : tiles;
 }
 
-// The tiles of all (sequence, head, row tile) one behind the other are dealt to the workgroups in equal runs.  A run ends
-// where it ends: what a workgroup has of a pair that began before its run or goes on after it is a part, at most two
-// per workgroup, and kv_join_kernel joins a pair's parts.  Fewer than 2^31 tiles (kv_attend_plan).
+// How the tiles of all (sequence, head, row tile), of all pairs for short, are dealt to the workgroups.
+//   Long calls: one behind the other in equal runs.  A run ends where it ends: what a workgroup has of a pair that began before
+//   its run or goes on after it is a part, at most two per workgroup.
+//   Short calls (runs below CROSSING tiles), where going over to another pair costs as much as the run itself: a workgroup
+//   has one pair or an even part of one.
+// kv_join_kernel joins a pair's parts.  Fewer than 2^31 tiles (kv_attend_plan).
+constexpr unsigned CROSSING = 64;
 struct Place {
     int b, pair, tile, tiles;      // sequence, (head, row tile) of it, tile of that, tiles of the sequence
-    int run;                       // tiles per workgroup
+    int run;                       // tiles of the workgroup
+    int whole;                     // tiles of every workgroup that has a part of this pair, but the last
 };
 // Where a pair's parts are: part 0 in slot 2 first + 1, part u > 0 in slot 2 (first + u).
 struct Parts {
     int first, count;
 };
+__device__ __forceinline__ unsigned wave_scan(unsigned v)     // sums of the lanes up to each
+{
+    auto moved = [](unsigned x, auto ctrl, auto rows) { return (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, decltype(ctrl)::value, decltype(rows)::value, 0xF, false); };
+    typedef std::integral_constant<int, 0xF> all;
+    v += moved(v, std::integral_constant<int, 0x111>(), all());       // 1, 2, 4 and 8 lanes back in a row of 16
+    v += moved(v, std::integral_constant<int, 0x112>(), all());
+    v += moved(v, std::integral_constant<int, 0x114>(), all());
+    v += moved(v, std::integral_constant<int, 0x118>(), all());
+    v += moved(v, std::integral_constant<int, 0x142>(), std::integral_constant<int, 0xA>());     // last lane of the row before
+    v += moved(v, std::integral_constant<int, 0x143>(), std::integral_constant<int, 0xC>());     // last lane of the first half
+    return v;
+}
 // Every wave for itself: a lane adds up some neighbouring sequences, the lanes' sums are scanned, the lane whose sequences
-// hold the run's first tile finds it.
+// hold the workgroup's first tile (or part) finds it.
 __device__ __forceinline__ bool first_place(const KvView &kv, const KvAttend &a, int pairs, int tile, int least, Place &out)
 {
     const int lane = threadIdx.x & 63;
@@ -88,17 +107,22 @@ __device__ __forceinline__ bool first_place(const KvView &kv, const KvAttend &a,
     unsigned mine = 0;
 #pragma unroll 4
     for (int b = b0; b < b1; ++b) mine += (unsigned)tiles_of(kv, a, a.lengths[b], tile);
-    unsigned upto = mine;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const unsigned t = __shfl_up(upto, o, 64);
-        if (lane >= o) upto += t;
-    }
-    const unsigned total = (unsigned)__builtin_amdgcn_readlane((int)upto, 63) * pairs;
-    unsigned run = __builtin_amdgcn_readfirstlane((int)((total + gridDim.x - 1) / gridDim.x));
+    unsigned upto = wave_scan(mine);
+    const unsigned total = (unsigned)__builtin_amdgcn_readlane((int)upto, 63) * pairs, all_pairs = (unsigned)a.nseq * pairs;
+    unsigned run = (total + gridDim.x - 1) / gridDim.x;
+    const bool apart = run < CROSSING && all_pairs < gridDim.x;
+    // apart: every pair rounds its number of parts up by less than one, so that this many tiles to a part fit the grid
+    if (apart) run = (total + gridDim.x - all_pairs - 1) / (gridDim.x - all_pairs);
     if (run < (unsigned)least) run = least;
-    const uint64_t from64 = (uint64_t)run * blockIdx.x;
-    if (from64 >= total) return false;
+    run = __builtin_amdgcn_readfirstlane((int)run);
+    auto weight = [&](unsigned tiles) { return apart ? (tiles + run - 1) / run : tiles; };
+    if (apart) {
+        mine = 0;
+        for (int b = b0; b < b1; ++b) mine += weight((unsigned)tiles_of(kv, a, a.lengths[b], tile));
+        upto = wave_scan(mine);
+    }
+    const uint64_t from64 = apart ? (uint64_t)blockIdx.x : (uint64_t)run * blockIdx.x;
+    if (from64 >= (uint64_t)(unsigned)__builtin_amdgcn_readlane((int)upto, 63) * pairs) return false;
     const unsigned from = (unsigned)from64;
     const int who = __ffsll((unsigned long long)__ballot(from < upto * pairs)) - 1;      // the first lane that reaches beyond it
     unsigned left = from - (upto - mine) * pairs;
@@ -106,17 +130,24 @@ __device__ __forceinline__ bool first_place(const KvView &kv, const KvAttend &a,
     if (lane == who) {
         for (; b < b1; ++b) {
             tiles = tiles_of(kv, a, a.lengths[b], tile);
-            if (left < (unsigned)tiles * pairs) break;
-            left -= (unsigned)tiles * pairs;
+            const unsigned w = weight((unsigned)tiles) * pairs;
+            if (left < w) break;
+            left -= w;
         }
     }
     out.b = __builtin_amdgcn_readlane(b, who);
     out.tiles = __builtin_amdgcn_readlane(tiles, who);
     left = __builtin_amdgcn_readlane((int)left, who);
     // (divisions leave their results in vector registers)
-    out.pair = __builtin_amdgcn_readfirstlane((int)(left / (unsigned)out.tiles));
-    out.tile = (int)left - out.pair * out.tiles;
-    out.run = (int)run;
+    const unsigned each = __builtin_amdgcn_readfirstlane((int)weight((unsigned)out.tiles));
+    out.pair = __builtin_amdgcn_readfirstlane((int)(left / each));
+    out.tile = (int)(left - out.pair * each);
+    out.run = out.whole = (int)run;
+    if (apart) {
+        out.whole = __builtin_amdgcn_readfirstlane((int)((out.tiles + each - 1) / each));      // even parts
+        out.tile *= out.whole;
+        out.run = out.whole < out.tiles - out.tile ? out.whole : out.tiles - out.tile;
+    }
     return true;
 }
 
@@ -255,12 +286,11 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, WIDE)) void 
         at.pair = blockIdx.x - at.b * pairs;
         at.tile = 0;
         at.tiles = tiles_of(kv, a, uniform(a.lengths)[at.b], TOK);
-        at.run = at.tiles;
+        at.run = at.whole = at.tiles;
     } else if (!first_place(kv, a, pairs, TOK, least, at)) {
         return;
     }
-    const int run = at.run;
-    int left = run, b = at.b, pair = at.pair, start = at.tile, tiles = at.tiles;
+    int left = at.run, b = at.b, pair = at.pair, start = at.tile, tiles = at.tiles;
 
     for (;;) {
         // ---- tiles [start, end) of a pair; all lanes have the same, and scalar registers hold it
@@ -556,7 +586,7 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, WIDE)) void 
         const bool whole = start == 0 && end == tiles;
         const int64_t slot = 2 * (int64_t)blockIdx.x + (start == 0 ? 1 : 0);
         if (least != 0 && start == 0 && threadIdx.x == 0)
-            ws.parts[(int64_t)b * pairs + pair] = {(int)blockIdx.x, 1 + (int)(((unsigned)(tiles - end) + run - 1) / run)};
+            ws.parts[(int64_t)b * pairs + pair] = {(int)blockIdx.x, 1 + (int)(((unsigned)(tiles - end) + at.whole - 1) / at.whole)};
 #pragma unroll 1
         for (int rt = 0; rt < RT; ++rt) {
             float top = NEG;
