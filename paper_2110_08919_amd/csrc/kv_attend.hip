@@ -39,10 +39,6 @@ constexpr float NEG = -INFINITY;
 constexpr float HEADROOM = 8.0f;     // how far scores may pass the maximum before it moves (powers of two)
 constexpr float LIFT = 6.0f;         // weights are exp2(t - m + LIFT): at most 2^14, and small ones stay normal fp16
 
-// Memory that no kernel of the call writes, read at addresses all lanes share: scalar loads.
-typedef const __attribute__((address_space(4))) int32_t *Uniform;
-__device__ __forceinline__ Uniform uniform(const int32_t *p) { return (Uniform)(uintptr_t)p; }
-
 // Tokens a wave has in registers: 64 where a row of codes has at
 // most 64 bytes, else 32.
 __host__ __device__ constexpr int tile_tokens(int dpad, bool packed) { return (packed ? dpad / 2 : dpad) <= 64 ? 64 : 32; }
@@ -285,7 +281,7 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, WIDE)) void 
         at.b = __builtin_amdgcn_readfirstlane(blockIdx.x / pairs);
         at.pair = blockIdx.x - at.b * pairs;
         at.tile = 0;
-        at.tiles = tiles_of(kv, a, uniform(a.lengths)[at.b], TOK);
+        at.tiles = tiles_of(kv, a, kv_uniform(a.lengths)[at.b], TOK);
         at.run = at.whole = at.tiles;
     } else if (!first_place(kv, a, pairs, TOK, least, at)) {
         return;
@@ -301,7 +297,7 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, WIDE)) void 
         left = __builtin_amdgcn_readfirstlane(left);
         const int h = __builtin_amdgcn_readfirstlane(pair / row_tiles), row0 = (pair - h * row_tiles) * 16 * RT;
         const int end = left < tiles - start ? start + left : tiles;
-        const int len = length_of(kv, a, uniform(a.lengths)[b]);
+        const int len = length_of(kv, a, kv_uniform(a.lengths)[b]);
         const int32_t *table = a.table + (int64_t)b * a.ld_table, *chosen = a.chosen + ((int64_t)b * kv.heads + h) * a.n_select;
         int lane = lane0, tid = threadIdx.x;
         asm volatile("" : "+v"(lane), "+v"(tid));      // nothing that depends on it is worth registers over all of a run
@@ -373,7 +369,7 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, WIDE)) void 
             const int r16 = i * PASS + tid / LR, r = row0 + r16;
             const bool on = r16 < 16 * RT && r < rows && 8 * qc < DP;
             const int64_t qat = (int64_t)b * q.ld_seq + (int64_t)(r / q.group) * q.ld_token + (int64_t)(h * q.group + r % q.group) * q.ld_head;
-            return kv_load8_raw(q.p, q.type, on ? qat + qc0 : 0, on ? kv.dim - qc0 : 0);
+            return kv_load8_raw(q.p, q.type, qat, qc0, on ? kv.dim : 0);
         };
         Raw8 raw = load_queries(0);
         float step[8];
@@ -656,7 +652,7 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, WIDE)) void 
         if (end == tiles && ++pair == pairs) {
             pair = 0;
             if (++b >= a.nseq) return;
-            tiles = tiles_of(kv, a, uniform(a.lengths)[b], TOK);
+            tiles = tiles_of(kv, a, kv_uniform(a.lengths)[b], TOK);
         }
         start = 0;
         __syncthreads();               // LDS is used again

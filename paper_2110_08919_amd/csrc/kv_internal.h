@@ -9,7 +9,7 @@ namespace lpq {
 enum { KV_MAX_DIM = 256, KV_MIN_PAGE = 16, KV_MAX_PAGE = 256,
        KV_MAX_SELECT_ROWS = 128,      // query rows per key-value head whose summed codes fit two 7-bit digits
        KV_ATTEND_GRID = 1024,         // most workgroups that share out an attention call: four per CU
-       KV_MAX_BLOCKS = 1 << 23 };     // workgroups of a launch: 256 threads each stay below 2^32
+       KV_MAX_BLOCKS = 1 << 22 };     // workgroups of a launch (twice that stays below 2^32 threads of 256 each)
 
 // Constants of Equation 1 and the step s = 1 / m, five arrays of [heads][dpad] floats on the device.  Features without
 // a range (S_e <= S_b) and padding hold S_b = -inf, S_e = inf, m = s = 0: they encode to 0 and read back as k (padding: 0).
@@ -86,39 +86,64 @@ KvAttendPlan kv_attend_plan(const KvView &kv, int64_t nseq, int new_tokens, int 
 hipError_t launch_kv_attend(const KvView &kv, const KvQueries &q, const KvAttend &a, const KvAttendPlan &plan, hipStream_t st);
 
 #if defined(__HIPCC__)
-// 8 consecutive features as they lie in memory, to be converted once they are there; those at or past `left` are 0.  Wide
-// loads whatever the alignment: the hardware takes them at any address of its elements.
+// Memory that no kernel of the call writes, read at addresses all lanes share: scalar loads.
+typedef const __attribute__((address_space(4))) int32_t *KvUniform;
+__device__ __forceinline__ KvUniform kv_uniform(const int32_t *p) { return (KvUniform)(uintptr_t)p; }
+
+// 8 consecutive features c0 .. c0 + 7 of a row of `dim`, as they lie in memory (`row`: element the row begins at), to be
+// converted once they are there; those past the row are 0.  Wide loads whatever the alignment: the hardware takes them at any
+// address of its elements.  The end of a row that is no multiple of 8 is loaded with what lies before it and moved down.
 struct Raw8 {
-    uint4 a, b;      // a 16-bit type: the first four words
+    uint32_t w[8];      // a 16-bit type: the first four
 };
-__device__ __forceinline__ Raw8 kv_load8_raw(const void *base, int type, int64_t at, int left)
+template <int WORDS>
+__device__ __forceinline__ void kv_move_down(uint32_t *w, int words)      // by 0 .. WORDS words, zeros from above
 {
-    Raw8 r = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
+#pragma unroll
+    for (int s = WORDS; s >= 1; s >>= 1)
+#pragma unroll
+        for (int i = 0; i < WORDS; ++i) w[i] = (words & s) ? (i + s < WORDS ? w[i + s] : 0u) : w[i];
+}
+__device__ __forceinline__ Raw8 kv_load8_raw(const void *base, int type, int64_t row, int c0, int dim)
+{
+    Raw8 r = {{0, 0, 0, 0, 0, 0, 0, 0}};
+    const int left = dim - c0, back = left >= 8 ? 0 : 8 - left;
+    if (left <= 0) return r;
     if (type == LPQ_TYPE_F32) {
-        const uint32_t *p = static_cast<const uint32_t *>(base) + at;
-        if (left >= 8) {
-            __builtin_memcpy(&r, p, 32);
+        const uint32_t *p = static_cast<const uint32_t *>(base) + row + c0;
+        if (dim >= 8) {
+            uint4 a, b;
+            __builtin_memcpy(&a, p - back, 16);
+            __builtin_memcpy(&b, p - back + 4, 16);
+            r = {{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}};
+            if (back) kv_move_down<8>(r.w, back);
         } else {
-            auto word = [&](int e) { return e < left ? p[e] : 0u; };
-            r.a = make_uint4(word(0), word(1), word(2), word(3));
-            r.b = make_uint4(word(4), word(5), word(6), 0u);
+#pragma unroll
+            for (int e = 0; e < 7; ++e) r.w[e] = e < left ? p[e] : 0u;
         }
     } else {
-        const uint16_t *p = static_cast<const uint16_t *>(base) + at;
-        if (left >= 8) {
-            __builtin_memcpy(&r.a, p, 16);
+        const uint16_t *p = static_cast<const uint16_t *>(base) + row + c0;
+        if (dim >= 8) {
+            uint4 a;
+            __builtin_memcpy(&a, p - back, 16);
+            r = {{a.x, a.y, a.z, a.w, 0, 0, 0, 0}};
+            if (back) {
+                kv_move_down<4>(r.w, back >> 1);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (back & 1) r.w[i] = r.w[i] >> 16 | (i < 3 ? r.w[i + 1] << 16 : 0u);
+            }
         } else {
-            auto word = [&](int e) {
-                return (e < left ? (uint32_t)p[e] : 0u) | (e + 1 < left ? (uint32_t)p[e + 1] << 16 : 0u);
-            };
-            r.a = make_uint4(word(0), word(2), word(4), word(6));
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                r.w[e] = (2 * e < left ? (uint32_t)p[2 * e] : 0u) | (2 * e + 1 < left ? (uint32_t)p[2 * e + 1] << 16 : 0u);
         }
     }
     return r;
 }
 __device__ __forceinline__ void kv_floats8(const Raw8 &r, int type, float *v)
 {
-    const uint32_t w[8] = {r.a.x, r.a.y, r.a.z, r.a.w, r.b.x, r.b.y, r.b.z, r.b.w};
+    const uint32_t *w = r.w;
     if (type == LPQ_TYPE_F32) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = __builtin_bit_cast(float, w[e]);
@@ -136,10 +161,6 @@ __device__ __forceinline__ void kv_floats8(const Raw8 &r, int type, float *v)
         }
     }
 }
-__device__ __forceinline__ void kv_load8(const void *base, int type, int64_t at, int left, float *v)
-{
-    kv_floats8(kv_load8_raw(base, type, at, left), type, v);
-}
 __device__ __forceinline__ void kv_load_floats8(const float *p, float *v)
 {
     const float4 a = *reinterpret_cast<const float4 *>(p), b = *reinterpret_cast<const float4 *>(p + 4);
@@ -153,32 +174,40 @@ __device__ __forceinline__ uint16_t kv_to16(float v, int type)
     return type == LPQ_TYPE_BF16 ? __builtin_bit_cast(uint16_t, (__bf16)v) : __builtin_bit_cast(uint16_t, (_Float16)v);
 }
 
-// N (4 or 8) consecutive features out; those at or past `left` are not written.
+// N (4 or 8) consecutive features out; those at or past `left` are not written: what there is goes in pieces of 4, 2 and 1.
+template <int N, typename T>
+__device__ __forceinline__ void kv_store_pieces(T *p, int left, const T *v)
+{
+    if (left >= N) {
+        __builtin_memcpy(p, v, sizeof(T) * N);
+        return;
+    }
+    T w[4] = {v[0], v[1], v[2], v[3]};
+    if (N == 8 && (left & 4)) {
+        __builtin_memcpy(p, w, sizeof(T) * 4);
+        p += 4;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[e] = v[N - 4 + e];
+    }
+    if (left & 2) {
+        __builtin_memcpy(p, w, sizeof(T) * 2);
+        p += 2;
+        w[0] = w[2];
+    }
+    if (left & 1) p[0] = w[0];
+}
 template <int N>
 __device__ __forceinline__ void kv_store(void *base, int type, int64_t at, int left, const float *v)
 {
+    if (left <= 0) return;
     if (type == LPQ_TYPE_F32) {
-        float *p = static_cast<float *>(base) + at;
-        if (left >= N) {
-            __builtin_memcpy(p, v, 4 * N);
-        } else {
-#pragma unroll
-            for (int e = 0; e < N - 1; ++e)
-                if (e < left) p[e] = v[e];
-        }
+        kv_store_pieces<N>(static_cast<float *>(base) + at, left, v);
         return;
     }
-    uint16_t *p = static_cast<uint16_t *>(base) + at;
     uint16_t h[N];
 #pragma unroll
     for (int e = 0; e < N; ++e) h[e] = kv_to16(v[e], type);
-    if (left >= N) {
-        __builtin_memcpy(p, h, 2 * N);
-    } else {
-#pragma unroll
-        for (int e = 0; e < N - 1; ++e)
-            if (e < left) p[e] = h[e];
-    }
+    kv_store_pieces<N>(static_cast<uint16_t *>(base) + at, left, h);
 }
 #endif
 
