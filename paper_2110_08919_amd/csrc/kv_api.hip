@@ -91,12 +91,15 @@ extern "C" int lpq_kv_create(lpq_kv **out, const lpq_quantizer *keys, const lpq_
     v.page_shift = __builtin_ctz(page);
     v.packed = packed != 0;
     const size_t each = (size_t)heads * v.dpad;
-    hipError_t e = hipMalloc(&kv->constants, 2 * 5 * each * sizeof(float));
-    for (int i = 0; i < 2 && e == hipSuccess; ++i) {
-        float *p = kv->constants + (size_t)i * 5 * each;
-        KvConstants c = {p, p + each, p + 2 * each, p + 3 * each, p + 4 * each, qp[i].bits};
-        (i ? v.value : v.key) = c;
-        e = launch_kv_constants(qp[i], heads, v.dim, v.dpad, p, nullptr);
+    hipError_t e = hipMalloc(&kv->constants, (2 * 5 * each + 2) * sizeof(float));
+    int *flags_dev = reinterpret_cast<int *>(kv->constants + 2 * 5 * each), flags[2] = {0, 0};
+    if (e == hipSuccess) e = hipMemset(flags_dev, 0, sizeof(flags));
+    for (int i = 0; i < 2 && e == hipSuccess; ++i)
+        e = launch_kv_constants(qp[i], heads, v.dim, v.dpad, v.packed, kv->constants + (size_t)i * 5 * each, flags_dev + i, nullptr);
+    if (e == hipSuccess) e = hipMemcpy(flags, flags_dev, sizeof(flags), hipMemcpyDeviceToHost);
+    for (int i = 0; i < 2; ++i) {
+        const float *p = kv->constants + (size_t)i * 5 * each;
+        (i ? v.value : v.key) = {p, p + each, p + 2 * each, p + 3 * each, p + 4 * each, qp[i].bits, flags[i] == 0};
     }
     if (e == hipSuccess) e = hipDeviceSynchronize();
     if (e != hipSuccess) {

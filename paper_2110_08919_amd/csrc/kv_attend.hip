@@ -369,7 +369,7 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, WIDE)) void 
             const int r16 = i * PASS + tid / LR, r = row0 + r16;
             const bool on = r16 < 16 * RT && r < rows && 8 * qc < DP;
             const int64_t qat = (int64_t)b * q.ld_seq + (int64_t)(r / q.group) * q.ld_token + (int64_t)(h * q.group + r % q.group) * q.ld_head;
-            return kv_load8_raw(q.p, q.type, qat, qc0, on ? kv.dim : 0);
+            return kv_load8(q.p, q.type, qat + qc0, on ? kv.dim - qc0 : 0);
         };
         Raw8 raw = load_queries(0);
         float step[8];
@@ -386,7 +386,7 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, WIDE)) void 
         for (int i = 0; i < PASSES; ++i) {
             const int r16 = i * PASS + tid / LR;
             float v[8], most = 0.0f;
-            kv_floats8(raw, q.type, v);
+            kv_floats8(raw, q.type, kv.dim - qc0, v);
             if (i + 1 < PASSES) raw = load_queries(i + 1);
             if (a.lse) {
                 float offset = 0.0f;

@@ -17,65 +17,89 @@ namespace {
 
 constexpr int KV_THREADS = 256;
 constexpr int KV_ROWS = 4;      // rows a thread has in flight
-constexpr int KV_WORKGROUPS = 2048;
+// Workgroups that a large call is shared out to.  One generation of them where each writes whole pages (25 000 rows of 6 x 100
+// features: 33 us; 2048 workgroups 34, 4096 35.5), more where rows are cut anywhere (155 000 rows of 8 x 128 back: 194, 193, 189).
+constexpr int KV_WRITERS = 1024, KV_READERS = 4096;
 
-// How a call is shared out: `groups` groups of `heads` heads each, `pieces` workgroups per sequence and group that take its
-// pages in turn; a workgroup's threads are `lanes` rows of `heads` heads of dpad / 8 threads.
+// How a call is shared out: `groups` groups of `heads` heads each, `rows` rows of the call to a workgroup of each group; a
+// workgroup's threads are `lanes` rows of `heads` heads of dpad / 8 threads.
 struct Share {
-    int heads, groups, lanes, pieces;
+    int heads, groups, lanes, rows;
+    unsigned per_word;      // x * per_word >> 20 = x / (dpad / 4) for the words of a workgroup's heads (fewer than 2048)
 };
-
-// Equation 1 for one value: two separately rounded operations, floor, clamp (NaN -> 0).
-__device__ __forceinline__ int kv_quantize(float x, float k, float sb, float se, float m, float lo, float top)
-{
-    const float t = __fmul_rn(__fsub_rn(x, k), m);
-    float f = __builtin_amdgcn_fmed3f(floorf(t), lo, top);
-    f = (x > se) ? top : f;
-    f = (x < sb) ? lo : f;
-    f = (t != t) ? 0.0f : f;
-    return (int)f;
-}
 
 typedef short Pair __attribute__((ext_vector_type(2)));
 
+// What a thread needs of the constants of its 8 features.
 struct Features8 {
-    float k[8], sb[8], se[8], m[8], bottom, top;
+    float k[8], m[8];
+    const float *sb, *se;
+    int bottom, top;
 };
+
+// For all of a wave's loads to be there, before the first of their values is used.  Left to itself the compiler waits at each use
+// behind a branch, for everything that is under way by then: the stores of the row before included.
+__device__ __forceinline__ void loads_done() { __builtin_amdgcn_s_waitcnt(0x0F70); }
 
 __device__ __forceinline__ void load_features(const KvConstants &c, bool packed, int at, Features8 &f)
 {
     kv_load_floats8(c.k + at, f.k);
-    kv_load_floats8(c.sb + at, f.sb);
-    kv_load_floats8(c.se + at, f.se);
     kv_load_floats8(c.m + at, f.m);
+    f.sb = c.sb + at;
+    f.se = c.se + at;
     const int half = 1 << (c.bits - 1), most = packed ? 7 : 127;
-    f.bottom = (float)-half;
-    f.top = (float)(half < most ? half : most);
+    f.bottom = -half;
+    f.top = half < most ? half : most;
 }
 
-__device__ __forceinline__ void encode8(const Raw8 &raw, int type, const Features8 &f, int *q)
+// floor(t) as an integer, saturated; 0 for a NaN (as the instruction has it, C++ does not say).
+__device__ __forceinline__ int floor_int(float t)
+{
+    int q;
+    asm("v_cvt_i32_f32 %0, %1" : "=v"(q) : "v"(floorf(t)));
+    return q;
+}
+
+// Equation 1 for 8 values: two separately rounded operations, floor, clamp (KvConstants::clamps).  Pairs of 16 bits: features
+// 2 e and 2 e + 1.
+template <bool clamps>
+__device__ __forceinline__ void encode8(const Raw8 &raw, int type, int left, const Features8 &f, Pair *q)
 {
     float x[8];
-    kv_floats8(raw, type, x);
+    int c[8];
+    kv_floats8(raw, type, left, x);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) q[e] = kv_quantize(x[e], f.k[e], f.sb[e], f.se[e], f.m[e], f.bottom, f.top);
+    for (int e = 0; e < 8; ++e) c[e] = floor_int(__fmul_rn(__fsub_rn(x[e], f.k[e]), f.m[e]));
+    if (!clamps) {
+        float sb[8], se[8];
+        kv_load_floats8(f.sb, sb);
+        kv_load_floats8(f.se, se);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) c[e] = x[e] > se[e] ? f.top : x[e] < sb[e] ? f.bottom : c[e];
+    }
+    const Pair lo = {(short)f.bottom, (short)f.bottom}, hi = {(short)f.top, (short)f.top};
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        q[e] = __builtin_elementwise_min(__builtin_elementwise_max(__builtin_bit_cast(Pair, __builtin_amdgcn_cvt_pk_i16(c[2 * e], c[2 * e + 1])), lo), hi);
 }
 
-__device__ __forceinline__ void store_codes8(uint8_t *row, int c0, bool packed, const int *q)
+__device__ __forceinline__ void store_codes8(uint8_t *row, int c0, bool packed, const Pair *q)
 {
-    if (packed) {
-        uint32_t w = 0;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) w |= (uint32_t)(q[e] + 8) << (4 * e);   // feature 2j low, 2j + 1 high half of byte j
-        *reinterpret_cast<uint32_t *>(row + (c0 >> 1)) = w;
-    } else {
-        uint2 w = {0, 0};
+    if (packed) {       // feature 2 j in the low, 2 j + 1 in the high half of byte j
+        const Pair eight = {8, 8};
+        uint32_t b[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            w.x |= (uint32_t)(q[e] & 255) << (8 * e);
-            w.y |= (uint32_t)(q[e + 4] & 255) << (8 * e);
+            const uint32_t u = __builtin_bit_cast(uint32_t, (Pair)(q[e] + eight));
+            b[e] = u | u >> 12;
         }
-        *reinterpret_cast<uint2 *>(row + c0) = w;
+        const uint32_t lo = __builtin_amdgcn_perm(b[1], b[0], 0x0c0c0400u), hi = __builtin_amdgcn_perm(b[3], b[2], 0x04000c0cu);
+        *reinterpret_cast<uint32_t *>(row + (c0 >> 1)) = lo | hi;
+    } else {
+        uint32_t u[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) u[e] = __builtin_bit_cast(uint32_t, q[e]);
+        *reinterpret_cast<uint2 *>(row + c0) = make_uint2(__builtin_amdgcn_perm(u[1], u[0], 0x06040200u), __builtin_amdgcn_perm(u[3], u[2], 0x06040200u));
     }
 }
 
@@ -84,74 +108,92 @@ __device__ __forceinline__ uint2 load_codes8(const uint8_t *row, int c0, bool pa
     if (packed) return make_uint2(*reinterpret_cast<const uint32_t *>(row + (c0 >> 1)), 0);
     return *reinterpret_cast<const uint2 *>(row + c0);
 }
-__device__ __forceinline__ void codes8(uint2 w, bool packed, int *q)
+__device__ __forceinline__ void codes8(uint2 w, bool packed, Pair *q)
 {
-    if (packed) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) q[e] = (int)((w.x >> (4 * e)) & 15) - 8;
-    } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            q[e] = (int8_t)(w.x >> (8 * e));
-            q[e + 4] = (int8_t)(w.y >> (8 * e));
+    for (int e = 0; e < 4; ++e) {
+        if (packed) {
+            q[e] = Pair{(short)((int)((w.x >> (8 * e)) & 15) - 8), (short)((int)((w.x >> (8 * e + 4)) & 15) - 8)};
+        } else {
+            const uint32_t x = (e < 2 ? w.x : w.y) >> (16 * (e & 1));
+            q[e] = Pair{(int8_t)x, (int8_t)(x >> 8)};
         }
     }
 }
-
-// Rows [row0, row0 + count) of a call that belong to sequence b.
-__device__ __forceinline__ void rows_of(const KvPlaces &pl, int b, int64_t &row0, int64_t &count)
+// c + 1/2 of 8 codes, exactly.
+__device__ __forceinline__ void middles8(uint2 w, bool packed, float *v)
 {
-    if (!pl.starts) {
-        row0 = b;
-        count = 1;
-        return;
+    const uint32_t a = packed ? w.x & 0x0f0f0f0fu : w.x ^ 0x80808080u, b = packed ? (w.x >> 4) & 0x0f0f0f0fu : w.y ^ 0x80808080u;
+    const float off = packed ? 7.5f : 127.5f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const uint32_t from = packed ? (e & 1 ? b : a) : (e < 4 ? a : b);
+        const int byte = packed ? e >> 1 : e & 3;
+        v[e] = (float)((from >> (8 * byte)) & 255u) - off;
     }
-    int64_t r0 = kv_uniform(pl.starts)[b], r1 = kv_uniform(pl.starts)[b + 1];
-    r0 = r0 < 0 ? 0 : (r0 > pl.n ? pl.n : r0);
-    r1 = r1 < r0 ? r0 : (r1 > pl.n ? pl.n : r1);
-    row0 = r0;
-    count = r1 - r0;
 }
 
-// One step of a workgroup: the part of a page that a call covers.
-struct PagePart {
-    int lo, hi;        // rows of the page [lo, hi)
-    int64_t source;    // row of the call that is row `lo`
-    int64_t page;      // of the pool; -1: there is none
+// Rows [begin, end) of a call that belong to sequence b, the first of them at position `first`.
+struct Sequence {
+    int64_t begin, end, first;
+    int b;
 };
-
-__device__ __forceinline__ PagePart page_part(const KvView &kv, const KvPlaces &pl, int b, int64_t first, int64_t row0, int64_t count,
-                                              int64_t column)
+// The sequence of a row, by all 64 lanes: each looks at one of 64 starts, then between two of them.  Rows of none: end = n.
+__device__ __forceinline__ Sequence sequence_of(const KvPlaces &pl, int64_t row)
 {
-    PagePart p;
-    const int64_t at = column << kv.page_shift;
-    const int64_t from = first < at ? at : first, to = first + count < at + kv.page ? first + count : at + kv.page;
-    p.lo = (int)(from - at);
-    p.hi = (int)(to - at);
-    p.source = row0 + (from - first);
-    p.page = -1;
-    if (column >= 0 && column < pl.table_pages) {
-        const int32_t t = kv_uniform(pl.table + (int64_t)b * pl.ld_table)[column];
-        if (t >= 0 && t < kv.pages) p.page = t;
+    Sequence s;
+    if (!pl.starts) {
+        s.b = (int)row;
+        s.begin = row;
+        s.end = row + 1;
+    } else {
+        const int lane = threadIdx.x & 63;
+        int lo = 0, count = pl.nseq + 1;                 // starts lo .. lo + count - 1: the last one <= row
+        while (count > 1) {
+            const int step = (count + 63) / 64, at = lane * step;
+            const bool below = at < count && pl.starts[lo + at] <= row;
+            const int hits = __popcll(__ballot(below));
+            lo += hits ? (hits - 1) * step : 0;
+            if (!hits) break;                            // before the first start
+            count = count - (hits - 1) * step < step ? count - (hits - 1) * step : step;
+        }
+        lo = __builtin_amdgcn_readfirstlane(lo);
+        s.b = lo < pl.nseq ? lo : pl.nseq - 1;
+        s.begin = kv_uniform(pl.starts)[s.b];
+        s.end = kv_uniform(pl.starts)[s.b + 1];
+        if (s.begin < 0 || s.begin > row || s.end <= row || s.end > pl.n) {      // starts that do not ascend from 0 to n
+            s.begin = row;
+            s.end = pl.n;
+            s.b = -1;
+        }
     }
-    return p;
+    s.first = s.b < 0 ? 0 : kv_uniform(pl.first)[s.b];
+    return s;
+}
+// Page of the pool that holds positions column * page on of sequence b; -1: there is none.
+__device__ __forceinline__ int64_t page_of(const KvView &kv, const KvPlaces &pl, int b, int64_t column)
+{
+    if (column < 0 || column >= pl.table_pages) return -1;
+    const int32_t t = kv_uniform(pl.table + (int64_t)b * pl.ld_table)[column];
+    return t >= 0 && t < kv.pages ? t : -1;
 }
 
-// What a thread has of a workgroup's page: features c0 .. c0 + 7 of head h, rows lane, lane + lanes, ... of its keys (which = 0)
-// or values.
+// What a thread has of a workgroup's rows: features c0 .. c0 + 7 of head h, rows lane, lane + lanes, ... of a page, of the keys
+// (which = 0) or of the values.  [begin, end): the workgroup's rows of the call.
 struct Seat {
-    int which, b, piece, h0, h, c0, lane;
+    int64_t begin, end;
+    int which, h0, h, c0, lane;
     bool on;
 };
-__device__ __forceinline__ Seat seat(const KvView &kv, const Share &sh)
+__device__ __forceinline__ Seat seat(const KvView &kv, const KvPlaces &pl, const Share &sh)
 {
     Seat s;
     const int chunks = kv.dpad >> 3, slot = threadIdx.x / chunks;
     s.which = blockIdx.x & 1;
-    const int work = blockIdx.x >> 1, per = __builtin_amdgcn_readfirstlane(work / sh.groups);
-    s.b = __builtin_amdgcn_readfirstlane(per / sh.pieces);
-    s.piece = per - s.b * sh.pieces;
-    s.h0 = (work - per * sh.groups) * sh.heads;
+    const int work = blockIdx.x >> 1, part = __builtin_amdgcn_readfirstlane(work / sh.groups);
+    s.begin = (int64_t)part * sh.rows;
+    s.end = s.begin + sh.rows < pl.n ? s.begin + sh.rows : pl.n;
+    s.h0 = (work - part * sh.groups) * sh.heads;
     s.c0 = 8 * (threadIdx.x - slot * chunks);
     s.lane = slot / sh.heads;
     s.h = s.h0 + slot - s.lane * sh.heads;
@@ -159,74 +201,71 @@ __device__ __forceinline__ Seat seat(const KvView &kv, const Share &sh)
     return s;
 }
 
-template <int type, bool packed>
+template <int type, bool packed, bool clamps>
 __global__ __launch_bounds__(KV_THREADS, 4) void kv_write_kernel(KvView kv, KvRows kr, KvRows vr, KvPlaces pl, Share sh)
 {
     __shared__ uint2 part_lo[KV_THREADS], part_hi[KV_THREADS];
-    const Seat s = seat(kv, sh);
+    const Seat s = seat(kv, pl, sh);
     const KvRows in = s.which ? vr : kr;
-    const int row_bytes = (packed ? kv.dpad >> 1 : kv.dpad);
-    int64_t row0, count, first = kv_uniform(pl.first)[s.b];
-    rows_of(pl, s.b, row0, count);
-    if (first < 0) {               // rows at negative positions have no place
-        const int64_t skip = count < -first ? count : -first;
-        row0 += skip;
-        count -= skip;
-        first = 0;
-    }
-    if (count <= 0) return;
-    const int64_t column0 = first >> kv.page_shift, columns = ((first + count - 1) >> kv.page_shift) - column0 + 1;
-    if (s.piece >= columns) return;
+    const int row_bytes = (packed ? kv.dpad >> 1 : kv.dpad), left = kv.dim - s.c0;
     Features8 f;
     if (s.on) load_features(s.which ? kv.value : kv.key, packed, s.h * kv.dpad + s.c0, f);
-    for (int64_t i = s.piece; i < columns; i += sh.pieces) {
-        const PagePart p = page_part(kv, pl, s.b, first, row0, count, column0 + i);
-        if (p.page < 0) continue;      // uniform over the workgroup
+    Sequence q;
+    q.end = -1;
+    // A workgroup takes the pages whose first row of the call is among its rows.
+    for (int64_t row = s.begin, end; row < s.end; row = end) {
+        if (row >= q.end) q = sequence_of(pl, row);
+        const int64_t at = q.first + (row - q.begin), column = at >> kv.page_shift;
+        const int inside = (int)(at & (kv.page - 1));
+        end = row + kv.page - inside < q.end ? row + kv.page - inside : q.end;
+        if (inside > 0 && row > q.begin) continue;                         // begun by the workgroup before
+        const int64_t page = q.b < 0 ? -1 : page_of(kv, pl, q.b, column);   // none at positions below 0
+        if (page < 0) continue;                                            // (all of this uniform over the workgroup)
+        const int lo_row = inside, hi_row = inside + (int)(end - row);     // rows of the page
         Pair mn[4], mx[4];           // of features 2 e and 2 e + 1
 #pragma unroll
         for (int e = 0; e < 4; ++e) { mn[e] = Pair{127, 127}; mx[e] = Pair{-128, -128}; }
-        auto widen = [&](const int *q) {
+        auto widen = [&](const Pair *c) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const Pair x = {(short)q[2 * e], (short)q[2 * e + 1]};
-                mn[e] = __builtin_elementwise_min(mn[e], x);
-                mx[e] = __builtin_elementwise_max(mx[e], x);
+                mn[e] = __builtin_elementwise_min(mn[e], c[e]);
+                mx[e] = __builtin_elementwise_max(mx[e], c[e]);
             }
         };
         if (s.on) {
-            uint8_t *rows = (s.which ? kv.v : kv.k) + (p.page * kv.heads + s.h) * kv.page * row_bytes;
-            const int64_t from = (p.source - p.lo) * in.ld_token + s.h * in.ld_head;
+            uint8_t *rows = (s.which ? kv.v : kv.k) + (page * kv.heads + s.h) * kv.page * row_bytes;
+            const int64_t from = (row - lo_row) * in.ld_token + s.h * in.ld_head + s.c0;
             auto encode = [&](const Raw8 &x, int t) {
-                int q[8];
-                encode8(x, type, f, q);
-                store_codes8(rows + t * row_bytes, s.c0, packed, q);
-                widen(q);
+                Pair c[4];
+                encode8<clamps>(x, type, left, f, c);
+                store_codes8(rows + t * row_bytes, s.c0, packed, c);
+                if (s.which == 0) widen(c);
             };
-            int t0 = p.lo + s.lane;
-            for (; t0 + (KV_ROWS - 1) * sh.lanes < p.hi; t0 += KV_ROWS * sh.lanes) {
+            for (int t0 = lo_row + s.lane; t0 < hi_row; t0 += KV_ROWS * sh.lanes) {
                 Raw8 x[KV_ROWS];
 #pragma unroll
-                for (int u = 0; u < KV_ROWS; ++u) x[u] = kv_load8_raw(in.p, type, from + (t0 + u * sh.lanes) * in.ld_token, s.c0, kv.dim);
+                for (int u = 0; u < KV_ROWS; ++u)
+                    if (t0 + u * sh.lanes < hi_row) x[u] = kv_load8(in.p, type, from + (t0 + u * sh.lanes) * in.ld_token, left);
+                loads_done();
 #pragma unroll
                 for (int u = 0; u < KV_ROWS; ++u) {
-                    encode(x[u], t0 + u * sh.lanes);
+                    if (t0 + u * sh.lanes < hi_row) encode(x[u], t0 + u * sh.lanes);
                     __builtin_amdgcn_sched_barrier(0);       // one row after the other: four at once do not fit the registers
                 }
             }
-            for (; t0 < p.hi; t0 += sh.lanes) encode(kv_load8_raw(in.p, type, from + t0 * in.ld_token, s.c0, kv.dim), t0);
             if (s.which == 0) {
-                for (int t1 = s.lane; t1 < p.lo; t1 += 2 * KV_ROWS * sh.lanes) {
+                for (int t1 = s.lane; t1 < lo_row; t1 += 2 * KV_ROWS * sh.lanes) {
                     uint2 w[2 * KV_ROWS];
 #pragma unroll
                     for (int u = 0; u < 2 * KV_ROWS; ++u) {
-                        const int t = t1 + u * sh.lanes < p.lo ? t1 + u * sh.lanes : t1;    // a row twice does not move the bounds
+                        const int t = t1 + u * sh.lanes < lo_row ? t1 + u * sh.lanes : t1;    // a row twice does not move the bounds
                         w[u] = load_codes8(rows + t * row_bytes, s.c0, packed);
                     }
 #pragma unroll
                     for (int u = 0; u < 2 * KV_ROWS; ++u) {
-                        int q[8];
-                        codes8(w[u], packed, q);
-                        widen(q);
+                        Pair c[4];
+                        codes8(w[u], packed, c);
+                        widen(c);
                         __builtin_amdgcn_sched_barrier(0);
                     }
                 }
@@ -244,24 +283,24 @@ __global__ __launch_bounds__(KV_THREADS, 4) void kv_write_kernel(KvView kv, KvRo
         part_lo[threadIdx.x] = lo;
         part_hi[threadIdx.x] = hi;
         __syncthreads();
-        {   // byte t of the group's heads' lower bounds, then of the upper ones: [lane][head][feature] -> [head][2][feature]
-            const int8_t *low = reinterpret_cast<const int8_t *>(part_lo), *high = reinterpret_cast<const int8_t *>(part_hi);
-            const int some = sh.heads < kv.heads - s.h0 ? sh.heads : kv.heads - s.h0, stride = sh.heads * kv.dpad;
-            int8_t *out = kv.bounds + (p.page * kv.heads + s.h0) * 2 * kv.dpad;
-            for (int t = threadIdx.x; t < 2 * some * kv.dpad; t += KV_THREADS) {
-                const bool upper = t >= some * kv.dpad;
-                const int at = upper ? t - some * kv.dpad : t;
-                const int8_t *src = (upper ? high : low) + at;
-                int best = src[0];
-                for (int u = 1; u < sh.lanes; ++u) {
-                    const int q = src[u * stride];
-                    best = upper ? (q > best ? q : best) : (q < best ? q : best);
+        {   // word t of the group's heads' lower bounds, then of the upper ones: [lane][head][feature] -> [head][2][feature]
+            const int some = sh.heads < kv.heads - s.h0 ? sh.heads : kv.heads - s.h0, words = kv.dpad >> 2, stride = sh.heads * words;
+            uint32_t *out = reinterpret_cast<uint32_t *>(kv.bounds + (page * kv.heads + s.h0) * 2 * kv.dpad);
+            for (int t = threadIdx.x; t < 2 * some * words; t += KV_THREADS) {
+                const bool upper = t >= some * words;
+                const int at = upper ? t - some * words : t, head = (int)((unsigned)at * sh.per_word >> 20);
+                const uint32_t *src = reinterpret_cast<const uint32_t *>(upper ? part_hi : part_lo) + at;
+                Pair even, odd;          // features 0 and 2, 1 and 3 of the word, sign in the high bytes
+                for (int u = 0; u < sh.lanes; ++u) {
+                    const uint32_t w = src[u * stride];
+                    const Pair a = __builtin_bit_cast(Pair, w << 8 & 0xff00ff00u), b = __builtin_bit_cast(Pair, w & 0xff00ff00u);
+                    even = u == 0 ? a : upper ? __builtin_elementwise_max(even, a) : __builtin_elementwise_min(even, a);
+                    odd = u == 0 ? b : upper ? __builtin_elementwise_max(odd, b) : __builtin_elementwise_min(odd, b);
                 }
-                const int head = at / kv.dpad;
-                out[(2 * head + (upper ? 1 : 0)) * kv.dpad + at - head * kv.dpad] = (int8_t)best;
+                out[(2 * head + (upper ? 1 : 0)) * words + at - head * words] = __builtin_bit_cast(uint32_t, even) >> 8 | __builtin_bit_cast(uint32_t, odd);
             }
         }
-        if (i + sh.pieces < columns) __syncthreads();       // the partial bounds are used again by the next page
+        __syncthreads();                                    // the partial bounds are used again by the next page
     }
 }
 
@@ -269,46 +308,54 @@ __global__ __launch_bounds__(KV_THREADS, 4) void kv_write_kernel(KvView kv, KvRo
 template <int type, bool packed>
 __global__ __launch_bounds__(KV_THREADS, 4) void kv_read_kernel(KvView kv, KvRows kr, KvRows vr, KvPlaces pl, Share sh)
 {
-    const Seat s = seat(kv, sh);
+    const Seat s = seat(kv, pl, sh);
     const KvRows out = s.which ? vr : kr;
-    const int row_bytes = (packed ? kv.dpad >> 1 : kv.dpad), left = kv.dim - s.c0;
-    if (!s.on || left <= 0) return;
-    int64_t row0, count;
-    const int64_t first = kv_uniform(pl.first)[s.b];
-    rows_of(pl, s.b, row0, count);
-    if (count <= 0) return;
-    const int64_t column0 = first >> kv.page_shift, columns = ((first + count - 1) >> kv.page_shift) - column0 + 1;
-    if (s.piece >= columns) return;
+    const int row_bytes = (packed ? kv.dpad >> 1 : kv.dpad), left = s.on ? kv.dim - s.c0 : 0;
     float k[8], step[8];
-    const int at = s.h * kv.dpad + s.c0;
-    kv_load_floats8((s.which ? kv.value.k : kv.key.k) + at, k);
-    kv_load_floats8((s.which ? kv.value.s : kv.key.s) + at, step);
-    for (int64_t i = s.piece; i < columns; i += sh.pieces) {
-        const PagePart p = page_part(kv, pl, s.b, first, row0, count, column0 + i);
-        const uint8_t *rows = (s.which ? kv.v : kv.k) + (p.page * kv.heads + s.h) * kv.page * row_bytes;
-        for (int t0 = p.lo + s.lane; t0 < p.hi; t0 += 2 * KV_ROWS * sh.lanes) {
+    if (left > 0) {
+        const int at = s.h * kv.dpad + s.c0;
+        kv_load_floats8((s.which ? kv.value.k : kv.key.k) + at, k);
+        kv_load_floats8((s.which ? kv.value.s : kv.key.s) + at, step);
+    }
+    Sequence q;
+    q.end = -1;
+    for (int64_t row = s.begin, end; row < s.end; row = end) {
+        if (row >= q.end) q = sequence_of(pl, row);
+        const int64_t at = q.first + (row - q.begin), column = at >> kv.page_shift;
+        const int inside = (int)(at & (kv.page - 1));
+        end = row + kv.page - inside < q.end ? row + kv.page - inside : q.end;
+        if (end > s.end) end = s.end;
+        if (q.b < 0 || left <= 0) continue;
+        const int64_t page = page_of(kv, pl, q.b, column);
+        const uint8_t *rows = (s.which ? kv.v : kv.k) + (page * kv.heads + s.h) * kv.page * row_bytes;
+        const int hi_row = inside + (int)(end - row);
+        for (int t0 = inside + s.lane; t0 < hi_row; t0 += 2 * KV_ROWS * sh.lanes) {
             uint2 w[2 * KV_ROWS];
 #pragma unroll
             for (int u = 0; u < 2 * KV_ROWS; ++u) {
                 const int t = t0 + u * sh.lanes;
-                if (t < p.hi && p.page >= 0) w[u] = load_codes8(rows + t * row_bytes, s.c0, packed);
+                if (t < hi_row && page >= 0) w[u] = load_codes8(rows + t * row_bytes, s.c0, packed);
             }
+            loads_done();
 #pragma unroll
             for (int u = 0; u < 2 * KV_ROWS; ++u) {
                 const int t = t0 + u * sh.lanes;
-                if (t >= p.hi) continue;
-                int q[8];
+                if (t >= hi_row) continue;
                 float x[8];
-                codes8(w[u], packed, q);
+                middles8(w[u], packed, x);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) x[e] = p.page >= 0 ? __fadd_rn(__fmul_rn((float)q[e] + 0.5f, step[e]), k[e]) : 0.0f;
-                kv_store<8>(out.p, type, (p.source + t - p.lo) * out.ld_token + s.h * out.ld_head + s.c0, left, x);
+                for (int e = 0; e < 8; ++e) x[e] = __fadd_rn(__fmul_rn(x[e], step[e]), k[e]);
+                if (page < 0) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) x[e] = 0.0f;
+                }
+                kv_store<8>(out.p, type, (row - inside + t) * out.ld_token + s.h * out.ld_head + s.c0, left, x);
             }
         }
     }
 }
 
-__global__ void kv_constants_kernel(QuantParams q, int heads, int dim, int dpad, float *out)
+__global__ void kv_constants_kernel(QuantParams q, int heads, int dim, int dpad, bool packed, float *out, int *not_all)
 {
     const int t = blockIdx.x * blockDim.x + threadIdx.x, total = heads * dpad;
     if (t >= total) return;
@@ -327,47 +374,57 @@ __global__ void kv_constants_kernel(QuantParams q, int heads, int dim, int dpad,
     out[2 * total + t] = se;
     out[3 * total + t] = m;
     out[4 * total + t] = m > 0.f ? 1.0f / m : 0.f;
+    // Rounding is monotone, so every x > S_e has a product no smaller than that of S_e: where that already rounds down to the
+    // top code or above, the clamp gives what the comparison with S_e would; likewise below S_b.
+    const int half = 1 << (q.bits - 1), most = packed ? 7 : 127;
+    const bool clamps = !(se < INFINITY) || (floorf(__fmul_rn(__fsub_rn(se, k), m)) >= (float)(half < most ? half : most) &&
+                                             floorf(__fmul_rn(__fsub_rn(sb, k), m)) <= (float)-half);
+    if (!clamps) *not_all = 1;
 }
 
-// A decoding step has one page per sequence; a prompt has as many as its share of the rows fills, and a longer one than the
-// others takes more turns of the same workgroups.  Neighbouring heads share a workgroup where that leaves enough of them
-// (rows of neighbouring heads lie side by side outside the cache).
-Share share_of(const KvView &kv, const KvPlaces &pl)
+// Rows in equal numbers to about as many workgroups as the chip holds at once, whole pages of them to one (a write); neighbouring
+// heads share a workgroup where that leaves enough of them, since their rows lie side by side outside the cache.
+Share share_of(const KvView &kv, const KvPlaces &pl, bool write)
 {
     Share s;
-    const int slots = KV_THREADS / (kv.dpad / 8);
-    const int64_t mean = ceil_div(pl.n, (int64_t)pl.nseq), most = ceil_div(pl.n, (int64_t)kv.page) + 1;
-    const int64_t pages = pl.n == pl.nseq ? pl.nseq : ceil_div(mean, (int64_t)kv.page) * pl.nseq;
+    const int slots = KV_THREADS / (kv.dpad / 8), workgroups = write ? KV_WRITERS : KV_READERS;
+    const int64_t units = pl.starts ? ceil_div(pl.n, (int64_t)kv.page) : pl.n;      // pages, roughly
     s.heads = 1;
     for (int h = 2; h <= kv.heads && h <= slots; ++h)
-        if (slots / h * h * 8 >= slots * 7 && kv.heads % h == 0 && pages * (kv.heads / h) >= KV_WORKGROUPS) s.heads = h;
+        if (slots / h * h * 8 >= slots * 7 && kv.heads % h == 0 && 2 * units * (kv.heads / h) >= workgroups) s.heads = h;
     s.lanes = slots / s.heads;
     s.groups = (int)ceil_div(kv.heads, s.heads);
-    int64_t pieces = pl.n == pl.nseq ? 1 : 2 * ceil_div(mean, (int64_t)kv.page) + 1;
-    const int64_t room = ceil_div(int64_t(4096), (int64_t)pl.nseq * s.groups);     // up to 16 workgroups per CU in any case
-    if (pl.n != pl.nseq && pieces < room) pieces = room;
-    const int64_t grid = KV_MAX_BLOCKS / ((int64_t)pl.nseq * s.groups);            // >= 1 (the entry points); keys and values twice as many
-    if (pieces > grid) pieces = grid;
-    s.pieces = (int)(pieces < most ? pieces : most);
+    int64_t rows = pl.starts ? ceil_div(pl.n * 2 * s.groups, (int64_t)workgroups) : 1;
+    const int64_t few = pl.starts ? (write ? kv.page : s.lanes * 2 * KV_ROWS) : 1, grid = KV_MAX_BLOCKS / s.groups;
+    if (rows < few) rows = few;
+    if (rows < ceil_div(pl.n, grid)) rows = ceil_div(pl.n, grid);
+    s.rows = (int)rows;
+    s.per_word = ((1u << 20) + kv.dpad / 4 - 1) / (kv.dpad / 4);
     return s;
 }
 
 }  // namespace
 
-hipError_t launch_kv_constants(const QuantParams &q, int heads, int dim, int dpad, float *out, hipStream_t st)
+hipError_t launch_kv_constants(const QuantParams &q, int heads, int dim, int dpad, bool packed, float *out, int *not_all, hipStream_t st)
 {
-    kv_constants_kernel<<<(unsigned)ceil_div(heads * dpad, 256), 256, 0, st>>>(q, heads, dim, dpad, out);
+    kv_constants_kernel<<<(unsigned)ceil_div(heads * dpad, 256), 256, 0, st>>>(q, heads, dim, dpad, packed, out, not_all);
     return hipGetLastError();
 }
 
 hipError_t launch_kv_write(const KvView &kv, const KvRows &k, const KvRows &v, const KvPlaces &pl, hipStream_t st)
 {
     if (pl.n <= 0 || pl.nseq <= 0) return hipSuccess;
-    const Share s = share_of(kv, pl);
-    const unsigned blocks = (unsigned)(2 * (int64_t)s.pieces * pl.nseq * s.groups);
+    const Share s = share_of(kv, pl, true);
+    const unsigned blocks = (unsigned)(2 * ceil_div(pl.n, (int64_t)s.rows) * s.groups);
+    auto launch_as = [&](auto type, auto packed, auto clamps) {
+        kv_write_kernel<decltype(type)::value, decltype(packed)::value, decltype(clamps)::value><<<blocks, KV_THREADS, 0, st>>>(kv, k, v, pl, s);
+    };
     auto launch = [&](auto type) {
-        if (kv.packed) kv_write_kernel<decltype(type)::value, true><<<blocks, KV_THREADS, 0, st>>>(kv, k, v, pl, s);
-        else kv_write_kernel<decltype(type)::value, false><<<blocks, KV_THREADS, 0, st>>>(kv, k, v, pl, s);
+        const bool clamps = kv.key.clamps && kv.value.clamps;
+        if (kv.packed && clamps) launch_as(type, std::true_type(), std::true_type());
+        else if (kv.packed) launch_as(type, std::true_type(), std::false_type());
+        else if (clamps) launch_as(type, std::false_type(), std::true_type());
+        else launch_as(type, std::false_type(), std::false_type());
     };
     if (k.type == LPQ_TYPE_F32) launch(std::integral_constant<int, LPQ_TYPE_F32>());
     else if (k.type == LPQ_TYPE_F16) launch(std::integral_constant<int, LPQ_TYPE_F16>());
@@ -378,8 +435,8 @@ hipError_t launch_kv_write(const KvView &kv, const KvRows &k, const KvRows &v, c
 hipError_t launch_kv_read(const KvView &kv, const KvRows &k, const KvRows &v, const KvPlaces &pl, hipStream_t st)
 {
     if (pl.n <= 0 || pl.nseq <= 0) return hipSuccess;
-    const Share s = share_of(kv, pl);
-    const unsigned blocks = (unsigned)(2 * (int64_t)s.pieces * pl.nseq * s.groups);
+    const Share s = share_of(kv, pl, false);
+    const unsigned blocks = (unsigned)(2 * ceil_div(pl.n, (int64_t)s.rows) * s.groups);
     auto launch = [&](auto type) {
         if (kv.packed) kv_read_kernel<decltype(type)::value, true><<<blocks, KV_THREADS, 0, st>>>(kv, k, v, pl, s);
         else kv_read_kernel<decltype(type)::value, false><<<blocks, KV_THREADS, 0, st>>>(kv, k, v, pl, s);

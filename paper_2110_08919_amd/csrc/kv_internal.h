@@ -16,6 +16,7 @@ enum { KV_MAX_DIM = 256, KV_MIN_PAGE = 16, KV_MAX_PAGE = 256,
 struct KvConstants {
     const float *k, *sb, *se, *m, *s;
     int bits;
+    bool clamps;       // clamping floor((x - k) m) to the codes' range makes the comparisons with S_b and S_e needless
 };
 
 // One layer's cache.  Codes [pages][heads][page][row_bytes], bounds [pages][heads][2][dpad] (smallest, largest key code).
@@ -50,7 +51,8 @@ struct KvQueries {
     int type, new_tokens, group;     // group: query heads per key-value head
 };
 
-hipError_t launch_kv_constants(const QuantParams &q, int heads, int dim, int dpad, float *out, hipStream_t st);
+// *not_all becomes 1 unless KvConstants::clamps holds for all features.
+hipError_t launch_kv_constants(const QuantParams &q, int heads, int dim, int dpad, bool packed, float *out, int *not_all, hipStream_t st);
 hipError_t launch_kv_write(const KvView &kv, const KvRows &k, const KvRows &v, const KvPlaces &pl, hipStream_t st);
 hipError_t launch_kv_read(const KvView &kv, const KvRows &k, const KvRows &v, const KvPlaces &pl, hipStream_t st);
 
@@ -90,60 +92,78 @@ hipError_t launch_kv_attend(const KvView &kv, const KvQueries &q, const KvAttend
 typedef const __attribute__((address_space(4))) int32_t *KvUniform;
 __device__ __forceinline__ KvUniform kv_uniform(const int32_t *p) { return (KvUniform)(uintptr_t)p; }
 
-// 8 consecutive features c0 .. c0 + 7 of a row of `dim`, as they lie in memory (`row`: element the row begins at), to be
-// converted once they are there; those past the row are 0.  Wide loads whatever the alignment: the hardware takes them at any
-// address of its elements.  The end of a row that is no multiple of 8 is loaded with what lies before it and moved down.
+// 8 consecutive features as they lie in memory: asked for by kv_load8, made floats by kv_floats8 once they are there.  Wide
+// loads whatever the alignment (the hardware takes them at any address of its elements); the end of a row that is no multiple
+// of 8, `left` < 8 features, comes in pieces of 4, 2 and 1 that kv_floats8 puts together.
 struct Raw8 {
     uint32_t w[8];      // a 16-bit type: the first four
 };
-template <int WORDS>
-__device__ __forceinline__ void kv_move_down(uint32_t *w, int words)      // by 0 .. WORDS words, zeros from above
+template <int BYTES>
+__device__ __forceinline__ void kv_pieces(const char *p, int left, uint32_t *w)
 {
+    constexpr int W = BYTES;        // words of 4 features, for 2 or 4 bytes each
+    if (left & 4) {
+        uint32_t t[W];
+        __builtin_memcpy(t, p, 4 * BYTES);
 #pragma unroll
-    for (int s = WORDS; s >= 1; s >>= 1)
+        for (int i = 0; i < W; ++i) w[i] = t[i];
+    }
+    if (left & 2) {
+        uint32_t t[W / 2];
+        __builtin_memcpy(t, p + (left & 4) * BYTES, 2 * BYTES);
 #pragma unroll
-        for (int i = 0; i < WORDS; ++i) w[i] = (words & s) ? (i + s < WORDS ? w[i + s] : 0u) : w[i];
+        for (int i = 0; i < W / 2; ++i) w[W + i] = t[i];
+    }
+    if (left & 1) {
+        if (BYTES == 2) w[3] = *reinterpret_cast<const uint16_t *>(p + (left & 6) * BYTES);
+        else w[6] = *reinterpret_cast<const uint32_t *>(p + (left & 6) * BYTES);
+    }
 }
-__device__ __forceinline__ Raw8 kv_load8_raw(const void *base, int type, int64_t row, int c0, int dim)
+__device__ __forceinline__ Raw8 kv_load8(const void *base, int type, int64_t at, int left)
 {
     Raw8 r = {{0, 0, 0, 0, 0, 0, 0, 0}};
-    const int left = dim - c0, back = left >= 8 ? 0 : 8 - left;
-    if (left <= 0) return r;
     if (type == LPQ_TYPE_F32) {
-        const uint32_t *p = static_cast<const uint32_t *>(base) + row + c0;
-        if (dim >= 8) {
+        const char *p = static_cast<const char *>(base) + 4 * at;
+        if (left >= 8) {
             uint4 a, b;
-            __builtin_memcpy(&a, p - back, 16);
-            __builtin_memcpy(&b, p - back + 4, 16);
+            __builtin_memcpy(&a, p, 16);
+            __builtin_memcpy(&b, p + 16, 16);
             r = {{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}};
-            if (back) kv_move_down<8>(r.w, back);
-        } else {
-#pragma unroll
-            for (int e = 0; e < 7; ++e) r.w[e] = e < left ? p[e] : 0u;
+        } else if (left > 0) {
+            kv_pieces<4>(p, left, r.w);
         }
     } else {
-        const uint16_t *p = static_cast<const uint16_t *>(base) + row + c0;
-        if (dim >= 8) {
+        const char *p = static_cast<const char *>(base) + 2 * at;
+        if (left >= 8) {
             uint4 a;
-            __builtin_memcpy(&a, p - back, 16);
+            __builtin_memcpy(&a, p, 16);
             r = {{a.x, a.y, a.z, a.w, 0, 0, 0, 0}};
-            if (back) {
-                kv_move_down<4>(r.w, back >> 1);
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (back & 1) r.w[i] = r.w[i] >> 16 | (i < 3 ? r.w[i + 1] << 16 : 0u);
-            }
-        } else {
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                r.w[e] = (2 * e < left ? (uint32_t)p[2 * e] : 0u) | (2 * e + 1 < left ? (uint32_t)p[2 * e + 1] << 16 : 0u);
+        } else if (left > 0) {
+            kv_pieces<2>(p, left, r.w);
         }
     }
     return r;
 }
-__device__ __forceinline__ void kv_floats8(const Raw8 &r, int type, float *v)
+__device__ __forceinline__ void kv_floats8(const Raw8 &r, int type, int left, float *v)
 {
-    const uint32_t *w = r.w;
+    uint32_t w[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) w[e] = r.w[e];
+    if (left < 8) {      // what is not there was set to 0
+        if (type == LPQ_TYPE_F32) {
+            if (!(left & 2)) { w[4] = w[6]; w[6] = 0; }
+            if (!(left & 4)) {
+                w[0] = w[4]; w[1] = w[5]; w[2] = w[6];
+                w[4] = w[5] = w[6] = 0;
+            }
+        } else {
+            if (!(left & 2)) { w[2] = w[3]; w[3] = 0; }
+            if (!(left & 4)) {
+                w[0] = w[2]; w[1] = w[3];
+                w[2] = w[3] = 0;
+            }
+        }
+    }
     if (type == LPQ_TYPE_F32) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = __builtin_bit_cast(float, w[e]);

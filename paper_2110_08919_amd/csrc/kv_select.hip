@@ -50,7 +50,7 @@ __global__ __launch_bounds__(THREADS) void kv_score_kernel(KvView kv, KvQueries 
     auto row_at = [&](int r) { return base + (int64_t)(r / q.group) * q.ld_token + (int64_t)(r % q.group) * q.ld_head; };
     auto load = [&](int t, float *v) {
         const int r = t / chunks, c0 = (t % chunks) * 8;
-        kv_floats8(kv_load8_raw(q.p, q.type, row_at(r), c0, kv.dim), q.type, v);
+        kv_floats8(kv_load8(q.p, q.type, row_at(r) + c0, kv.dim - c0), q.type, kv.dim - c0, v);
         const float *st = kv.key.s + h * DP + c0;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
