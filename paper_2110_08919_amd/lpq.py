@@ -108,6 +108,14 @@ def _stream() -> int:
     return torch.cuda.current_stream().cuda_stream
 
 
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
+def _stream_of(t: torch.Tensor) -> int:
+    """_stream() on the device of t.  A call of a few microseconds feels that the Stream object costs 2.7 us to make."""
+    return _raw_stream(t.get_device()) if _raw_stream is not None else torch.cuda.current_stream(t.device).cuda_stream
+
+
 def _ptr(t):
     return None if t is None else t.data_ptr()
 
@@ -346,7 +354,7 @@ _TYPE = {torch.float32: TYPE_F32, torch.float16: TYPE_F16, torch.bfloat16: TYPE_
 
 
 def _dev_ints(t: torch.Tensor, n: int):
-    assert t.is_cuda and t.dtype == torch.int32 and t.is_contiguous() and t.dim() == 1 and t.numel() == n, \
+    assert t.is_cuda and t.dtype is torch.int32 and t.dim() == 1 and t.shape[0] == n and t.is_contiguous(), \
         f"need {n} contiguous int32 values on the device"
     return t.data_ptr()
 
@@ -387,22 +395,29 @@ class KVCache:
         return self._bounds[..., :self.dim]
 
     def _table(self, table: torch.Tensor):
-        p, nseq, ld = _dev_matrix(table, torch.int32)
-        return nseq, (p, ld, table.shape[1])
+        assert table.is_cuda and table.dtype is torch.int32 and table.dim() == 2, "need a device table int32 [sequences, columns]"
+        nseq, columns = table.shape
+        ld, inner = table.stride()
+        assert inner == 1 or columns == 1, "need the columns of the table side by side"
+        return nseq, (table.data_ptr(), ld if nseq > 1 else max(ld, columns), columns)
 
-    def _rows(self, t: torch.Tensor, dtype, n: int):
-        assert t.is_cuda and t.dtype == dtype and t.shape == (n, self.heads, self.dim) and (t.stride(2) == 1 or self.dim == 1), \
-            f"need device rows [{n}, {self.heads}, {self.dim}] of {dtype}, features contiguous"
-        return t.data_ptr(), t.stride(0), t.stride(1)
+    def _rows(self, t: torch.Tensor, dtype):
+        assert t.is_cuda and t.dtype is dtype and t.dim() == 3, f"need device rows of {dtype}"
+        n, heads, dim = t.shape
+        by_row, by_head, inner = t.stride()
+        assert heads == self.heads and dim == self.dim and (inner == 1 or dim == 1), \
+            f"need rows [n, {self.heads}, {self.dim}], features side by side"
+        return n, (t.data_ptr(), by_row, by_head)
 
     def write(self, k: torch.Tensor, v: torch.Tensor, first: torch.Tensor, table: torch.Tensor, starts: torch.Tensor = None):
         """New rows [n, heads, features] (float32, float16 or bfloat16): rows starts[b] .. starts[b + 1] go to positions
         first[b] on of sequence b; without starts one row per sequence."""
         nseq, tab = self._table(table)
-        n = k.shape[0]
-        _check(lib().lpq_kv_write(self._h, *self._rows(k, k.dtype, n), *self._rows(v, k.dtype, n), _TYPE[k.dtype], n, nseq,
-                                  _dev_ints(first, nseq), None if starts is None else _dev_ints(starts, nseq + 1), *tab,
-                                  _stream()))
+        n, keys = self._rows(k, k.dtype)
+        same, values = self._rows(v, k.dtype)
+        assert n == same, "as many values as keys"
+        _check(_lib.lpq_kv_write(self._h, *keys, *values, _TYPE[k.dtype], n, nseq, _dev_ints(first, nseq),
+                                 None if starts is None else _dev_ints(starts, nseq + 1), *tab, _stream_of(table)))
 
     def read(self, first: torch.Tensor, table: torch.Tensor, starts: torch.Tensor = None, rows: int = None,
              dtype=torch.float32, out=None):
@@ -413,30 +428,40 @@ class KVCache:
         k, v = out if out is not None else (
             torch.empty((n, self.heads, self.dim), dtype=dtype, device=table.device),
             torch.empty((n, self.heads, self.dim), dtype=dtype, device=table.device))
-        _check(lib().lpq_kv_read(self._h, *self._rows(k, k.dtype, n), *self._rows(v, k.dtype, n), _TYPE[k.dtype], n, nseq,
-                                 _dev_ints(first, nseq), None if starts is None else _dev_ints(starts, nseq + 1), *tab,
-                                 _stream()))
+        a, keys = self._rows(k, k.dtype)
+        b, values = self._rows(v, k.dtype)
+        assert a == n and b == n, f"need {n} rows"
+        _check(_lib.lpq_kv_read(self._h, *keys, *values, _TYPE[k.dtype], n, nseq, _dev_ints(first, nseq),
+                                None if starts is None else _dev_ints(starts, nseq + 1), *tab, _stream_of(table)))
         return k, v
 
     def _queries(self, q: torch.Tensor, nseq: int):
-        assert q.is_cuda and q.dtype in _TYPE and q.dim() == 4 and q.shape[0] == nseq and q.shape[3] == self.dim and (
-            q.stride(3) == 1 or self.dim == 1), "need device queries [sequences, new tokens, query heads, features], features contiguous"
-        return q.data_ptr(), q.stride(0), q.stride(1), q.stride(2)
+        assert q.is_cuda and q.dtype in _TYPE and q.dim() == 4, "need device queries of float32, float16 or bfloat16"
+        n, new, heads, dim = q.shape
+        by_seq, by_token, by_head, inner = q.stride()
+        assert n == nseq and dim == self.dim and (inner == 1 or dim == 1), \
+            f"need queries [{nseq}, new tokens, query heads, {self.dim}], features side by side"
+        return new, heads, (q.data_ptr(), by_seq, by_token, by_head)
+
+    @staticmethod
+    def _workspace(given: torch.Tensor, need: int, device):
+        """The workspace to pass: memory of this call's own unless some was given (calls on several streams do not share any)."""
+        if given is None and need:
+            given = torch.empty(need, dtype=torch.uint8, device=device)
+        return (given, None, 0) if given is None else (given, given.data_ptr(), given.numel() * given.element_size())
 
     def select(self, q: torch.Tensor, lengths: torch.Tensor, table: torch.Tensor, n_select: int, keep_first: int = 0,
                keep_last: int = 1, out: torch.Tensor = None, workspace: torch.Tensor = None) -> torch.Tensor:
         """int32 [sequences, heads, n_select]: the pages with the largest bounds of the queries' integer products,
         ascending, -1 at the end."""
         nseq, tab = self._table(table)
+        new, q_heads, queries = self._queries(q, nseq)
         if out is None:
             out = torch.empty((nseq, self.heads, n_select), dtype=torch.int32, device=q.device)
-        assert out.is_cuda and out.dtype == torch.int32 and out.is_contiguous() and out.shape == (nseq, self.heads, n_select)
-        if workspace is None:
-            need = lib().lpq_kv_select_workspace_bytes(self._h, nseq, table.shape[1])
-            workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
-        _check(lib().lpq_kv_select(self._h, *self._queries(q, nseq), _TYPE[q.dtype], nseq, q.shape[1], q.shape[2],
-                                   _dev_ints(lengths, nseq), *tab, n_select, keep_first, keep_last, out.data_ptr(),
-                                   workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream()))
+        assert out.is_cuda and out.dtype is torch.int32 and out.is_contiguous() and out.shape == (nseq, self.heads, n_select)
+        workspace, ws, size = self._workspace(workspace, _lib.lpq_kv_select_workspace_bytes(self._h, nseq, tab[2]), q.device)
+        _check(_lib.lpq_kv_select(self._h, *queries, _TYPE[q.dtype], nseq, new, q_heads, _dev_ints(lengths, nseq), *tab,
+                                  n_select, keep_first, keep_last, out.data_ptr(), ws, size, _stream_of(q)))
         return out
 
     def attend(self, q: torch.Tensor, lengths: torch.Tensor, table: torch.Tensor, pages: torch.Tensor = None,
@@ -444,22 +469,24 @@ class KVCache:
         """Attention of q [sequences, new tokens, query heads, features] over the cache (the last new_tokens positions of
         each length are the queries' own), or over the `pages` that select() names; scale 1 / sqrt(features) by default."""
         nseq, tab = self._table(table)
+        new, q_heads, queries = self._queries(q, nseq)
         if out is None:
             out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        assert out.shape == q.shape and out.dtype == q.dtype
+            outputs = (out.data_ptr(), new * q_heads * self.dim, q_heads * self.dim, self.dim)
+        else:
+            assert out.shape == q.shape and out.dtype is q.dtype
+            outputs = self._queries(out, nseq)[2]
         lse = torch.empty(q.shape[:3], dtype=torch.float32, device=q.device) if return_lse else None
         n_select = 0
         if pages is not None:
             n_select = pages.shape[-1]
-            assert pages.is_cuda and pages.dtype == torch.int32 and pages.is_contiguous() and pages.shape == (nseq, self.heads, n_select), \
+            assert pages.is_cuda and pages.dtype is torch.int32 and pages.is_contiguous() and pages.shape == (nseq, self.heads, n_select), \
                 "need contiguous int32 pages [sequences, heads, pages]"
-        if workspace is None:
-            need = lib().lpq_kv_attend_workspace_bytes(self._h, nseq, q.shape[1], q.shape[2], table.shape[1], n_select)
-            workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
-        _check(lib().lpq_kv_attend(self._h, *self._queries(q, nseq), _TYPE[q.dtype], nseq, q.shape[1], q.shape[2],
-                                   self.dim ** -0.5 if scale is None else scale, _dev_ints(lengths, nseq), *tab, _ptr(pages),
-                                   n_select, *self._queries(out, nseq), _ptr(lse), workspace.data_ptr(),
-                                   workspace.numel() * workspace.element_size(), _stream()))
+        workspace, ws, size = self._workspace(
+            workspace, _lib.lpq_kv_attend_workspace_bytes(self._h, nseq, new, q_heads, tab[2], n_select), q.device)
+        _check(_lib.lpq_kv_attend(self._h, *queries, _TYPE[q.dtype], nseq, new, q_heads,
+                                  self.dim ** -0.5 if scale is None else scale, _dev_ints(lengths, nseq), *tab, _ptr(pages), n_select,
+                                  *outputs, _ptr(lse), ws, size, _stream_of(q)))
         return (out, lse) if return_lse else out
 
 
