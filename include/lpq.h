@@ -295,7 +295,7 @@ int lpq_kv_read(const lpq_kv *kv, void *k_dev, int64_t ldk_token, int64_t ldk_he
  * an upper bound, summed over the rows, of the integer product with any token of the page.  pages_dev
  * [nseq][heads][n_select] receives the numbers (columns of the table) of the first keep_first and the last keep_last of
  * a sequence's pages and of those with the largest scores, ties to the lower number, ascending; -1 behind them where
- * there are fewer.  Integers throughout: the result is unique.  Workspace: 256-byte aligned.
+ * there are fewer.  Integers throughout: the result is unique.  Workspace: 256-byte aligned (0 bytes for small tables).
  * LPQ_EINVAL: null argument, n_select < 1, keep_first or keep_last < 0 or more than n_select together, q_heads not a
  * multiple of heads; LPQ_ERANGE: new_tokens * G > 128, workspace too small, sizes as above. */
 size_t lpq_kv_select_workspace_bytes(const lpq_kv *kv, int64_t nseq, int64_t table_pages);

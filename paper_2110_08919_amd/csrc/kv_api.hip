@@ -221,7 +221,7 @@ static int kv_queries(const lpq_kv *kv, const void *q, int64_t ld_seq, int64_t l
 
 extern "C" size_t lpq_kv_select_workspace_bytes(const lpq_kv *kv, int64_t nseq, int64_t table_pages)
 {
-    if (!kv || nseq < 0 || table_pages < 1) return 0;
+    if (!kv || nseq < 0 || table_pages < 1 || !kv_select_needs_scores(table_pages)) return 0;
     return (size_t)nseq * kv->view.heads * table_pages * sizeof(int32_t);
 }
 

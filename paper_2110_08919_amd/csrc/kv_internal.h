@@ -63,6 +63,7 @@ struct KvSelect {
     int32_t *pages;                  // [nseq][heads][n_select]
     int32_t *scores;                 // workspace [nseq][heads][table_pages]
 };
+bool kv_select_needs_scores(int64_t table_pages);     // KvSelect::scores is used
 hipError_t launch_kv_select(const KvView &kv, const KvQueries &q, const KvSelect &s, hipStream_t st);
 
 struct KvAttend {

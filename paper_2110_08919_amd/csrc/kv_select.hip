@@ -11,6 +11,9 @@
 // registers, finds the n_select-th largest by bisection over the bits that differ between them (each step counts with
 // one ballot per register, no atomics, so the result does not depend on any order), and writes the pages out in
 // ascending order.
+//
+// Tables of up to 512 pages: one launch, whose workgroup scores all pages of a (sequence, head) and picks; the second launch and
+// the scores' way through memory would cost more than the larger part of the chip gains.  Bound by round trips to memory.
 #include "kv_internal.h"
 #include "wave_ops.h"
 
@@ -20,116 +23,16 @@ namespace {
 
 typedef int v4i __attribute__((ext_vector_type(4)));
 
-constexpr int THREADS = 256, WAVES = THREADS / 64;
+constexpr int THREADS = 256;
 constexpr int UNROLL = 4;                              // groups of 16 pages a wave has in flight
-constexpr int BLOCK_PAGES = 16 * UNROLL * WAVES;
+constexpr int block_pages(int threads) { return threads / 64 * 16 * UNROLL; }
+constexpr int FUSED_PAGES = block_pages(512);
 
 __device__ __forceinline__ int pages_of(int len, int page_shift, int table_pages)
 {
     if (len <= 0) return 0;
     const int np = (int)(((int64_t)len + (1 << page_shift) - 1) >> page_shift);
     return np < table_pages ? np : table_pages;
-}
-
-template <int DP>
-__global__ __launch_bounds__(THREADS) void kv_score_kernel(KvView kv, KvQueries q, KvSelect s, int blocks_per)
-{
-    constexpr int STEPS = 2 * DP / 64;
-    __shared__ float red[WAVES];
-    __shared__ __align__(16) int8_t digit[2][2 * DP];
-    __shared__ int wsum[2 * DP];
-    const int pair = blockIdx.x / blocks_per, part = blockIdx.x % blocks_per;
-    const int h = pair % kv.heads, b = pair / kv.heads;
-    const int np = pages_of(s.lengths[b], kv.page_shift, s.table_pages);
-    if (part * BLOCK_PAGES >= np) return;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-
-    // Query codes: z = rint(q s * (127 / A)), A the largest |q s| of the head's rows; what is not finite counts as 0.
-    const int rows = q.new_tokens * q.group, chunks = DP / 8;
-    const int64_t base = (int64_t)b * q.ld_seq + (int64_t)h * q.group * q.ld_head;
-    auto row_at = [&](int r) { return base + (int64_t)(r / q.group) * q.ld_token + (int64_t)(r % q.group) * q.ld_head; };
-    auto load = [&](int t, float *v) {
-        const int r = t / chunks, c0 = (t % chunks) * 8;
-        kv_floats8(kv_load8(q.p, q.type, row_at(r) + c0, kv.dim - c0), q.type, kv.dim - c0, v);
-        const float *st = kv.key.s + h * DP + c0;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const float x = __fmul_rn(v[e], st[e]);
-            v[e] = fabsf(x) <= 3.402823466e38f ? x : 0.0f;
-        }
-    };
-    for (int i = tid; i < 2 * DP; i += THREADS) wsum[i] = 0;
-    float most = 0.0f;
-    for (int t = tid; t < rows * chunks; t += THREADS) {
-        float v[8];
-        load(t, v);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(v[e]));
-    }
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) most = fmaxf(most, __shfl_xor(most, o, 64));
-    if (lane == 0) red[wave] = most;
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < WAVES; ++w) most = fmaxf(most, red[w]);
-    // below that, 127 / A would leave the range of binary32
-    const float f = most > 1e-30f ? __fdiv_rn(127.0f, most) : 0.0f;
-    for (int t = tid; t < rows * chunks; t += THREADS) {
-        float v[8];
-        load(t, v);
-        const int c0 = (t % chunks) * 8;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const int z = (int)rintf(__fmul_rn(v[e], f));
-            if (z) atomicAdd(&wsum[(z > 0 ? DP : 0) + c0 + e], z);      // integers: the order does not matter
-        }
-    }
-    __syncthreads();
-    for (int i = tid; i < 2 * DP; i += THREADS) {
-        const int w = wsum[i], a = w < 0 ? -w : w, hi = a >> 7, lo = a & 127;
-        digit[0][i] = (int8_t)(w < 0 ? -hi : hi);
-        digit[1][i] = (int8_t)(w < 0 ? -lo : lo);
-    }
-    __syncthreads();
-
-    const int n = lane & 15, g = lane >> 4;
-    v4i wd[STEPS];
-#pragma unroll
-    for (int st = 0; st < STEPS; ++st) {
-        const v4i zero = {0, 0, 0, 0};
-        wd[st] = n < 2 ? *reinterpret_cast<const v4i *>(&digit[n & 1][st * 64 + g * 16]) : zero;
-    }
-    const int32_t *table = s.table + (int64_t)b * s.ld_table;
-    const int page0 = part * BLOCK_PAGES + wave * 16 * UNROLL;
-    int32_t id[UNROLL];
-#pragma unroll
-    for (int u = 0; u < UNROLL; ++u) {
-        const int page = page0 + 16 * u + n;
-        id[u] = page < np ? table[page] : -1;
-        if (id[u] >= kv.pages) id[u] = -1;
-    }
-    v4i x[UNROLL][STEPS];
-#pragma unroll
-    for (int u = 0; u < UNROLL; ++u) {
-        const int8_t *row = kv.bounds + ((int64_t)(id[u] < 0 ? 0 : id[u]) * kv.heads + h) * 2 * DP + g * 16;
-#pragma unroll
-        for (int st = 0; st < STEPS; ++st) x[u][st] = *reinterpret_cast<const v4i *>(row + 64 * st);
-    }
-    int32_t *out = s.scores + (int64_t)pair * s.table_pages;
-#pragma unroll
-    for (int u = 0; u < UNROLL; ++u) {
-        v4i acc = {0, 0, 0, 0};
-#pragma unroll
-        for (int st = 0; st < STEPS; ++st) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(x[u][st], wd[st], acc, 0, 0, 0);
-        // column 0: the high digits, column 1: the low ones; register j of lane (n, g): page 4 g + j
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int low = __shfl_xor(acc[j], 1, 64);
-            const int there = __shfl(id[u], 4 * g + j, 64);
-            const int page = page0 + 16 * u + 4 * g + j;
-            if (n == 0 && page < np) out[page] = there < 0 ? INT32_MIN : 128 * acc[j] + low;
-        }
-    }
 }
 
 // Sortable image of a page's score: 0 = not there, all ones = kept in any case.
@@ -140,19 +43,16 @@ __device__ __forceinline__ uint32_t key_of(int32_t score, int page, int np, int 
     return (uint32_t)score ^ 0x80000000u;
 }
 
-// NT threads with KEYS scores each.  More pages than that (beyond NT * KEYS) are read again from memory at every step.
+// By a workgroup of NT threads with KEYS scores each.  More pages than that (beyond NT * KEYS) are read again from memory at
+// every step.
 template <int NT, int KEYS, bool AGAIN>
-__global__ __launch_bounds__(NT) void kv_pick_kernel(KvView kv, KvSelect s)
+__device__ __forceinline__ void pick(const int32_t *score, int np, const KvSelect &s, int32_t *out)
 {
     constexpr int W = NT / 64;
     __shared__ uint32_t red[2][W];
     __shared__ int count[2][W];
     __shared__ int before[2][KEYS * W];
-    const int pair = blockIdx.x, b = pair / kv.heads;
-    const int np = pages_of(s.lengths[b], kv.page_shift, s.table_pages);
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int32_t *score = s.scores + (int64_t)pair * s.table_pages;
-    int32_t *out = s.pages + (int64_t)pair * s.n_select;
     const int rounds = AGAIN ? (np + NT * KEYS - 1) / (NT * KEYS) : 1;
     uint32_t key[KEYS];
     auto fetch = [&](int round) {
@@ -281,20 +181,151 @@ __global__ __launch_bounds__(NT) void kv_pick_kernel(KvView kv, KvSelect s)
     for (int i = want + tid; i < s.n_select; i += NT) out[i] = -1;
 }
 
+template <int NT, int KEYS, bool AGAIN>
+__global__ __launch_bounds__(NT) void kv_pick_kernel(KvView kv, KvSelect s)
+{
+    const int pair = blockIdx.x, np = pages_of(kv_uniform(s.lengths)[pair / kv.heads], kv.page_shift, s.table_pages);
+    pick<NT, KEYS, AGAIN>(s.scores + (int64_t)pair * s.table_pages, np, s, s.pages + (int64_t)pair * s.n_select);
+}
+
+template <int DP, int NT, bool FUSED>
+__global__ __launch_bounds__(NT) void kv_score_kernel(KvView kv, KvQueries q, KvSelect s, int blocks_per)
+{
+    constexpr int STEPS = 2 * DP / 64, WAVES = NT / 64, BLOCK_PAGES = block_pages(NT);
+    __shared__ float red[WAVES];
+    __shared__ __align__(16) int8_t digit[2][2 * DP];
+    __shared__ int wsum[2 * DP];
+    const int pair = blockIdx.x / blocks_per, part = blockIdx.x % blocks_per;
+    const int h = pair % kv.heads, b = pair / kv.heads;
+    const int np = pages_of(kv_uniform(s.lengths)[b], kv.page_shift, s.table_pages);
+    if (!FUSED && part * BLOCK_PAGES >= np) return;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = lane & 15, g = lane >> 4;
+
+    // The pages' bounds are under way while the queries are made ready.
+    const int32_t *table = s.table + (int64_t)b * s.ld_table;
+    const int page0 = part * BLOCK_PAGES + wave * 16 * UNROLL;
+    int32_t id[UNROLL];
+#pragma unroll
+    for (int u = 0; u < UNROLL; ++u) {
+        const int page = page0 + 16 * u + n;
+        id[u] = page < np ? table[page] : -1;
+        if (id[u] >= kv.pages) id[u] = -1;
+    }
+    v4i x[UNROLL][STEPS];
+#pragma unroll
+    for (int u = 0; u < UNROLL; ++u) {
+        const int8_t *row = kv.bounds + ((int64_t)(id[u] < 0 ? 0 : id[u]) * kv.heads + h) * 2 * DP + g * 16;
+#pragma unroll
+        for (int st = 0; st < STEPS; ++st) x[u][st] = *reinterpret_cast<const v4i *>(row + 64 * st);
+    }
+
+    // Query codes: z = rint(q s * (127 / A)), A the largest |q s| of the head's rows; what is not finite counts as 0.
+    const int rows = q.new_tokens * q.group, chunks = DP / 8;
+    const int64_t base = (int64_t)b * q.ld_seq + (int64_t)h * q.group * q.ld_head;
+    auto row_at = [&](int r) { return base + (int64_t)(r / q.group) * q.ld_token + (int64_t)(r % q.group) * q.ld_head; };
+    auto load = [&](int t, float *v) {
+        const int r = t / chunks, c0 = (t % chunks) * 8;
+        kv_floats8(kv_load8(q.p, q.type, row_at(r) + c0, kv.dim - c0), q.type, kv.dim - c0, v);
+        const float *st = kv.key.s + h * DP + c0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float x = __fmul_rn(v[e], st[e]);
+            v[e] = fabsf(x) <= 3.402823466e38f ? x : 0.0f;
+        }
+    };
+    for (int i = tid; i < 2 * DP; i += NT) wsum[i] = 0;
+    float most = 0.0f;
+    for (int t = tid; t < rows * chunks; t += NT) {
+        float v[8];
+        load(t, v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(v[e]));
+    }
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) most = fmaxf(most, __shfl_xor(most, o, 64));
+    if (lane == 0) red[wave] = most;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) most = fmaxf(most, red[w]);
+    // below that, 127 / A would leave the range of binary32
+    const float f = most > 1e-30f ? __fdiv_rn(127.0f, most) : 0.0f;
+    for (int t = tid; t < rows * chunks; t += NT) {
+        float v[8];
+        load(t, v);
+        const int c0 = (t % chunks) * 8;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const int z = (int)rintf(__fmul_rn(v[e], f));
+            if (z) atomicAdd(&wsum[(z > 0 ? DP : 0) + c0 + e], z);      // integers: the order does not matter
+        }
+    }
+    __syncthreads();
+    for (int i = tid; i < 2 * DP; i += NT) {
+        const int w = wsum[i], a = w < 0 ? -w : w, hi = a >> 7, lo = a & 127;
+        digit[0][i] = (int8_t)(w < 0 ? -hi : hi);
+        digit[1][i] = (int8_t)(w < 0 ? -lo : lo);
+    }
+    __syncthreads();
+
+    v4i wd[STEPS];
+#pragma unroll
+    for (int st = 0; st < STEPS; ++st) {
+        const v4i zero = {0, 0, 0, 0};
+        wd[st] = n < 2 ? *reinterpret_cast<const v4i *>(&digit[n & 1][st * 64 + g * 16]) : zero;
+    }
+    __shared__ int32_t local[FUSED ? BLOCK_PAGES : 1];
+    int32_t *out = FUSED ? local : s.scores + (int64_t)pair * s.table_pages;
+#pragma unroll
+    for (int u = 0; u < UNROLL; ++u) {
+        v4i acc = {0, 0, 0, 0};
+#pragma unroll
+        for (int st = 0; st < STEPS; ++st) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(x[u][st], wd[st], acc, 0, 0, 0);
+        // column 0: the high digits, column 1: the low ones; register j of lane (n, g): page 4 g + j
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int low = __shfl_xor(acc[j], 1, 64);
+            const int there = __shfl(id[u], 4 * g + j, 64);
+            const int page = page0 + 16 * u + 4 * g + j;
+            if (n == 0 && page < np) out[page] = there < 0 ? INT32_MIN : 128 * acc[j] + low;
+        }
+    }
+    if (FUSED) {
+        __syncthreads();
+        pick<NT, BLOCK_PAGES / NT, false>(local, np, s, s.pages + (int64_t)pair * s.n_select);
+    }
+}
+
+template <int DP>
+void launch_scores(const KvView &kv, const KvQueries &q, const KvSelect &s, hipStream_t st)
+{
+    const int pairs = s.nseq * kv.heads;
+    if (s.table_pages <= block_pages(256)) kv_score_kernel<DP, 256, true><<<pairs, 256, 0, st>>>(kv, q, s, 1);
+    else if (s.table_pages <= FUSED_PAGES) kv_score_kernel<DP, 512, true><<<pairs, 512, 0, st>>>(kv, q, s, 1);
+    else {
+        const int per = (int)ceil_div(s.table_pages, block_pages(THREADS));
+        kv_score_kernel<DP, THREADS, false><<<pairs * per, THREADS, 0, st>>>(kv, q, s, per);
+    }
+}
+
 }  // namespace
+
+bool kv_select_needs_scores(int64_t table_pages) { return table_pages > FUSED_PAGES; }
 
 hipError_t launch_kv_select(const KvView &kv, const KvQueries &q, const KvSelect &s, hipStream_t st)
 {
     if (s.nseq <= 0) return hipSuccess;
     const int pairs = s.nseq * kv.heads;
-    const int per = (int)ceil_div(s.table_pages, BLOCK_PAGES);
     switch (kv.dpad) {
-    case 64: kv_score_kernel<64><<<pairs * per, THREADS, 0, st>>>(kv, q, s, per); break;
-    case 128: kv_score_kernel<128><<<pairs * per, THREADS, 0, st>>>(kv, q, s, per); break;
-    case 192: kv_score_kernel<192><<<pairs * per, THREADS, 0, st>>>(kv, q, s, per); break;
-    default: kv_score_kernel<256><<<pairs * per, THREADS, 0, st>>>(kv, q, s, per); break;
+    case 64: launch_scores<64>(kv, q, s, st); break;
+    case 128: launch_scores<128>(kv, q, s, st); break;
+    case 192: launch_scores<192>(kv, q, s, st); break;
+    default: launch_scores<256>(kv, q, s, st); break;
     }
+    // as few keys to a thread as there are pages for: each step of the bisection looks at all of them
+    if (s.table_pages <= FUSED_PAGES) return hipGetLastError();
     if (s.table_pages <= 256 * 4) kv_pick_kernel<256, 4, false><<<pairs, 256, 0, st>>>(kv, s);
+    else if (s.table_pages <= 512 * 4) kv_pick_kernel<512, 4, false><<<pairs, 512, 0, st>>>(kv, s);
+    else if (s.table_pages <= 1024 * 4) kv_pick_kernel<1024, 4, false><<<pairs, 1024, 0, st>>>(kv, s);
     else if (s.table_pages <= 1024 * 16) kv_pick_kernel<1024, 16, false><<<pairs, 1024, 0, st>>>(kv, s);
     else kv_pick_kernel<1024, 16, true><<<pairs, 1024, 0, st>>>(kv, s);
     return hipGetLastError();

@@ -218,6 +218,10 @@ SELECT = [  # heads, dim, page, lengths, group, new, n_select, keep_first, keep_
     (1, 192, 16, [5000, 4000], 8, 2, 33, 0, 0, True),
     (2, 256, 64, [700], 16, 1, 1, 0, 1, False),
     (1, 40, 16, [20000], 1, 1, 100, 1, 1, False),          # 1250 pages
+    (2, 128, 16, [8100, 5000], 3, 1, 40, 1, 1, False),     # 507 pages
+    (1, 256, 16, [9000, 16000], 2, 1, 600, 1, 1, True),    # 1000 pages, and fewer than asked for
+    (1, 64, 16, [40000, 100], 1, 1, 64, 0, 1, False),      # 2500 pages
+    (1, 64, 16, [80000], 2, 1, 700, 3, 3, False),          # 5000 pages
     (1, 64, 16, [400], 16, 8, 9, 0, 0, False),             # 128 query rows
 ]
 
@@ -496,7 +500,8 @@ def test_refusals(lpq):
     assert code(cache.select, q, lengths, c.table, 2, -1, 1) == lpq.EINVAL
     assert code(cache.select, q[:, :, :3], lengths, c.table, 2) == lpq.EINVAL                      # 3 query heads on 2
     assert code(cache.select, c.queries(20, 7).cuda(), lengths, c.table, 2) == lpq.ERANGE          # 140 query rows
-    assert code(cache.select, q, lengths, c.table, 2, workspace=torch.empty(8, dtype=torch.uint8, device="cuda")) == lpq.ERANGE
+    wide = torch.full((2, 600), -1, dtype=torch.int32, device="cuda")                              # columns enough for a workspace
+    assert code(cache.select, q, lengths, wide, 2, workspace=torch.empty(8, dtype=torch.uint8, device="cuda")) == lpq.ERANGE
     assert code(cache.attend, q, lengths, c.table, scale=float("nan")) == lpq.EINVAL
     assert code(cache.attend, q[:, :, :1], lengths, c.table) == lpq.EINVAL
     assert code(cache.attend, q, lengths, c.table, out=torch.empty_like(q[:1]).expand(2, -1, -1, -1)) == lpq.EINVAL
