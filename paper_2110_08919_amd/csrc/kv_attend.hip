@@ -42,11 +42,16 @@ constexpr float LIFT = 6.0f;         // weights are exp2(t - m + LIFT): at most 
 // Tokens a wave has in registers: 64 where a row of codes has at
 // most 64 bytes, else 32.
 __host__ __device__ constexpr int tile_tokens(int dpad, bool packed) { return (packed ? dpad / 2 : dpad) <= 64 ? 64 : 32; }
+// Whether more than 16 query rows go through a tile of tokens 32 at a time.  Once through memory for 32 rows instead of twice: 16
+// conversations of 32 000 to 56 000 tokens, 8 heads of 128, 32 rows each, 285 against 466 us (float32 queries); 4-bit codes with
+// 16-bit queries, 32 conversations, 415 against 584.  Where packed codes and the registers of 32 rows leave one workgroup to a CU,
+// 16 at a time are faster: 8 conversations, one head of 192, 48 rows, float32 71 against 43 us, bfloat16 60 against 37; heads of
+// 128, float32, 305 against 286.
+__host__ __device__ constexpr bool two_row_tiles(int dpad, bool packed, bool wide) { return !packed || dpad == 64 || (!wide && dpad != 192); }
 // Workgroups of four waves that a CU's registers hold.
 __host__ __device__ constexpr int blocks_per_cu(int dpad, bool packed, int rt, bool wide)
 {
     if (dpad > 128) return rt == 1 ? 2 : 1;
-    if (rt > 1 && wide && packed && dpad > 64) return 1;
     if (rt > 1) return 2;
     return wide || (packed && dpad > 64) ? 3 : 4;
 }
@@ -659,12 +664,13 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, WIDE)) void 
     }
 }
 
-// Parts of a row joined: a workgroup per row, dpad / 4 threads side by side per part.
-__global__ __launch_bounds__(THREADS) void kv_join_kernel(KvView kv, KvQueries q, KvAttend a, int row_tiles, int tile_rows, int grid)
+// Parts of a row joined: a workgroup of NT threads per row, dpad / 4 of them side by side per part.
+template <int NT>
+__global__ __launch_bounds__(NT) void kv_join_kernel(KvView kv, KvQueries q, KvAttend a, int row_tiles, int tile_rows, int grid)
 {
-    __shared__ float4 sums[THREADS];
+    __shared__ float4 sums[NT];
     __shared__ float weight[KV_ATTEND_GRID];
-    __shared__ float red[WAVES], redl[WAVES];
+    __shared__ float red[NT / 64], redl[NT / 64];
     const int rows = q.new_tokens * q.group;
     const int r = blockIdx.x % rows, bh = blockIdx.x / rows, h = bh % kv.heads, b = bh / kv.heads;
     const Workspace ws = workspace(a.part, 2 * (int64_t)grid, tile_rows, kv.dpad);
@@ -673,7 +679,7 @@ __global__ __launch_bounds__(THREADS) void kv_join_kernel(KvView kv, KvQueries q
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, inside = r % tile_rows;
     auto row_of = [&](int u) { return (2 * ((int64_t)parts.first + u) + (u == 0 ? 1 : 0)) * tile_rows + inside; };
     float top = NEG;
-    for (int u = tid; u < parts.count; u += THREADS) {
+    for (int u = tid; u < parts.count; u += NT) {
         const float m = ws.ml[row_of(u) * 2];
         weight[u] = m;
         top = fmaxf(top, m);
@@ -683,9 +689,9 @@ __global__ __launch_bounds__(THREADS) void kv_join_kernel(KvView kv, KvQueries q
     if (lane == 0) red[wave] = top;
     __syncthreads();
 #pragma unroll
-    for (int w = 0; w < WAVES; ++w) top = fmaxf(top, red[w]);
+    for (int w = 0; w < NT / 64; ++w) top = fmaxf(top, red[w]);
     float l = 0.0f;
-    for (int u = tid; u < parts.count; u += THREADS) {
+    for (int u = tid; u < parts.count; u += NT) {
         const float f = top == NEG ? 1.0f : __builtin_amdgcn_exp2f(weight[u] - top);
         weight[u] = f;
         l += ws.ml[row_of(u) * 2 + 1] * f;
@@ -696,8 +702,8 @@ __global__ __launch_bounds__(THREADS) void kv_join_kernel(KvView kv, KvQueries q
     __syncthreads();
     l = 0.0f;
 #pragma unroll
-    for (int w = 0; w < WAVES; ++w) l += redl[w];
-    const int cols = kv.dpad >> 2, groups = THREADS / cols, col = tid % cols, grp = tid / cols;
+    for (int w = 0; w < NT / 64; ++w) l += redl[w];
+    const int cols = kv.dpad >> 2, groups = NT / cols, col = tid % cols, grp = tid / cols;
     float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
     if (grp < groups) {
 #pragma unroll 4
@@ -728,24 +734,26 @@ __global__ __launch_bounds__(THREADS) void kv_join_kernel(KvView kv, KvQueries q
     }
 }
 
-template <int DP, bool PACKED>
+template <int DP, bool PACKED, bool WIDE>
 void launch_rows(const KvView &kv, const KvQueries &q, const KvAttend &a, const KvAttendPlan &p, hipStream_t st)
 {
-    const bool wide = q.type == LPQ_TYPE_F32;
-    if (p.rows == 16) {
-        if (wide) kv_attend_kernel<DP, PACKED, 1, true><<<p.grid, THREADS, 0, st>>>(kv, q, a, p.row_tiles, p.least);
-        else kv_attend_kernel<DP, PACKED, 1, false><<<p.grid, THREADS, 0, st>>>(kv, q, a, p.row_tiles, p.least);
-    } else {
-        if (wide) kv_attend_kernel<DP, PACKED, 2, true><<<p.grid, THREADS, 0, st>>>(kv, q, a, p.row_tiles, p.least);
-        else kv_attend_kernel<DP, PACKED, 2, false><<<p.grid, THREADS, 0, st>>>(kv, q, a, p.row_tiles, p.least);
+    if constexpr (two_row_tiles(DP, PACKED, WIDE)) {
+        if (p.rows == 32) {
+            kv_attend_kernel<DP, PACKED, 2, WIDE><<<p.grid, THREADS, 0, st>>>(kv, q, a, p.row_tiles, p.least);
+            return;
+        }
     }
+    kv_attend_kernel<DP, PACKED, 1, WIDE><<<p.grid, THREADS, 0, st>>>(kv, q, a, p.row_tiles, p.least);
 }
 
 template <int DP>
 void launch_dim(const KvView &kv, const KvQueries &q, const KvAttend &a, const KvAttendPlan &p, hipStream_t st)
 {
-    if (kv.packed) launch_rows<DP, true>(kv, q, a, p, st);
-    else launch_rows<DP, false>(kv, q, a, p, st);
+    const bool wide = q.type == LPQ_TYPE_F32;
+    if (kv.packed && wide) launch_rows<DP, true, true>(kv, q, a, p, st);
+    else if (kv.packed) launch_rows<DP, true, false>(kv, q, a, p, st);
+    else if (wide) launch_rows<DP, false, true>(kv, q, a, p, st);
+    else launch_rows<DP, false, false>(kv, q, a, p, st);
 }
 
 }  // namespace
@@ -756,7 +764,7 @@ KvAttendPlan kv_attend_plan(const KvView &kv, int64_t nseq, int new_tokens, int 
 {
     KvAttendPlan p;
     const int64_t rows = (int64_t)new_tokens * group;
-    p.rows = rows <= 16 ? 16 : 32;
+    p.rows = rows > 16 && two_row_tiles(kv.dpad, kv.packed, wide) ? 32 : 16;
     p.row_tiles = (int)ceil_div(rows, (int64_t)p.rows);
     const int64_t pairs = nseq * kv.heads * p.row_tiles, tile = tile_tokens(kv.dpad, kv.packed);
     p.least = 0;
@@ -784,7 +792,9 @@ hipError_t launch_kv_attend(const KvView &kv, const KvQueries &q, const KvAttend
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.least == 0) return e;
     const unsigned rows = (unsigned)((int64_t)a.nseq * kv.heads * q.new_tokens * q.group);
-    kv_join_kernel<<<rows, THREADS, 0, st>>>(kv, q, a, p.row_tiles, p.rows, (int)p.grid);
+    // Many rows fill the chip with a wave each, few rows of many parts want more.
+    if (rows >= 1024) kv_join_kernel<64><<<rows, 64, 0, st>>>(kv, q, a, p.row_tiles, p.rows, (int)p.grid);
+    else kv_join_kernel<256><<<rows, 256, 0, st>>>(kv, q, a, p.row_tiles, p.rows, (int)p.grid);
     return hipGetLastError();
 }
 
