@@ -71,19 +71,21 @@ __device__ __forceinline__ int tiles_of(const KvView &kv, const KvAttend &a, int
     return tiles < 1 ? 1 : tiles;
 }
 
-// How the tiles of all (sequence, head, row tile), of all pairs for short, are dealt to the workgroups.
+// How the tiles of all (sequence, head), of all pairs for short, are dealt to the workgroups.  Where a head's rows take several
+// row tiles, as many workgroups have the same share, next to each other on one XCD (workgroups are dealt to the 8 of them in
+// turn), so that what one of them reads the others find in its L2.
 //   Long calls: one behind the other in equal runs.  A run ends where it ends: what a workgroup has of a pair that began before
 //   its run or goes on after it is a part, at most two per workgroup.
 //   Short calls (runs below CROSSING tiles), where going over to another pair costs as much as the run itself: a workgroup
 //   has one pair or an even part of one.
 // kv_join_kernel joins a pair's parts.  Fewer than 2^31 tiles (kv_attend_plan).
-constexpr unsigned CROSSING = 64;
+constexpr unsigned CROSSING = 200;
 struct Place {
-    int b, pair, tile, tiles;      // sequence, (head, row tile) of it, tile of that, tiles of the sequence
+    int b, pair, tile, tiles;      // sequence, head, tile of it, tiles of the sequence
     int run;                       // tiles of the workgroup
     int whole;                     // tiles of every workgroup that has a part of this pair, but the last
 };
-// Where a pair's parts are: part 0 in slot 2 first + 1, part u > 0 in slot 2 (first + u).
+// Where a pair's parts are, with r row tiles: part 0 of row tile t in slot 2 (first r + t) + 1, part u > 0 in 2 ((first + u) r + t).
 struct Parts {
     int first, count;
 };
@@ -101,19 +103,19 @@ __device__ __forceinline__ unsigned wave_scan(unsigned v)     // sums of the lan
 }
 // Every wave for itself: a lane adds up some neighbouring sequences, the lanes' sums are scanned, the lane whose sequences
 // hold the workgroup's first tile (or part) finds it.
-__device__ __forceinline__ bool first_place(const KvView &kv, const KvAttend &a, int pairs, int tile, int least, Place &out)
+__device__ __forceinline__ bool first_place(const KvView &kv, const KvAttend &a, unsigned me, unsigned of, int tile, int least, Place &out)
 {
-    const int lane = threadIdx.x & 63;
+    const int lane = threadIdx.x & 63, pairs = kv.heads;      // of a sequence
     const int per = (a.nseq + 63) / 64, b0 = lane * per, b1 = b0 + per < a.nseq ? b0 + per : a.nseq;
     unsigned mine = 0;
 #pragma unroll 4
     for (int b = b0; b < b1; ++b) mine += (unsigned)tiles_of(kv, a, a.lengths[b], tile);
     unsigned upto = wave_scan(mine);
     const unsigned total = (unsigned)__builtin_amdgcn_readlane((int)upto, 63) * pairs, all_pairs = (unsigned)a.nseq * pairs;
-    unsigned run = (total + gridDim.x - 1) / gridDim.x;
-    const bool apart = run < CROSSING && all_pairs < gridDim.x;
+    unsigned run = (total + of - 1) / of;
+    const bool apart = run < CROSSING && all_pairs < of;
     // apart: every pair rounds its number of parts up by less than one, so that this many tiles to a part fit the grid
-    if (apart) run = (total + gridDim.x - all_pairs - 1) / (gridDim.x - all_pairs);
+    if (apart) run = (total + of - all_pairs - 1) / (of - all_pairs);
     if (run < (unsigned)least) run = least;
     run = __builtin_amdgcn_readfirstlane((int)run);
     auto weight = [&](unsigned tiles) { return apart ? (tiles + run - 1) / run : tiles; };
@@ -122,7 +124,7 @@ __device__ __forceinline__ bool first_place(const KvView &kv, const KvAttend &a,
         for (int b = b0; b < b1; ++b) mine += weight((unsigned)tiles_of(kv, a, a.lengths[b], tile));
         upto = wave_scan(mine);
     }
-    const uint64_t from64 = apart ? (uint64_t)blockIdx.x : (uint64_t)run * blockIdx.x;
+    const uint64_t from64 = apart ? (uint64_t)me : (uint64_t)run * me;
     if (from64 >= (uint64_t)(unsigned)__builtin_amdgcn_readlane((int)upto, 63) * pairs) return false;
     const unsigned from = (unsigned)from64;
     const int who = __ffsll((unsigned long long)__ballot(from < upto * pairs)) - 1;      // the first lane that reaches beyond it
@@ -278,19 +280,28 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, WIDE)) void 
     __shared__ float row_scale[16 * RT], row_shift[16 * RT];
 
     const int lane0 = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int pairs = kv.heads * row_tiles, rows = q.new_tokens * q.group;
+    const int rows = q.new_tokens * q.group;
     const int64_t head_bytes = (int64_t)kv.page * RB;
     const Workspace ws = workspace(a.part, 2 * (int64_t)gridDim.x, 16 * RT, DP);
     Place at;
-    if (least == 0) {            // a workgroup per pair
-        at.b = __builtin_amdgcn_readfirstlane(blockIdx.x / pairs);
-        at.pair = blockIdx.x - at.b * pairs;
+    int row_tile;
+    unsigned share;                // of the tiles
+    if (least == 0) {              // a workgroup per pair and row tile
+        const int pair = __builtin_amdgcn_readfirstlane(blockIdx.x / row_tiles);
+        row_tile = blockIdx.x - pair * row_tiles;
+        share = pair;
+        at.b = __builtin_amdgcn_readfirstlane(pair / kv.heads);
+        at.pair = pair - at.b * kv.heads;
         at.tile = 0;
         at.tiles = tiles_of(kv, a, kv_uniform(a.lengths)[at.b], TOK);
         at.run = at.whole = at.tiles;
-    } else if (!first_place(kv, a, pairs, TOK, least, at)) {
-        return;
+    } else {
+        const unsigned eights = __builtin_amdgcn_readfirstlane(blockIdx.x / (8 * row_tiles)), in = blockIdx.x - eights * 8 * row_tiles;
+        row_tile = in >> 3;
+        share = eights * 8 + (in & 7);
+        if (!first_place(kv, a, share, gridDim.x / row_tiles, TOK, least, at)) return;
     }
+    const int row0 = row_tile * 16 * RT;
     int left = at.run, b = at.b, pair = at.pair, start = at.tile, tiles = at.tiles;
 
     for (;;) {
@@ -300,7 +311,7 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, WIDE)) void 
         start = __builtin_amdgcn_readfirstlane(start);
         tiles = __builtin_amdgcn_readfirstlane(tiles);
         left = __builtin_amdgcn_readfirstlane(left);
-        const int h = __builtin_amdgcn_readfirstlane(pair / row_tiles), row0 = (pair - h * row_tiles) * 16 * RT;
+        const int h = pair;
         const int end = left < tiles - start ? start + left : tiles;
         const int len = length_of(kv, a, kv_uniform(a.lengths)[b]);
         const int32_t *table = a.table + (int64_t)b * a.ld_table, *chosen = a.chosen + ((int64_t)b * kv.heads + h) * a.n_select;
@@ -585,9 +596,9 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, WIDE)) void 
         }
         __syncthreads();
         const bool whole = start == 0 && end == tiles;
-        const int64_t slot = 2 * (int64_t)blockIdx.x + (start == 0 ? 1 : 0);
-        if (least != 0 && start == 0 && threadIdx.x == 0)
-            ws.parts[(int64_t)b * pairs + pair] = {(int)blockIdx.x, 1 + (int)(((unsigned)(tiles - end) + at.whole - 1) / at.whole)};
+        const int64_t slot = 2 * ((int64_t)share * row_tiles + row_tile) + (start == 0 ? 1 : 0);
+        if (least != 0 && start == 0 && threadIdx.x == 0 && row_tile == 0)
+            ws.parts[(int64_t)b * kv.heads + pair] = {(int)share, 1 + (int)(((unsigned)(tiles - end) + at.whole - 1) / at.whole)};
 #pragma unroll 1
         for (int rt = 0; rt < RT; ++rt) {
             float top = NEG;
@@ -654,7 +665,7 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, WIDE)) void 
         // ---- on to what follows in the workgroup's run
         left -= end - start;
         if (left <= 0) return;
-        if (end == tiles && ++pair == pairs) {
+        if (end == tiles && ++pair == kv.heads) {
             pair = 0;
             if (++b >= a.nseq) return;
             tiles = tiles_of(kv, a, kv_uniform(a.lengths)[b], TOK);
@@ -674,10 +685,10 @@ __global__ __launch_bounds__(NT) void kv_join_kernel(KvView kv, KvQueries q, KvA
     const int rows = q.new_tokens * q.group;
     const int r = blockIdx.x % rows, bh = blockIdx.x / rows, h = bh % kv.heads, b = bh / kv.heads;
     const Workspace ws = workspace(a.part, 2 * (int64_t)grid, tile_rows, kv.dpad);
-    const Parts parts = ws.parts[(int64_t)bh * row_tiles + r / tile_rows];
+    const Parts parts = ws.parts[bh];
     if (parts.count <= 1) return;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, inside = r % tile_rows;
-    auto row_of = [&](int u) { return (2 * ((int64_t)parts.first + u) + (u == 0 ? 1 : 0)) * tile_rows + inside; };
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, row_tile = r / tile_rows, inside = r - row_tile * tile_rows;
+    auto row_of = [&](int u) { return (2 * (((int64_t)parts.first + u) * row_tiles + row_tile) + (u == 0 ? 1 : 0)) * tile_rows + inside; };
     float top = NEG;
     for (int u = tid; u < parts.count; u += NT) {
         const float m = ws.ml[row_of(u) * 2];
@@ -758,23 +769,26 @@ void launch_dim(const KvView &kv, const KvQueries &q, const KvAttend &a, const K
 
 }  // namespace
 
-// Sequences of up to 1024 tokens get a workgroup per (sequence, head, row tile): joining parts would cost more than it
-// gives.  Otherwise as many workgroups as the chip holds at once, and no fewer than 8 tiles each.
+// Sequences of up to 1024 tokens get a workgroup per pair and row tile: joining parts would cost more than it
+// gives.  Otherwise as many workgroups as the chip holds at once, and no fewer than 4 tiles each.
 KvAttendPlan kv_attend_plan(const KvView &kv, int64_t nseq, int new_tokens, int group, int64_t tokens, bool wide)
 {
     KvAttendPlan p;
     const int64_t rows = (int64_t)new_tokens * group;
     p.rows = rows > 16 && two_row_tiles(kv.dpad, kv.packed, wide) ? 32 : 16;
     p.row_tiles = (int)ceil_div(rows, (int64_t)p.rows);
-    const int64_t pairs = nseq * kv.heads * p.row_tiles, tile = tile_tokens(kv.dpad, kv.packed);
+    const int64_t pairs = nseq * kv.heads, tile = tile_tokens(kv.dpad, kv.packed);
     p.least = 0;
-    p.grid = (unsigned)pairs;
+    p.grid = (unsigned)(pairs * p.row_tiles);
     p.bytes = 0;
     const int64_t tiles = ceil_div(tokens, tile);
     if (tokens > 1024 && pairs * tiles < (int64_t(1) << 31)) {      // (beyond that there are pairs enough)
-        p.least = 8;
-        const int64_t most = ceil_div(tiles, (int64_t)p.least) * pairs, room = 256 * blocks_per_cu(kv.dpad, kv.packed, p.rows / 16, wide);
-        p.grid = (unsigned)(most < room ? most : room);
+        p.least = 4;
+        const int64_t most = ceil_div(tiles, (int64_t)p.least) * pairs;
+        const int64_t room = ceil_div((int64_t)256 * blocks_per_cu(kv.dpad, kv.packed, p.rows / 16, wide), (int64_t)p.row_tiles);
+        int64_t shares = most < room ? most : room;
+        if (p.row_tiles > 1) shares = round_up(shares, 8);
+        p.grid = (unsigned)(shares * p.row_tiles);
         p.bytes = ((size_t)2 * p.grid * p.rows * (kv.dpad + 2) + (size_t)2 * pairs) * sizeof(float);
     }
     return p;
