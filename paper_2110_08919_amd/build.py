@@ -47,7 +47,7 @@ def device_asm(src: str) -> str:
 
 
 def keeps_asm(src: str) -> bool:
-    return os.path.basename(src).startswith("search_mfma")
+    return os.path.basename(src).startswith(("search_mfma", "kv_attend", "kv_select"))
 
 
 def _compile(src: str, force: bool, ablation: bool) -> str:
