@@ -11,8 +11,8 @@
 // value), three for float32 (Qmax = 2088895, 2^-22).
 // Weights exp2(t - m) are rounded to fp16 (float32 calls: two fp16 terms) and multiply the value codes, which fp16 holds
 // exactly, on the fp16 matrix instruction with float32 sums.  The sum of weights is taken of the rounded ones.  m is a
-// maximum that may lag behind by 2^8 (the weights of a tile reach 2^14 then, and 2^-24 below that the smallest that counts):
-// it moves, and the sums are rescaled, only in tiles where a score passes it by more.
+// maximum that may lag behind by 2 (weights are lifted by 2^13, reach 2^15, and are rounded to 2^-24 at the small end, 2^-37 of
+// the largest token's): it moves, and the sums are rescaled, only in tiles where a score passes it by more.
 //
 // Layout.  Tokens are the rows of the first product (S^T = K Q^T) and the summed index of the second (O^T = V^T P^T), so
 // the registers that hold scores of a token group are the operand of the second product as they are: register j of lane
@@ -36,8 +36,8 @@ typedef _Float16 v8h __attribute__((ext_vector_type(8)));
 
 constexpr int THREADS = 256, WAVES = 4;
 constexpr float NEG = -INFINITY;
-constexpr float HEADROOM = 8.0f;     // how far scores may pass the maximum before it moves (powers of two)
-constexpr float LIFT = 6.0f;         // weights are exp2(t - m + LIFT): at most 2^14, and small ones stay normal fp16
+constexpr float HEADROOM = 2.0f;     // how far scores may pass the maximum before it moves (powers of two)
+constexpr float LIFT = 13.0f;        // weights are exp2(t - m + LIFT): at most 2^15, and fp16 holds them to 2^-37 of the largest
 
 // Tokens a wave has in registers: 64 where a row of codes has at
 // most 64 bytes, else 32.
@@ -114,8 +114,19 @@ __device__ __forceinline__ bool first_place(const KvView &kv, const KvAttend &a,
     const unsigned total = (unsigned)__builtin_amdgcn_readlane((int)upto, 63) * pairs, all_pairs = (unsigned)a.nseq * pairs;
     unsigned run = (total + of - 1) / of;
     const bool apart = run < CROSSING && all_pairs < of;
-    // apart: every pair rounds its number of parts up by less than one, so that this many tiles to a part fit the grid
-    if (apart) run = (total + of - all_pairs - 1) / (of - all_pairs);
+    if (apart) {
+        // The smallest run whose parts fit the grid, or nearly: at least total / of, and every pair rounds its number of parts up
+        // by less than one, so that total / (of - all_pairs) is enough.
+        unsigned enough = (total + of - all_pairs - 1) / (of - all_pairs);
+        for (int i = 0; i < 4 && run + 1 < enough; ++i) {
+            const unsigned mid = (run + enough) / 2;
+            unsigned parts = 0;
+            for (int b = b0; b < b1; ++b) parts += ((unsigned)tiles_of(kv, a, a.lengths[b], tile) + mid - 1) / mid;
+            if ((unsigned)__builtin_amdgcn_readlane((int)wave_scan(parts), 63) * pairs <= of) enough = mid;
+            else run = mid + 1;
+        }
+        run = enough;
+    }
     if (run < (unsigned)least) run = least;
     run = __builtin_amdgcn_readfirstlane((int)run);
     auto weight = [&](unsigned tiles) { return apart ? (tiles + run - 1) / run : tiles; };
@@ -687,8 +698,16 @@ __global__ __launch_bounds__(NT) void kv_join_kernel(KvView kv, KvQueries q, KvA
     const Workspace ws = workspace(a.part, 2 * (int64_t)grid, tile_rows, kv.dpad);
     const Parts parts = ws.parts[bh];
     if (parts.count <= 1) return;
+    const int cols = kv.dpad >> 2, groups = NT / cols;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, row_tile = r / tile_rows, inside = r - row_tile * tile_rows;
     auto row_of = [&](int u) { return (2 * (((int64_t)parts.first + u) * row_tiles + row_tile) + (u == 0 ? 1 : 0)) * tile_rows + inside; };
+    const int col = tid % cols, grp = tid / cols;
+    // the first parts' sums are under way while the weights are made
+    auto sums_of = [&](int u) { return *reinterpret_cast<const float4 *>(ws.sums + row_of(u < parts.count ? u : 0) * kv.dpad + 4 * col); };
+    constexpr int AHEAD = 4;
+    float4 ahead[AHEAD];
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) ahead[i] = sums_of(grp + i * groups);
     float top = NEG;
     for (int u = tid; u < parts.count; u += NT) {
         const float m = ws.ml[row_of(u) * 2];
@@ -714,13 +733,18 @@ __global__ __launch_bounds__(NT) void kv_join_kernel(KvView kv, KvQueries q, KvA
     l = 0.0f;
 #pragma unroll
     for (int w = 0; w < NT / 64; ++w) l += redl[w];
-    const int cols = kv.dpad >> 2, groups = NT / cols, col = tid % cols, grp = tid / cols;
     float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
     if (grp < groups) {
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            const float f = grp + i * groups < parts.count ? weight[grp + i * groups] : 0.0f;
+            const float4 y = ahead[i];
+            if (f != 0.0f) { x.x += y.x * f; x.y += y.y * f; x.z += y.z * f; x.w += y.w * f; }
+        }
 #pragma unroll 4
-        for (int u = grp; u < parts.count; u += groups) {
+        for (int u = grp + AHEAD * groups; u < parts.count; u += groups) {
             const float f = weight[u];
-            const float4 y = *reinterpret_cast<const float4 *>(ws.sums + row_of(u) * kv.dpad + 4 * col);
+            const float4 y = sums_of(u);
             x.x += y.x * f; x.y += y.y * f; x.z += y.z * f; x.w += y.w * f;
         }
         sums[tid] = x;

@@ -52,6 +52,8 @@ __device__ __forceinline__ void pick(const int32_t *score, int np, const KvSelec
     __shared__ uint32_t red[2][W];
     __shared__ int count[2][W];
     __shared__ int before[2][KEYS * W];
+    constexpr int CUTS = KEYS == 1 ? 7 : 3;
+    __shared__ int cut[2][W][CUTS];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int rounds = AGAIN ? (np + NT * KEYS - 1) / (NT * KEYS) : 1;
     uint32_t key[KEYS];
@@ -92,34 +94,45 @@ __device__ __forceinline__ void pick(const int32_t *score, int np, const KvSelec
         there += count[0][w];
     }
     const int want = there < s.n_select ? there : s.n_select;
-    // Largest bound T with at least `want` keys >= T, T in [lo, hi] or all ones (only kept pages are wanted then).
-    // Keys of all ones are >= every T, so with want <= their number T ends at hi or above; taken care of by the last test.
-    auto at_least = [&](uint32_t t, int buf) {
-        int c = 0;
+    // Largest bound T with at least `want` keys >= T: T in [lo, hi], or all ones where the pages kept in any case are enough.
+    // Each step counts for CUTS bounds at once (ballots of a wave, summed over the waves through LDS) and leaves one of
+    // CUTS + 1 parts of the interval.
+    auto enough = [&](uint32_t from, uint32_t by, uint32_t span, int buf) {      // how many of from + by, from + 2 by .. are low enough
+        int c[CUTS] = {};
         for (int r = 0; r < rounds; ++r) {
             if (AGAIN) fetch(r);
 #pragma unroll
-            for (int i = 0; i < KEYS; ++i) c += __popcll(__ballot(key[i] >= t));
-        }
-        if (lane == 0) count[buf][wave] = c;
-        __syncthreads();
-        c = 0;
+            for (int j = 0; j < CUTS; ++j) {
+                const uint32_t at = from + ((j + 1) * by < span ? (j + 1) * by : span);
 #pragma unroll
-        for (int w = 0; w < W; ++w) c += count[buf][w];
-        return c;
+                for (int i = 0; i < KEYS; ++i) c[j] += __popcll(__ballot(key[i] >= at));
+            }
+        }
+        int mine = 0;
+#pragma unroll
+        for (int j = 0; j < CUTS; ++j) mine = lane == j ? c[j] : mine;
+        if (lane < CUTS) cut[buf][wave][lane] = mine;
+        __syncthreads();
+        mine = 0;
+        if (lane < CUTS) {
+#pragma unroll
+            for (int w = 0; w < W; ++w) mine += cut[buf][w][lane];
+        }
+        return __popcll(__ballot(lane < CUTS && mine >= want));
     };
-    __syncthreads();
     uint32_t T = 0xFFFFFFFFu;
     int buf = 0;
-    if (want > 0 && at_least(0xFFFFFFFFu, buf) < want) {
-        buf ^= 1;
+    if (want > 0 && enough(0xFFFFFFFFu, 0, 0, buf) == 0) {
         // here some scored page is wanted: lo <= hi, and at least `want` keys are >= lo
-        uint32_t a = lo, z = hi;
-        while (a < z) {
-            const uint32_t mid = a + (z - a + 1) / 2;       // a < mid <= z
-            if (at_least(mid, buf) >= want) a = mid;
-            else z = mid - 1;
+        uint32_t a = lo, span = hi - lo;
+        while (span) {
             buf ^= 1;
+            const uint32_t by = span / (CUTS + 1) + 1;       // CUTS by < 2^32
+            const int k = enough(a, by, span, buf);
+            const uint32_t under = k * by < span ? k * by : span;
+            if (k < CUTS) span = (k + 1) * by < span ? (k + 1) * by - 1 : span - 1;      // that one is too high
+            span -= under;
+            a += under;
         }
         T = a;
     }
