@@ -214,7 +214,27 @@ __global__ __launch_bounds__(NT) void kv_score_kernel(KvView kv, KvQueries q, Kv
     if (!FUSED && part * BLOCK_PAGES >= np) return;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = lane & 15, g = lane >> 4;
 
-    // The pages' bounds are under way while the queries are made ready.
+    // Query codes: z = rint(q s * (127 / A)), A the largest |q s| of the head's rows; what is not finite counts as 0.
+    const int rows = q.new_tokens * q.group, chunks = DP / 8, items = rows * chunks;
+    const int64_t base = (int64_t)b * q.ld_seq + (int64_t)h * q.group * q.ld_head;
+    auto row_at = [&](int r) { return base + (int64_t)(r / q.group) * q.ld_token + (int64_t)(r % q.group) * q.ld_head; };
+    auto fetch = [&](int t, float *st) {
+        const int r = t / chunks, c0 = (t % chunks) * 8;
+        kv_load_floats8(kv.key.s + h * DP + c0, st);
+        return kv_load8(q.p, q.type, row_at(r) + c0, t < items ? kv.dim - c0 : 0);
+    };
+    auto scaled = [&](int t, Raw8 raw, const float *st, float *v) {
+        kv_floats8(raw, q.type, t < items ? kv.dim - (t % chunks) * 8 : 0, v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float x = __fmul_rn(v[e], st[e]);
+            v[e] = fabsf(x) <= 3.402823466e38f ? x : 0.0f;
+        }
+    };
+    float step[8], mine[8];
+    const Raw8 raw = fetch(tid, step);
+
+    // The pages' bounds, behind the first queries: loads are waited for in order, so these arrive while the queries are made ready.
     const int32_t *table = s.table + (int64_t)b * s.ld_table;
     const int page0 = part * BLOCK_PAGES + wave * 16 * UNROLL;
     int32_t id[UNROLL];
@@ -232,25 +252,15 @@ __global__ __launch_bounds__(NT) void kv_score_kernel(KvView kv, KvQueries q, Kv
         for (int st = 0; st < STEPS; ++st) x[u][st] = *reinterpret_cast<const v4i *>(row + 64 * st);
     }
 
-    // Query codes: z = rint(q s * (127 / A)), A the largest |q s| of the head's rows; what is not finite counts as 0.
-    const int rows = q.new_tokens * q.group, chunks = DP / 8;
-    const int64_t base = (int64_t)b * q.ld_seq + (int64_t)h * q.group * q.ld_head;
-    auto row_at = [&](int r) { return base + (int64_t)(r / q.group) * q.ld_token + (int64_t)(r % q.group) * q.ld_head; };
-    auto load = [&](int t, float *v) {
-        const int r = t / chunks, c0 = (t % chunks) * 8;
-        kv_floats8(kv_load8(q.p, q.type, row_at(r) + c0, kv.dim - c0), q.type, kv.dim - c0, v);
-        const float *st = kv.key.s + h * DP + c0;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const float x = __fmul_rn(v[e], st[e]);
-            v[e] = fabsf(x) <= 3.402823466e38f ? x : 0.0f;
-        }
-    };
     for (int i = tid; i < 2 * DP; i += NT) wsum[i] = 0;
     float most = 0.0f;
-    for (int t = tid; t < rows * chunks; t += NT) {
-        float v[8];
-        load(t, v);
+    scaled(tid, raw, step, mine);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(mine[e]));
+    for (int t = tid + NT; t < items; t += NT) {
+        float st[8], v[8];
+        const Raw8 x = fetch(t, st);
+        scaled(t, x, st, v);
 #pragma unroll
         for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(v[e]));
     }
@@ -262,15 +272,20 @@ __global__ __launch_bounds__(NT) void kv_score_kernel(KvView kv, KvQueries q, Kv
     for (int w = 0; w < WAVES; ++w) most = fmaxf(most, red[w]);
     // below that, 127 / A would leave the range of binary32
     const float f = most > 1e-30f ? __fdiv_rn(127.0f, most) : 0.0f;
-    for (int t = tid; t < rows * chunks; t += NT) {
-        float v[8];
-        load(t, v);
+    auto add = [&](int t, const float *v) {
         const int c0 = (t % chunks) * 8;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const int z = (int)rintf(__fmul_rn(v[e], f));
             if (z) atomicAdd(&wsum[(z > 0 ? DP : 0) + c0 + e], z);      // integers: the order does not matter
         }
+    };
+    add(tid, mine);
+    for (int t = tid + NT; t < items; t += NT) {
+        float st[8], v[8];
+        const Raw8 x = fetch(t, st);
+        scaled(t, x, st, v);
+        add(t, v);
     }
     __syncthreads();
     for (int i = tid; i < 2 * DP; i += NT) {
