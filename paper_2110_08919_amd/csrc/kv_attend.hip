@@ -20,8 +20,6 @@
 // 4 g .. 4 g + 3 of two groups.  A lane owns dpad / 16 neighbouring features of the values: it loads them from the rows
 // of its 8 tokens and gathers the operand of each with byte permutes.  Nothing goes through LDS until the end.  Each wave
 // walks its own tiles of 32 or 64 tokens with the next tile's loads in flight.
-#include <type_traits>
-
 #include "kv_internal.h"
 #include "wave_ops.h"
 
@@ -89,18 +87,6 @@ struct Place {
 struct Parts {
     int first, count;
 };
-__device__ __forceinline__ unsigned wave_scan(unsigned v)     // sums of the lanes up to each
-{
-    auto moved = [](unsigned x, auto ctrl, auto rows) { return (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, decltype(ctrl)::value, decltype(rows)::value, 0xF, false); };
-    typedef std::integral_constant<int, 0xF> all;
-    v += moved(v, std::integral_constant<int, 0x111>(), all());       // 1, 2, 4 and 8 lanes back in a row of 16
-    v += moved(v, std::integral_constant<int, 0x112>(), all());
-    v += moved(v, std::integral_constant<int, 0x114>(), all());
-    v += moved(v, std::integral_constant<int, 0x118>(), all());
-    v += moved(v, std::integral_constant<int, 0x142>(), std::integral_constant<int, 0xA>());     // last lane of the row before
-    v += moved(v, std::integral_constant<int, 0x143>(), std::integral_constant<int, 0xC>());     // last lane of the first half
-    return v;
-}
 // Every wave for itself: a lane adds up some neighbouring sequences, the lanes' sums are scanned, the lane whose sequences
 // hold the workgroup's first tile (or part) finds it.
 __device__ __forceinline__ bool first_place(const KvView &kv, const KvAttend &a, unsigned me, unsigned of, int tile, int least, Place &out)
@@ -714,8 +700,7 @@ __global__ __launch_bounds__(NT) void kv_join_kernel(KvView kv, KvQueries q, KvA
         weight[u] = m;
         top = fmaxf(top, m);
     }
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
+    top = __uint_as_float(wave_all(__float_as_uint(top), [](uint32_t x, uint32_t y) { return __float_as_uint(fmaxf(__uint_as_float(x), __uint_as_float(y))); }));
     if (lane == 0) red[wave] = top;
     __syncthreads();
 #pragma unroll
@@ -726,8 +711,7 @@ __global__ __launch_bounds__(NT) void kv_join_kernel(KvView kv, KvQueries q, KvA
         weight[u] = f;
         l += ws.ml[row_of(u) * 2 + 1] * f;
     }
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) l += __shfl_xor(l, o, 64);
+    l = __uint_as_float(wave_all(__float_as_uint(l), [](uint32_t x, uint32_t y) { return __float_as_uint(__uint_as_float(x) + __uint_as_float(y)); }));
     if (lane == 0) redl[wave] = l;
     __syncthreads();
     l = 0.0f;

@@ -78,12 +78,8 @@ __device__ __forceinline__ void pick(const int32_t *score, int np, const KvSelec
             }
         }
     }
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const uint32_t a = __shfl_xor(lo, o, 64), c = __shfl_xor(hi, o, 64);
-        lo = a < lo ? a : lo;
-        hi = c > hi ? c : hi;
-    }
+    lo = wave_all(lo, [](uint32_t x, uint32_t y) { return x < y ? x : y; });
+    hi = wave_all(hi, [](uint32_t x, uint32_t y) { return x > y ? x : y; });
     if (lane == 0) { red[0][wave] = lo; red[1][wave] = hi; count[0][wave] = there; }
     __syncthreads();
     there = 0;
@@ -137,13 +133,12 @@ __device__ __forceinline__ void pick(const int32_t *score, int np, const KvSelec
         T = a;
     }
     // Pages above T all, of those at T the first ones.
-    int above_all = 0;                                       // keys > T of the rounds before
-    int equal_all = 0;
+    int above_all = 0, equal_all = 0;                        // keys > T, == T of the rounds before
     int total_above = 0;
-    {
+    if (AGAIN) {
         int c = 0;
         for (int r = 0; r < rounds; ++r) {
-            if (AGAIN) fetch(r);
+            fetch(r);
 #pragma unroll
             for (int i = 0; i < KEYS; ++i) c += __popcll(__ballot(key[i] > T));
         }
@@ -153,7 +148,6 @@ __device__ __forceinline__ void pick(const int32_t *score, int np, const KvSelec
 #pragma unroll
         for (int w = 0; w < W; ++w) total_above += count[0][w];
     }
-    const int ties = want - total_above;                     // keys equal to T to take
     for (int r = 0; r < rounds; ++r) {
         if (AGAIN) fetch(r);
 #pragma unroll
@@ -166,18 +160,15 @@ __device__ __forceinline__ void pick(const int32_t *score, int np, const KvSelec
             int run = wave == 0 ? above_all : equal_all;
             for (int e0 = 0; e0 < KEYS * W; e0 += 64) {
                 const int v = e0 + lane < KEYS * W ? before[wave][e0 + lane] : 0;
-                int sum = v;
-#pragma unroll
-                for (int o = 1; o < 64; o <<= 1) {
-                    const int t = __shfl_up(sum, o, 64);
-                    if (lane >= o) sum += t;
-                }
+                const int sum = (int)wave_scan((uint32_t)v);
                 if (e0 + lane < KEYS * W) before[wave][e0 + lane] = run + sum - v;
-                run += __shfl(sum, 63, 64);
+                run += __builtin_amdgcn_readlane(sum, 63);
             }
             if (lane == 0) count[wave][0] = run;
         }
         __syncthreads();
+        if (!AGAIN) total_above = count[0][0];
+        const int ties = want - total_above;                 // keys equal to T to take
         const uint64_t below = lane == 0 ? 0 : ~0ull >> (64 - lane);
 #pragma unroll
         for (int i = 0; i < KEYS; ++i) {
@@ -264,8 +255,7 @@ __global__ __launch_bounds__(NT) void kv_score_kernel(KvView kv, KvQueries q, Kv
 #pragma unroll
         for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(v[e]));
     }
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) most = fmaxf(most, __shfl_xor(most, o, 64));
+    most = __uint_as_float(wave_all(__float_as_uint(most), [](uint32_t x, uint32_t y) { return x > y ? x : y; }));      // 0 or more: ordered as integers too
     if (lane == 0) red[wave] = most;
     __syncthreads();
 #pragma unroll

@@ -50,4 +50,34 @@ __device__ __forceinline__ int wave_max_i32(int v)
 
 __device__ __forceinline__ int wave_min_i32(int v) { return -wave_max_i32(-v); }
 
+// op over all lanes, the same in each of them; the four rows come together through scalar registers.
+template <class F>
+__device__ __forceinline__ uint32_t wave_all(uint32_t v, F op)
+{
+    v = op(v, (uint32_t)dpp_move<DPP_XOR1>((int)v));
+    v = op(v, (uint32_t)dpp_move<DPP_XOR2>((int)v));
+    v = op(v, (uint32_t)dpp_move<DPP_HALF_MIRROR>((int)v));
+    v = op(v, (uint32_t)dpp_move<DPP_ROW_MIRROR>((int)v));
+    const int r0 = __builtin_amdgcn_readlane((int)v, 0), r1 = __builtin_amdgcn_readlane((int)v, 16);
+    const int r2 = __builtin_amdgcn_readlane((int)v, 32), r3 = __builtin_amdgcn_readlane((int)v, 48);
+    return op(op((uint32_t)r0, (uint32_t)r1), op((uint32_t)r2, (uint32_t)r3));
+}
+
+// Sums of the lanes up to each: 1, 2, 4 and 8 lanes back in a row, then the last lane of the row before, then of the first half.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t dpp_or_zero(uint32_t v)
+{
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xF, false);
+}
+__device__ __forceinline__ uint32_t wave_scan(uint32_t v)
+{
+    v += dpp_or_zero<0x111, 0xF>(v);
+    v += dpp_or_zero<0x112, 0xF>(v);
+    v += dpp_or_zero<0x114, 0xF>(v);
+    v += dpp_or_zero<0x118, 0xF>(v);
+    v += dpp_or_zero<0x142, 0xA>(v);
+    v += dpp_or_zero<0x143, 0xC>(v);
+    return v;
+}
+
 }  // namespace lpq
