@@ -786,8 +786,10 @@ void launch_dim(const KvView &kv, const KvQueries &q, const KvAttend &a, const K
 
 }  // namespace
 
-// Sequences of up to 1024 tokens get a workgroup per pair and row tile: joining parts would cost more than it
-// gives.  Otherwise as many workgroups as the chip holds at once, and no fewer than 4 tiles each.
+// Short sequences get a workgroup per pair and row tile: joining parts would cost more than it gives.  Otherwise as many workgroups as
+// the chip holds at once, and no fewer than 4 tiles each.  Short is up to 1024 tokens, fewer where a tile is much work and workgroups
+// are few: 16 pairs, whole against split and joined, us: 1000 tokens of 64 features 10.9, 12.8, of 128 13.6, 13.5, of 256 19.6, 17.2;
+// 32 rows at a time: 500 tokens of 128 17.0, 17.1, 700 of 128 19.0, 17.7, 350 of 256 25.8, 21.2.  512 pairs of 128, 1000 tokens: 24.4, 31.3.
 KvAttendPlan kv_attend_plan(const KvView &kv, int64_t nseq, int new_tokens, int group, int64_t tokens, bool wide)
 {
     KvAttendPlan p;
@@ -799,7 +801,8 @@ KvAttendPlan kv_attend_plan(const KvView &kv, int64_t nseq, int new_tokens, int 
     p.grid = (unsigned)(pairs * p.row_tiles);
     p.bytes = 0;
     const int64_t tiles = ceil_div(tokens, tile);
-    if (tokens > 1024 && pairs * tiles < (int64_t(1) << 31)) {      // (beyond that there are pairs enough)
+    const bool few = (int64_t)p.grid < 256 && tokens * kv.dpad * (p.rows / 16) > 128 * 1024;
+    if ((tokens > 1024 || few) && pairs * tiles < (int64_t(1) << 31)) {      // (beyond that there are pairs enough)
         p.least = 4;
         const int64_t most = ceil_div(tiles, (int64_t)p.least) * pairs;
         const int64_t room = ceil_div((int64_t)256 * blocks_per_cu(kv.dpad, kv.packed, p.rows / 16, wide), (int64_t)p.row_tiles);
