@@ -10,7 +10,8 @@
 // digits for 16-bit queries (Qmax = 16319: an error of 2^-15 of the row's largest q', where bfloat16 holds 2^-9 of each
 // value), three for float32 (Qmax = 2088895, 2^-22).
 // Weights exp2(t - m) are rounded to fp16 (float32 calls: two fp16 terms) and multiply the value codes, which fp16 holds
-// exactly, on the fp16 matrix instruction with float32 sums.  The sum of weights is taken of the rounded ones.  m is a
+// exactly, on the fp16 matrix instruction with float32 sums.  The sum of weights is taken of the rounded ones, as their product
+// with ones: a sixteenth of what it takes the vector pipe.  m is a
 // maximum that may lag behind by 2 (weights are lifted by 2^13, reach 2^15, and are rounded to 2^-24 at the small end, 2^-37 of
 // the largest token's): it moves, and the sums are rescaled, only in tiles where a score passes it by more.
 //
@@ -211,27 +212,19 @@ struct Tile {
     uint32_t v[TG / 2][8][VW];
 };
 
-// Halves [features t of token e | of token e + 1] as fp16, from the two tokens' shares of a row.
+// Halves [features t of token e | of token e + 1] as fp16 c 2^-9, exactly, from the two tokens' shares of a row.  A byte alone in a half
+// is the fp16 number u 2^-24 (c + 128, packed: c + 8 or 16 c + 128, below 2^10): one multiplication by 2^15 or 2^11 and an addition.
+constexpr float VALUE_SCALE = 512.0f;
 template <bool PACKED>
-__device__ __forceinline__ uint32_t value_pair(uint32_t w0, uint32_t w1, int t)
+__device__ __forceinline__ uint32_t value_pair(uint32_t w0, uint32_t w1, int t, v2h off)
 {
     const int byte = PACKED ? (t >> 1) & 3 : t & 3;
-    const uint32_t sel = 0x0c000c00u | (uint32_t)byte | (uint32_t)(4 + byte) << 16;
-    const uint32_t x = __builtin_amdgcn_perm(w1, w0, sel);
-    if constexpr (!PACKED) {
-        const v2h off = {(_Float16)1152.0f, (_Float16)1152.0f};                 // 1024 + 128 + c, less that: exact
-        const v2h y = __builtin_bit_cast(v2h, x ^ 0x64806480u) - off;
-        return __builtin_bit_cast(uint32_t, y);
-    } else if ((t & 1) == 0) {
-        const v2h off = {(_Float16)1032.0f, (_Float16)1032.0f};                 // 1024 + 8 + c
-        const v2h y = __builtin_bit_cast(v2h, (x & 0x000f000fu) | 0x64006400u) - off;
-        return __builtin_bit_cast(uint32_t, y);
-    } else {
-        const v2h off = {(_Float16)1152.0f, (_Float16)1152.0f}, f = {(_Float16)0.0625f, (_Float16)0.0625f};
-        const v2h y = (__builtin_bit_cast(v2h, (x & 0x00f000f0u) | 0x64006400u) - off) * f;    // 1024 + 128 + 16 c
-        return __builtin_bit_cast(uint32_t, y);
-    }
+    uint32_t x = __builtin_amdgcn_perm(w1, w0, 0x0c000c00u | (uint32_t)byte | (uint32_t)(4 + byte) << 16);
+    const _Float16 up = (_Float16)(PACKED && (t & 1) ? 2048.0f : 32768.0f);
+    if (PACKED) x &= t & 1 ? 0x00f000f0u : 0x000f000fu;
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(__builtin_bit_cast(v2h, x), v2h{up, up}, off));
 }
+__device__ __forceinline__ uint32_t value_word(bool packed, uint32_t w) { return packed ? w : w ^ 0x80808080u; }
 
 // Workspace: sums [2 grid][rows of a tile][DP], then maximum and sum of weights [2 grid][rows of a tile][2], then Parts per pair.
 struct Workspace {
@@ -284,7 +277,7 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, WIDE)) void 
     __shared__ float row_scale[16 * RT], row_shift[16 * RT];
 
     const int lane0 = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int rows = q.new_tokens * q.group;
+    const int rows = q.new_tokens * q.group, type = WIDE ? LPQ_TYPE_F32 : q.type == LPQ_TYPE_F16 ? LPQ_TYPE_F16 : LPQ_TYPE_BF16;
     const int64_t head_bytes = (int64_t)kv.page * RB;
     const Workspace ws = workspace(a.part, 2 * (int64_t)gridDim.x, 16 * RT, DP);
     Place at;
@@ -389,14 +382,13 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, WIDE)) void 
             const int r16 = i * PASS + tid / LR, r = row0 + r16;
             const bool on = r16 < 16 * RT && r < rows && 8 * qc < DP;
             const int64_t qat = (int64_t)b * q.ld_seq + (int64_t)(r / q.group) * q.ld_token + (int64_t)(h * q.group + r % q.group) * q.ld_head;
-            return kv_load8(q.p, q.type, qat + qc0, on ? kv.dim - qc0 : 0);
+            return kv_load8(q.p, type, qat + qc0, on ? kv.dim - qc0 : 0);
         };
         Raw8 raw = load_queries(0);
         float step[8];
         kv_load_floats8(kv.key.s + h * DP + qc0, step);
         Where now, next;
         look_up(0, page_now, pos_now);
-        if (turns > PER) look_up(PER, page_then, pos_then);
         find(0, now);
         load_keys(now);
         load_values(now);
@@ -406,7 +398,7 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, WIDE)) void 
         for (int i = 0; i < PASSES; ++i) {
             const int r16 = i * PASS + tid / LR;
             float v[8], most = 0.0f;
-            kv_floats8(raw, q.type, kv.dim - qc0, v);
+            kv_floats8(raw, type, kv.dim - qc0, v);
             if (i + 1 < PASSES) raw = load_queries(i + 1);
             if (a.lse) {
                 float offset = 0.0f;
@@ -425,7 +417,7 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, WIDE)) void 
             }
             most = row_max<LR>(most);
             const bool bad = most == INFINITY, use = !bad && most > 1e-30f;  // below that QMAX / most leaves the range of binary32, and scores are 0
-            const float f = use ? QMAX / most : 0.0f;
+            const float f = use ? __uint_as_float(__float_as_uint(QMAX / most) | (__float_as_uint(a.scale) & 0x80000000u)) : 0.0f;      // of scale's sign
             int8_t d[ND][8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
@@ -453,12 +445,17 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, WIDE)) void 
                         *reinterpret_cast<uint2 *>(row + 8 * qc) = make_uint2(w[0], w[1]);
                     }
                 }
-                if (qc == 0) row_scale[r16] = bad ? NAN : (use ? most / QMAX * a.scale * (PACKED ? 1.44269504088896f / 16.0f : 1.44269504088896f) : 0.0f);
+                // above 0, so that -inf in the place of a masked score stays that (below 1e-30 scores are 0 in any case)
+                if (qc == 0) row_scale[r16] = bad ? NAN : fmaxf(most / QMAX * fabsf(a.scale) * (PACKED ? 1.44269504088896f / 16.0f : 1.44269504088896f), 1e-30f);
             }
         }
         __syncthreads();
         v4i qd[RT][ND][NS];      // lane (n, g): features 64 st + 16 g .. + 15 of row n
-        float rs[RT], m[RT], l[RT];
+        float rs[RT], m[RT];
+        v4f l[RT];               // sums of the weights, four times the same
+        v8h ones;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) ones[e] = (_Float16)1.0f;
         int last[RT];            // last position a row sees
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
@@ -469,7 +466,7 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, WIDE)) void 
             }
             rs[rt] = row_scale[rt * 16 + n];
             m[rt] = NEG;
-            l[rt] = 0.0f;
+            l[rt] = v4f{0.f, 0.f, 0.f, 0.f};
             const int r = row0 + rt * 16 + n;
             const int see = len - q.new_tokens + r / q.group;
             last[rt] = r < rows ? (see < -1 ? -1 : see) : -1;
@@ -481,6 +478,8 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, WIDE)) void 
         for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
             for (int t = 0; t < NT; ++t) acc[rt][t] = v4f{0.f, 0.f, 0.f, 0.f};
+
+        if (turns > PER) look_up(PER, page_then, pos_then);
 
         // ---- the wave's tiles: the next tile's keys are asked for as soon as this one's are used up, its values likewise
         // (behind the last tile as well, with nothing to fetch: loads that every turn makes are waited for one kind at a time)
@@ -517,15 +516,18 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, WIDE)) void 
                     }
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        if constexpr (WIDE) s[rt][tg][j] = ((float)sum[0][j] * 16384.0f + (float)(sum[1][j] * 128 + sum[2][j])) * rs[rt];
-                        else s[rt][tg][j] = (float)(sum[0][j] * 128 + sum[1][j]) * rs[rt];
+                        if constexpr (WIDE) s[rt][tg][j] = __builtin_fmaf((float)sum[0][j], 16384.0f, (float)(sum[1][j] * 128 + sum[2][j]));
+                        else s[rt][tg][j] = (float)(sum[0][j] * 128 + sum[1][j]);
                     }
                 }
             load_keys(next);
+            v2h off = {(_Float16)(PACKED ? -8.0f / VALUE_SCALE : -128.0f / VALUE_SCALE), (_Float16)(PACKED ? -8.0f / VALUE_SCALE : -128.0f / VALUE_SCALE)};
+            asm("" : "+v"(off));           // in a vector register: an instruction takes one scalar constant, and that is the other factor
             v8h w[RT][NP][TG / 2];
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt) {
                 if (part) {
+                    asm volatile("");      // a branch: few tiles need it
 #pragma unroll
                     for (int tg = 0; tg < TG; ++tg)
 #pragma unroll
@@ -537,6 +539,7 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, WIDE)) void 
                 for (int tg = 0; tg < TG; ++tg)
 #pragma unroll
                     for (int j = 0; j < 4; ++j) top = fmaxf(top, s[rt][tg][j]);
+                top *= rs[rt];
                 if (__any(top > m[rt] + HEADROOM)) {
                     top = fmaxf(top, __shfl_xor(top, 16, 64));
                     top = fmaxf(top, __shfl_xor(top, 32, 64));
@@ -549,32 +552,33 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, WIDE)) void 
 #pragma unroll
                         for (int j = 0; j < 4; ++j) acc[rt][t_][j] *= f;
                 }
-                const float base = (m[rt] == NEG ? 0.0f : m[rt]) - LIFT;
-                float add = 0.0f;
+                const float up = LIFT - (m[rt] == NEG ? 0.0f : m[rt]);
 #pragma unroll
                 for (int tg = 0; tg < TG; ++tg)
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        const float p = __builtin_amdgcn_exp2f(s[rt][tg][j] - base);
+                        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rt][tg][j], rs[rt], up));
                         const _Float16 p0 = (_Float16)p;
                         w[rt][0][tg >> 1][(tg & 1) * 4 + j] = p0;
-                        add += (float)p0;
-                        if constexpr (WIDE) {
-                            const _Float16 p1 = (_Float16)(p - (float)p0);
-                            w[rt][1][tg >> 1][(tg & 1) * 4 + j] = p1;
-                            add += (float)p1;
-                        }
+                        if constexpr (WIDE) w[rt][1][tg >> 1][(tg & 1) * 4 + j] = (_Float16)(p - (float)p0);
                     }
-                l[rt] += add;
+#pragma unroll
+                for (int half = 0; half < TG / 2; ++half)
+#pragma unroll
+                    for (int p = 0; p < NP; ++p) l[rt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ones, w[rt][p][half], l[rt], 0, 0, 0);
             }
 #pragma unroll
-            for (int half = 0; half < TG / 2; ++half)
+            for (int half = 0; half < TG / 2; ++half) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+#pragma unroll
+                    for (int i = 0; i < T::VW; ++i) t.v[half][e][i] = value_word(PACKED, t.v[half][e][i]);
 #pragma unroll
                 for (int f = 0; f < NT; ++f) {
                     const int word = PACKED ? f >> 3 : f >> 2;
                     uint32_t two[4];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) two[e] = value_pair<PACKED>(t.v[half][2 * e][word], t.v[half][2 * e + 1][word], f);
+                    for (int e = 0; e < 4; ++e) two[e] = value_pair<PACKED>(t.v[half][2 * e][word], t.v[half][2 * e + 1][word], f, off);
                     v8h vf;
                     __builtin_memcpy(&vf, two, 16);
 #pragma unroll
@@ -583,6 +587,7 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, WIDE)) void 
                         for (int p = 0; p < NP; ++p)
                             acc[rt][f] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, w[rt][p][half], acc[rt][f], 0, 0, 0);
                 }
+            }
             load_values(next);
             now = next;
         }
@@ -591,11 +596,9 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, WIDE)) void 
         // ---- the waves' parts joined
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
-            l[rt] += __shfl_xor(l[rt], 16, 64);
-            l[rt] += __shfl_xor(l[rt], 32, 64);
             if (g == 0) {
                 red_m[wave][rt * 16 + n] = m[rt];
-                red_l[wave][rt * 16 + n] = l[rt];
+                red_l[wave][rt * 16 + n] = l[rt][0];
             }
         }
         __syncthreads();
@@ -614,7 +617,7 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, WIDE)) void 
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
 #pragma unroll
-                    for (int t_ = 0; t_ < NT; ++t_) sums[wave][n][feature_of<DP, PACKED>(4 * g + j, t_)] = x[t_][j] * f;
+                    for (int t_ = 0; t_ < NT; ++t_) sums[wave][n][feature_of<DP, PACKED>(4 * g + j, t_)] = x[t_][j] * (f * VALUE_SCALE);
             };
             if (RT == 1 || rt == 0) put(acc[0]);
             else put(acc[RT - 1]);
@@ -654,7 +657,7 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, WIDE)) void 
                         const float *vs = kv.value.s + h * DP + c0, *vk = kv.value.k + h * DP + c0;
 #pragma unroll
                         for (int e = 0; e < 4; ++e) x[e] = ll == 0.0f ? 0.0f : (x[e] * inv + 0.5f) * vs[e] + vk[e];
-                        kv_store<4>(a.out, q.type, out_row + c0, kv.dim - c0, x);
+                        kv_store<4>(a.out, type, out_row + c0, kv.dim - c0, x);
                     } else {
                         *reinterpret_cast<float4 *>(ws.sums + row * DP + c0) = make_float4(x[0], x[1], x[2], x[3]);
                     }
