@@ -515,3 +515,50 @@ def test_refusals(lpq):
         with pytest.raises(AssertionError):
             cache.attend(bad.get("q", q), bad.get("lengths", lengths), c.table)
     assert torch.equal(before, cache.k)
+
+
+@pytest.mark.parametrize("scale", [-0.4, 0.0, -0.0, 1e-33, 2.5])
+@pytest.mark.parametrize("kind,packed", [("f32", False), ("f16", True), ("bf16", False)])
+def test_scales_of_any_sign(lpq, kind, packed, scale):
+    c = Case(lpq, 2, 96, 16, [70, 5], kind, packed, seed=11)
+    q = c.queries(3, 2, strength=0.3)
+    out, lse = c.cache.attend(q.cuda(), ints(c.lengths), c.table, scale=scale, return_lse=True)
+    c.check_attention(q, out, lse, 3, scale=scale)
+
+
+def test_many_small_weights_beside_a_large_one(lpq):
+    """30 000 tokens whose weights are 2^-30 to 2^-24 of one token's: together they still move the result."""
+    n = 30_000
+    c = Case(lpq, 1, 64, 64, [n], "f32", seed=12)
+    k = np.broadcast_to(c.mean, (n, 64)) + 0.05 * c.std * c.rng.standard_normal((n, 64))
+    k[17] = c.mean + 3.0 * c.std
+    k = torch.from_numpy(k.astype(np.float32)).view(n, 1, 64)
+    c.cache.write(k.cuda(), c.v[0].cuda(), ints([0]), c.table, ints([0, n]))
+    c.kcodes = [plain.codes(k.numpy(), c.kc, False)]
+    c.kx = [plain.values(c.kcodes[0], c.kc).astype(np.float64)]
+    q = torch.from_numpy((0.8 / c.std).astype(np.float32)).view(1, 1, 1, 64)
+    out, lse = c.cache.attend(q.cuda(), ints([n]), c.table, return_lse=True)
+    c.check_attention(q, out, lse, 1)
+
+
+@pytest.mark.parametrize("heads,dim,page,kind,packed", [(3, 64, 128, "bf16", False), (7, 192, 32, "f16", True), (2, 33, 16, "f32", False)])
+def test_few_rows_of_many_sequences(lpq, heads, dim, page, kind, packed):
+    rng = np.random.default_rng(5)
+    lengths = [int(x) for x in rng.integers(0, 12, 150)] + [page, 2 * page + 1]
+    before = [int(rng.integers(0, n + 1)) for n in lengths]
+    c = Case(lpq, heads, dim, page, lengths, kind, packed, write=False, seed=13)
+    for part in (0, 1):
+        span = [(0, a) if part == 0 else (a, n) for a, n in zip(before, lengths)]
+        k, v = (torch.cat([x[a:e] for x, (a, e) in zip(rows, span)]).cuda() for rows in (c.k, c.v))
+        first, starts = [a for a, _ in span], np.concatenate([[0], np.cumsum([e - a for a, e in span])]).tolist()
+        c.cache.write(k, v, ints(first), c.table, ints(starts))
+        back = c.cache.read(ints(first), c.table, ints(starts), starts[-1])
+        for got, codes, consts in ((back[0], c.kcodes, c.kc), (back[1], c.vcodes, c.vc)):
+            want = plain.values(np.concatenate([x[a:e] for x, (a, e) in zip(codes, span)]), consts)
+            assert np.array_equal(got.cpu().numpy(), want)
+    bounds = c.cache.bounds.cpu().numpy()
+    for b, n in enumerate(lengths):
+        assert np.array_equal(c.stored(b, "k"), c.kcodes[b]) and np.array_equal(c.stored(b, "v"), c.vcodes[b])
+        for p in range(-(-n // page)):
+            codes = c.kcodes[b][p * page:(p + 1) * page]
+            assert np.array_equal(bounds[c.table_np[b, p]], np.stack([codes.min(0), codes.max(0)], 1))
