@@ -558,6 +558,8 @@ def test_few_rows_of_many_sequences(lpq, heads, dim, page, kind, packed):
             assert np.array_equal(got.cpu().numpy(), want)
     bounds = c.cache.bounds.cpu().numpy()
     for b, n in enumerate(lengths):
+        if n == 0:
+            continue
         assert np.array_equal(c.stored(b, "k"), c.kcodes[b]) and np.array_equal(c.stored(b, "v"), c.vcodes[b])
         for p in range(-(-n // page)):
             codes = c.kcodes[b][p * page:(p + 1) * page]
