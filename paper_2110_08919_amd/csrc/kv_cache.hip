@@ -8,10 +8,9 @@
 // result does not depend on how its tokens were grouped into calls.  Bound by memory in large calls, by the round trips to
 // it in small ones: a thread asks for its rows of keys, of values and for old codes before it uses any.
 //
-// Measured (write, read): one row of 8 heads of 128, bfloat16: 4.9, 3.5 us; 64 rows of 64 sequences 6.9, 4.3; 26 244 rows of 6 x 100
-// float16 features of 12 prompts to packed codes 31.8 (vector instructions for 20 of them: 133 to a thread's 8 values; float32 rows 42, the rows' bytes come on top)
-// and back 22.7;
-// 151 419 rows of 8 x 128 back to bfloat16: 188 us, 4.9 TB/s of codes and rows (a copy of memory: 4.7).
+// Measured (write, read): one row of 8 heads of 128, bfloat16: 5.1, 3.6 us; 64 rows of 64 sequences 6.7, 4.2; 26 244 rows of 6 x 100
+// float16 features of 12 prompts to packed codes 31.8 (vector instructions for 20 of them, 133 to a thread's 8 values, memory for 11;
+// float32 rows 42) and back 22.6; 151 419 rows of 8 x 128 back to bfloat16: 188 us, 4.9 TB/s of codes and rows (a copy of memory: 4.7).
 #include <type_traits>
 
 #include "kv_internal.h"
