@@ -49,12 +49,15 @@ constexpr float LIFT = 13.0f;        // weights are exp2(t - m + LIFT): at most 
 // Tokens a wave has in registers: 64 where a row of codes has at
 // most 64 bytes, else 32.
 __host__ __device__ constexpr int tile_tokens(int dpad, bool packed) { return (packed ? dpad / 2 : dpad) <= 64 ? 64 : 32; }
-// Whether more than 16 query rows go through a tile of tokens 32 at a time.  Once through memory for 32 rows instead of twice: 16
-// conversations of 32 000 to 56 000 tokens, 8 heads of 128, 32 rows each, 285 against 466 us (float32 queries); 4-bit codes with
-// 16-bit queries, 32 conversations, 415 against 584.  Where packed codes and the registers of 32 rows leave one workgroup to a CU,
-// 16 at a time are faster: 8 conversations, one head of 192, 48 rows, float32 71 against 43 us, bfloat16 60 against 37; heads of
-// 128, float32, 305 against 286.
+// Whether there is a kernel that takes more than 16 query rows through a tile of tokens 32 at a time: codes are unpacked and made fp16 once
+// for 32 rows.  16 conversations of 32 000 to 56 000 tokens, 8 heads of 128, 32 rows each, 32 against 16 at a time, us: bfloat16 152, 182 on
+// 4-bit codes, float32 280, 339 on 8-bit codes; heads of 256, bfloat16 517, 584.  Not so for 4-bit codes in heads of 192 (298, 273), whose
+// 32 rows leave one workgroup to a CU, and for float32 rows on 4-bit codes in heads of more than 64, for whose 32 rows registers run short.
 __host__ __device__ constexpr bool two_row_tiles(int dpad, bool packed, bool wide) { return !packed || dpad == 64 || (!wide && dpad != 192); }
+// Whether a call is long enough for it, in tokens of all (sequence, head) as the table has room for.  One tile is twice the time then, which
+// short calls wait for: 8 heads of 128, 32 bfloat16 rows, 4000 to 8000 tokens, 32 against 16 at a time, us: 1 conversation 16.5, 14.0, 4 20.9,
+// 20.6, 8 27.3, 28.2, 16 47, 54; on 4-bit codes 15.1, 12.7, 21.0, 19.2, 26.7, 24.4, 36, 38; heads of 256 22, 17, 33, 28, 52, 52, 100, 105.
+constexpr int64_t TWO_ROW_TOKENS = int64_t(1) << 19;
 // Workgroups of four waves that a CU's registers hold.
 __host__ __device__ constexpr int blocks_per_cu(int dpad, bool packed, int rt, bool wide)
 {
@@ -791,21 +794,22 @@ void launch_dim(const KvView &kv, const KvQueries &q, const KvAttend &a, const K
 }  // namespace
 
 // Short sequences get a workgroup per pair and row tile: joining parts would cost more than it gives.  Otherwise as many workgroups as
-// the chip holds at once, and no fewer than 4 tiles each.  Short is up to 1024 tokens, fewer where a tile is much work and workgroups
-// are few: 16 pairs, whole against split and joined, us: 1000 tokens of 64 features 10.9, 12.8, of 128 13.6, 13.5, of 256 19.6, 17.2;
-// 32 rows at a time: 500 tokens of 128 17.0, 17.1, 700 of 128 19.0, 17.7, 350 of 256 25.8, 21.2.  512 pairs of 128, 1000 tokens: 24.4, 31.3.
+// the chip holds at once, and no fewer than 4 tiles each.  Short is up to 1024 tokens, of more than 128 features fewer where workgroups are
+// few: 16 pairs, whole against split and joined, us: 1000 tokens of 64 features 10.9, 12.8, of 128 13.6, 13.5, of 256 19.6, 17.2; 500 of 256
+// 15.6, 16.1.  512 pairs of 128, 1000 tokens: 24.4, 31.3.
 KvAttendPlan kv_attend_plan(const KvView &kv, int64_t nseq, int new_tokens, int group, int64_t tokens, bool wide)
 {
     KvAttendPlan p;
     const int64_t rows = (int64_t)new_tokens * group;
-    p.rows = rows > 16 && two_row_tiles(kv.dpad, kv.packed, wide) ? 32 : 16;
+    const int64_t pairs = nseq * kv.heads;
+    p.rows = rows > 16 && pairs * tokens > TWO_ROW_TOKENS && two_row_tiles(kv.dpad, kv.packed, wide) ? 32 : 16;
     p.row_tiles = (int)ceil_div(rows, (int64_t)p.rows);
-    const int64_t pairs = nseq * kv.heads, tile = tile_tokens(kv.dpad, kv.packed);
+    const int64_t tile = tile_tokens(kv.dpad, kv.packed);
     p.least = 0;
     p.grid = (unsigned)(pairs * p.row_tiles);
     p.bytes = 0;
     const int64_t tiles = ceil_div(tokens, tile);
-    const bool few = (int64_t)p.grid < 256 && tokens * kv.dpad * (p.rows / 16) > 128 * 1024;
+    const bool few = (int64_t)p.grid < 256 && tokens * kv.dpad > 128 * 1024;
     if ((tokens > 1024 || few) && pairs * tiles < (int64_t(1) << 31)) {      // (beyond that there are pairs enough)
         p.least = 4;
         const int64_t most = ceil_div(tiles, (int64_t)p.least) * pairs;

@@ -564,3 +564,28 @@ def test_few_rows_of_many_sequences(lpq, heads, dim, page, kind, packed):
         for p in range(-(-n // page)):
             codes = c.kcodes[b][p * page:(p + 1) * page]
             assert np.array_equal(bounds[c.table_np[b, p]], np.stack([codes.min(0), codes.max(0)], 1))
+
+
+@pytest.mark.parametrize("heads,dim,page,lengths,group,new,kind,packed", [
+    (1, 192, 16, [130, 33, 1], 12, 4, "f32", True),
+    (1, 256, 128, [500, 128], 16, 2, "f16", False),
+    (1, 64, 256, [2000, 0], 40, 1, "f32", True),
+    (1, 192, 32, [400], 8, 9, "bf16", False),
+    (2, 128, 32, [300, 70], 20, 1, "bf16", True),
+    (1, 128, 64, [700, 90], 24, 1, "f32", False),
+    (1, 128, 16, [333, 16], 9, 4, "f32", True),
+    (1, 256, 16, [260, 40], 6, 3, "f16", True),
+    (1, 256, 64, [90, 300], 17, 1, "f32", True),
+    (2, 50, 16, [45, 2], 6, 4, "bf16", False),
+])
+def test_attention_of_many_rows_in_tables_with_room_for_long_sequences(lpq, heads, dim, page, lengths, group, new, kind, packed):
+    """What a table has room for decides how a call is shared out, and how many rows go through a tile at a time."""
+    c = Case(lpq, heads, dim, page, lengths, kind, packed, seed=14)
+    q = c.queries(group, new)
+    columns = (1 << 20) // (page * heads * len(lengths))
+    table = torch.full((len(lengths), columns), -1, dtype=torch.int32, device="cuda")
+    table[:, :c.table.shape[1]] = c.table
+    out, lse = c.cache.attend(q.cuda(), ints(lengths), table, return_lse=True)
+    c.check_attention(q, out, lse, group)
+    short, short_lse = c.cache.attend(q.cuda(), ints(lengths), c.table, return_lse=True)
+    c.check_attention(q, short, short_lse, group)
