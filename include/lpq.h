@@ -267,11 +267,13 @@ void lpq_kv_destroy(lpq_kv *kv);
 
 /* Encodes n new rows of keys and values, k_dev / v_dev [n][heads][D] of `type` (strides in elements, the features
  * of a head contiguous), and stores them: row starts_dev[b] + i goes to position first_dev[b] + i of sequence b
- * (starts_dev int32 [nseq + 1], ascending from 0 to n; null: one row per sequence, n = nseq).  Rows at negative
- * positions are dropped.  Bounds of the pages touched become those of their tokens up to the last one written,
- * so that a sequence may be cut back and written on.  No page may be touched twice by one call.
+ * (starts_dev int32 [nseq + 1], ascending; null: one row per sequence, n = nseq).  Rows at negative positions and rows
+ * of no sequence, ahead of starts_dev[0] or from starts_dev[nseq] on, are dropped.  Bounds of the pages touched become
+ * those of their tokens up to the last one written, so that a sequence may be cut back and written on.  No page may be
+ * touched twice by one call.
  * Asynchronous on stream.  n = 0 is a no-op.
- * LPQ_EINVAL: null argument, n or nseq < 0, strides that overlap, unknown type, starts_dev null and n != nseq;
+ * LPQ_EINVAL: null argument, n or nseq < 0, strides that overlap, unknown type, starts_dev null and n != nseq,
+ * rows but no sequence;
  * LPQ_ERANGE: nseq * heads or table_pages * page too large. */
 int lpq_kv_write(const lpq_kv *kv, const void *k_dev, int64_t ldk_token, int64_t ldk_head, const void *v_dev,
                  int64_t ldv_token, int64_t ldv_head, int type, int64_t n, int64_t nseq, const int32_t *first_dev,
@@ -279,7 +281,7 @@ int lpq_kv_write(const lpq_kv *kv, const void *k_dev, int64_t ldk_token, int64_t
                  void *stream);
 
 /* The way back: rows of the same numbering receive x^ of their position, rounded to `type`; positions without a
- * page give zeros.  Errors as above. */
+ * page and rows of no sequence give zeros.  Errors as above. */
 int lpq_kv_read(const lpq_kv *kv, void *k_dev, int64_t ldk_token, int64_t ldk_head, void *v_dev, int64_t ldv_token,
                 int64_t ldv_head, int type, int64_t n, int64_t nseq, const int32_t *first_dev,
                 const int32_t *starts_dev, const int32_t *table_dev, int64_t ld_table, int64_t table_pages,

@@ -149,6 +149,7 @@ static int kv_rows(const lpq_kv *kv, const void *k, int64_t ldk_token, int64_t l
     if (rc) return rc;
     if (n > 0 && nseq > 0 && (!k || !v || !first)) return kv_fail(LPQ_EINVAL, "null argument");
     if (!starts && n != nseq) return kv_fail(LPQ_EINVAL, "n = %lld rows for %lld sequences without starts", (long long)n, (long long)nseq);
+    if (n > 0 && nseq == 0) return kv_fail(LPQ_EINVAL, "n = %lld rows, but no sequence", (long long)n);
     if (n >= (int64_t(1) << 31)) return kv_fail(LPQ_ERANGE, "n = %lld, must stay below 2^31", (long long)n);
     const int64_t dim = kv->view.dim, heads = kv->view.heads;
     int64_t strides[2][2] = {{ldk_token, ldk_head}, {ldv_token, ldv_head}};

@@ -137,12 +137,13 @@ __device__ __forceinline__ void middles8(uint2 w, bool packed, float *v)
     }
 }
 
-// Rows [begin, end) of a call that belong to sequence b, the first of them at position `first`.
+// Rows [begin, end) of a call that belong to sequence b, the first of them at position `first`; of b = -1: to none.
 struct Sequence {
     int64_t begin, end, first;
     int b;
 };
-// The sequence of a row, by all 64 lanes: each looks at one of 64 starts, then between two of them.  Rows of none: end = n.
+// The sequence of a row, by all 64 lanes: each looks at one of 64 starts, then between two of them.  Rows ahead of the first start,
+// from the last one on, or at starts that do not ascend belong to none.
 __device__ __forceinline__ Sequence sequence_of(const KvPlaces &pl, int64_t row)
 {
     Sequence s;
@@ -165,11 +166,13 @@ __device__ __forceinline__ Sequence sequence_of(const KvPlaces &pl, int64_t row)
         s.b = lo < pl.nseq ? lo : pl.nseq - 1;
         s.begin = kv_uniform(pl.starts)[s.b];
         s.end = kv_uniform(pl.starts)[s.b + 1];
-        if (s.begin < 0 || s.begin > row || s.end <= row || s.end > pl.n) {      // starts that do not ascend from 0 to n
+        if (s.begin < 0 || s.begin > row || s.end <= row) {
+            // to the first start or to the end, else one at a time
+            s.end = s.begin > row ? s.begin : s.begin >= 0 && lo == pl.nseq ? pl.n : row + 1;
             s.begin = row;
-            s.end = pl.n;
             s.b = -1;
         }
+        if (s.end > pl.n) s.end = pl.n;
     }
     s.first = s.b < 0 ? 0 : kv_uniform(pl.first)[s.b];
     return s;
@@ -308,7 +311,7 @@ __global__ __launch_bounds__(KV_THREADS, 4) void kv_write_kernel(KvView kv, KvRo
     }
 }
 
-// x^ = k + (c + 1/2) s, each operation rounded to binary32; rows without a page are zeros.
+// x^ = k + (c + 1/2) s, each operation rounded to binary32; rows without a page or a sequence are zeros.
 template <int type, bool packed>
 __global__ __launch_bounds__(KV_THREADS, 4) void kv_read_kernel(KvView kv, KvRows kr, KvRows vr, KvPlaces pl, Share sh)
 {
@@ -329,8 +332,8 @@ __global__ __launch_bounds__(KV_THREADS, 4) void kv_read_kernel(KvView kv, KvRow
         const int inside = (int)(at & (kv.page - 1));
         end = row + kv.page - inside < q.end ? row + kv.page - inside : q.end;
         if (end > s.end) end = s.end;
-        if (q.b < 0 || left <= 0) continue;
-        const int64_t page = page_of(kv, pl, q.b, column);
+        if (left <= 0) continue;
+        const int64_t page = q.b < 0 ? -1 : page_of(kv, pl, q.b, column);
         const uint8_t *rows = (s.which ? kv.v : kv.k) + (page * kv.heads + s.h) * kv.page * row_bytes;
         const int hi_row = inside + (int)(end - row);
         for (int t0 = inside + s.lane; t0 < hi_row; t0 += 2 * KV_ROWS * sh.lanes) {

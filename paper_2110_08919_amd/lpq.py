@@ -421,7 +421,8 @@ class KVCache:
 
     def read(self, first: torch.Tensor, table: torch.Tensor, starts: torch.Tensor = None, rows: int = None,
              dtype=torch.float32, out=None):
-        """Keys and values [rows, heads, features] as they read back, numbered as in write()."""
+        """Keys and values [rows, heads, features] as they read back, numbered as in write(); zeros where there is nothing, as in
+        rows from starts[-1] on."""
         nseq, tab = self._table(table)
         n = nseq if starts is None else rows
         assert n is not None, "with starts, say how many rows"

@@ -1,0 +1,48 @@
+"""Key-value cache on a real MI355X at the edges of what a caller may pass."""
+import numpy as np
+import pytest
+import torch
+
+import kv_plain as plain
+from test_gpu_kv_cache import TYPES, Case, ints, lpq  # noqa: F401  (lpq is a fixture)
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("packed", [False, True])
+@pytest.mark.parametrize("starts", [[0, 20, 40], [5, 20, 53], [0, 0, 0], [53, 53, 53], [3, 8, 8]])
+def test_rows_of_no_sequence_are_dropped_and_read_back_as_zeros(lpq, starts, packed):
+    """More rows than the sequences have, at the end or ahead of the first: a caller with rows for the most there can be."""
+    c = Case(lpq, 3, 40, 16, [20, 53], "f16", packed)
+    n = 53
+    rows = [np.zeros((n, 3, 40)) for _ in range(2)]
+    for b in range(2):
+        for out, held in zip(rows, (c.kx, c.vx)):
+            out[starts[b]:starts[b + 1]] = held[b][:starts[b + 1] - starts[b]]
+    into = [torch.full((n, 3, 40), 7.0, dtype=torch.float16, device="cuda") for _ in range(2)]
+    c.cache.read(ints([0, 0]), c.table, ints(starts), n, out=into)
+    for got, want in zip(into, rows):
+        assert torch.equal(got.cpu(), torch.from_numpy(want).to(torch.float16))
+    # the same rows written leave what the sequences hold as it is
+    other = Case(lpq, 3, 40, 16, [20, 53], "f16", packed, write=False)
+    given = [torch.full((n, 3, 40), 9.0, dtype=torch.float16) for _ in range(2)]
+    for b in range(2):
+        for out, held in zip(given, (c.k, c.v)):
+            out[starts[b]:starts[b + 1]] = held[b][:starts[b + 1] - starts[b]]
+    other.cache.k.fill_(3)
+    other.cache.write(*(x.cuda() for x in given), ints([0, 0]), other.table, ints(starts))
+    pool = other.cache.k.cpu().numpy()
+    written = np.zeros(pool.shape[0] * 16, bool)
+    for b in range(2):
+        at = np.arange(starts[b + 1] - starts[b])
+        written[other.table_np[b][at // 16] * 16 + at % 16] = True
+    assert (pool.transpose(0, 2, 1, 3).reshape(len(written), -1)[~written] == 3).all()
+
+
+def test_rows_without_any_sequence_are_refused(lpq):
+    c = Case(lpq, 3, 40, 16, [20], "f16")
+    none, rows = torch.zeros(0, 3, dtype=torch.int32, device="cuda"), c.k[0][:4].cuda()
+    for call in (lambda: c.cache.read(ints([]), none, ints([0]), 4), lambda: c.cache.write(rows, rows, ints([]), none, ints([0]))):
+        with pytest.raises(lpq.LpqError) as e:
+            call()
+        assert e.value.code == lpq.EINVAL
