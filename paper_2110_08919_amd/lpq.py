@@ -481,8 +481,8 @@ class KVCache:
         n_select = 0
         if pages is not None:
             n_select = pages.shape[-1]
-            assert pages.is_cuda and pages.dtype is torch.int32 and pages.is_contiguous() and pages.shape == (nseq, self.heads, n_select), \
-                "need contiguous int32 pages [sequences, heads, pages]"
+            assert pages.is_cuda and pages.dtype is torch.int32 and pages.is_contiguous() and pages.shape == (nseq, self.heads, n_select) \
+                and n_select > 0, "need contiguous int32 pages [sequences, heads, pages], at least one of them"
         workspace, ws, size = self._workspace(
             workspace, _lib.lpq_kv_attend_workspace_bytes(self._h, nseq, new, q_heads, tab[2], n_select), q.device)
         _check(_lib.lpq_kv_attend(self._h, *queries, _TYPE[q.dtype], nseq, new, q_heads,

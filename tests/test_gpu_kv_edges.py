@@ -46,3 +46,9 @@ def test_rows_without_any_sequence_are_refused(lpq):
         with pytest.raises(lpq.LpqError) as e:
             call()
         assert e.value.code == lpq.EINVAL
+
+
+def test_a_list_without_pages_is_refused(lpq):
+    c = Case(lpq, 2, 64, 16, [40, 20])
+    with pytest.raises(AssertionError):
+        c.cache.attend(c.queries(2).cuda(), ints(c.lengths), c.table, pages=torch.zeros(2, 2, 0, dtype=torch.int32, device="cuda"))
