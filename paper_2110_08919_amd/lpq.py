@@ -370,6 +370,7 @@ class KVCache:
     def __init__(self, keys: Quantizer, values: Quantizer, heads: int, page: int, pages: int, packed: bool = False,
                  device="cuda"):
         assert heads >= 1 and keys.d % heads == 0, "d of the quantizers must be a multiple of heads"
+        assert torch.device(device).type == "cuda", "the cache lies in device memory"
         row = C.c_int()
         self.heads, self.dim, self.page, self.pages, self.packed = heads, keys.d // heads, page, pages, packed
         _check(lib().lpq_kv_storage_bytes(heads, self.dim, page, pages, 1 if packed else 0, None, None, C.byref(row)))
@@ -377,8 +378,7 @@ class KVCache:
         kind = torch.uint8 if packed else torch.int8
         self.k, self.v = (torch.zeros(shape, dtype=kind, device=device) for _ in range(2))
         self._bounds = torch.zeros((pages, heads, 2, row.value), dtype=torch.int8, device=device)
-        if self.k.is_cuda:
-            torch.cuda.current_stream().synchronize()       # calls on any stream find it cleared
+        torch.cuda.current_stream().synchronize()           # calls on any stream find it cleared
         h = C.c_void_p()
         _check(lib().lpq_kv_create(C.byref(h), keys._h, values._h, heads, page, pages, 1 if packed else 0, self.k.data_ptr(),
                                    self.v.data_ptr(), self._bounds.data_ptr()))
@@ -447,7 +447,9 @@ class KVCache:
     @staticmethod
     def _workspace(given: torch.Tensor, need: int, device):
         """The workspace to pass: memory of this call's own unless some was given (calls on several streams do not share any)."""
-        if given is None and need:
+        if given is not None:
+            assert given.is_cuda and given.is_contiguous(), "need a workspace that is one run of device memory"
+        elif need:
             given = torch.empty(need, dtype=torch.uint8, device=device)
         return (given, None, 0) if given is None else (given, given.data_ptr(), given.numel() * given.element_size())
 
