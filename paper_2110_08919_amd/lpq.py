@@ -470,7 +470,9 @@ class KVCache:
     def attend(self, q: torch.Tensor, lengths: torch.Tensor, table: torch.Tensor, pages: torch.Tensor = None,
                scale: float = None, out: torch.Tensor = None, return_lse: bool = False, workspace: torch.Tensor = None):
         """Attention of q [sequences, new tokens, query heads, features] over the cache (the last new_tokens positions of
-        each length are the queries' own), or over the `pages` that select() names; scale 1 / sqrt(features) by default."""
+        each length are the queries' own), or over the `pages` that select() names; scale 1 / sqrt(features) by default.
+        There is no way back through the codes: queries that require a gradient are refused."""
+        assert not (q.requires_grad and torch.is_grad_enabled()), "attention over codes has no gradient: use torch.no_grad() or q.detach()"
         nseq, tab = self._table(table)
         new, q_heads, queries = self._queries(q, nseq)
         if out is None:

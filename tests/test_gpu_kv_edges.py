@@ -52,3 +52,14 @@ def test_a_list_without_pages_is_refused(lpq):
     c = Case(lpq, 2, 64, 16, [40, 20])
     with pytest.raises(AssertionError):
         c.cache.attend(c.queries(2).cuda(), ints(c.lengths), c.table, pages=torch.zeros(2, 2, 0, dtype=torch.int32, device="cuda"))
+
+
+def test_queries_that_require_a_gradient_are_refused(lpq):
+    c = Case(lpq, 2, 64, 16, [40, 20], "f32")
+    q = c.queries(2).cuda()
+    want = c.cache.attend(q, ints(c.lengths), c.table)
+    q.requires_grad_()
+    with pytest.raises(AssertionError):
+        c.cache.attend(q, ints(c.lengths), c.table)
+    with torch.no_grad():
+        assert torch.equal(c.cache.attend(q, ints(c.lengths), c.table), want)
