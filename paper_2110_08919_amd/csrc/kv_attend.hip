@@ -449,8 +449,9 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, WIDE)) void 
                         *reinterpret_cast<uint2 *>(row + 8 * qc) = make_uint2(w[0], w[1]);
                     }
                 }
-                // above 0, so that -inf in the place of a masked score stays that (below 1e-30 scores are 0 in any case)
-                if (qc == 0) row_scale[r16] = bad ? NAN : fmaxf(most / QMAX * fabsf(a.scale) * (PACKED ? 1.44269504088896f / 16.0f : 1.44269504088896f), 1e-30f);
+                // above 0, so that -inf in the place of a masked score stays that (below 1e-30 scores are 0 in any case); negative: the row is
+                // not finite
+                if (qc == 0) row_scale[r16] = bad ? -1.0f : fmaxf(most / QMAX * fabsf(a.scale) * (PACKED ? 1.44269504088896f / 16.0f : 1.44269504088896f), 1e-30f);
             }
         }
         __syncthreads();
@@ -468,7 +469,7 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, WIDE)) void 
 #pragma unroll
                 for (int st = 0; st < NS; ++st) qd[rt][dd][st] = *reinterpret_cast<const v4i *>(&digits[dd][rt * 16 + n][64 * st + 16 * g]);
             }
-            rs[rt] = row_scale[rt * 16 + n];
+            rs[rt] = fabsf(row_scale[rt * 16 + n]);
             m[rt] = NEG;
             l[rt] = v4f{0.f, 0.f, 0.f, 0.f};
             const int r = row0 + rt * 16 + n;
@@ -602,7 +603,8 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, WIDE)) void 
         for (int rt = 0; rt < RT; ++rt) {
             if (g == 0) {
                 red_m[wave][rt * 16 + n] = m[rt];
-                red_l[wave][rt * 16 + n] = l[rt][0];
+                // a row that is not finite is not a number from the first token on that it sees
+                red_l[wave][rt * 16 + n] = row_scale[rt * 16 + n] < 0.0f && l[rt][0] > 0.0f ? NAN : l[rt][0];
             }
         }
         __syncthreads();

@@ -63,3 +63,35 @@ def test_queries_that_require_a_gradient_are_refused(lpq):
         c.cache.attend(q, ints(c.lengths), c.table)
     with torch.no_grad():
         assert torch.equal(c.cache.attend(q, ints(c.lengths), c.table), want)
+
+
+@pytest.mark.parametrize("room", [None, 1 << 12, 1 << 20])
+@pytest.mark.parametrize("group,kind,packed", [(2, "bf16", False), (3, "f16", True), (12, "f32", False)])
+def test_rows_that_see_no_token_are_zeros_whatever_the_query_holds(lpq, group, kind, packed, room):
+    """Places of a batch without a sequence often hold whatever was in memory; room: tokens that the tables have columns for."""
+    c = Case(lpq, 2, 64, 16, [0, 40, 2, 30, 0, 700], kind, packed, seed=3)
+    q = c.queries(group, 4)
+    table = c.table
+    if room:
+        table = torch.full((len(c.lengths), room // 16), -1, dtype=torch.int32, device="cuda")
+        table[:, :c.table.shape[1]] = c.table
+    table = table.clone()
+    table[3] = -1                                    # tokens, but no page that holds them
+    dead = [np.full(n, b == 3) for b, n in enumerate(c.lengths)]
+    lengths = list(c.lengths)
+    lengths[4] = -7
+    clean, clean_lse = c.cache.attend(q.cuda(), ints(lengths), table, return_lse=True)
+    c.check_attention(q, clean, clean_lse, group, dead=dead)
+    empty = torch.isneginf(clean_lse)
+    bad = q.clone()
+    bad[0], bad[3, :, ::2], bad[4] = float("nan"), float("inf"), float("nan")
+    bad[2, 0, :], bad[2, 1, 0, 5], bad[2, 3, 1, 2] = -float("inf"), float("nan"), float("nan")
+    bad[5, 2, 1, 7] = float("inf")
+    out, lse = c.cache.attend(bad.cuda(), ints(lengths), table, return_lse=True)
+    assert empty[0].all() and empty[3].all() and empty[4].all() and empty[2, :2].all() and not empty[2, 2:].any()
+    assert not out[empty].any() and torch.isneginf(lse[empty]).all()
+    spoiled = ~torch.isfinite(bad).all(-1).cuda() & ~empty
+    assert spoiled.sum() == 2
+    assert torch.isnan(out[spoiled]).all() and torch.isnan(lse[spoiled]).all()
+    rest = ~spoiled & ~empty
+    assert torch.equal(out[rest], clean[rest]) and torch.equal(lse[rest], clean_lse[rest])
