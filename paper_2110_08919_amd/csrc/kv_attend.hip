@@ -45,6 +45,9 @@ constexpr int THREADS = 256, WAVES = 4;
 constexpr float NEG = -INFINITY;
 constexpr float HEADROOM = 2.0f;     // how far scores may pass the maximum before it moves (powers of two)
 constexpr float LIFT = 13.0f;        // weights are exp2(t - m + LIFT): at most 2^15, and fp16 holds them to 2^-37 of the largest
+constexpr float FAR = 1024.0f;       // maxima beyond it are subtracted from the scores before these are multiplied by their scale
+constexpr float MAXIMUM = 0x1p-40f;  // maxima that go from wave to wave and from part to part are times this: finite for any query and scale
+__device__ __forceinline__ float lag(float m, float top) { return top == NEG ? 1.0f : __builtin_amdgcn_exp2f((m - top) * (1.0f / MAXIMUM)); }
 
 // Tokens a wave has in registers: 64 where a row of codes has at
 // most 64 bytes, else 32.
@@ -449,14 +452,17 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, WIDE)) void 
                         *reinterpret_cast<uint2 *>(row + 8 * qc) = make_uint2(w[0], w[1]);
                     }
                 }
-                // above 0, so that -inf in the place of a masked score stays that (below 1e-30 scores are 0 in any case); negative: the row is
-                // not finite
-                if (qc == 0) row_scale[r16] = bad ? -1.0f : fmaxf(most / QMAX * fabsf(a.scale) * (PACKED ? 1.44269504088896f / 16.0f : 1.44269504088896f), 1e-30f);
+                // above 0 and finite, so that -inf in the place of a masked score stays that and equal scores stay equal (below 1e-30 scores are 0
+                // in any case, at the other end the largest take all); negative: the row is not finite
+                if (qc == 0) {
+                    const float by = most / QMAX * fabsf(a.scale) * (PACKED ? 1.44269504088896f / 16.0f : 1.44269504088896f);
+                    row_scale[r16] = bad ? -1.0f : fminf(fmaxf(by, 1e-30f), 3.402823466e38f);
+                }
             }
         }
         __syncthreads();
         v4i qd[RT][ND][NS];      // lane (n, g): features 64 st + 16 g .. + 15 of row n
-        float rs[RT], m[RT];
+        float rs[RT], m[RT];     // scale of the scores (integers so far) and their maximum, as an integer
         v4f l[RT];               // sums of the weights, four times the same
         v8h ones;
 #pragma unroll
@@ -544,12 +550,11 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, WIDE)) void 
                 for (int tg = 0; tg < TG; ++tg)
 #pragma unroll
                     for (int j = 0; j < 4; ++j) top = fmaxf(top, s[rt][tg][j]);
-                top *= rs[rt];
-                if (__any(top > m[rt] + HEADROOM)) {
+                if (__any((top - m[rt]) * rs[rt] > HEADROOM)) {
                     top = fmaxf(top, __shfl_xor(top, 16, 64));
                     top = fmaxf(top, __shfl_xor(top, 32, 64));
                     const float next = fmaxf(m[rt], top);
-                    const float f = next == NEG ? 1.0f : __builtin_amdgcn_exp2f(m[rt] - next);
+                    const float f = next == NEG ? 1.0f : __builtin_amdgcn_exp2f((m[rt] - next) * rs[rt]);
                     m[rt] = next;
                     l[rt] *= f;
 #pragma unroll
@@ -557,7 +562,16 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, WIDE)) void 
 #pragma unroll
                         for (int j = 0; j < 4; ++j) acc[rt][t_][j] *= f;
                 }
-                const float up = LIFT - (m[rt] == NEG ? 0.0f : m[rt]);
+                const float most = m[rt] == NEG ? 0.0f : m[rt];
+                float up = LIFT - most * rs[rt];
+                if (__any(fabsf(up) > FAR)) {      // a difference of numbers this large keeps too little of it: by 2^27 weights were beyond fp16
+                    asm volatile("");
+#pragma unroll
+                    for (int tg = 0; tg < TG; ++tg)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) s[rt][tg][j] -= most;
+                    up = LIFT;
+                }
 #pragma unroll
                 for (int tg = 0; tg < TG; ++tg)
 #pragma unroll
@@ -602,7 +616,7 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, WIDE)) void 
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
             if (g == 0) {
-                red_m[wave][rt * 16 + n] = m[rt];
+                red_m[wave][rt * 16 + n] = m[rt] * MAXIMUM * rs[rt];
                 // a row that is not finite is not a number from the first token on that it sees
                 red_l[wave][rt * 16 + n] = row_scale[rt * 16 + n] < 0.0f && l[rt][0] > 0.0f ? NAN : l[rt][0];
             }
@@ -617,7 +631,7 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, WIDE)) void 
             float top = NEG;
 #pragma unroll
             for (int w = 0; w < WAVES; ++w) top = fmaxf(top, red_m[w][rt * 16 + n]);
-            const float f = top == NEG ? 1.0f : __builtin_amdgcn_exp2f(red_m[wave][rt * 16 + n] - top);
+            const float f = lag(red_m[wave][rt * 16 + n], top);
             if (rt) __syncthreads();
             auto put = [&](const v4f *x) {
 #pragma unroll
@@ -633,9 +647,9 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, WIDE)) void 
                     float sum = 0.0f;
 #pragma unroll
                     for (int w = 0; w < WAVES; ++w)
-                        sum += red_l[w][rt * 16 + n] * (top == NEG ? 1.0f : __builtin_amdgcn_exp2f(red_m[w][rt * 16 + n] - top));
+                        sum += red_l[w][rt * 16 + n] * lag(red_m[w][rt * 16 + n], top);
                     const int64_t lat = ((int64_t)b * q.new_tokens + r / q.group) * ((int64_t)kv.heads * q.group) + h * q.group + r % q.group;
-                    a.lse[lat] = !whole ? row_shift[rt * 16 + n] : sum == 0.0f ? NEG : (top - LIFT + __log2f(sum)) * 0.69314718055994531f + row_shift[rt * 16 + n];
+                    a.lse[lat] = !whole ? row_shift[rt * 16 + n] : sum == 0.0f ? NEG : (top * (1.0f / MAXIMUM) - LIFT + __log2f(sum)) * 0.69314718055994531f + row_shift[rt * 16 + n];
                 }
             }
             __syncthreads();
@@ -646,7 +660,7 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, WIDE)) void 
                 for (int w = 0; w < WAVES; ++w) mm = fmaxf(mm, red_m[w][rt * 16 + r16]);
 #pragma unroll
                 for (int w = 0; w < WAVES; ++w)
-                    ll += red_l[w][rt * 16 + r16] * (mm == NEG ? 1.0f : __builtin_amdgcn_exp2f(red_m[w][rt * 16 + r16] - mm));
+                    ll += red_l[w][rt * 16 + r16] * lag(red_m[w][rt * 16 + r16], mm);
                 const float inv = ll == 0.0f ? 0.0f : 1.0f / ll;
                 const int64_t row = slot * (16 * RT) + rt * 16 + r16;
                 const int64_t out_row = (int64_t)b * a.ldo_seq + (int64_t)(r / q.group) * a.ldo_token + (int64_t)(h * q.group + r % q.group) * a.ldo_head;
@@ -725,7 +739,7 @@ __global__ __launch_bounds__(NT) void kv_join_kernel(KvView kv, KvQueries q, KvA
     for (int w = 0; w < NT / 64; ++w) top = fmaxf(top, red[w]);
     float l = 0.0f;
     for (int u = tid; u < parts.count; u += NT) {
-        const float f = top == NEG ? 1.0f : __builtin_amdgcn_exp2f(weight[u] - top);
+        const float f = lag(weight[u], top);
         weight[u] = f;
         l += ws.ml[row_of(u) * 2 + 1] * f;
     }
@@ -767,7 +781,7 @@ __global__ __launch_bounds__(NT) void kv_join_kernel(KvView kv, KvQueries q, KvA
     kv_store<4>(a.out, q.type, out_row + c0, kv.dim - c0, v);
     if (a.lse && col == 0) {
         const int64_t lat = ((int64_t)b * q.new_tokens + r / q.group) * ((int64_t)kv.heads * q.group) + h * q.group + r % q.group;
-        a.lse[lat] = l == 0.0f ? NEG : (top - LIFT + __log2f(l)) * 0.69314718055994531f + a.lse[lat];
+        a.lse[lat] = l == 0.0f ? NEG : (top * (1.0f / MAXIMUM) - LIFT + __log2f(l)) * 0.69314718055994531f + a.lse[lat];
     }
 }
 

@@ -95,3 +95,45 @@ def test_rows_that_see_no_token_are_zeros_whatever_the_query_holds(lpq, group, k
     assert torch.isnan(out[spoiled]).all() and torch.isnan(lse[spoiled]).all()
     rest = ~spoiled & ~empty
     assert torch.equal(out[rest], clean[rest]) and torch.equal(lse[rest], clean_lse[rest])
+
+
+def with_keys(c, k):
+    """The first sequence of the case with keys k [n, heads, dim] (numpy) instead of its own."""
+    k = torch.from_numpy(np.ascontiguousarray(k, np.float32)).to(TYPES[c.kind])
+    n = len(k)
+    c.cache.write(k.cuda(), c.v[0].cuda(), ints([0]), c.table[:1], ints([0, n]))
+    c.kcodes[0] = plain.codes(k.float().numpy(), c.kc, c.packed)
+    c.kx[0] = plain.values(c.kcodes[0], c.kc).astype(np.float64)
+
+
+@pytest.mark.parametrize("n", [300, 9000])
+@pytest.mark.parametrize("kind,packed,strength,scale", [
+    ("bf16", False, 1e6, None), ("bf16", True, 1e7, None), ("f32", False, 3e7, None), ("f32", True, 1e9, None), ("f32", False, 1e25, None),
+    ("f16", False, 1e3, 1e6), ("f16", True, 1e3, -1e30), ("bf16", False, 1e30, 1.0), ("f32", False, 1e37, 1.0), ("bf16", False, 1e36, 1e30)])
+def test_one_token_or_two_alike_take_all(lpq, kind, packed, strength, scale, n):
+    """Scores far beyond those at which a float holds whole numbers.  Two tokens with the same keys have the same integer product and
+    share the weight; every other token is behind by more than what is rounded, so the result is their values' mean to a few
+    roundings: of the sum, the half step, the step and the offset, and to the type."""
+    c = Case(lpq, 1, 64, 64, [n], kind, packed, seed=21)
+    assert c.dim == 64
+    sign = np.where(c.rng.random(64) < 0.5, -1.0, 1.0)
+    q = (strength / c.std * sign).astype(np.float32).reshape(1, 1, 1, 64)
+    q = torch.from_numpy(np.concatenate([q, 0.5 * q], 2)).to(TYPES[kind])
+    by = c.dim ** -0.5 if scale is None else float(np.float32(scale))
+    toward = np.sign(by) * sign * c.std
+    k = c.mean + 0.5 * c.std * c.rng.standard_normal((n, 64))
+    k[[n // 3, n - 5]] = c.mean + 2.0 * toward
+    with_keys(c, k.reshape(n, 1, 64))
+    qf = q.float().numpy()[0, 0].astype(np.float64)
+    t = by * (c.kx[0][:, 0, None] * qf[None]).sum(2)                            # [n, rows]; equal tokens have equal sums
+    ranked = np.sort(t, 0)
+    e = abs(by) * np.abs(qf * c.kc.s[0]).max(1) / (2 * 16319) * np.abs(c.kcodes[0][:, 0]).sum(1).max()
+    assert (ranked[-1] == ranked[-2]).all() and (ranked[-2] - ranked[-3] > 4 * e + 1000).all()
+    want = 0.5 * (c.vx[0][n // 3, 0] + c.vx[0][n - 5, 0])
+    out, lse = c.cache.attend(q.cuda(), ints([n]), c.table, scale=scale, return_lse=True)
+    size = np.maximum(np.abs(c.vx[0][n // 3, 0]), np.abs(c.vx[0][n - 5, 0])) + 256 * c.vc.s[0]
+    assert (np.abs(out[0, 0].double().cpu().numpy() - want) <= (plain.UNIT[kind] + 8 * 2.0 ** -24) * size).all()
+    want_lse = t.max(0) + np.log(2.0)
+    inside = np.abs(want_lse) < 1e38
+    total = np.abs(by) * (np.abs(qf) @ np.abs(c.kx[0][:, 0]).max(0))
+    assert (np.abs(lse[0, 0].double().cpu().numpy() - want_lse) <= e + 2.0 ** -19 * total + 1e-5)[inside].all()
