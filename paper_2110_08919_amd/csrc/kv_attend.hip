@@ -404,40 +404,50 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, WIDE)) void 
 #pragma unroll 1
         for (int i = 0; i < PASSES; ++i) {
             const int r16 = i * PASS + tid / LR;
-            float v[8], most = 0.0f;
+            float v[8], most;
             kv_floats8(raw, type, kv.dim - qc0, v);
             if (i + 1 < PASSES) raw = load_queries(i + 1);
             if (a.lse) {
                 float offset = 0.0f;
                 const float *k = kv.key.k + h * DP + qc0;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) offset += v[e] * (k[e] + 0.5f * step[e]);
+                for (int e = 0; e < 8; ++e) offset += v[e] * a.scale * (k[e] + 0.5f * step[e]);
 #pragma unroll
                 for (int o = 1; o < LR; o <<= 1) offset += __shfl_xor(offset, o, 64);
-                if (qc == 0 && r16 < 16 * RT) row_shift[r16] = offset * a.scale;
+                if (qc == 0 && r16 < 16 * RT) row_shift[r16] = offset;
             }
+            float x[8];
+            auto with_steps = [&](float by) {
+                most = 0.0f;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                v[e] *= step[e];
-                const float x = fabsf(v[e]);
-                most = fmaxf(most, x <= 3.402823466e38f ? x : INFINITY);     // a NaN counts as infinite
+                for (int e = 0; e < 8; ++e) {
+                    x[e] = v[e] * by * by * step[e];
+                    const float size = fabsf(x[e]);
+                    most = fmaxf(most, size <= 3.402823466e38f ? size : INFINITY);     // a NaN counts as infinite
+                }
+                most = row_max<LR>(most);
+            };
+            with_steps(1.0f);
+            float back = 1.0f;
+            if (__any(most == INFINITY || (most > 0.0f && most <= 1e-30f))) {     // rare: by a power of two into the middle of binary32's range
+                back = most == INFINITY ? 0x1p64f : most > 0.0f && most <= 1e-30f ? 0x1p-64f : 1.0f;
+                with_steps(1.0f / back);
             }
-            most = row_max<LR>(most);
-            const bool bad = most == INFINITY, use = !bad && most > 1e-30f;  // below that QMAX / most leaves the range of binary32, and scores are 0
+            const bool bad = most == INFINITY, use = !bad && most > 1e-30f;  // below 1e-30 now: scores are 0 at any scale
             const float f = use ? __uint_as_float(__float_as_uint(QMAX / most) | (__float_as_uint(a.scale) & 0x80000000u)) : 0.0f;      // of scale's sign
             int8_t d[ND][8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 // packed rows have the even features of 16 first (low nibbles of 8 bytes), then the odd ones
                 const int to = PACKED ? (e >> 1) + 4 * (e & 1) : e;
-                int x = use ? (int)rintf(v[e] * f) : 0;
+                int z = use ? (int)rintf(x[e] * f) : 0;
 #pragma unroll
                 for (int dd = ND - 1; dd > 0; --dd) {
-                    const int up = (x + 64) >> 7;
-                    d[dd][to] = (int8_t)(x - (up << 7));                     // -64 .. 63
-                    x = up;
+                    const int up = (z + 64) >> 7;
+                    d[dd][to] = (int8_t)(z - (up << 7));                     // -64 .. 63
+                    z = up;
                 }
-                d[0][to] = (int8_t)x;
+                d[0][to] = (int8_t)z;
             }
             if (8 * qc < DP && r16 < 16 * RT) {
 #pragma unroll
@@ -455,7 +465,7 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, WIDE)) void 
                 // above 0 and finite, so that -inf in the place of a masked score stays that and equal scores stay equal (below 1e-30 scores are 0
                 // in any case, at the other end the largest take all); negative: the row is not finite
                 if (qc == 0) {
-                    const float by = most / QMAX * fabsf(a.scale) * (PACKED ? 1.44269504088896f / 16.0f : 1.44269504088896f);
+                    const float by = most / QMAX * (PACKED ? 1.44269504088896f / 16.0f : 1.44269504088896f) * back * fabsf(a.scale) * back;
                     row_scale[r16] = bad ? -1.0f : fminf(fmaxf(by, 1e-30f), 3.402823466e38f);
                 }
             }

@@ -137,3 +137,42 @@ def test_one_token_or_two_alike_take_all(lpq, kind, packed, strength, scale, n):
     inside = np.abs(want_lse) < 1e38
     total = np.abs(by) * (np.abs(qf) @ np.abs(c.kx[0][:, 0]).max(0))
     assert (np.abs(lse[0, 0].double().cpu().numpy() - want_lse) <= e + 2.0 ** -19 * total + 1e-5)[inside].all()
+
+
+def scaled_case(lpq, factor, *args, **kw):
+    """A case whose key features are `factor` (a number or one per feature) times as wide and as far out."""
+    c = Case(lpq, *args, write=False, **kw)
+    bits, f = c.kc.bits, c.heads * c.dim
+    c.std, c.mean = c.std * factor, c.mean * factor
+    width = 4.0 if bits == 8 else 2.5
+    ranges = [x.astype(np.float32) for x in (c.mean, c.mean - width * c.std, c.mean + width * c.std)]
+    c.kc = plain.Constants(*ranges, bits, c.heads)
+    values = lpq.Quantizer(f, bits).set_params(*(x.reshape(-1) for x in (c.vc.k, c.vc.sb, c.vc.se)))
+    c.cache = lpq.KVCache(lpq.Quantizer(f, bits).set_params(*ranges), values, heads=c.heads, page=c.page, pages=c.cache.pages, packed=c.packed)
+    c.k = [torch.from_numpy((c.rng.standard_normal((n, f)) * c.std + c.mean).astype(np.float32)).to(TYPES[c.kind]).view(n, c.heads, c.dim)
+           for n in c.lengths]
+    c.kcodes = [plain.codes(x.float().numpy(), c.kc, c.packed) for x in c.k]
+    c.kx = [plain.values(x, c.kc).astype(np.float64) for x in c.kcodes]
+    c.cache.write(torch.cat(c.k).cuda(), torch.cat(c.v).cuda(), ints([0] * len(c.lengths)), c.table, ints(c.starts.tolist()))
+    return c
+
+
+@pytest.mark.parametrize("lengths", [[300, 1, 0], [5000]])
+@pytest.mark.parametrize("kind,packed,factor,size", [("f32", False, 1e4, 1e37), ("bf16", False, 1e4, 1e37), ("f32", True, 1e4, 2e37),
+                                                     ("f32", False, 1.0, 1e-33), ("bf16", False, 1.0, 3e-36), ("f32", True, 1.0, 1e-38)])
+def test_queries_whose_products_with_the_steps_are_very_large_or_small(lpq, kind, packed, factor, size, lengths):
+    """Finite queries q with q s beyond binary32, or far below 1, at a scale that makes the scores ordinary numbers."""
+    c = scaled_case(lpq, factor, 1, 64, 64, lengths, kind, packed, seed=22)
+    q = torch.from_numpy((c.rng.standard_normal((len(lengths), 2, 3, 64)) * size).astype(np.float32)).to(TYPES[kind])
+    scaled = q.double().numpy() * c.kc.s[0].astype(np.float64)
+    assert torch.isfinite(q).all() and (np.abs(scaled).max() > 3.5e38 if factor > 1 else np.abs(scaled).max() < 1e-30)
+    scale = float(np.float32(2.0 / (np.sqrt((c.std ** 2).sum()) * size)))
+    assert 0 < scale < 3e38
+    out, lse = c.cache.attend(q.cuda(), ints(lengths), c.table, scale=scale, return_lse=True)
+    c.check_attention(q, out, None, 3, scale=scale)
+    for b, n in enumerate(lengths):                  # the bound of lse holds sums of |q| |k| that float32 does not
+        qb = q[b].double().numpy()
+        want = plain.attend(qb, c.kx[b], c.vx[b], 3, scale)[1]
+        bound = plain.attend_bound(qb, c.kcodes[b], c.vx[b], c.kc, 3, scale, kind)[1]
+        got, seen = lse[b].double().cpu().numpy(), np.isfinite(want)
+        assert np.isfinite(bound).all() and (np.abs(got - want)[seen] <= bound[seen]).all() and np.isneginf(got[~seen]).all()
