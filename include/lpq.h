@@ -312,8 +312,8 @@ int lpq_kv_select(const lpq_kv *kv, const void *q_dev, int64_t ldq_seq, int64_t 
  * none; a page named twice counts twice).  lse_dev: null, or float [nseq][new_tokens][q_heads], the logarithm of the sum of
  * exp(scale q . x^_j), with which attention over other tokens can be joined.  A row that sees no token gives
  * zeros and -inf, whatever it holds; else a row of queries that holds a NaN or an infinity gives NaN.  Scores are exact
- * sums of a query rounded to 15 bits (float32: 22) of its largest q s; weights are rounded to fp16 (float32: to 22 bits);
- * sums are in 32 bits.
+ * sums of a query rounded to 16 bits (float16: 24, float32: 32) of its largest q s; weights are rounded to fp16
+ * (float32: to 22 bits); sums are in 32 bits.
  * The order of all sums is fixed: equal calls give equal bits.
  * The workspace (256-byte aligned) holds the parts a long sequence is split into.
  * LPQ_EINVAL: null argument, new_tokens < 1, q_heads not a multiple of heads, strides that overlap, unknown type,

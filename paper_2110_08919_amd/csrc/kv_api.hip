@@ -259,8 +259,8 @@ extern "C" size_t lpq_kv_attend_workspace_bytes(const lpq_kv *kv, int64_t nseq, 
     const int64_t pages = n_select ? n_select : table_pages;
     // enough for queries of any type
     size_t most = 0;
-    for (const bool wide : {false, true})
-        most = std::max(most, kv_attend_plan(kv->view, nseq, new_tokens, q_heads / kv->view.heads, pages * kv->view.page, wide).bytes);
+    for (const int type : {LPQ_TYPE_F32, LPQ_TYPE_F16, LPQ_TYPE_BF16})
+        most = std::max(most, kv_attend_plan(kv->view, nseq, new_tokens, q_heads / kv->view.heads, pages * kv->view.page, type).bytes);
     return most;
 }
 
@@ -286,7 +286,7 @@ extern "C" int lpq_kv_attend(const lpq_kv *kv, const void *q_dev, int64_t ldq_se
     if (!disjoint(dim, {{{ldo_seq, nseq}, {ldo_token, new_tokens}, {ldo_head, q_heads}}}))
         return kv_fail(LPQ_EINVAL, "strides %lld, %lld, %lld of the output overlap", (long long)ldo_seq, (long long)ldo_token, (long long)ldo_head);
     const int64_t pages = chosen_dev ? n_select : table_pages;
-    const KvAttendPlan plan = kv_attend_plan(kv->view, nseq, new_tokens, q.group, pages * kv->view.page, type == LPQ_TYPE_F32);
+    const KvAttendPlan plan = kv_attend_plan(kv->view, nseq, new_tokens, q.group, pages * kv->view.page, type);
     if (plan.bytes && (!workspace_dev || (uintptr_t)workspace_dev % 256)) return kv_fail(LPQ_EINVAL, "workspace null or not 256-byte aligned");
     if (workspace_bytes < plan.bytes) return kv_fail(LPQ_ERANGE, "workspace of %zu bytes, %zu needed", workspace_bytes, plan.bytes);
     const KvAttend a = {lengths_dev, table_dev, ld_table, (int)nseq, (int)table_pages, chosen_dev, n_select, scale, out_dev, ldo_seq,

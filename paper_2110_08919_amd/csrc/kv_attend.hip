@@ -6,11 +6,13 @@
 // the products as the integers they are.  Likewise o_i = k_i + s_i (1/2 + sum_j p_j c_ji / sum_j p_j).
 //
 // Scores on the int8 matrix instruction (16x16x64), so that key codes need no conversion: a row of q' = q s is rounded to
-// Q = rint(q' Qmax / max |q'|) and split into signed digits of 7 bits, one product each, summed exactly in int32.  Two
-// digits for 16-bit queries (Qmax = 16319: an error of 2^-15 of the row's largest q', where bfloat16 holds 2^-9 of each
-// value), three for float32 (Qmax = 2088895, 2^-22).
+// Q = rint(q' Qmax / max |q'|) and split into signed digits of 8 bits, one product each, summed exactly in int32: two digits for
+// bfloat16, three for float16, four for float32, so that features far below the row's largest keep the bits their type has
+// (query_digits).
 // Weights exp2(t - m) are rounded to fp16 (float32 calls: two fp16 terms) and multiply the value codes, which fp16 holds
-// exactly, on the fp16 matrix instruction with float32 sums.  The sum of weights is taken of the rounded ones, as their product
+// exactly, on the fp16 matrix instruction with float32 sums.  To float16 results that is an error like that of their own rounding, 1.3e-4 of the
+// root mean square at most beside 2.1e-4; two terms would take 3 to 15 % more time wherever the vector pipe is the bound (8 heads
+// of 128 on 4-bit codes, 32 float16 rows each: 222 us for 191).  The sum of weights is taken of the rounded ones, as their product
 // with ones: a sixteenth of what it takes the vector pipe.  m is a
 // maximum that may lag behind by 2 (weights are lifted by 2^13, reach 2^15, and are rounded to 2^-24 at the small end, 2^-37 of
 // the largest token's): it moves, and the sums are rescaled, only in tiles where a score passes it by more.
@@ -46,27 +48,41 @@ constexpr float NEG = -INFINITY;
 constexpr float HEADROOM = 2.0f;     // how far scores may pass the maximum before it moves (powers of two)
 constexpr float LIFT = 13.0f;        // weights are exp2(t - m + LIFT): at most 2^15, and fp16 holds them to 2^-37 of the largest
 constexpr float FAR = 1024.0f;       // maxima beyond it are subtracted from the scores before these are multiplied by their scale
-constexpr float MAXIMUM = 0x1p-40f;  // maxima that go from wave to wave and from part to part are times this: finite for any query and scale
+constexpr float MAXIMUM = 0x1p-48f;  // maxima that go from wave to wave and from part to part are times this: finite for any query and scale
 __device__ __forceinline__ float lag(float m, float top) { return top == NEG ? 1.0f : __builtin_amdgcn_exp2f((m - top) * (1.0f / MAXIMUM)); }
 
+// Digits of 8 bits that hold a row of queries.  Rounded to 2^-16 of the row's largest q' a bfloat16 value keeps its 8 bits down to 2^-8 of the
+// largest, to 2^-24 a float16 value its 11 down to 2^-13, to 2^-32 a float32 value its 24 down to 2^-8.  Keys of 128 features, one of them 20 (100)
+// times as wide, scores of standard deviation 8, error of the result before it is rounded, of its root mean square: float16 in two digits
+// 4.1e-4 (5.6e-4), in three 0.7e-4 (0.8e-4), all of it the weights' (its own rounding: 2.1e-4); bfloat16 in two 3.1e-4 (4.6e-4; 1.6e-3); float32 in
+// three up to 1.5 times that of scores in float32, in four below it.  Time, 16 conversations of 32 000 to 56 000 tokens, 8 heads of 128: up to 16 rows
+// the same, bound by memory; 32 float32 rows on 4-bit codes 220 us in three digits, 237 in four; 32 float16 rows on 4-bit codes, for which
+// registers then do not hold two row tiles, 152 in two, 191 in three.
+__host__ __device__ constexpr int query_digits(int type) { return type == LPQ_TYPE_BF16 ? 2 : type == LPQ_TYPE_F16 ? 3 : 4; }
 // Tokens a wave has in registers: 64 where a row of codes has at
 // most 64 bytes, else 32.
 __host__ __device__ constexpr int tile_tokens(int dpad, bool packed) { return (packed ? dpad / 2 : dpad) <= 64 ? 64 : 32; }
 // Whether there is a kernel that takes more than 16 query rows through a tile of tokens 32 at a time: codes are unpacked and made fp16 once
 // for 32 rows.  16 conversations of 32 000 to 56 000 tokens, 8 heads of 128, 32 rows each, 32 against 16 at a time, us: bfloat16 152, 182 on
-// 4-bit codes, float32 280, 339 on 8-bit codes; heads of 256, bfloat16 517, 584.  Not so for 4-bit codes in heads of 192 (298, 273), whose
-// 32 rows leave one workgroup to a CU, and for float32 rows on 4-bit codes in heads of more than 64, for whose 32 rows registers run short.
-__host__ __device__ constexpr bool two_row_tiles(int dpad, bool packed, bool wide) { return !packed || dpad == 64 || (!wide && dpad != 192); }
+// 4-bit codes, float32 285, 339 on 8-bit codes; heads of 256, bfloat16 517, 584.  Not so for 4-bit codes in heads of 192 (298, 273), whose
+// 32 rows leave one workgroup to a CU, and where registers run short: on 4-bit codes in heads of more than 64 float32 rows and, of 128, float16
+// rows (heads of 256: 518, 534), in heads of 256 float32 rows.
+__host__ __device__ constexpr bool two_row_tiles(int dpad, bool packed, int type) 
+{
+    if (packed) return dpad == 64 || (type == LPQ_TYPE_BF16 && dpad != 192) || (type == LPQ_TYPE_F16 && dpad == 256);
+    return dpad < 256 || type != LPQ_TYPE_F32;
+}
 // Whether a call is long enough for it, in tokens of all (sequence, head) as the table has room for.  One tile is twice the time then, which
 // short calls wait for: 8 heads of 128, 32 bfloat16 rows, 4000 to 8000 tokens, 32 against 16 at a time, us: 1 conversation 16.5, 14.0, 4 20.9,
 // 20.6, 8 27.3, 28.2, 16 47, 54; on 4-bit codes 15.1, 12.7, 21.0, 19.2, 26.7, 24.4, 36, 38; heads of 256 22, 17, 33, 28, 52, 52, 100, 105.
 constexpr int64_t TWO_ROW_TOKENS = int64_t(1) << 19;
 // Workgroups of four waves that a CU's registers hold.
-__host__ __device__ constexpr int blocks_per_cu(int dpad, bool packed, int rt, bool wide)
+__host__ __device__ constexpr int blocks_per_cu(int dpad, bool packed, int rt, int type)
 {
-    if (dpad > 128) return rt == 1 ? 2 : 1;
+    if (dpad > 128) return rt == 1 && !(dpad > 192 && type == LPQ_TYPE_F32) ? 2 : 1;
     if (rt > 1) return 2;
-    return wide || (packed && dpad > 64) ? 3 : 4;
+    if (type == LPQ_TYPE_F32) return 3;
+    return dpad > 64 && (packed || type == LPQ_TYPE_F16) ? 3 : 4;
 }
 
 // Positions of sequence b that exist, and tiles of tokens a call goes through for it: at least one, so that a sequence
@@ -270,21 +286,22 @@ __device__ __forceinline__ int row_sum_of(int v)
     return v;
 }
 
-template <int DP, bool PACKED, int RT, bool WIDE>
-__global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, WIDE)) void kv_attend_kernel(KvView kv, KvQueries q, KvAttend a, int row_tiles,
+template <int DP, bool PACKED, int RT, int TYPE>
+__global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, TYPE)) void kv_attend_kernel(KvView kv, KvQueries q, KvAttend a, int row_tiles,
                                                                                        int least)
 {
     typedef Tile<DP, PACKED> T;
     constexpr int TG = T::TG, NS = T::NS, NT = T::NT, TOK = 16 * TG;
-    constexpr int ND = WIDE ? 3 : 2, NP = WIDE ? 2 : 1, RB = PACKED ? DP / 2 : DP;
-    constexpr float QMAX = WIDE ? 2088895.0f : 16319.0f;
+    constexpr int ND = query_digits(TYPE), NP = TYPE == LPQ_TYPE_F32 ? 2 : 1, RB = PACKED ? DP / 2 : DP;
+    // what ND digits hold, less a rounding
+    constexpr float QMAX = ND == 4 ? 2139061888.0f : ND == 3 ? 8355600.0f : 32639.0f;
     __shared__ float red_m[WAVES][16 * RT], red_l[WAVES][16 * RT];
     __shared__ __align__(16) float sums[WAVES][16][DP + 4];
     __shared__ __align__(16) int8_t digits[ND][16 * RT][DP + 16];
     __shared__ float row_scale[16 * RT], row_shift[16 * RT];
 
     const int lane0 = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int rows = q.new_tokens * q.group, type = WIDE ? LPQ_TYPE_F32 : q.type == LPQ_TYPE_F16 ? LPQ_TYPE_F16 : LPQ_TYPE_BF16;
+    const int rows = q.new_tokens * q.group;
     const int64_t head_bytes = (int64_t)kv.page * RB;
     const Workspace ws = workspace(a.part, 2 * (int64_t)gridDim.x, 16 * RT, DP);
     Place at;
@@ -389,7 +406,7 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, WIDE)) void 
             const int r16 = i * PASS + tid / LR, r = row0 + r16;
             const bool on = r16 < 16 * RT && r < rows && 8 * qc < DP;
             const int64_t qat = (int64_t)b * q.ld_seq + (int64_t)(r / q.group) * q.ld_token + (int64_t)(h * q.group + r % q.group) * q.ld_head;
-            return kv_load8(q.p, type, qat + qc0, on ? kv.dim - qc0 : 0);
+            return kv_load8(q.p, TYPE, qat + qc0, on ? kv.dim - qc0 : 0);
         };
         Raw8 raw = load_queries(0);
         float step[8];
@@ -405,7 +422,7 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, WIDE)) void 
         for (int i = 0; i < PASSES; ++i) {
             const int r16 = i * PASS + tid / LR;
             float v[8], most;
-            kv_floats8(raw, type, kv.dim - qc0, v);
+            kv_floats8(raw, TYPE, kv.dim - qc0, v);
             if (i + 1 < PASSES) raw = load_queries(i + 1);
             if (a.lse) {
                 float offset = 0.0f;
@@ -443,8 +460,8 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, WIDE)) void 
                 int z = use ? (int)rintf(x[e] * f) : 0;
 #pragma unroll
                 for (int dd = ND - 1; dd > 0; --dd) {
-                    const int up = (z + 64) >> 7;
-                    d[dd][to] = (int8_t)(z - (up << 7));                     // -64 .. 63
+                    const int up = (z + 128) >> 8;
+                    d[dd][to] = (int8_t)(z - (up << 8));                     // -128 .. 127
                     z = up;
                 }
                 d[0][to] = (int8_t)z;
@@ -537,8 +554,10 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, WIDE)) void 
                     }
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        if constexpr (WIDE) s[rt][tg][j] = __builtin_fmaf((float)sum[0][j], 16384.0f, (float)(sum[1][j] * 128 + sum[2][j]));
-                        else s[rt][tg][j] = (float)(sum[0][j] * 128 + sum[1][j]);
+                        const float low = (float)(sum[ND - 2][j] * 256 + sum[ND - 1][j]);
+                        if constexpr (ND == 4) s[rt][tg][j] = __builtin_fmaf((float)(sum[0][j] * 256 + sum[1][j]), 65536.0f, low);
+                        else if constexpr (ND == 3) s[rt][tg][j] = __builtin_fmaf((float)sum[0][j], 65536.0f, low);
+                        else s[rt][tg][j] = low;
                     }
                 }
             load_keys(next);
@@ -589,7 +608,7 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, WIDE)) void 
                         const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rt][tg][j], rs[rt], up));
                         const _Float16 p0 = (_Float16)p;
                         w[rt][0][tg >> 1][(tg & 1) * 4 + j] = p0;
-                        if constexpr (WIDE) w[rt][1][tg >> 1][(tg & 1) * 4 + j] = (_Float16)(p - (float)p0);
+                        if constexpr (NP == 2) w[rt][1][tg >> 1][(tg & 1) * 4 + j] = (_Float16)(p - (float)p0);
                     }
 #pragma unroll
                 for (int half = 0; half < TG / 2; ++half)
@@ -687,7 +706,7 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, WIDE)) void 
                         const float *vs = kv.value.s + h * DP + c0, *vk = kv.value.k + h * DP + c0;
 #pragma unroll
                         for (int e = 0; e < 4; ++e) x[e] = ll == 0.0f ? 0.0f : (x[e] * inv + 0.5f) * vs[e] + vk[e];
-                        kv_store<4>(a.out, type, out_row + c0, kv.dim - c0, x);
+                        kv_store<4>(a.out, TYPE, out_row + c0, kv.dim - c0, x);
                     } else {
                         *reinterpret_cast<float4 *>(ws.sums + row * DP + c0) = make_float4(x[0], x[1], x[2], x[3]);
                     }
@@ -795,26 +814,31 @@ __global__ __launch_bounds__(NT) void kv_join_kernel(KvView kv, KvQueries q, KvA
     }
 }
 
-template <int DP, bool PACKED, bool WIDE>
+template <int DP, bool PACKED, int TYPE>
 void launch_rows(const KvView &kv, const KvQueries &q, const KvAttend &a, const KvAttendPlan &p, hipStream_t st)
 {
-    if constexpr (two_row_tiles(DP, PACKED, WIDE)) {
+    if constexpr (two_row_tiles(DP, PACKED, TYPE)) {
         if (p.rows == 32) {
-            kv_attend_kernel<DP, PACKED, 2, WIDE><<<p.grid, THREADS, 0, st>>>(kv, q, a, p.row_tiles, p.least);
+            kv_attend_kernel<DP, PACKED, 2, TYPE><<<p.grid, THREADS, 0, st>>>(kv, q, a, p.row_tiles, p.least);
             return;
         }
     }
-    kv_attend_kernel<DP, PACKED, 1, WIDE><<<p.grid, THREADS, 0, st>>>(kv, q, a, p.row_tiles, p.least);
+    kv_attend_kernel<DP, PACKED, 1, TYPE><<<p.grid, THREADS, 0, st>>>(kv, q, a, p.row_tiles, p.least);
+}
+
+template <int DP, int TYPE>
+void launch_codes(const KvView &kv, const KvQueries &q, const KvAttend &a, const KvAttendPlan &p, hipStream_t st)
+{
+    if (kv.packed) launch_rows<DP, true, TYPE>(kv, q, a, p, st);
+    else launch_rows<DP, false, TYPE>(kv, q, a, p, st);
 }
 
 template <int DP>
 void launch_dim(const KvView &kv, const KvQueries &q, const KvAttend &a, const KvAttendPlan &p, hipStream_t st)
 {
-    const bool wide = q.type == LPQ_TYPE_F32;
-    if (kv.packed && wide) launch_rows<DP, true, true>(kv, q, a, p, st);
-    else if (kv.packed) launch_rows<DP, true, false>(kv, q, a, p, st);
-    else if (wide) launch_rows<DP, false, true>(kv, q, a, p, st);
-    else launch_rows<DP, false, false>(kv, q, a, p, st);
+    if (q.type == LPQ_TYPE_F32) launch_codes<DP, LPQ_TYPE_F32>(kv, q, a, p, st);
+    else if (q.type == LPQ_TYPE_F16) launch_codes<DP, LPQ_TYPE_F16>(kv, q, a, p, st);
+    else launch_codes<DP, LPQ_TYPE_BF16>(kv, q, a, p, st);
 }
 
 }  // namespace
@@ -823,12 +847,12 @@ void launch_dim(const KvView &kv, const KvQueries &q, const KvAttend &a, const K
 // the chip holds at once, and no fewer than 4 tiles each.  Short is up to 1024 tokens, of more than 128 features fewer where workgroups are
 // few: 16 pairs, whole against split and joined, us: 1000 tokens of 64 features 10.9, 12.8, of 128 13.6, 13.5, of 256 19.6, 17.2; 500 of 256
 // 15.6, 16.1.  512 pairs of 128, 1000 tokens: 24.4, 31.3.
-KvAttendPlan kv_attend_plan(const KvView &kv, int64_t nseq, int new_tokens, int group, int64_t tokens, bool wide)
+KvAttendPlan kv_attend_plan(const KvView &kv, int64_t nseq, int new_tokens, int group, int64_t tokens, int type)
 {
     KvAttendPlan p;
     const int64_t rows = (int64_t)new_tokens * group;
     const int64_t pairs = nseq * kv.heads;
-    p.rows = rows > 16 && pairs * tokens > TWO_ROW_TOKENS && two_row_tiles(kv.dpad, kv.packed, wide) ? 32 : 16;
+    p.rows = rows > 16 && pairs * tokens > TWO_ROW_TOKENS && two_row_tiles(kv.dpad, kv.packed, type) ? 32 : 16;
     p.row_tiles = (int)ceil_div(rows, (int64_t)p.rows);
     const int64_t tile = tile_tokens(kv.dpad, kv.packed);
     p.least = 0;
@@ -839,7 +863,7 @@ KvAttendPlan kv_attend_plan(const KvView &kv, int64_t nseq, int new_tokens, int 
     if ((tokens > 1024 || few) && pairs * tiles < (int64_t(1) << 31)) {      // (beyond that there are pairs enough)
         p.least = 4;
         const int64_t most = ceil_div(tiles, (int64_t)p.least) * pairs;
-        const int64_t room = ceil_div((int64_t)256 * blocks_per_cu(kv.dpad, kv.packed, p.rows / 16, wide), (int64_t)p.row_tiles);
+        const int64_t room = ceil_div((int64_t)256 * blocks_per_cu(kv.dpad, kv.packed, p.rows / 16, type), (int64_t)p.row_tiles);
         int64_t shares = most < room ? most : room;
         if (p.row_tiles > 1) shares = round_up(shares, 8);
         p.grid = (unsigned)(shares * p.row_tiles);

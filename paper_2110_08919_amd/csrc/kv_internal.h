@@ -84,7 +84,7 @@ struct KvAttendPlan {
     unsigned grid;
     size_t bytes;                    // of workspace
 };
-KvAttendPlan kv_attend_plan(const KvView &kv, int64_t nseq, int new_tokens, int group, int64_t tokens, bool wide);
+KvAttendPlan kv_attend_plan(const KvView &kv, int64_t nseq, int new_tokens, int group, int64_t tokens, int type);
 hipError_t launch_kv_attend(const KvView &kv, const KvQueries &q, const KvAttend &a, const KvAttendPlan &plan, hipStream_t st);
 
 #if defined(__HIPCC__)

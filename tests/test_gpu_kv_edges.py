@@ -176,3 +176,34 @@ def test_queries_whose_products_with_the_steps_are_very_large_or_small(lpq, kind
         bound = plain.attend_bound(qb, c.kcodes[b], c.vx[b], c.kc, 3, scale, kind)[1]
         got, seen = lse[b].double().cpu().numpy(), np.isfinite(want)
         assert np.isfinite(bound).all() and (np.abs(got - want)[seen] <= bound[seen]).all() and np.isneginf(got[~seen]).all()
+
+
+@pytest.mark.parametrize("spread", [20.0, 100.0])
+@pytest.mark.parametrize("kind,packed", [("f16", False), ("f16", True), ("bf16", False), ("bf16", True), ("f32", False), ("f32", True)])
+def test_features_of_very_different_sizes(lpq, kind, packed, spread):
+    """One key feature far wider than the others, queries that do not make up for it, scores of standard deviation 8: what a query loses
+    where its row is held to a number of bits of its largest entry.  Root mean square error over the rows against 64 bits.
+
+    16-bit results: relative to what rounding the exact result to the type costs (u / sqrt(3) or less of each value).  Weights in fp16 have
+    an error of the same kind and, for float16, of at most the same size: a factor of sqrt(2) there, 1.01 for bfloat16; a query's own
+    rounding may add a third of the result's to bfloat16 (1.05) and nothing that shows to float16.  float32: no further off than
+    scores, weights and sums in float32 of the same keys and values."""
+    factor = np.ones(256)
+    factor[[5, 128 + 77]] = spread
+    c = scaled_case(lpq, factor, 2, 128, 64, [4000, 1500], kind, packed, seed=23)
+    q = c.rng.standard_normal((2, 1, 2, 4, 128))
+    q *= 8.0 * 128 ** 0.5 / np.sqrt((c.std ** 2).reshape(2, 1, 128).sum(2, keepdims=True))
+    q = torch.from_numpy(q.reshape(2, 1, 8, 128).astype(np.float32)).to(TYPES[kind])
+    out = c.cache.attend(q.cuda(), ints(c.lengths), c.table).double().cpu().numpy()
+    exact = np.stack([plain.attend(q[b].float().numpy(), c.kx[b], c.vx[b], 4, 128 ** -0.5)[0] for b in range(2)])
+    if kind == "f32":
+        least, factor = np.zeros_like(exact), 1.0
+        for b in range(2):
+            for j in range(8):
+                t = (torch.from_numpy(c.kx[b][:, j // 4]).float() @ q[b, 0, j]) * 128 ** -0.5
+                least[b, 0, j] = (torch.softmax(t, 0) @ torch.from_numpy(c.vx[b][:, j // 4]).float()).double().numpy()
+    else:
+        least, factor = torch.from_numpy(exact).to(TYPES[kind]).double().numpy(), {"f16": 1.42, "bf16": 1.1}[kind]
+    off, most = (np.sqrt(((x - exact) ** 2).mean()) for x in (out, least))
+    print(f"error {off:.3e}, of the reference form {most:.3e}")
+    assert off <= factor * most
