@@ -593,7 +593,9 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, TYPE)) void 
                 }
                 const float most = m[rt] == NEG ? 0.0f : m[rt];
                 float up = LIFT - most * rs[rt];
-                if (__any(fabsf(up) > FAR)) {      // a difference of numbers this large keeps too little of it: by 2^27 weights were beyond fp16
+                // A difference of numbers this large keeps too little of it: by 2^27 weights were beyond fp16.  In float32 calls none is taken, so that the
+                // largest score's weight is 2^13 to the last bit, and a token that has all the weight comes out as it reads back.
+                if (NP == 2 || __any(fabsf(up) > FAR)) {
                     asm volatile("");
 #pragma unroll
                     for (int tg = 0; tg < TG; ++tg)

@@ -207,3 +207,15 @@ def test_features_of_very_different_sizes(lpq, kind, packed, spread):
     off, most = (np.sqrt(((x - exact) ** 2).mean()) for x in (out, least))
     print(f"error {off:.3e}, of the reference form {most:.3e}")
     assert off <= factor * most
+
+
+@pytest.mark.parametrize("room", [16, 4096])
+@pytest.mark.parametrize("kind,packed", [("f32", False), ("f32", True), ("f16", False), ("bf16", False), ("bf16", True)])
+def test_a_token_alone_comes_out_as_it_reads_back(lpq, kind, packed, room):
+    """Also where its offset and its code nearly cancel: the same bits as read() gives."""
+    c = Case(lpq, 5, 100, 16, [1] * 60, kind, packed, seed=24)
+    table = torch.full((60, room // 16), -1, dtype=torch.int32, device="cuda")
+    table[:, :1] = c.table
+    out = c.cache.attend(c.queries(3).cuda(), ints(c.lengths), table)
+    want = c.cache.read(ints([0] * 60), c.table, dtype=TYPES[kind])[1]
+    assert torch.equal(out, want.repeat_interleave(3, 1).view(out.shape))
