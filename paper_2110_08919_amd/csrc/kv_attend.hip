@@ -31,6 +31,8 @@
 // page numbers, keys, and at the end LDS, the part or the output, and the join (4 to 6 us): 64 chosen pages of 64 tokens, 8 heads: 9.5 us;
 // 4 sequences of up to 300 tokens, 12 heads of 64: 8.6; 48 float32 rows on one head of 192, 4 bits, 8 sequences of 3500 to 9000
 // tokens: 18.4; 256 pages of 32, 4 bits, 16 sequences of 4 heads of 96, 6 rows each: 20.4.
+#include <algorithm>
+
 #include "kv_internal.h"
 #include "wave_ops.h"
 
@@ -740,7 +742,7 @@ template <int NT>
 __global__ __launch_bounds__(NT) void kv_join_kernel(KvView kv, KvQueries q, KvAttend a, int row_tiles, int tile_rows, int grid)
 {
     __shared__ float4 sums[NT];
-    __shared__ float weight[KV_ATTEND_GRID];
+    __shared__ float weight[KV_ATTEND_SHARES];
     __shared__ float red[NT / 64], redl[NT / 64];
     const int rows = q.new_tokens * q.group;
     const int r = blockIdx.x % rows, bh = blockIdx.x / rows, h = bh % kv.heads, b = bh / kv.heads;
@@ -848,7 +850,8 @@ void launch_dim(const KvView &kv, const KvQueries &q, const KvAttend &a, const K
 // Short sequences get a workgroup per pair and row tile: joining parts would cost more than it gives.  Otherwise as many workgroups as
 // the chip holds at once, and no fewer than 4 tiles each.  Short is up to 1024 tokens, of more than 128 features fewer where workgroups are
 // few: 16 pairs, whole against split and joined, us: 1000 tokens of 64 features 10.9, 12.8, of 128 13.6, 13.5, of 256 19.6, 17.2; 500 of 256
-// 15.6, 16.1.  512 pairs of 128, 1000 tokens: 24.4, 31.3.
+// 15.6, 16.1.  512 pairs of 128, 1000 tokens: 24.4, 31.3.  Nor are sequences split where a pair's row tiles fill the chip by themselves: 16 384
+// bfloat16 rows on one head of 128, 2000 tokens 69 us, split into 8 shares and joined 135, 50 000 tokens 1123, 1168 (and 136 MB of parts).
 KvAttendPlan kv_attend_plan(const KvView &kv, int64_t nseq, int new_tokens, int group, int64_t tokens, int type)
 {
     KvAttendPlan p;
@@ -862,10 +865,11 @@ KvAttendPlan kv_attend_plan(const KvView &kv, int64_t nseq, int new_tokens, int 
     p.bytes = 0;
     const int64_t tiles = ceil_div(tokens, tile);
     const bool few = (int64_t)p.grid < 256 && tokens * kv.dpad > 128 * 1024;
-    if ((tokens > 1024 || few) && pairs * tiles < (int64_t(1) << 31)) {      // (beyond that there are pairs enough)
+    const int64_t chip = std::min<int64_t>(256 * blocks_per_cu(kv.dpad, kv.packed, p.rows / 16, type), KV_ATTEND_SHARES);
+    if ((tokens > 1024 || few) && p.row_tiles < chip && pairs * tiles < (int64_t(1) << 31)) {      // (beyond that there are pairs enough)
         p.least = 4;
         const int64_t most = ceil_div(tiles, (int64_t)p.least) * pairs;
-        const int64_t room = ceil_div((int64_t)256 * blocks_per_cu(kv.dpad, kv.packed, p.rows / 16, type), (int64_t)p.row_tiles);
+        const int64_t room = ceil_div(chip, (int64_t)p.row_tiles);
         int64_t shares = most < room ? most : room;
         if (p.row_tiles > 1) shares = round_up(shares, 8);
         p.grid = (unsigned)(shares * p.row_tiles);

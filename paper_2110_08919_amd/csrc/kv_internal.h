@@ -8,7 +8,7 @@ namespace lpq {
 
 enum { KV_MAX_DIM = 256, KV_MIN_PAGE = 16, KV_MAX_PAGE = 256,
        KV_MAX_SELECT_ROWS = 128,      // query rows per key-value head whose summed codes fit two 7-bit digits
-       KV_ATTEND_GRID = 1024,         // most workgroups that share out an attention call: four per CU
+       KV_ATTEND_SHARES = 1024,       // most shares of an attention call, so most parts of a sequence: four workgroups per CU
        KV_MAX_BLOCKS = 1 << 22 };     // workgroups of a launch (twice that stays below 2^32 threads of 256 each)
 
 // Constants of Equation 1 and the step s = 1 / m, five arrays of [heads][dpad] floats on the device.  Features without
@@ -77,8 +77,9 @@ struct KvAttend {
     float *lse;                      // null or [nseq][new_tokens][heads * group]
     float *part;                     // workspace of kv_attend_plan
 };
-// How a call is shared out: `row_tiles` tiles of `rows` query rows cover a key-value head's; `grid` workgroups take equal
-// runs of all tiles of tokens, at least `least` each, or (least = 0) one (sequence, head, row tile) each.
+// How a call is shared out: `row_tiles` tiles of `rows` query rows cover a key-value head's; `grid` workgroups, as many
+// of them per row tile as there are shares, take equal runs of all tiles of tokens, at least `least` each, or (least = 0) one (sequence,
+// head, row tile) each.
 struct KvAttendPlan {
     int row_tiles, rows, least;
     unsigned grid;

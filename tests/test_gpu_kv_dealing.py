@@ -33,9 +33,10 @@ def planned(dim, packed, kind, pairs, rows, tokens):
     high = 32 if rows > 16 and pairs * tokens > 1 << 19 and two_row_tiles(dpad, packed, kind) else 16
     row_tiles = -(-rows // high)
     grid, tiles = pairs * row_tiles, -(-tokens // tile)
-    if not (tokens > 1024 or (grid < 256 and tokens * dpad > 128 * 1024)):
+    chip = 256 * blocks_per_cu(dpad, packed, high, kind)
+    if not (tokens > 1024 or (grid < 256 and tokens * dpad > 128 * 1024)) or row_tiles >= chip:
         return high, row_tiles, pairs, False, 0
-    shares = min(-(-tiles // 4) * pairs, -(-256 * blocks_per_cu(dpad, packed, high, kind) // row_tiles))
+    shares = min(-(-tiles // 4) * pairs, -(-chip // row_tiles))
     if row_tiles > 1:
         shares = -(-shares // 8) * 8
     return high, row_tiles, shares, True, 4 * (2 * shares * row_tiles * high * (dpad + 2) + 2 * pairs)
@@ -183,3 +184,13 @@ def test_small_weights_in_tiles_with_a_large_one(lpq, kind):
     if kind == "f32":
         assert (np.abs(lost_o - o)[0, 0] > 2 * bound).all()
     assert (np.abs(got[0].double().cpu().numpy() - o)[0, 0] <= bound).all()
+
+
+@pytest.mark.parametrize("dim,kind,packed,group", [(128, "bf16", False, 16384), (256, "f32", True, 4096 + 5), (192, "f16", False, 8192)])
+def test_row_tiles_that_fill_the_chip_take_no_workspace(lpq, dim, kind, packed, group):
+    """Some of the rows are checked.  (The size that the library names is enough for queries of any type, this call's takes none.)"""
+    c = Case(lpq, 1, dim, 64, [1500, 90], kind, packed, seed=37)
+    q = c.queries(group)
+    out, lse = c.cache.attend(q.cuda(), ints(c.lengths), c.table, return_lse=True, workspace=torch.empty(0, dtype=torch.uint8, device="cuda"))
+    some = np.r_[0:3, 700:703, group - 5:group]
+    c.check_attention(q[:, :, some], out[:, :, some], lse[:, :, some], len(some))
