@@ -105,6 +105,8 @@ class Decoder:
 
     def step(self, pages: int, watch=None):
         """One token for every conversation; pages > 0: attention over that many selected pages of each head."""
+        if watch is None:
+            self.kept = None                             # this step's keys and values are not kept
         x = self.embedding[self.tokens]
         first = self.lengths.clone()
         self.lengths += 1
@@ -122,7 +124,8 @@ class Decoder:
 
     def errors(self, pages: int):
         """One step, with the relative error of each layer's attention against attention over the unquantised keys and
-        values of all tokens: [layers] (root mean square over conversations, heads and features)."""
+        values of all tokens: [layers] (root mean square over conversations, heads and features).  Before any step() only."""
+        assert self.kept is not None, "the keys and values of an earlier step were not kept"
         out = []
 
         def watch(i, q, k, v, o):

@@ -27,3 +27,14 @@ def test_command_prints_errors_and_speed(capsys):
     out = capsys.readouterr().out
     assert "tokens/s" in out and set(r) == {"all_pages", "selected_pages"}
     assert max(r["all_pages"]) < 0.06
+
+
+def test_errors_are_compared_with_every_token_so_far():
+    """A step in between leaves its keys and values out of what the errors are measured against: that is refused."""
+    from paper_2110_08919_amd import decode
+    shape = decode.Shape(layers=1, width=128, heads=2, kv_heads=1, dim=32, vocabulary=100, page=16)
+    d = decode.Decoder(shape, [[1, 2, 3], list(range(40))], 8)
+    assert max(d.errors(0)) < 0.06 and max(d.errors(0)) < 0.06
+    d.step(0)
+    with pytest.raises(AssertionError):
+        d.errors(0)
