@@ -58,27 +58,29 @@ __device__ __forceinline__ float lag(float m, float top) { return top == NEG ? 1
 // times as wide, scores of standard deviation 8, error of the result before it is rounded, of its root mean square: float16 in two digits
 // 4.1e-4 (5.6e-4), in three 0.7e-4 (0.8e-4), all of it the weights' (its own rounding: 2.1e-4); bfloat16 in two 3.1e-4 (4.6e-4; 1.6e-3); float32 in
 // three up to 1.5 times that of scores in float32, in four below it.  Time, 16 conversations of 32 000 to 56 000 tokens, 8 heads of 128: up to 16 rows
-// the same, bound by memory; 32 float32 rows on 4-bit codes 220 us in three digits, 237 in four; 32 float16 rows on 4-bit codes, for which
-// registers then do not hold two row tiles, 152 in two, 191 in three.
+// the same, bound by memory; 32 float32 rows on 4-bit codes 220 us in three digits, 237 in four, in heads of 256 on 8-bit codes 577, 670;
+// 32 float16 rows on 4-bit codes, for which registers then do not hold two row tiles, 152 in two, 191 in three.
 __host__ __device__ constexpr int query_digits(int type) { return type == LPQ_TYPE_BF16 ? 2 : type == LPQ_TYPE_F16 ? 3 : 4; }
 // Tokens a wave has in registers: 64 where a row of codes has at
 // most 64 bytes, else 32.
 __host__ __device__ constexpr int tile_tokens(int dpad, bool packed) { return (packed ? dpad / 2 : dpad) <= 64 ? 64 : 32; }
 // Whether there is a kernel that takes more than 16 query rows through a tile of tokens 32 at a time: codes are unpacked and made fp16 once
-// for 32 rows.  16 conversations of 32 000 to 56 000 tokens, 8 heads of 128, 32 rows each, 32 against 16 at a time, us: bfloat16 152, 182 on
-// 4-bit codes, float32 285, 339 on 8-bit codes; heads of 256, bfloat16 517, 584.  Not so for 4-bit codes in heads of 192 (298, 273), whose
-// 32 rows leave one workgroup to a CU, and where registers run short: on 4-bit codes in heads of more than 64 float32 rows and, of 128, float16
-// rows (heads of 256: 518, 534), in heads of 256 float32 rows.
-__host__ __device__ constexpr bool two_row_tiles(int dpad, bool packed, int type) 
+// for 32 rows.  16 conversations of 32 000 to 56 000 tokens, 8 heads of 128, 32 rows each, 32 against 16 at a time, us: bfloat16 161, 200 on
+// 4-bit codes, 274, 322 on 8-bit codes, float32 287, 343 on 8-bit codes; heads of 256, bfloat16 511, 594.  Not so for 4-bit codes in heads of
+// 192 (298, 273), whose 32 rows leave one workgroup to a CU, and where three or four digits leave too few registers: 4-bit codes in heads of
+// more than 64 (float16 rows of 256: 453, 457), float32 rows in heads of 192 (470, 448) and 256.
+__host__ __device__ constexpr bool two_row_tiles(int dpad, bool packed, int type)
 {
-    if (packed) return dpad == 64 || (type == LPQ_TYPE_BF16 && dpad != 192) || (type == LPQ_TYPE_F16 && dpad == 256);
-    return dpad < 256 || type != LPQ_TYPE_F32;
+    if (packed) return dpad == 64 || (type == LPQ_TYPE_BF16 && dpad != 192);
+    return dpad < 192 || type != LPQ_TYPE_F32;
 }
 // Whether a call is long enough for it, in tokens of all (sequence, head) as the table has room for.  One tile is twice the time then, which
 // short calls wait for: 8 heads of 128, 32 bfloat16 rows, 4000 to 8000 tokens, 32 against 16 at a time, us: 1 conversation 16.5, 14.0, 4 20.9,
 // 20.6, 8 27.3, 28.2, 16 47, 54; on 4-bit codes 15.1, 12.7, 21.0, 19.2, 26.7, 24.4, 36, 38; heads of 256 22, 17, 33, 28, 52, 52, 100, 105.
 constexpr int64_t TWO_ROW_TOKENS = int64_t(1) << 19;
-// Workgroups of four waves that a CU's registers hold.
+// Workgroups of four waves that a CU's registers hold.  Compiled so, no kernel has vector registers in scratch (three go to accumulation
+// registers where 32 rows of 256 bfloat16 features are taken); 47 to 83 scalar registers live in lanes of vector registers, nearly all of them what
+// is the same for a whole run, outside the loop over tiles.
 __host__ __device__ constexpr int blocks_per_cu(int dpad, bool packed, int rt, int type)
 {
     if (dpad > 128) return rt == 1 && !(dpad > 192 && type == LPQ_TYPE_F32) ? 2 : 1;
@@ -110,6 +112,9 @@ __device__ __forceinline__ int tiles_of(const KvView &kv, const KvAttend &a, int
 //   Short calls (runs below CROSSING tiles), where going over to another pair costs as much as the run itself: a workgroup
 //   has one pair or an even part of one.
 // kv_join_kernel joins a pair's parts.  Fewer than 2^31 tiles (kv_attend_plan).
+// CROSSING: attention and join, equal runs against even parts, us, 8 heads of 128, 8 bfloat16 rows each, tables of 32 000 to 56 000 tokens:
+// 4 conversations (runs of 43 tiles) 80, 76, 8 (86) 141, 137, 16 (172) 263, 262, 24 (258) 384, 386, 32 (344) 505, 517, 64 (690) 962, 1028; of 900 to
+// 8000 tokens, 4 rows: 64 (71) 118, 114; of 4000 to 32 000: 48 (211) 310, 313, 96 (422) 608, 633.
 constexpr unsigned CROSSING = 200;
 struct Place {
     int b, pair, tile, tiles;      // sequence, head, tile of it, tiles of the sequence

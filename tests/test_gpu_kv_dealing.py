@@ -22,8 +22,8 @@ def blocks_per_cu(dpad, packed, rows, kind):
 
 def two_row_tiles(dpad, packed, kind):
     if packed:
-        return dpad == 64 or (kind == "bf16" and dpad != 192) or (kind == "f16" and dpad == 256)
-    return dpad < 256 or kind != "f32"
+        return dpad == 64 or (kind == "bf16" and dpad != 192)
+    return dpad < 192 or kind != "f32"
 
 
 def planned(dim, packed, kind, pairs, rows, tokens):
