@@ -27,10 +27,11 @@
 // Bound by reading keys and values once.  Measured, heads of 128, bfloat16: 64 sequences of 32 000 to 56 000 tokens, 8 heads of 8
 // query rows (5.75 GB): 967 us, 5.95 TB/s where a plain streaming read has 6.16; 32 of 1000 to 8000, 8 heads of 4 rows (298 MB): 59 us,
 // 5.0 TB/s.  Many query rows, float32 queries and packed codes are bound by the vector pipe (scores to weights, codes to fp16): 48
-// bfloat16 rows on 3 heads of 128 at 4 bits, 32 sequences of 15 000 to 32 000 tokens: 126 us where reading takes 48.  Small calls are round trips to memory one behind the other, with few tiles to a wave between them: arguments, lengths,
-// page numbers, keys, and at the end LDS, the part or the output, and the join (4 to 6 us): 64 chosen pages of 64 tokens, 8 heads: 9.5 us;
-// 4 sequences of up to 300 tokens, 12 heads of 64: 8.6; 48 float32 rows on one head of 192, 4 bits, 8 sequences of 3500 to 9000
-// tokens: 18.4; 256 pages of 32, 4 bits, 16 sequences of 4 heads of 96, 6 rows each: 20.4.
+// bfloat16 rows on 3 heads of 128 at 4 bits, 32 sequences of 15 000 to 32 000 tokens: 128 us where reading takes 48.  Small calls are round trips to memory one behind the
+// other, with few tiles to a wave between them: arguments, lengths, page numbers, keys, and at the end LDS, the part or the output, and the
+// join (4 to 6 us): 64 chosen pages of 64 tokens, 8 heads: 9.4 us; 4 sequences of up to 300 tokens, 12 heads of 64: 8.6; 48 float32 rows on
+// one head of 192, 4 bits, 8 sequences of 3500 to 9000 tokens: 18.8; 256 pages of 32, 4 bits, 16 sequences of 4 heads of 96, 6 float16 rows
+// each: 21.2.
 #include <algorithm>
 
 #include "kv_internal.h"
