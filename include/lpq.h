@@ -272,8 +272,8 @@ void lpq_kv_destroy(lpq_kv *kv);
  * those of their tokens up to the last one written, so that a sequence may be cut back and written on.  No page may be
  * touched twice by one call.
  * Asynchronous on stream.  n = 0 is a no-op.
- * LPQ_EINVAL: null argument, n or nseq < 0, strides that overlap, unknown type, starts_dev null and n != nseq,
- * rows but no sequence;
+ * LPQ_EINVAL: null argument, n or nseq < 0, strides that overlap (of rows that are written, by lpq_kv_read), unknown type,
+ * starts_dev null and n != nseq, rows but no sequence;
  * LPQ_ERANGE: nseq * heads or table_pages * page too large. */
 int lpq_kv_write(const lpq_kv *kv, const void *k_dev, int64_t ldk_token, int64_t ldk_head, const void *v_dev,
                  int64_t ldv_token, int64_t ldv_head, int type, int64_t n, int64_t nseq, const int32_t *first_dev,

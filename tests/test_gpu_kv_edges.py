@@ -219,3 +219,15 @@ def test_a_token_alone_comes_out_as_it_reads_back(lpq, kind, packed, room):
     out = c.cache.attend(c.queries(3).cuda(), ints(c.lengths), table)
     want = c.cache.read(ints([0] * 60), c.table, dtype=TYPES[kind])[1]
     assert torch.equal(out, want.repeat_interleave(3, 1).view(out.shape))
+
+
+@pytest.mark.parametrize("n", [1, 20, 33])
+def test_fewer_rows_than_the_sequences_have(lpq, n):
+    c = Case(lpq, 3, 40, 16, [20, 53], "f16")
+    k, v = c.cache.read(ints([0, 0]), c.table, ints([0, 20, 73]), n, TYPES["f16"])
+    for got, held in ((k, c.kx), (v, c.vx)):
+        assert torch.equal(got.cpu(), torch.from_numpy(np.concatenate(held)[:n]).to(torch.float16))
+    other = Case(lpq, 3, 40, 16, [20, 53], "f16", write=False)
+    other.cache.write(torch.cat(other.k)[:n].cuda(), torch.cat(other.v)[:n].cuda(), ints([0, 0]), other.table, ints([0, 20, 73]))
+    k, _ = other.cache.read(ints([0, 0]), other.table, ints([0, 20, 73]), n, TYPES["f16"])
+    assert torch.equal(k.cpu(), torch.from_numpy(np.concatenate(c.kx)[:n]).to(torch.float16))
