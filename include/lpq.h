@@ -326,6 +326,28 @@ int lpq_kv_attend(const lpq_kv *kv, const void *q_dev, int64_t ldq_seq, int64_t 
                   int n_select, void *out_dev, int64_t ldo_seq, int64_t ldo_token, int64_t ldo_head, float *lse_dev,
                   void *workspace_dev, size_t workspace_bytes, void *stream);
 
+/* The same where new tokens see less.  One of
+ *   window > 0   a token at position p sees the positions j <= p with j > p - window, and those with j < sinks (the window
+ *                counts the token itself; window 0: none, and then no sinks);
+ *   tree_dev     not null: drafted tokens that do not follow one another.  A new token sees every position ahead of the
+ *                new ones (below length - new_tokens), and of the new ones those that its row of tree_dev [nseq][new_tokens]
+ *                [new_tokens] names (bytes, 0: not seen; the last axis contiguous, strides of the others in bytes, 0 where a
+ *                mask is shared): itself and its ancestors, as a rule.  A row that names nothing sees the tokens ahead
+ *                only.  New tokens whose own position is below 0 see nothing, as in lpq_kv_attend;
+ * or neither: lpq_kv_attend.  Of chosen pages, the tokens that are seen.  Only pages that a row sees something of are read (chosen pages:
+ * all of them).
+ * A row's result depends neither on the rows beside it nor on what is stored at positions that it does not see.
+ * LPQ_EINVAL beside what is named above: window or sinks below 0, sinks without a window, window and tree, strides of the
+ * tree below 0 or beyond 2^40; LPQ_ERANGE: a tree of more than 4096 new tokens. */
+size_t lpq_kv_attend_masked_workspace_bytes(const lpq_kv *kv, int64_t nseq, int new_tokens, int q_heads,
+                                            int64_t table_pages, int n_select, int64_t window, int sinks, int tree);
+int lpq_kv_attend_masked(const lpq_kv *kv, const void *q_dev, int64_t ldq_seq, int64_t ldq_token, int64_t ldq_head,
+                         int type, int64_t nseq, int new_tokens, int q_heads, float scale, const int32_t *lengths_dev,
+                         const int32_t *table_dev, int64_t ld_table, int64_t table_pages, const int32_t *chosen_dev,
+                         int n_select, int64_t window, int sinks, const uint8_t *tree_dev, int64_t ldt_seq,
+                         int64_t ldt_token, void *out_dev, int64_t ldo_seq, int64_t ldo_token, int64_t ldo_head,
+                         float *lse_dev, void *workspace_dev, size_t workspace_bytes, void *stream);
+
 /* ---------------------------------------------------------------- diagnostics ---- */
 
 /* Process-wide tuning knobs for measurements; 0 restores the built-in choice.

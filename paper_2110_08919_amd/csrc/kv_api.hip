@@ -252,23 +252,45 @@ extern "C" int lpq_kv_select(const lpq_kv *kv, const void *q_dev, int64_t ldq_se
     return e == hipSuccess ? LPQ_OK : hip_fail(e, "lpq_kv_select");
 }
 
-extern "C" size_t lpq_kv_attend_workspace_bytes(const lpq_kv *kv, int64_t nseq, int new_tokens, int q_heads, int64_t table_pages,
-                                                int n_select)
+// A window that no sequence outgrows is none.
+static int window_of(const lpq_kv *kv, int64_t table_pages, int64_t window) { return window >= table_pages * kv->view.page ? 0 : (int)window; }
+
+// The plan of a call; chosen pages are all gone through, whatever the window.
+static KvAttendPlan attend_plan(const lpq_kv *kv, int64_t nseq, int new_tokens, int group, int64_t pages, bool chosen, int type, KvMask mask)
+{
+    const int64_t tokens = pages * kv->view.page;
+    if (chosen && mask.window) mask.window = (int)std::min<int64_t>(tokens, INT32_MAX);
+    return kv_attend_plan(kv->view, nseq, new_tokens, group, tokens, type, mask);
+}
+
+static size_t attend_bytes(const lpq_kv *kv, int64_t nseq, int new_tokens, int q_heads, int64_t table_pages, int n_select, const KvMask &mask)
 {
     if (!kv || nseq < 1 || new_tokens < 1 || q_heads < kv->view.heads || q_heads % kv->view.heads || table_pages < 1 || n_select < 0) return 0;
-    const int64_t pages = n_select ? n_select : table_pages;
     // enough for queries of any type
     size_t most = 0;
     for (const int type : {LPQ_TYPE_F32, LPQ_TYPE_F16, LPQ_TYPE_BF16})
-        most = std::max(most, kv_attend_plan(kv->view, nseq, new_tokens, q_heads / kv->view.heads, pages * kv->view.page, type).bytes);
+        most = std::max(most, attend_plan(kv, nseq, new_tokens, q_heads / kv->view.heads, n_select ? n_select : table_pages, n_select > 0, type, mask).bytes);
     return most;
 }
 
-extern "C" int lpq_kv_attend(const lpq_kv *kv, const void *q_dev, int64_t ldq_seq, int64_t ldq_token, int64_t ldq_head,
-                             int type, int64_t nseq, int new_tokens, int q_heads, float scale,
-                             const int32_t *lengths_dev, const int32_t *table_dev, int64_t ld_table, int64_t table_pages,
-                             const int32_t *chosen_dev, int n_select, void *out_dev, int64_t ldo_seq, int64_t ldo_token,
-                             int64_t ldo_head, float *lse_dev, void *workspace_dev, size_t workspace_bytes, void *stream)
+extern "C" size_t lpq_kv_attend_workspace_bytes(const lpq_kv *kv, int64_t nseq, int new_tokens, int q_heads, int64_t table_pages,
+                                                int n_select)
+{
+    return attend_bytes(kv, nseq, new_tokens, q_heads, table_pages, n_select, {0, 0, nullptr, 0, 0});
+}
+
+extern "C" size_t lpq_kv_attend_masked_workspace_bytes(const lpq_kv *kv, int64_t nseq, int new_tokens, int q_heads, int64_t table_pages,
+                                                       int n_select, int64_t window, int sinks, int tree)
+{
+    if (!kv || table_pages < 1 || table_pages > INT32_MAX / kv->view.page || window < 0 || sinks < 0) return 0;
+    static const uint8_t some = 0;
+    return attend_bytes(kv, nseq, new_tokens, q_heads, table_pages, n_select, {window_of(kv, table_pages, window), sinks, tree ? &some : nullptr, 0, 0});
+}
+
+static int attend(const lpq_kv *kv, const void *q_dev, int64_t ldq_seq, int64_t ldq_token, int64_t ldq_head, int type, int64_t nseq, int new_tokens,
+                  int q_heads, float scale, const int32_t *lengths_dev, const int32_t *table_dev, int64_t ld_table, int64_t table_pages,
+                  const int32_t *chosen_dev, int n_select, const KvMask &mask, void *out_dev, int64_t ldo_seq, int64_t ldo_token, int64_t ldo_head,
+                  float *lse_dev, void *workspace_dev, size_t workspace_bytes, void *stream, const char *name)
 {
     KvQueries q;
     const int rc = kv_queries(kv, q_dev, ldq_seq, ldq_token, ldq_head, type, nseq, new_tokens, q_heads, lengths_dev, table_dev,
@@ -285,12 +307,48 @@ extern "C" int lpq_kv_attend(const lpq_kv *kv, const void *q_dev, int64_t ldq_se
     if (q_heads == 1) ldo_head = 0;
     if (!disjoint(dim, {{{ldo_seq, nseq}, {ldo_token, new_tokens}, {ldo_head, q_heads}}}))
         return kv_fail(LPQ_EINVAL, "strides %lld, %lld, %lld of the output overlap", (long long)ldo_seq, (long long)ldo_token, (long long)ldo_head);
-    const int64_t pages = chosen_dev ? n_select : table_pages;
-    const KvAttendPlan plan = kv_attend_plan(kv->view, nseq, new_tokens, q.group, pages * kv->view.page, type);
+    const KvAttendPlan plan = attend_plan(kv, nseq, new_tokens, q.group, chosen_dev ? n_select : table_pages, chosen_dev != nullptr, type, mask);
     if (plan.bytes && (!workspace_dev || (uintptr_t)workspace_dev % 256)) return kv_fail(LPQ_EINVAL, "workspace null or not 256-byte aligned");
     if (workspace_bytes < plan.bytes) return kv_fail(LPQ_ERANGE, "workspace of %zu bytes, %zu needed", workspace_bytes, plan.bytes);
     const KvAttend a = {lengths_dev, table_dev, ld_table, (int)nseq, (int)table_pages, chosen_dev, n_select, scale, out_dev, ldo_seq,
                         ldo_token, ldo_head, lse_dev, static_cast<float *>(workspace_dev)};
-    const hipError_t e = launch_kv_attend(kv->view, q, a, plan, (hipStream_t)stream);
-    return e == hipSuccess ? LPQ_OK : hip_fail(e, "lpq_kv_attend");
+    const hipError_t e = launch_kv_attend(kv->view, q, a, mask, plan, (hipStream_t)stream);
+    return e == hipSuccess ? LPQ_OK : hip_fail(e, name);
+}
+
+extern "C" int lpq_kv_attend(const lpq_kv *kv, const void *q_dev, int64_t ldq_seq, int64_t ldq_token, int64_t ldq_head,
+                             int type, int64_t nseq, int new_tokens, int q_heads, float scale,
+                             const int32_t *lengths_dev, const int32_t *table_dev, int64_t ld_table, int64_t table_pages,
+                             const int32_t *chosen_dev, int n_select, void *out_dev, int64_t ldo_seq, int64_t ldo_token,
+                             int64_t ldo_head, float *lse_dev, void *workspace_dev, size_t workspace_bytes, void *stream)
+{
+    return attend(kv, q_dev, ldq_seq, ldq_token, ldq_head, type, nseq, new_tokens, q_heads, scale, lengths_dev, table_dev, ld_table, table_pages,
+                  chosen_dev, n_select, {0, 0, nullptr, 0, 0}, out_dev, ldo_seq, ldo_token, ldo_head, lse_dev, workspace_dev, workspace_bytes, stream,
+                  "lpq_kv_attend");
+}
+
+extern "C" int lpq_kv_attend_masked(const lpq_kv *kv, const void *q_dev, int64_t ldq_seq, int64_t ldq_token, int64_t ldq_head,
+                                    int type, int64_t nseq, int new_tokens, int q_heads, float scale,
+                                    const int32_t *lengths_dev, const int32_t *table_dev, int64_t ld_table, int64_t table_pages,
+                                    const int32_t *chosen_dev, int n_select, int64_t window, int sinks, const uint8_t *tree_dev,
+                                    int64_t ldt_seq, int64_t ldt_token, void *out_dev, int64_t ldo_seq, int64_t ldo_token,
+                                    int64_t ldo_head, float *lse_dev, void *workspace_dev, size_t workspace_bytes, void *stream)
+{
+    if (!kv) return kv_fail(LPQ_EINVAL, "null argument");
+    if (window < 0 || sinks < 0) return kv_fail(LPQ_EINVAL, "window = %lld, sinks = %d: neither may be below 0", (long long)window, sinks);
+    if (sinks > 0 && window == 0) return kv_fail(LPQ_EINVAL, "%d sinks without a window", sinks);
+    if (tree_dev && window > 0) return kv_fail(LPQ_EINVAL, "a window and a tree: the positions of drafted tokens are not known");
+    if (tree_dev) {
+        if (new_tokens > KV_MAX_TREE) return kv_fail(LPQ_ERANGE, "a tree of %d new tokens, at most %d", new_tokens, (int)KV_MAX_TREE);
+        if (ldt_seq < 0 || ldt_token < 0 || ldt_seq > MAX_STRIDE || ldt_token > MAX_STRIDE)
+            return kv_fail(LPQ_EINVAL, "strides %lld, %lld of the tree", (long long)ldt_seq, (long long)ldt_token);
+        if (nseq <= 1) ldt_seq = 0;            // a stride over one element means nothing
+        if (new_tokens == 1) ldt_token = 0;
+    }
+    const int rc = check_places(kv, nseq, table_dev, ld_table, table_pages);      // before the window is compared with the table
+    if (rc) return rc;
+    const int within = window_of(kv, table_pages, window);
+    return attend(kv, q_dev, ldq_seq, ldq_token, ldq_head, type, nseq, new_tokens, q_heads, scale, lengths_dev, table_dev, ld_table, table_pages,
+                  chosen_dev, n_select, {within, sinks, tree_dev, ldt_seq, ldt_token}, out_dev, ldo_seq, ldo_token, ldo_head, lse_dev, workspace_dev,
+                  workspace_bytes, stream, "lpq_kv_attend_masked");
 }

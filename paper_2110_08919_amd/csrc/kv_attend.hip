@@ -33,6 +33,7 @@
 // one head of 192, 4 bits, 8 sequences of 3500 to 9000 tokens: 18.8; 256 pages of 32, 4 bits, 16 sequences of 4 heads of 96, 6 float16 rows
 // each: 21.2.
 #include <algorithm>
+#include <type_traits>
 
 #include "kv_internal.h"
 #include "wave_ops.h"
@@ -70,8 +71,10 @@ __host__ __device__ constexpr int tile_tokens(int dpad, bool packed) { return (p
 // 4-bit codes, 274, 322 on 8-bit codes, float32 287, 343 on 8-bit codes; heads of 256, bfloat16 511, 594.  Not so for 4-bit codes in heads of
 // 192 (298, 273), whose 32 rows leave one workgroup to a CU, and where three or four digits leave too few registers: 4-bit codes in heads of
 // more than 64 (float16 rows of 256: 453, 457), float32 rows in heads of 192 (470, 448) and 256.
-__host__ __device__ constexpr bool two_row_tiles(int dpad, bool packed, int type)
+// Nor for trees, float16 in heads of 256 on 8-bit codes: 32 rows would have 10 registers in scratch.
+__host__ __device__ constexpr bool two_row_tiles(int dpad, bool packed, int type, bool tree)
 {
+    if (tree && dpad == 256 && !packed && type == LPQ_TYPE_F16) return false;
     if (packed) return dpad == 64 || (type == LPQ_TYPE_BF16 && dpad != 192);
     return dpad < 192 || type != LPQ_TYPE_F32;
 }
@@ -82,8 +85,10 @@ constexpr int64_t TWO_ROW_TOKENS = int64_t(1) << 19;
 // Workgroups of four waves that a CU's registers hold.  Compiled so, no kernel has vector registers in scratch (three go to accumulation
 // registers where 32 rows of 256 bfloat16 features are taken); 47 to 83 scalar registers live in lanes of vector registers, nearly all of them what
 // is the same for a whole run, outside the loop over tiles.
-__host__ __device__ constexpr int blocks_per_cu(int dpad, bool packed, int rt, int type)
+// With a window, four workgroups of bfloat16 rows of 128 features would have 3 registers in scratch.
+__host__ __device__ constexpr int blocks_per_cu(int dpad, bool packed, int rt, int type, bool window)
 {
+    if (window && dpad == 128 && !packed && rt == 1) return 3;
     if (dpad > 128) return rt == 1 && !(dpad > 192 && type == LPQ_TYPE_F32) ? 2 : 1;
     if (rt > 1) return 2;
     if (type == LPQ_TYPE_F32) return 3;
@@ -103,6 +108,48 @@ __device__ __forceinline__ int tiles_of(const KvView &kv, const KvAttend &a, int
     if (a.chosen && len > 0) len = a.n_select << kv.page_shift;
     const int tiles = (int)(((unsigned)len + tile - 1) / tile);
     return tiles < 1 ? 1 : tiles;
+}
+
+// With a window: what the rows of one row tile, new tokens [from, to], can see of a sequence, in groups of 16 positions: the first
+// `sink` groups, then those from `low` on, `groups` in all.
+struct RowTokens {
+    int from, to;
+};
+struct Span {
+    int sink, low, groups;
+};
+__device__ __forceinline__ RowTokens row_tokens(const KvQueries &q, int row0, int tile_rows)
+{
+    const int rows = q.new_tokens * q.group, end = row0 + tile_rows < rows ? row0 + tile_rows : rows;
+    return {__builtin_amdgcn_readfirstlane(row0 / q.group), __builtin_amdgcn_readfirstlane((end - 1) / q.group)};
+}
+// The first position that a token at position `me` has in its window.
+__device__ __forceinline__ int window_from(const KvWindow &a, int me)
+{
+    const int first = me < 0 ? 0 : me + 1 - a.window;
+    return first < 0 ? 0 : first;
+}
+__device__ __forceinline__ Span span_of(const KvWindow &a, const KvQueries &q, RowTokens t, int len)
+{
+    const int end = len - q.new_tokens + t.to + 1, above = end < 0 ? 0 : end;
+    Span s;
+    s.low = window_from(a, len - q.new_tokens + t.from) >> 4;
+    const int sinks = a.sinks < above ? a.sinks : above;
+    s.sink = (int)(((unsigned)sinks + 15) >> 4);
+    if (s.sink > s.low) s.sink = s.low;
+    s.groups = above ? s.sink + (int)(((unsigned)above + 15) >> 4) - s.low : 0;
+    return s;
+}
+template <typename CALL>
+__device__ __forceinline__ int tiles_seen(const KvView &kv, const KvQueries &q, const CALL &a, RowTokens t, int given, int tile)
+{
+    if constexpr (std::is_same<CALL, KvWindow>::value) {
+        if (!a.chosen) {
+            const int per = tile >> 4, tiles = (span_of(a, q, t, length_of(kv, a, given)).groups + per - 1) / per;
+            return tiles < 1 ? 1 : tiles;
+        }
+    }
+    return tiles_of(kv, a, given, tile);
 }
 
 // How the tiles of all (sequence, head), of all pairs for short, are dealt to the workgroups.  Where a head's rows take several
@@ -128,13 +175,16 @@ struct Parts {
 };
 // Every wave for itself: a lane adds up some neighbouring sequences, the lanes' sums are scanned, the lane whose sequences
 // hold the workgroup's first tile (or part) finds it.
-__device__ __forceinline__ bool first_place(const KvView &kv, const KvAttend &a, unsigned me, unsigned of, int tile, int least, Place &out)
+template <typename CALL>
+__device__ __forceinline__ bool first_place(const KvView &kv, const KvQueries &q, const CALL &a, RowTokens rows, unsigned me, unsigned of, int tile,
+                                            int least, Place &out)
 {
+    auto tiles_of = [&](int b) { return tiles_seen(kv, q, a, rows, a.lengths[b], tile); };
     const int lane = threadIdx.x & 63, pairs = kv.heads;      // of a sequence
     const int per = (a.nseq + 63) / 64, b0 = lane * per, b1 = b0 + per < a.nseq ? b0 + per : a.nseq;
     unsigned mine = 0;
 #pragma unroll 4
-    for (int b = b0; b < b1; ++b) mine += (unsigned)tiles_of(kv, a, a.lengths[b], tile);
+    for (int b = b0; b < b1; ++b) mine += (unsigned)tiles_of(b);
     unsigned upto = wave_scan(mine);
     const unsigned total = (unsigned)__builtin_amdgcn_readlane((int)upto, 63) * pairs, all_pairs = (unsigned)a.nseq * pairs;
     unsigned run = (total + of - 1) / of;
@@ -146,7 +196,7 @@ __device__ __forceinline__ bool first_place(const KvView &kv, const KvAttend &a,
         for (int i = 0; i < 4 && run + 1 < enough; ++i) {
             const unsigned mid = (run + enough) / 2;
             unsigned parts = 0;
-            for (int b = b0; b < b1; ++b) parts += ((unsigned)tiles_of(kv, a, a.lengths[b], tile) + mid - 1) / mid;
+            for (int b = b0; b < b1; ++b) parts += ((unsigned)tiles_of(b) + mid - 1) / mid;
             if ((unsigned)__builtin_amdgcn_readlane((int)wave_scan(parts), 63) * pairs <= of) enough = mid;
             else run = mid + 1;
         }
@@ -157,7 +207,7 @@ __device__ __forceinline__ bool first_place(const KvView &kv, const KvAttend &a,
     auto weight = [&](unsigned tiles) { return apart ? (tiles + run - 1) / run : tiles; };
     if (apart) {
         mine = 0;
-        for (int b = b0; b < b1; ++b) mine += weight((unsigned)tiles_of(kv, a, a.lengths[b], tile));
+        for (int b = b0; b < b1; ++b) mine += weight((unsigned)tiles_of(b));
         upto = wave_scan(mine);
     }
     const uint64_t from64 = apart ? (uint64_t)me : (uint64_t)run * me;
@@ -168,7 +218,7 @@ __device__ __forceinline__ bool first_place(const KvView &kv, const KvAttend &a,
     int b = b0, tiles = 1;
     if (lane == who) {
         for (; b < b1; ++b) {
-            tiles = tiles_of(kv, a, a.lengths[b], tile);
+            tiles = tiles_of(b);
             const unsigned w = weight((unsigned)tiles) * pairs;
             if (left < w) break;
             left -= w;
@@ -294,11 +344,12 @@ __device__ __forceinline__ int row_sum_of(int v)
     return v;
 }
 
-template <int DP, bool PACKED, int RT, int TYPE>
-__global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, TYPE)) void kv_attend_kernel(KvView kv, KvQueries q, KvAttend a, int row_tiles,
+template <int DP, bool PACKED, int RT, int TYPE, typename CALL>
+__global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, TYPE, std::is_same<CALL, KvWindow>::value)) void kv_attend_kernel(KvView kv, KvQueries q, CALL a, int row_tiles,
                                                                                        int least)
 {
     typedef Tile<DP, PACKED> T;
+    constexpr bool WINDOW = std::is_same<CALL, KvWindow>::value, TREE = std::is_same<CALL, KvTree>::value, MASKED = WINDOW || TREE;
     constexpr int TG = T::TG, NS = T::NS, NT = T::NT, TOK = 16 * TG;
     constexpr int ND = query_digits(TYPE), NP = TYPE == LPQ_TYPE_F32 ? 2 : 1, RB = PACKED ? DP / 2 : DP;
     // what ND digits hold, less a rounding
@@ -307,6 +358,7 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, TYPE)) void 
     __shared__ __align__(16) float sums[WAVES][16][DP + 4];
     __shared__ __align__(16) int8_t digits[ND][16 * RT][DP + 16];
     __shared__ float row_scale[16 * RT], row_shift[16 * RT];
+    __shared__ int4 row_sees[MASKED ? 16 * RT : 1];
 
     const int lane0 = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int rows = q.new_tokens * q.group;
@@ -322,13 +374,13 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, TYPE)) void 
         at.b = __builtin_amdgcn_readfirstlane(pair / kv.heads);
         at.pair = pair - at.b * kv.heads;
         at.tile = 0;
-        at.tiles = tiles_of(kv, a, kv_uniform(a.lengths)[at.b], TOK);
+        at.tiles = tiles_seen(kv, q, a, row_tokens(q, row_tile * 16 * RT, 16 * RT), kv_uniform(a.lengths)[at.b], TOK);
         at.run = at.whole = at.tiles;
     } else {
         const unsigned eights = __builtin_amdgcn_readfirstlane(blockIdx.x / (8 * row_tiles)), in = blockIdx.x - eights * 8 * row_tiles;
         row_tile = in >> 3;
         share = eights * 8 + (in & 7);
-        if (!first_place(kv, a, share, gridDim.x / row_tiles, TOK, least, at)) return;
+        if (!first_place(kv, q, a, row_tokens(q, row_tile * 16 * RT, 16 * RT), share, gridDim.x / row_tiles, TOK, least, at)) return;
     }
     const int row0 = row_tile * 16 * RT;
     int left = at.run, b = at.b, pair = at.pair, start = at.tile, tiles = at.tiles;
@@ -352,10 +404,24 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, TYPE)) void 
         // PER tiles at once, and again while these are gone through; a tile's come out by lane number.  Position INT32_MAX:
         // there is none.
         constexpr int PER = 64 / TG;
+        // Positions between the sinks' groups and the windows' are left out.  (The loop over tiles has the two numbers from LDS: registers.)
+        struct Gap {
+            int from, width;
+        };
+        Gap gap = {0, 0};
+        if constexpr (WINDOW) {
+            if (!a.chosen) {
+                const Span span = span_of(a, q, row_tokens(q, row0, 16 * RT), len);
+                gap = {16 * span.sink, 16 * (span.low - span.sink)};
+            }
+        }
         const int columns = a.chosen ? a.n_select : a.table_pages, pool_pages = (int)kv.pages;      // below 2^31
         const int first_tile = start + wave;
-        auto look_up = [&](int turn, int &page, int &pos) {
-            const unsigned token = 16u * ((first_tile + (turn + lane / TG) * WAVES) * TG + lane % TG);
+        auto look_up = [&](int turn, int &page, int &pos, Gap gap) {
+            unsigned token = 16u * ((first_tile + (turn + lane / TG) * WAVES) * TG + lane % TG);
+            if constexpr (WINDOW) {
+                if (token >= (unsigned)gap.from) token += gap.width;      // (the last tile may reach beyond what the rows see)
+            }
             const int want = (int)(token >> kv.page_shift), inside = (int)token & (kv.page - 1);
             bool there = want < columns;
             int column = there ? want : columns - 1;
@@ -420,7 +486,7 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, TYPE)) void 
         float step[8];
         kv_load_floats8(kv.key.s + h * DP + qc0, step);
         Where now, next;
-        look_up(0, page_now, pos_now);
+        look_up(0, page_now, pos_now, gap);
         find(0, now);
         load_keys(now);
         load_values(now);
@@ -495,6 +561,36 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, TYPE)) void 
                 }
             }
         }
+        // Of a window: a row sees .x positions from .y on, and those below .z.  Of a tree: positions up to .x (-1: none) that are below .y, or
+        // whose bits are set in its token's words, bit p & 31 of word .z + (p >> 5); .y is a multiple of 32 at or ahead of the first new token, so
+        // that four neighbours are in one word.  The bits are in the memory that joins the waves at the end.
+        uint32_t *tree_bits = reinterpret_cast<uint32_t *>(&sums[0][0][0]);
+        if constexpr (WINDOW) {
+            if (tid < 16 * RT) {
+                const int r = row0 + tid, me = r < rows ? len - q.new_tokens + r / q.group : -1;
+                const int first = window_from(a, me), sinks = me < a.sinks ? me + 1 : a.sinks;
+                const int kept = tid == 0 ? gap.from : gap.width;
+                row_sees[tid] = me < 0 ? make_int4(0, 0, 0, kept) : make_int4(me + 1 - first, first, sinks, kept);
+            }
+        }
+        if constexpr (TREE) {
+            static_assert(sizeof(sums) >= 16 * RT * ((KV_MAX_TREE + 31 + 63) / 64) * 8, "a row tile's bits");
+            const RowTokens mine = row_tokens(q, row0, 16 * RT);
+            const int words = (q.new_tokens + 31 + 63) >> 6, drafts = len - q.new_tokens, begin = drafts & ~31;      // words of 64 positions
+            if (tid < 16 * RT) {
+                const int r = row0 + tid, token = r / q.group;
+                row_sees[tid] = make_int4(r < rows && drafts + token >= 0 ? len - 1 : -1, begin, (token - mine.from) * 2 * words - (begin >> 5), 0);
+            }
+            const int count = (mine.to - mine.from + 1) * words;
+            const uint8_t *mask = a.tree + (int64_t)b * a.ldt_seq;
+            for (int i = wave; i < count; i += WAVES) {
+                const int token = i / words, to = (i - token * words) * 64 + lane - (drafts - begin);
+                bool sees = to < 0;
+                if (to >= 0 && to < q.new_tokens) sees = mask[(int64_t)(mine.from + token) * a.ldt_token + to] != 0;
+                const uint64_t all = __ballot(sees);
+                if (lane == 0) reinterpret_cast<uint64_t *>(tree_bits)[i] = all;
+            }
+        }
         __syncthreads();
         v4i qd[RT][ND][NS];      // lane (n, g): features 64 st + 16 g .. + 15 of row n
         float rs[RT], m[RT];     // scale of the scores (integers so far) and their maximum, as an integer
@@ -513,11 +609,20 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, TYPE)) void 
             rs[rt] = fabsf(row_scale[rt * 16 + n]);
             m[rt] = NEG;
             l[rt] = v4f{0.f, 0.f, 0.f, 0.f};
-            const int r = row0 + rt * 16 + n;
-            const int see = len - q.new_tokens + r / q.group;
-            last[rt] = r < rows ? (see < -1 ? -1 : see) : -1;
+            if constexpr (!MASKED) {
+                const int r = row0 + rt * 16 + n;
+                const int see = len - q.new_tokens + r / q.group;
+                last[rt] = r < rows ? (see < -1 ? -1 : see) : -1;
+            }
         }
-        const int seen = len - q.new_tokens;       // a tile that ends at or before this position is seen by every row
+        int seen = len - q.new_tokens;       // a tile that ends at or before this position is seen by every row (with a window: where it begins
+        int windows = 0;                     // at or behind `windows`; the sinks are few)
+        if constexpr (WINDOW) {
+            const RowTokens mine = row_tokens(q, row0, 16 * RT);
+            windows = window_from(a, seen + mine.to);
+            seen += mine.from;
+        }
+        if constexpr (TREE) --seen;
 
         v4f acc[RT][NT];
 #pragma unroll
@@ -525,7 +630,11 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, TYPE)) void 
 #pragma unroll
             for (int t = 0; t < NT; ++t) acc[rt][t] = v4f{0.f, 0.f, 0.f, 0.f};
 
-        if (turns > PER) look_up(PER, page_then, pos_then);
+        auto gap_kept = [&]() {
+            if constexpr (WINDOW) return Gap{__builtin_amdgcn_readfirstlane(row_sees[0].w), __builtin_amdgcn_readfirstlane(row_sees[1].w)};
+            else return Gap{0, 0};
+        };
+        if (turns > PER) look_up(PER, page_then, pos_then, gap_kept());
 
         // ---- the wave's tiles: the next tile's keys are asked for as soon as this one's are used up, its values likewise
         // (behind the last tile as well, with nothing to fetch: loads that every turn makes are waited for one kind at a time)
@@ -533,12 +642,15 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, TYPE)) void 
             if ((turn + 1) % PER == 0) {
                 page_now = page_then;
                 pos_now = pos_then;
-                if (turns > turn + 1 + PER) look_up(turn + 1 + PER, page_then, pos_then);
+                if (turns > turn + 1 + PER) look_up(turn + 1 + PER, page_then, pos_then, gap_kept());
             }
             find(turn + 1, next);
             bool part = false;
 #pragma unroll
-            for (int tg = 0; tg < TG; ++tg) part |= now.pos[tg] > seen - 15;     // also where a group does not count
+            for (int tg = 0; tg < TG; ++tg) {
+                part |= now.pos[tg] > seen - 15;     // also where a group does not count
+                if constexpr (WINDOW) part |= now.pos[tg] < windows;
+            }
             float s[RT][TG][4];
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt)
@@ -576,11 +688,31 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, TYPE)) void 
             for (int rt = 0; rt < RT; ++rt) {
                 if (part) {
                     asm volatile("");      // a branch: few tiles need it
+                    if constexpr (MASKED) {
+                        const int4 row = row_sees[rt * 16 + n];
 #pragma unroll
-                    for (int tg = 0; tg < TG; ++tg)
+                        for (int tg = 0; tg < TG; ++tg) {
+                            uint32_t named = ~0u;
+                            if constexpr (TREE) {
+                                const int at = now.pos[tg] + 4 * g;
+                                if (now.pos[tg] <= row.x && at >= row.y) named = tree_bits[row.z + (at >> 5)] >> (at & 31);
+                            }
 #pragma unroll
-                        for (int j = 0; j < 4; ++j)
-                            if (now.pos[tg] > last[rt] - (4 * g + j)) s[rt][tg][j] = NEG;
+                            for (int j = 0; j < 4; ++j) {
+                                const int e = 4 * g + j;
+                                bool sees;
+                                if (WINDOW) sees = (unsigned)(now.pos[tg] - row.y) + e < (unsigned)row.x || now.pos[tg] < row.z - e;
+                                else sees = now.pos[tg] <= row.x - e && ((named >> j) & 1);
+                                if (!sees) s[rt][tg][j] = NEG;
+                            }
+                        }
+                    } else {
+#pragma unroll
+                        for (int tg = 0; tg < TG; ++tg)
+#pragma unroll
+                            for (int j = 0; j < 4; ++j)
+                                if (now.pos[tg] > last[rt] - (4 * g + j)) s[rt][tg][j] = NEG;
+                    }
                 }
                 float top = s[rt][0][0];
 #pragma unroll
@@ -663,8 +795,8 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, TYPE)) void 
         __syncthreads();
         const bool whole = start == 0 && end == tiles;
         const int64_t slot = 2 * ((int64_t)share * row_tiles + row_tile) + (start == 0 ? 1 : 0);
-        if (least != 0 && start == 0 && threadIdx.x == 0 && row_tile == 0)
-            ws.parts[(int64_t)b * kv.heads + pair] = {(int)share, 1 + (int)(((unsigned)(tiles - end) + at.whole - 1) / at.whole)};
+        if (least != 0 && start == 0 && threadIdx.x == 0 && (MASKED || row_tile == 0))
+            ws.parts[MASKED ? ((int64_t)b * kv.heads + pair) * row_tiles + row_tile : (int64_t)b * kv.heads + pair] = {(int)share, 1 + (int)(((unsigned)(tiles - end) + at.whole - 1) / at.whole)};
 #pragma unroll 1
         for (int rt = 0; rt < RT; ++rt) {
             float top = NEG;
@@ -734,7 +866,7 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, TYPE)) void 
         if (end == tiles && ++pair == kv.heads) {
             pair = 0;
             if (++b >= a.nseq) return;
-            tiles = tiles_of(kv, a, kv_uniform(a.lengths)[b], TOK);
+            tiles = tiles_seen(kv, q, a, row_tokens(q, row0, 16 * RT), kv_uniform(a.lengths)[b], TOK);
         }
         start = 0;
         __syncthreads();               // LDS is used again
@@ -744,7 +876,7 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, TYPE)) void 
 // Parts of a row joined, o = sum_u o_u 2^(m_u - m) / sum_u l_u 2^(m_u - m): a workgroup of NT threads per row, dpad / 4 of them side by
 // side per part.  Bound by two round trips to memory (which parts, then the parts, all asked for at once up to 4 per thread): 1024 rows
 // of 2 to 8 parts 4.7 us, 4096 rows 6.4, 32 rows of 32 parts 4.0.
-template <int NT>
+template <int NT, bool MASKED>
 __global__ __launch_bounds__(NT) void kv_join_kernel(KvView kv, KvQueries q, KvAttend a, int row_tiles, int tile_rows, int grid)
 {
     __shared__ float4 sums[NT];
@@ -753,7 +885,7 @@ __global__ __launch_bounds__(NT) void kv_join_kernel(KvView kv, KvQueries q, KvA
     const int rows = q.new_tokens * q.group;
     const int r = blockIdx.x % rows, bh = blockIdx.x / rows, h = bh % kv.heads, b = bh / kv.heads;
     const Workspace ws = workspace(a.part, 2 * (int64_t)grid, tile_rows, kv.dpad);
-    const Parts parts = ws.parts[bh];
+    const Parts parts = ws.parts[MASKED ? (int64_t)bh * row_tiles + r / tile_rows : bh];
     if (parts.count <= 1) return;
     const int cols = kv.dpad >> 2, groups = NT / cols;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, row_tile = r / tile_rows, inside = r - row_tile * tile_rows;
@@ -824,10 +956,10 @@ __global__ __launch_bounds__(NT) void kv_join_kernel(KvView kv, KvQueries q, KvA
     }
 }
 
-template <int DP, bool PACKED, int TYPE>
-void launch_rows(const KvView &kv, const KvQueries &q, const KvAttend &a, const KvAttendPlan &p, hipStream_t st)
+template <int DP, bool PACKED, int TYPE, typename CALL>
+void launch_rows(const KvView &kv, const KvQueries &q, const CALL &a, const KvAttendPlan &p, hipStream_t st)
 {
-    if constexpr (two_row_tiles(DP, PACKED, TYPE)) {
+    if constexpr (two_row_tiles(DP, PACKED, TYPE, std::is_same<CALL, KvTree>::value)) {
         if (p.rows == 32) {
             kv_attend_kernel<DP, PACKED, 2, TYPE><<<p.grid, THREADS, 0, st>>>(kv, q, a, p.row_tiles, p.least);
             return;
@@ -836,57 +968,24 @@ void launch_rows(const KvView &kv, const KvQueries &q, const KvAttend &a, const 
     kv_attend_kernel<DP, PACKED, 1, TYPE><<<p.grid, THREADS, 0, st>>>(kv, q, a, p.row_tiles, p.least);
 }
 
-template <int DP, int TYPE>
-void launch_codes(const KvView &kv, const KvQueries &q, const KvAttend &a, const KvAttendPlan &p, hipStream_t st)
+template <int DP, int TYPE, typename CALL>
+void launch_codes(const KvView &kv, const KvQueries &q, const CALL &a, const KvAttendPlan &p, hipStream_t st)
 {
     if (kv.packed) launch_rows<DP, true, TYPE>(kv, q, a, p, st);
     else launch_rows<DP, false, TYPE>(kv, q, a, p, st);
 }
 
-template <int DP>
-void launch_dim(const KvView &kv, const KvQueries &q, const KvAttend &a, const KvAttendPlan &p, hipStream_t st)
+template <int DP, typename CALL>
+void launch_dim(const KvView &kv, const KvQueries &q, const CALL &a, const KvAttendPlan &p, hipStream_t st)
 {
     if (q.type == LPQ_TYPE_F32) launch_codes<DP, LPQ_TYPE_F32>(kv, q, a, p, st);
     else if (q.type == LPQ_TYPE_F16) launch_codes<DP, LPQ_TYPE_F16>(kv, q, a, p, st);
     else launch_codes<DP, LPQ_TYPE_BF16>(kv, q, a, p, st);
 }
 
-}  // namespace
-
-// Short sequences get a workgroup per pair and row tile: joining parts would cost more than it gives.  Otherwise as many workgroups as
-// the chip holds at once, and no fewer than 4 tiles each.  Short is up to 1024 tokens, of more than 128 features fewer where workgroups are
-// few: 16 pairs, whole against split and joined, us: 1000 tokens of 64 features 10.9, 12.8, of 128 13.6, 13.5, of 256 19.6, 17.2; 500 of 256
-// 15.6, 16.1.  512 pairs of 128, 1000 tokens: 24.4, 31.3.  Nor are sequences split where a pair's row tiles fill the chip by themselves: 16 384
-// bfloat16 rows on one head of 128, 2000 tokens 69 us, split into 8 shares and joined 135, 50 000 tokens 1123, 1168 (and 136 MB of parts).
-KvAttendPlan kv_attend_plan(const KvView &kv, int64_t nseq, int new_tokens, int group, int64_t tokens, int type)
+template <typename CALL>
+hipError_t launch_all(const KvView &kv, const KvQueries &q, const CALL &a, const KvAttendPlan &p, hipStream_t st)
 {
-    KvAttendPlan p;
-    const int64_t rows = (int64_t)new_tokens * group;
-    const int64_t pairs = nseq * kv.heads;
-    p.rows = rows > 16 && pairs * tokens > TWO_ROW_TOKENS && two_row_tiles(kv.dpad, kv.packed, type) ? 32 : 16;
-    p.row_tiles = (int)ceil_div(rows, (int64_t)p.rows);
-    const int64_t tile = tile_tokens(kv.dpad, kv.packed);
-    p.least = 0;
-    p.grid = (unsigned)(pairs * p.row_tiles);
-    p.bytes = 0;
-    const int64_t tiles = ceil_div(tokens, tile);
-    const bool few = (int64_t)p.grid < 256 && tokens * kv.dpad > 128 * 1024;
-    const int64_t chip = std::min<int64_t>(256 * blocks_per_cu(kv.dpad, kv.packed, p.rows / 16, type), KV_ATTEND_SHARES);
-    if ((tokens > 1024 || few) && p.row_tiles < chip && pairs * tiles < (int64_t(1) << 31)) {      // (beyond that there are pairs enough)
-        p.least = 4;
-        const int64_t most = ceil_div(tiles, (int64_t)p.least) * pairs;
-        const int64_t room = ceil_div(chip, (int64_t)p.row_tiles);
-        int64_t shares = most < room ? most : room;
-        if (p.row_tiles > 1) shares = round_up(shares, 8);
-        p.grid = (unsigned)(shares * p.row_tiles);
-        p.bytes = ((size_t)2 * p.grid * p.rows * (kv.dpad + 2) + (size_t)2 * pairs) * sizeof(float);
-    }
-    return p;
-}
-
-hipError_t launch_kv_attend(const KvView &kv, const KvQueries &q, const KvAttend &a, const KvAttendPlan &p, hipStream_t st)
-{
-    if (a.nseq <= 0) return hipSuccess;
     switch (kv.dpad) {
     case 64: launch_dim<64>(kv, q, a, p, st); break;
     case 128: launch_dim<128>(kv, q, a, p, st); break;
@@ -896,10 +995,54 @@ hipError_t launch_kv_attend(const KvView &kv, const KvQueries &q, const KvAttend
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.least == 0) return e;
     const unsigned rows = (unsigned)((int64_t)a.nseq * kv.heads * q.new_tokens * q.group);
+    constexpr bool MASKED = !std::is_same<CALL, KvAttend>::value;
     // Many rows fill the chip with a wave each, few rows of many parts want more.
-    if (rows >= 1024) kv_join_kernel<64><<<rows, 64, 0, st>>>(kv, q, a, p.row_tiles, p.rows, (int)p.grid);
-    else kv_join_kernel<256><<<rows, 256, 0, st>>>(kv, q, a, p.row_tiles, p.rows, (int)p.grid);
+    if (rows >= 1024) kv_join_kernel<64, MASKED><<<rows, 64, 0, st>>>(kv, q, a, p.row_tiles, p.rows, (int)p.grid);
+    else kv_join_kernel<256, MASKED><<<rows, 256, 0, st>>>(kv, q, a, p.row_tiles, p.rows, (int)p.grid);
     return hipGetLastError();
+}
+
+}  // namespace
+
+// Short sequences get a workgroup per pair and row tile: joining parts would cost more than it gives.  Otherwise as many workgroups as
+// the chip holds at once, and no fewer than 4 tiles each.  Short is up to 1024 tokens, of more than 128 features fewer where workgroups are
+// few: 16 pairs, whole against split and joined, us: 1000 tokens of 64 features 10.9, 12.8, of 128 13.6, 13.5, of 256 19.6, 17.2; 500 of 256
+// 15.6, 16.1.  512 pairs of 128, 1000 tokens: 24.4, 31.3.  Nor are sequences split where a pair's row tiles fill the chip by themselves: 16 384
+// bfloat16 rows on one head of 128, 2000 tokens 69 us, split into 8 shares and joined 135, 50 000 tokens 1123, 1168 (and 136 MB of parts).
+KvAttendPlan kv_attend_plan(const KvView &kv, int64_t nseq, int new_tokens, int group, int64_t tokens, int type, const KvMask &mask)
+{
+    KvAttendPlan p;
+    const int64_t rows = (int64_t)new_tokens * group;
+    const int64_t pairs = nseq * kv.heads;
+    // What a row tile has to go through at most, of tokens that lie side by side: the sinks, and the windows of its new tokens.
+    if (mask.window) tokens = std::min<int64_t>(tokens, round_up((int64_t)mask.sinks, 16) + mask.window + std::min<int64_t>(new_tokens, 32 / group + 2) + 30);
+    p.rows = rows > 16 && pairs * tokens > TWO_ROW_TOKENS && two_row_tiles(kv.dpad, kv.packed, type, mask.tree != nullptr) ? 32 : 16;
+    p.row_tiles = (int)ceil_div(rows, (int64_t)p.rows);
+    const int64_t tile = tile_tokens(kv.dpad, kv.packed);
+    p.least = 0;
+    p.grid = (unsigned)(pairs * p.row_tiles);
+    p.bytes = 0;
+    const int64_t tiles = ceil_div(tokens, tile);
+    const bool few = (int64_t)p.grid < 256 && tokens * kv.dpad > 128 * 1024;
+    const int64_t chip = std::min<int64_t>(256 * blocks_per_cu(kv.dpad, kv.packed, p.rows / 16, type, mask.window != 0), KV_ATTEND_SHARES);
+    if ((tokens > 1024 || few) && p.row_tiles < chip && pairs * tiles < (int64_t(1) << 31)) {      // (beyond that there are pairs enough)
+        p.least = 4;
+        const int64_t most = ceil_div(tiles, (int64_t)p.least) * pairs;
+        const int64_t room = ceil_div(chip, (int64_t)p.row_tiles);
+        int64_t shares = most < room ? most : room;
+        if (p.row_tiles > 1) shares = round_up(shares, 8);
+        p.grid = (unsigned)(shares * p.row_tiles);
+        p.bytes = ((size_t)2 * p.grid * p.rows * (kv.dpad + 2) + (size_t)2 * pairs * (mask.window || mask.tree ? p.row_tiles : 1)) * sizeof(float);
+    }
+    return p;
+}
+
+hipError_t launch_kv_attend(const KvView &kv, const KvQueries &q, const KvAttend &a, const KvMask &mask, const KvAttendPlan &p, hipStream_t st)
+{
+    if (a.nseq <= 0) return hipSuccess;
+    if (mask.window) return launch_all(kv, q, KvWindow{a, mask.window, mask.sinks}, p, st);
+    if (mask.tree) return launch_all(kv, q, KvTree{a, mask.tree, mask.ldt_seq, mask.ldt_token}, p, st);
+    return launch_all(kv, q, a, p, st);
 }
 
 }  // namespace lpq

@@ -9,6 +9,7 @@ namespace lpq {
 enum { KV_MAX_DIM = 256, KV_MIN_PAGE = 16, KV_MAX_PAGE = 256,
        KV_MAX_SELECT_ROWS = 128,      // query rows per key-value head whose summed codes fit two 7-bit digits
        KV_ATTEND_SHARES = 1024,       // most shares of an attention call, so most parts of a sequence: four workgroups per CU
+       KV_MAX_TREE = 4096,            // new tokens of a call with a tree: their mask's bits fit LDS
        KV_MAX_BLOCKS = 1 << 22 };     // workgroups of a launch (twice that stays below 2^32 threads of 256 each)
 
 // Constants of Equation 1 and the step s = 1 / m, five arrays of [heads][dpad] floats on the device.  Features without
@@ -77,6 +78,21 @@ struct KvAttend {
     float *lse;                      // null or [nseq][new_tokens][heads * group]
     float *part;                     // workspace of kv_attend_plan
 };
+// What a call's new tokens see besides, one of both or none.  With a window (0: none), one at position p sees positions above p - window and
+// those below `sinks`, of these those up to p; in a tree (null: none) all that are ahead of the new tokens, and of the new ones those that its
+// row of the mask [nseq][new_tokens][new_tokens] names.
+struct KvMask {
+    int window, sinks;
+    const uint8_t *tree;
+    int64_t ldt_seq, ldt_token;
+};
+struct KvWindow : KvAttend {
+    int window, sinks;
+};
+struct KvTree : KvAttend {
+    const uint8_t *tree;
+    int64_t ldt_seq, ldt_token;
+};
 // How a call is shared out: `row_tiles` tiles of `rows` query rows cover a key-value head's; `grid` workgroups, as many
 // of them per row tile as there are shares, take equal runs of all tiles of tokens, at least `least` each, or (least = 0) one (sequence,
 // head, row tile) each.
@@ -85,8 +101,8 @@ struct KvAttendPlan {
     unsigned grid;
     size_t bytes;                    // of workspace
 };
-KvAttendPlan kv_attend_plan(const KvView &kv, int64_t nseq, int new_tokens, int group, int64_t tokens, int type);
-hipError_t launch_kv_attend(const KvView &kv, const KvQueries &q, const KvAttend &a, const KvAttendPlan &plan, hipStream_t st);
+KvAttendPlan kv_attend_plan(const KvView &kv, int64_t nseq, int new_tokens, int group, int64_t tokens, int type, const KvMask &mask);
+hipError_t launch_kv_attend(const KvView &kv, const KvQueries &q, const KvAttend &a, const KvMask &mask, const KvAttendPlan &plan, hipStream_t st);
 
 #if defined(__HIPCC__)
 // Memory that no kernel of the call writes, read at addresses all lanes share: scalar loads.

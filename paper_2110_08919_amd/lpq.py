@@ -90,6 +90,9 @@ def lib() -> C.CDLL:
             "lpq_kv_attend_workspace_bytes": (C.c_size_t, [vp, i64, i32, i32, i64, i32]),
             "lpq_kv_attend": (i32, [vp, vp, i64, i64, i64, i32, i64, i32, i32, f32, vp, vp, i64, i64, vp, i32, vp, i64, i64,
                                     i64, vp, vp, C.c_size_t, vp]),
+            "lpq_kv_attend_masked_workspace_bytes": (C.c_size_t, [vp, i64, i32, i32, i64, i32, i64, i32, i32]),
+            "lpq_kv_attend_masked": (i32, [vp, vp, i64, i64, i64, i32, i64, i32, i32, f32, vp, vp, i64, i64, vp, i32, i64, i32, vp, i64, i64,
+                                           vp, i64, i64, i64, vp, vp, C.c_size_t, vp]),
             "lpq_last_error": (C.c_char_p, []),
         }
         for name, (res, args) in sig.items():
@@ -468,9 +471,13 @@ class KVCache:
         return out
 
     def attend(self, q: torch.Tensor, lengths: torch.Tensor, table: torch.Tensor, pages: torch.Tensor = None,
-               scale: float = None, out: torch.Tensor = None, return_lse: bool = False, workspace: torch.Tensor = None):
+               scale: float = None, out: torch.Tensor = None, return_lse: bool = False, workspace: torch.Tensor = None,
+               window: int = None, sinks: int = 0, tree: torch.Tensor = None):
         """Attention of q [sequences, new tokens, query heads, features] over the cache (the last new_tokens positions of
         each length are the queries' own), or over the `pages` that select() names; scale 1 / sqrt(features) by default.
+        window: a token sees the last `window` positions up to its own, and the first `sinks`.  tree: bool [sequences, new
+        tokens, new tokens] (or without the first axis, for all sequences), which new tokens each sees beside all the
+        tokens ahead of them: drafted tokens, themselves and their ancestors.
         There is no way back through the codes: queries that require a gradient are refused."""
         assert not (q.requires_grad and torch.is_grad_enabled()), "attention over codes has no gradient: use torch.no_grad() or q.detach()"
         nseq, tab = self._table(table)
@@ -487,12 +494,32 @@ class KVCache:
             n_select = pages.shape[-1]
             assert pages.is_cuda and pages.dtype is torch.int32 and pages.is_contiguous() and pages.shape == (nseq, self.heads, n_select) \
                 and n_select > 0, "need contiguous int32 pages [sequences, heads, pages], at least one of them"
+        if window is not None or sinks or tree is not None:
+            return self._attend_masked(q, queries, nseq, new, q_heads, lengths, tab, pages, n_select, scale, out, outputs, lse, workspace,
+                                       window, sinks, tree)
         workspace, ws, size = self._workspace(
             workspace, _lib.lpq_kv_attend_workspace_bytes(self._h, nseq, new, q_heads, tab[2], n_select), q.device)
         _check(_lib.lpq_kv_attend(self._h, *queries, _TYPE[q.dtype], nseq, new, q_heads,
                                   self.dim ** -0.5 if scale is None else scale, _dev_ints(lengths, nseq), *tab, _ptr(pages), n_select,
                                   *outputs, _ptr(lse), ws, size, _stream_of(q)))
         return (out, lse) if return_lse else out
+
+    def _attend_masked(self, q, queries, nseq, new, q_heads, lengths, tab, pages, n_select, scale, out, outputs, lse, workspace, window, sinks,
+                       tree):
+        assert window is None or window >= 1, "a window holds one position at least"
+        assert 0 <= sinks < 2 ** 31, "sinks are counted from 0"
+        mask, by_seq, by_token = None, 0, 0
+        if tree is not None:
+            assert tree.is_cuda and tree.dtype is torch.bool and tree.shape in ((nseq, new, new), (new, new)) and (tree.stride(-1) == 1 or new == 1), \
+                f"need a device tree bool [{nseq}, {new}, {new}], the last axis contiguous"
+            mask, by_seq, by_token = tree.data_ptr(), tree.stride(0) if tree.dim() == 3 else 0, tree.stride(-2)
+        width = 0 if window is None else min(window, 2 ** 40)
+        workspace, ws, size = self._workspace(
+            workspace, _lib.lpq_kv_attend_masked_workspace_bytes(self._h, nseq, new, q_heads, tab[2], n_select, width, sinks, mask is not None), q.device)
+        _check(_lib.lpq_kv_attend_masked(self._h, *queries, _TYPE[q.dtype], nseq, new, q_heads, self.dim ** -0.5 if scale is None else scale,
+                                         _dev_ints(lengths, nseq), *tab, _ptr(pages), n_select, width, sinks, mask, by_seq, by_token, *outputs,
+                                         _ptr(lse), ws, size, _stream_of(q)))
+        return out if lse is None else (out, lse)
 
 
 def rerank_f32(x: torch.Tensor, q: torch.Tensor, cand_ids: torch.Tensor, k: int, metric="l2sq"):
