@@ -280,6 +280,26 @@ int lpq_kv_write(const lpq_kv *kv, const void *k_dev, int64_t ldk_token, int64_t
                  const int32_t *starts_dev, const int32_t *table_dev, int64_t ld_table, int64_t table_pages,
                  void *stream);
 
+/* lpq_kv_write of keys that are turned by the angles of their positions first (values are not), and with them the
+ * queries of the same tokens.  cos_dev, sin_dev float [angles][rotated / 2], ld_angles apart: row p belongs to position p.  The
+ * first `rotated` features of a head are turned in pairs, (i, i + rotated / 2) or, interleaved != 0, (2 i, 2 i + 1), the others not:
+ *   a' = fl(fl(a cos) - fl(b sin)),  b' = fl(fl(b cos) + fl(a sin))   in binary32,
+ * and the keys encoded from that, without a rounding to their type between.  A row's position is the one that it is written to, or
+ * positions_dev[row] (int32 [n], null: none given), as for drafted tokens that share a depth in a tree.
+ * q_dev null, or n rows [n][q_heads][D] numbered as the keys, of the same type: out_dev receives them turned, rounded to
+ * the type; q_heads a multiple of heads.  out_dev may be q_dev with its strides (turned in place); else the two must not overlap.
+ * Rows at positions below 0 and rows of no sequence are not turned (queries come out as they are; keys as in lpq_kv_write); at positions beyond the table's
+ * the turned features are NaN (which a key's code holds as 0).
+ * Errors as lpq_kv_write; LPQ_EINVAL: rotated odd, below 2 or above D, angles < 1, ld_angles < rotated / 2, queries without an
+ * output, q_heads not a multiple of heads, strides of the output that overlap; LPQ_ERANGE: angles >= 2^31, q_heads > 65536. */
+int lpq_kv_write_rotated(const lpq_kv *kv, const void *k_dev, int64_t ldk_token, int64_t ldk_head, const void *v_dev,
+                         int64_t ldv_token, int64_t ldv_head, int type, int64_t n, int64_t nseq,
+                         const int32_t *first_dev, const int32_t *starts_dev, const int32_t *table_dev, int64_t ld_table,
+                         int64_t table_pages, const float *cos_dev, const float *sin_dev, int64_t ld_angles,
+                         int64_t angles, int rotated, int interleaved, const int32_t *positions_dev, const void *q_dev,
+                         int64_t ldq_token, int64_t ldq_head, int q_heads, void *out_dev, int64_t ldo_token,
+                         int64_t ldo_head, void *stream);
+
 /* The way back: rows of the same numbering receive x^ of their position, rounded to `type`; positions without a
  * page and rows of no sequence give zeros.  Errors as above. */
 int lpq_kv_read(const lpq_kv *kv, void *k_dev, int64_t ldk_token, int64_t ldk_head, void *v_dev, int64_t ldv_token,

@@ -182,6 +182,48 @@ extern "C" int lpq_kv_write(const lpq_kv *kv, const void *k_dev, int64_t ldk_tok
     return e == hipSuccess ? LPQ_OK : hip_fail(e, "lpq_kv_write");
 }
 
+extern "C" int lpq_kv_write_rotated(const lpq_kv *kv, const void *k_dev, int64_t ldk_token, int64_t ldk_head, const void *v_dev,
+                                    int64_t ldv_token, int64_t ldv_head, int type, int64_t n, int64_t nseq,
+                                    const int32_t *first_dev, const int32_t *starts_dev, const int32_t *table_dev,
+                                    int64_t ld_table, int64_t table_pages, const float *cos_dev, const float *sin_dev,
+                                    int64_t ld_angles, int64_t angles, int rotated, int interleaved, const int32_t *positions_dev,
+                                    const void *q_dev, int64_t ldq_token, int64_t ldq_head, int q_heads, void *out_dev,
+                                    int64_t ldo_token, int64_t ldo_head, void *stream)
+{
+    KvRows kr, vr;
+    KvPlaces pl;
+    const int rc = kv_rows(kv, k_dev, ldk_token, ldk_head, v_dev, ldv_token, ldv_head, type, n, nseq, first_dev, starts_dev,
+                           table_dev, ld_table, table_pages, false, &kr, &vr, &pl);
+    if (rc) return rc;
+    const int dim = kv->view.dim;
+    if (rotated < 2 || rotated % 2 || rotated > dim) return kv_fail(LPQ_EINVAL, "rotated = %d of %d features: an even number from 2 on", rotated, dim);
+    if (n > 0 && (!cos_dev || !sin_dev)) return kv_fail(LPQ_EINVAL, "null argument");
+    if (angles < 1 || ld_angles < rotated / 2 || ld_angles > MAX_STRIDE)
+        return kv_fail(LPQ_EINVAL, "angles of %lld positions, %lld apart", (long long)angles, (long long)ld_angles);
+    if (angles > INT32_MAX) return kv_fail(LPQ_ERANGE, "angles of %lld positions", (long long)angles);
+    KvAngles a = {cos_dev, sin_dev, ld_angles, angles, positions_dev, rotated / 2, interleaved != 0, {nullptr, 0, 0, type}, {nullptr, 0, 0, type}, 0};
+    if (q_dev && n > 0) {
+        if (q_heads < kv->view.heads || q_heads % kv->view.heads)
+            return kv_fail(LPQ_EINVAL, "%d query heads on %d key-value heads", q_heads, kv->view.heads);
+        if (q_heads > 65536) return kv_fail(LPQ_ERANGE, "%d query heads", q_heads);
+        if (!out_dev) return kv_fail(LPQ_EINVAL, "null output");
+        int64_t strides[2][2] = {{ldq_token, ldq_head}, {ldo_token, ldo_head}};
+        for (auto &s : strides) {
+            if (s[0] < 0 || s[1] < 0 || s[0] > MAX_STRIDE || s[1] > MAX_STRIDE)
+                return kv_fail(LPQ_EINVAL, "strides %lld, %lld of queries", (long long)s[0], (long long)s[1]);
+            if (n <= 1) s[0] = 0;
+            if (q_heads == 1) s[1] = 0;
+        }
+        if (!disjoint(dim, {{{strides[1][0], n}, {strides[1][1], q_heads}, {0, 1}}}))
+            return kv_fail(LPQ_EINVAL, "strides %lld, %lld of the output overlap", (long long)ldo_token, (long long)ldo_head);
+        a.q = {const_cast<void *>(q_dev), strides[0][0], strides[0][1], type};
+        a.out = {out_dev, strides[1][0], strides[1][1], type};
+        a.q_heads = q_heads;
+    }
+    const hipError_t e = launch_kv_write_rotated(kv->view, kr, vr, pl, a, (hipStream_t)stream);
+    return e == hipSuccess ? LPQ_OK : hip_fail(e, "lpq_kv_write_rotated");
+}
+
 extern "C" int lpq_kv_read(const lpq_kv *kv, void *k_dev, int64_t ldk_token, int64_t ldk_head, void *v_dev,
                            int64_t ldv_token, int64_t ldv_head, int type, int64_t n, int64_t nseq,
                            const int32_t *first_dev, const int32_t *starts_dev, const int32_t *table_dev,

@@ -11,6 +11,7 @@
 // Measured (write, read): one row of 8 heads of 128, bfloat16: 5.1, 3.6 us; 64 rows of 64 sequences 6.7, 4.2; 26 244 rows of 6 x 100
 // float16 features of 12 prompts to packed codes 31.8 (vector instructions for 20 of them, 133 to a thread's 8 values, memory for 11;
 // float32 rows 42) and back 22.6; 151 419 rows of 8 x 128 back to bfloat16: 188 us, 4.9 TB/s of codes and rows (a copy of memory: 4.7).
+#include <algorithm>
 #include <type_traits>
 
 #include "kv_internal.h"
@@ -21,9 +22,10 @@ namespace {
 
 constexpr int KV_THREADS = 256;
 constexpr int KV_ROWS = 4;      // rows a thread has in flight
+constexpr int KV_TURNED_ROWS = 2;      // where their angles and the other features of their pairs are in flight too
 // Workgroups that a large call is shared out to.  One generation of them where each writes whole pages (25 000 rows of 6 x 100
 // features: 33 us; 2048 workgroups 34, 4096 35.5), more where rows are cut anywhere (155 000 rows of 8 x 128 back: 194, 193, 189).
-constexpr int KV_WRITERS = 1024, KV_READERS = 4096;
+constexpr int KV_WRITERS = 1024, KV_READERS = 4096, KV_TURNERS = 2048;
 
 // How a call is shared out: `groups` groups of `heads` heads each, `rows` rows of the call to a workgroup of each group; a
 // workgroup's threads are `lanes` rows of `heads` heads of dpad / 8 threads.
@@ -67,11 +69,9 @@ __device__ __forceinline__ int floor_int(float t)
 // Equation 1 for 8 values: two separately rounded operations, floor, clamp (KvConstants::clamps).  Pairs of 16 bits: features
 // 2 e and 2 e + 1.
 template <bool clamps>
-__device__ __forceinline__ void encode8(const Raw8 &raw, int type, int left, const Features8 &f, Pair *q)
+__device__ __forceinline__ void encode8(const float *x, const Features8 &f, Pair *q)
 {
-    float x[8];
     int c[8];
-    kv_floats8(raw, type, left, x);
 #pragma unroll
     for (int e = 0; e < 8; ++e) c[e] = floor_int(__fmul_rn(__fsub_rn(x[e], f.k[e]), f.m[e]));
     if (!clamps) {
@@ -208,9 +208,195 @@ __device__ __forceinline__ Seat seat(const KvView &kv, const KvPlaces &pl, const
     return s;
 }
 
-template <int type, bool packed, bool clamps>
-__global__ __launch_bounds__(KV_THREADS, 4) void kv_write_kernel(KvView kv, KvRows kr, KvRows vr, KvPlaces pl, Share sh)
+// Rotation.  Of a pair (a, b) of features and the angles (c, s) of its position: a' = fl(fl(a c) - fl(b s)), b' = fl(fl(b c) + fl(a s)) in binary32,
+// so that what is written does not depend on the order of operations.  A row without an angle (of no sequence, or at a position below 0)
+// stays as it is; one beyond the table becomes NaN, which its reader notices, and not some other position's row.
+template <bool NEIGHBOURS>
+struct Turn {
+    KvAngles angles;
+    unsigned writers;              // workgroups that write; those behind them turn queries
+    int rows, units;               // rows of such a workgroup, units of a row (turn_queries)
+};
+enum { TURN_HEADS = 4 };           // heads that a thread turns with the angles it has loaded
+
+// Up to N neighbouring angles from table row `at`; the others turn nothing.
+template <int N>
+__device__ __forceinline__ void load_angles(const KvAngles &a, int64_t at, int first, int left, float *c, float *s)
 {
+    const int64_t from = at * a.ld + first;
+    if (left >= N) {
+        __builtin_memcpy(c, a.cos + from, 4 * N);
+        __builtin_memcpy(s, a.sin + from, 4 * N);
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+        c[e] = 1.0f;
+        s[e] = 0.0f;
+        if (e < left) {
+            c[e] = a.cos[from + e];
+            s[e] = a.sin[from + e];
+        }
+    }
+}
+
+// What it takes to turn features c0 .. c0 + 7 of a row: angles, and (pairs that lie apart) the other features of their pairs.
+template <bool NEIGHBOURS>
+struct Turned8 {
+    float c[NEIGHBOURS ? 4 : 8], s[NEIGHBOURS ? 4 : 8];     // pairs apart: s with the sign it is added with
+    Raw8 other;
+    int count;                     // features turned; 0: none
+    bool off;                      // the position is beyond the table
+};
+template <int type, bool NEIGHBOURS>
+__device__ __forceinline__ void load_turn(const KvAngles &a, const KvRows &in, int64_t row, int c0, int64_t position, Turned8<NEIGHBOURS> &t)
+{
+    const int two = 2 * a.half;
+    t.count = position < 0 || c0 >= two ? 0 : two - c0 < 8 ? two - c0 : 8;
+    t.off = position >= a.count;
+    if (t.count == 0) return;
+    const int64_t at = t.off ? 0 : position;
+    if constexpr (NEIGHBOURS) {
+        load_angles<4>(a, at, c0 >> 1, a.half - (c0 >> 1), t.c, t.s);
+    } else if (c0 + 8 <= a.half) {
+        t.other = kv_load8(in.p, type, row + c0 + a.half, 8);
+        load_angles<8>(a, at, c0, 8, t.c, t.s);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) t.s[e] = -t.s[e];
+    } else if (c0 >= a.half && c0 + 8 <= two) {
+        t.other = kv_load8(in.p, type, row + c0 - a.half, 8);
+        load_angles<8>(a, at, c0 - a.half, 8, t.c, t.s);
+    } else {                       // 8 features that end one half, and may begin the other: one at a time
+        t.other = {{0, 0, 0, 0, 0, 0, 0, 0}};
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const int f = c0 + e, first = f < a.half ? f : f - a.half;
+            t.c[e] = 1.0f;
+            t.s[e] = 0.0f;
+            if (f >= two) continue;
+            t.c[e] = a.cos[at * a.ld + first];
+            t.s[e] = a.sin[at * a.ld + first];
+            if (f < a.half) t.s[e] = -t.s[e];
+            const int64_t from = row + (f < a.half ? f + a.half : first);
+            if (type == LPQ_TYPE_F32) t.other.w[e] = static_cast<const uint32_t *>(in.p)[from];
+            else t.other.w[e >> 1] |= (uint32_t) static_cast<const uint16_t *>(in.p)[from] << (16 * (e & 1));
+        }
+    }
+}
+template <int type, bool NEIGHBOURS>
+__device__ __forceinline__ void turn8(const Turned8<NEIGHBOURS> &t, float *x)
+{
+    if (t.count == 0) return;
+    float y[8];
+    if constexpr (NEIGHBOURS) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            y[2 * e] = __fsub_rn(__fmul_rn(x[2 * e], t.c[e]), __fmul_rn(x[2 * e + 1], t.s[e]));
+            y[2 * e + 1] = __fadd_rn(__fmul_rn(x[2 * e + 1], t.c[e]), __fmul_rn(x[2 * e], t.s[e]));
+        }
+    } else {
+        float o[8];
+        kv_floats8(t.other, type, 8, o);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[e] = __fadd_rn(__fmul_rn(x[e], t.c[e]), __fmul_rn(o[e], t.s[e]));
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        if (e < t.count) x[e] = t.off ? NAN : y[e];
+}
+
+// Queries, by the workgroups behind those that write.  A thread takes one unit of TURN_HEADS heads of a row with one load of angles: 8 features and
+// the 8 that they are paired with (pairs of neighbours: 8 features, 4 pairs), or 8 that are not turned.  A thread has read all that its
+// results replace, so rows may be turned where they lie.  Bound by memory: each row is read and written once.
+template <int type, bool NEIGHBOURS>
+__device__ __forceinline__ void turn_queries(const KvView &kv, const KvPlaces &pl, const Turn<NEIGHBOURS> &t)
+{
+    const KvAngles &a = t.angles;
+    const int64_t begin = (int64_t)(blockIdx.x - t.writers) * t.rows, end = begin + t.rows < pl.n ? begin + t.rows : pl.n;
+    const unsigned head_groups = (a.q_heads + TURN_HEADS - 1) / TURN_HEADS, per_row = head_groups * t.units;
+    const int halves = NEIGHBOURS ? 0 : (a.half + 7) >> 3;         // units that are two runs of features
+    for (int64_t row0 = begin, to; row0 < end; row0 = to) {
+        Sequence q = {0, 0, 0, 0};
+        to = end;
+        if (pl.starts) {
+            q = sequence_of(pl, row0);
+            if (q.end < to) to = q.end;
+        }
+        const unsigned items = (unsigned)(to - row0) * per_row;
+        for (unsigned i = threadIdx.x; i < items; i += KV_THREADS) {
+            const unsigned r = i / per_row, in_row = i - r * per_row, hg = in_row / t.units, unit = in_row - hg * t.units;
+            const int64_t row = row0 + r;
+            const int h0 = hg * TURN_HEADS;
+            const bool pairs = NEIGHBOURS || (int)unit < halves;
+            const int c0 = NEIGHBOURS || pairs ? 8 * (int)unit : 2 * a.half + 8 * ((int)unit - halves);
+            const int left = !NEIGHBOURS && pairs ? a.half - c0 : kv.dim - c0;
+            const int64_t from = row * a.q.ld_token + c0, into = row * a.out.ld_token + c0;
+            Raw8 x[TURN_HEADS], y[TURN_HEADS];
+#pragma unroll
+            for (int h = 0; h < TURN_HEADS; ++h) {
+                if (h0 + h >= a.q_heads) continue;
+                x[h] = kv_load8(a.q.p, type, from + (h0 + h) * a.q.ld_head, left);
+                if (!NEIGHBOURS && pairs) y[h] = kv_load8(a.q.p, type, from + a.half + (h0 + h) * a.q.ld_head, left);
+            }
+            int64_t position = -1;
+            if (q.b >= 0) position = a.positions ? a.positions[row] : pl.starts ? q.first + (row - q.begin) : pl.first[row];
+            const bool off = position >= a.count;
+            const int64_t at = off ? 0 : position;
+            constexpr int N = NEIGHBOURS ? 4 : 8;
+            const int first = NEIGHBOURS ? c0 >> 1 : c0, angles = !pairs || position < 0 ? 0 : a.half - first;
+            float c[N], s[N];
+            if (angles > 0) load_angles<N>(a, at, first, angles, c, s);
+#pragma unroll
+            for (int h = 0; h < TURN_HEADS; ++h) {
+                if (h0 + h >= a.q_heads) continue;
+                float u[8], w[8];
+                kv_floats8(x[h], type, left, u);
+                if constexpr (NEIGHBOURS) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (e < angles) {
+                            const float p = u[2 * e], o = u[2 * e + 1];
+                            u[2 * e] = off ? NAN : __fsub_rn(__fmul_rn(p, c[e]), __fmul_rn(o, s[e]));
+                            u[2 * e + 1] = off ? NAN : __fadd_rn(__fmul_rn(o, c[e]), __fmul_rn(p, s[e]));
+                        }
+                } else if (pairs) {
+                    kv_floats8(y[h], type, left, w);
+                    if (angles > 0) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            const float p = u[e], o = w[e];
+                            u[e] = off ? NAN : __fsub_rn(__fmul_rn(p, c[e]), __fmul_rn(o, s[e]));
+                            w[e] = off ? NAN : __fadd_rn(__fmul_rn(o, c[e]), __fmul_rn(p, s[e]));
+                        }
+                    }
+                    kv_store<8>(a.out.p, type, into + a.half + (h0 + h) * a.out.ld_head, left, w);
+                }
+                kv_store<8>(a.out.p, type, into + (h0 + h) * a.out.ld_head, left, u);
+            }
+        }
+    }
+}
+
+template <typename... TURN>
+struct Turns {
+    static constexpr bool some = false, neighbours = false;
+};
+template <bool NEIGHBOURS>
+struct Turns<Turn<NEIGHBOURS>> {
+    static constexpr bool some = true, neighbours = NEIGHBOURS;
+};
+
+template <int type, bool packed, bool clamps, typename... TURN>
+__global__ __launch_bounds__(KV_THREADS, sizeof...(TURN) ? 2 : 4) void kv_write_kernel(KvView kv, KvRows kr, KvRows vr, KvPlaces pl, Share sh, TURN... turn)
+{
+    constexpr bool TURNED = Turns<TURN...>::some, NEIGHBOURS = Turns<TURN...>::neighbours;
+    constexpr int ROWS = TURNED ? KV_TURNED_ROWS : KV_ROWS;
+    if constexpr (TURNED) {
+        if (blockIdx.x >= (turn.writers, ...)) {
+            turn_queries<type, NEIGHBOURS>(kv, pl, turn...);
+            return;
+        }
+    }
     __shared__ uint2 part_lo[KV_THREADS], part_hi[KV_THREADS];
     const Seat s = seat(kv, pl, sh);
     const KvRows in = s.which ? vr : kr;
@@ -242,21 +428,39 @@ __global__ __launch_bounds__(KV_THREADS, 4) void kv_write_kernel(KvView kv, KvRo
         if (s.on) {
             uint8_t *rows = (s.which ? kv.v : kv.k) + (page * kv.heads + s.h) * kv.page * row_bytes;
             const int64_t from = (row - lo_row) * in.ld_token + s.h * in.ld_head + s.c0;
-            auto encode = [&](const Raw8 &x, int t) {
+            Turned8<NEIGHBOURS> turned[ROWS];
+            auto encode = [&](const Raw8 &raw, int t, int u) {
+                float x[8];
                 Pair c[4];
-                encode8<clamps>(x, type, left, f, c);
+                kv_floats8(raw, type, left, x);
+                if constexpr (TURNED) {
+                    if (s.which == 0) turn8<type>(turned[u], x);
+                }
+                encode8<clamps>(x, f, c);
                 store_codes8(rows + t * row_bytes, s.c0, packed, c);
                 if (s.which == 0) widen(c);
             };
-            for (int t0 = lo_row + s.lane; t0 < hi_row; t0 += KV_ROWS * sh.lanes) {
-                Raw8 x[KV_ROWS];
+            for (int t0 = lo_row + s.lane; t0 < hi_row; t0 += ROWS * sh.lanes) {
+                Raw8 x[ROWS];
 #pragma unroll
-                for (int u = 0; u < KV_ROWS; ++u)
+                for (int u = 0; u < ROWS; ++u)
                     if (t0 + u * sh.lanes < hi_row) x[u] = kv_load8(in.p, type, from + (t0 + u * sh.lanes) * in.ld_token, left);
+                if constexpr (TURNED) {
+                    if (s.which == 0) {
+#pragma unroll
+                        for (int u = 0; u < ROWS; ++u) {
+                            const int t = t0 + u * sh.lanes;
+                            if (t >= hi_row) continue;
+                            const KvAngles &a = (turn.angles, ...);
+                            const int64_t position = a.positions ? a.positions[row + (t - lo_row)] : (column << kv.page_shift) + t;
+                            load_turn<type, NEIGHBOURS>(a, in, from - s.c0 + t * in.ld_token, s.c0, position, turned[u]);
+                        }
+                    }
+                }
                 loads_done();
 #pragma unroll
-                for (int u = 0; u < KV_ROWS; ++u) {
-                    if (t0 + u * sh.lanes < hi_row) encode(x[u], t0 + u * sh.lanes);
+                for (int u = 0; u < ROWS; ++u) {
+                    if (t0 + u * sh.lanes < hi_row) encode(x[u], t0 + u * sh.lanes, u);
                     __builtin_amdgcn_sched_barrier(0);       // one row after the other: four at once do not fit the registers
                 }
             }
@@ -424,14 +628,10 @@ hipError_t launch_kv_constants(const QuantParams &q, int heads, int dim, int dpa
     return hipGetLastError();
 }
 
-hipError_t launch_kv_write(const KvView &kv, const KvRows &k, const KvRows &v, const KvPlaces &pl, hipStream_t st)
+// A kernel of the type's, the storage's and the constants' own.
+template <typename LAUNCH>
+static hipError_t launch_write(const KvView &kv, int type, LAUNCH launch_as)
 {
-    if (pl.n <= 0 || pl.nseq <= 0) return hipSuccess;
-    const Share s = share_of(kv, pl, true);
-    const unsigned blocks = (unsigned)(2 * ceil_div(pl.n, (int64_t)s.rows) * s.groups);
-    auto launch_as = [&](auto type, auto packed, auto clamps) {
-        kv_write_kernel<decltype(type)::value, decltype(packed)::value, decltype(clamps)::value><<<blocks, KV_THREADS, 0, st>>>(kv, k, v, pl, s);
-    };
     auto launch = [&](auto type) {
         const bool clamps = kv.key.clamps && kv.value.clamps;
         if (kv.packed && clamps) launch_as(type, std::true_type(), std::true_type());
@@ -439,10 +639,46 @@ hipError_t launch_kv_write(const KvView &kv, const KvRows &k, const KvRows &v, c
         else if (clamps) launch_as(type, std::false_type(), std::true_type());
         else launch_as(type, std::false_type(), std::false_type());
     };
-    if (k.type == LPQ_TYPE_F32) launch(std::integral_constant<int, LPQ_TYPE_F32>());
-    else if (k.type == LPQ_TYPE_F16) launch(std::integral_constant<int, LPQ_TYPE_F16>());
+    if (type == LPQ_TYPE_F32) launch(std::integral_constant<int, LPQ_TYPE_F32>());
+    else if (type == LPQ_TYPE_F16) launch(std::integral_constant<int, LPQ_TYPE_F16>());
     else launch(std::integral_constant<int, LPQ_TYPE_BF16>());
     return hipGetLastError();
+}
+
+hipError_t launch_kv_write(const KvView &kv, const KvRows &k, const KvRows &v, const KvPlaces &pl, hipStream_t st)
+{
+    if (pl.n <= 0 || pl.nseq <= 0) return hipSuccess;
+    const Share s = share_of(kv, pl, true);
+    const unsigned blocks = (unsigned)(2 * ceil_div(pl.n, (int64_t)s.rows) * s.groups);
+    return launch_write(kv, k.type, [&](auto type, auto packed, auto clamps) {
+        kv_write_kernel<decltype(type)::value, decltype(packed)::value, decltype(clamps)::value><<<blocks, KV_THREADS, 0, st>>>(kv, k, v, pl, s);
+    });
+}
+
+hipError_t launch_kv_write_rotated(const KvView &kv, const KvRows &k, const KvRows &v, const KvPlaces &pl, const KvAngles &a, hipStream_t st)
+{
+    if (pl.n <= 0 || pl.nseq <= 0) return hipSuccess;
+    const Share s = share_of(kv, pl, true);
+    const unsigned writers = (unsigned)(2 * ceil_div(pl.n, (int64_t)s.rows) * s.groups);
+    unsigned blocks = writers;
+    int rows = 1, units = 1;
+    if (a.q.p) {
+        units = a.neighbours ? (kv.dim + 7) / 8 : (a.half + 7) / 8 + (kv.dim - 2 * a.half + 7) / 8;
+        const int64_t per_row = ceil_div(a.q_heads, (int)TURN_HEADS) * (int64_t)units;          // below 2^20 (a.q_heads <= 65536)
+        int64_t share = std::max(ceil_div((int64_t)KV_THREADS, per_row), ceil_div(pl.n, (int64_t)KV_TURNERS));
+        if (!pl.starts) share = std::max<int64_t>(1, std::min(share, ceil_div(pl.n, (int64_t)256)));
+        rows = (int)std::min<int64_t>(share, (int64_t(1) << 30) / per_row);
+        blocks += (unsigned)ceil_div(pl.n, (int64_t)rows);
+    }
+    return launch_write(kv, k.type, [&](auto type, auto packed, auto clamps) {
+        auto launch = [&](auto neighbours) {
+            typedef Turn<decltype(neighbours)::value> T;
+            kv_write_kernel<decltype(type)::value, decltype(packed)::value, decltype(clamps)::value, T>
+                <<<blocks, KV_THREADS, 0, st>>>(kv, k, v, pl, s, T{a, writers, rows, units});
+        };
+        if (a.neighbours) launch(std::true_type());
+        else launch(std::false_type());
+    });
 }
 
 hipError_t launch_kv_read(const KvView &kv, const KvRows &k, const KvRows &v, const KvPlaces &pl, hipStream_t st)

@@ -45,6 +45,18 @@ struct KvPlaces {
     int nseq, table_pages;
 };
 
+// Angles that rows are turned by: row p of cos and sin [count][half] for a row at position p.  The pairs of features are (i, i + half), or
+// (2 i, 2 i + 1).  Queries of the same numbering as the rows are turned by the same angles.
+struct KvAngles {
+    const float *cos, *sin;
+    int64_t ld, count;
+    const int32_t *positions;        // null: a row's position in the cache; else [n]
+    int half;
+    bool neighbours;
+    KvRows q, out;                   // null: no queries
+    int q_heads;
+};
+
 struct KvQueries {
     const void *p;
     int64_t ld_seq, ld_token, ld_head;
@@ -54,6 +66,7 @@ struct KvQueries {
 // *not_all becomes 1 unless KvConstants::clamps holds for all features.
 hipError_t launch_kv_constants(const QuantParams &q, int heads, int dim, int dpad, bool packed, float *out, int *not_all, hipStream_t st);
 hipError_t launch_kv_write(const KvView &kv, const KvRows &k, const KvRows &v, const KvPlaces &pl, hipStream_t st);
+hipError_t launch_kv_write_rotated(const KvView &kv, const KvRows &k, const KvRows &v, const KvPlaces &pl, const KvAngles &angles, hipStream_t st);
 hipError_t launch_kv_read(const KvView &kv, const KvRows &k, const KvRows &v, const KvPlaces &pl, hipStream_t st);
 
 struct KvSelect {

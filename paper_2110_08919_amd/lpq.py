@@ -83,6 +83,8 @@ def lib() -> C.CDLL:
             "lpq_kv_create": (i32, [C.POINTER(vp), vp, vp, i32, i32, i64, i32, vp, vp, vp]),
             "lpq_kv_destroy": (None, [vp]),
             "lpq_kv_write": (i32, [vp, vp, i64, i64, vp, i64, i64, i32, i64, i64, vp, vp, vp, i64, i64, vp]),
+            "lpq_kv_write_rotated": (i32, [vp, vp, i64, i64, vp, i64, i64, i32, i64, i64, vp, vp, vp, i64, i64, vp, vp, i64, i64, i32, i32, vp,
+                                           vp, i64, i64, i32, vp, i64, i64, vp]),
             "lpq_kv_read": (i32, [vp, vp, i64, i64, vp, i64, i64, i32, i64, i64, vp, vp, vp, i64, i64, vp]),
             "lpq_kv_select_workspace_bytes": (C.c_size_t, [vp, i64, i64]),
             "lpq_kv_select": (i32, [vp, vp, i64, i64, i64, i32, i64, i32, i32, vp, vp, i64, i64, i32, i32, i32, vp, vp,
@@ -421,6 +423,44 @@ class KVCache:
         assert n == same, "as many values as keys"
         _check(_lib.lpq_kv_write(self._h, *keys, *values, _TYPE[k.dtype], n, nseq, _dev_ints(first, nseq),
                                  None if starts is None else _dev_ints(starts, nseq + 1), *tab, _stream_of(table)))
+
+    def write_rotated(self, k: torch.Tensor, v: torch.Tensor, first: torch.Tensor, table: torch.Tensor, cos: torch.Tensor, sin: torch.Tensor,
+                      starts: torch.Tensor = None, positions: torch.Tensor = None, q: torch.Tensor = None, out: torch.Tensor = None,
+                      interleaved: bool = False):
+        """write() of keys that are turned by their positions' angles on the way, and the queries q [n, query heads, features] of
+        the same rows turned with them (returned; out=q: in place).  cos, sin: float32 [positions, turned features / 2]; features are
+        paired with those half the turned ones further, interleaved: with their neighbours.  positions: int32 [n], where a row
+        stands if not at the position it is written to."""
+        nseq, tab = self._table(table)
+        n, keys = self._rows(k, k.dtype)
+        same, values = self._rows(v, k.dtype)
+        assert n == same, "as many values as keys"
+        assert cos.is_cuda and cos.dtype is torch.float32 and cos.dim() == 2 and cos.stride(1) == 1, "need device angles float32 [positions, pairs]"
+        count, pairs = cos.shape
+        apart = cos.stride(0) if count > 1 else max(cos.stride(0), pairs)
+        assert sin.is_cuda and sin.dtype is torch.float32 and sin.shape == cos.shape and sin.stride(1) == 1 and (count == 1 or sin.stride(0) == apart), \
+            "need sines laid out as the cosines"
+        queries, q_heads = (None, 0, 0), 0
+        into = (None, 0, 0)
+        if q is not None:
+            assert not (q.requires_grad and torch.is_grad_enabled()), "rotated queries have no gradient here: use torch.no_grad() or q.detach()"
+            if out is None:
+                out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            q_heads, queries = self._query_rows(q, n, k.dtype)
+            more, into = self._query_rows(out, n, k.dtype)
+            assert more == q_heads, "as many heads in the output"
+        _check(_lib.lpq_kv_write_rotated(self._h, *keys, *values, _TYPE[k.dtype], n, nseq, _dev_ints(first, nseq),
+                                         None if starts is None else _dev_ints(starts, nseq + 1), *tab, cos.data_ptr(), sin.data_ptr(), apart, count,
+                                         2 * pairs, interleaved, None if positions is None else _dev_ints(positions, n), *queries, q_heads, *into,
+                                         _stream_of(table)))
+        return out
+
+    def _query_rows(self, t: torch.Tensor, n: int, dtype):
+        assert t.is_cuda and t.dtype is dtype and t.dim() == 3, f"need device queries of {dtype}"
+        rows, heads, dim = t.shape
+        by_row, by_head, inner = t.stride()
+        assert rows == n and dim == self.dim and (inner == 1 or dim == 1), f"need queries [{n}, query heads, {self.dim}], features side by side"
+        return heads, (t.data_ptr(), by_row, by_head)
 
     def read(self, first: torch.Tensor, table: torch.Tensor, starts: torch.Tensor = None, rows: int = None,
              dtype=torch.float32, out=None):
