@@ -95,6 +95,12 @@ def lib() -> C.CDLL:
             "lpq_kv_attend_masked_workspace_bytes": (C.c_size_t, [vp, i64, i32, i32, i64, i32, i64, i32, i32]),
             "lpq_kv_attend_masked": (i32, [vp, vp, i64, i64, i64, i32, i64, i32, i32, f32, vp, vp, i64, i64, vp, i32, i64, i32, vp, i64, i64,
                                            vp, i64, i64, i64, vp, vp, C.c_size_t, vp]),
+            "lpq_row_codes_stride": (i64, [i32]),
+            "lpq_encode_rows": (i32, [vp, i64, i32, i64, i32, vp, i64, vp, vp]),
+            "lpq_matmul_i8_workspace_bytes": (C.c_size_t, [i64, i64, i32]),
+            "lpq_matmul_i8": (i32, [vp, i64, vp, i64, vp, i64, vp, i64, i32, vp, vp, i64, i32, vp, C.c_size_t, vp]),
+            "lpq_linear8_workspace_bytes": (C.c_size_t, [i64, i64, i32]),
+            "lpq_linear8": (i32, [vp, i64, i32, i64, vp, i64, vp, i64, i32, vp, vp, i64, vp, C.c_size_t, vp]),
             "lpq_last_error": (C.c_char_p, []),
         }
         for name, (res, args) in sig.items():
@@ -560,6 +566,113 @@ class KVCache:
                                          _dev_ints(lengths, nseq), *tab, _ptr(pages), n_select, width, sinks, mask, by_seq, by_token, *outputs,
                                          _ptr(lse), ws, size, _stream_of(q)))
         return out if lse is None else (out, lse)
+
+
+def _typed_matrix(t: torch.Tensor, what: str):
+    assert t.is_cuda and t.dtype in _TYPE and t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] == 1), \
+        f"need {what} of float32, float16 or bfloat16 on the device, a row's values side by side"
+    n, d = t.shape
+    return n, d, t.stride(0) if n > 1 else max(t.stride(0), d)
+
+
+class RowCodes:
+    """Rows [n, d] as 8-bit codes with a scale each: what encode_rows() makes and matmul_i8() takes.  `codes` int8 [n, stride] (features d on are
+    0) and `scales` float32 [n]; a row reads back as codes * scale."""
+
+    def __init__(self, codes: torch.Tensor, scales: torch.Tensor, d: int):
+        assert codes.is_cuda and codes.dtype is torch.int8 and codes.dim() == 2 and codes.stride(1) == 1, "need rows of device codes"
+        assert scales.is_cuda and scales.dtype is torch.float32 and scales.is_contiguous() and scales.shape == codes.shape[:1] \
+            and scales.device == codes.device, "need a float32 scale for each row, on the codes' device"
+        assert 1 <= d <= codes.shape[1] and codes.shape[1] >= lib().lpq_row_codes_stride(d) > 0, "rows are as long as their stride"
+        self.codes, self.scales, self.d = codes, scales, d
+
+    @property
+    def n(self) -> int:
+        return self.codes.shape[0]
+
+    def float(self) -> torch.Tensor:
+        """The rows as they read back, float32 [n, d]."""
+        return self.codes[:, :self.d].float() * self.scales[:, None]
+
+    def _args(self):
+        return self.codes.data_ptr(), max(self.codes.stride(0), self.codes.shape[1]), self.scales.data_ptr()
+
+
+def encode_rows(x: torch.Tensor) -> RowCodes:
+    """lpq_encode_rows of x [n, d] (float32, float16 or bfloat16): each row's largest magnitude becomes 127.  There is no way back through
+    the codes: rows that require a gradient are refused."""
+    assert not (x.requires_grad and torch.is_grad_enabled()), "codes have no gradient: use torch.no_grad() or x.detach()"
+    n, d, ld = _typed_matrix(x, "rows")
+    stride = lib().lpq_row_codes_stride(d)
+    assert stride > 0, f"rows of 1 to 131072 values, not {d}"
+    with torch.cuda.device(x.device):
+        out = RowCodes(torch.empty((n, stride), dtype=torch.int8, device=x.device), torch.empty(n, dtype=torch.float32, device=x.device), d)
+        _check(lib().lpq_encode_rows(x.data_ptr(), ld, _TYPE[x.dtype], n, d, out.codes.data_ptr(), stride, out.scales.data_ptr(), _stream_of(x)))
+    return out
+
+
+def _bias(bias: torch.Tensor, n: int, device):
+    if bias is None:
+        return None
+    assert bias.shape == (n,) and bias.device == device, f"need a bias [{n}] on the weights' device"
+    return bias.detach().float().contiguous()
+
+
+def matmul_i8(a: RowCodes, b: RowCodes, bias: torch.Tensor = None, dtype=torch.bfloat16, out: torch.Tensor = None) -> torch.Tensor:
+    """[rows of a, rows of b] of `dtype`: the products of all rows of a with all rows of b (and bias, one for each row of b)."""
+    assert a.d == b.d, f"rows of {a.d} and of {b.d} codes"
+    assert a.codes.device == b.codes.device, "both on one device"
+    if out is None:
+        out = torch.empty((a.n, b.n), dtype=dtype, device=a.codes.device)
+    m, n, ldo = _typed_matrix(out, "an output")
+    assert (m, n) == (a.n, b.n) and out.device == a.codes.device, f"need an output [{a.n}, {b.n}] on the codes' device"
+    bias = _bias(bias, n, a.codes.device)
+    pa, lda, sa = a._args()
+    pb, ldb, sb = b._args()
+    with torch.cuda.device(out.device):
+        ws, size = _scratch(lib().lpq_matmul_i8_workspace_bytes(m, n, a.d), out.device)
+        _check(lib().lpq_matmul_i8(pa, lda, sa, m, pb, ldb, sb, n, a.d, _ptr(bias), out.data_ptr(), ldo, _TYPE[out.dtype], _ptr(ws), size, _stream_of(out)))
+    return out
+
+
+def _scratch(need: int, device):
+    return (None, 0) if need == 0 else (torch.empty(need, dtype=torch.uint8, device=device), need)
+
+
+class Linear8:
+    """lpq_linear8: y = x w^T + bias with w [channels, d] kept as 8-bit codes (a scale for each channel) and the rows of x made codes on
+    the way (a scale for each row).  For serving: inputs that require a gradient are refused."""
+
+    def __init__(self, weight: torch.Tensor, bias: torch.Tensor = None):
+        self.weight = encode_rows(weight.detach())
+        self.d, self.channels, self.device = self.weight.d, self.weight.n, weight.device
+        self.bias = _bias(bias, self.channels, self.device)
+        if bias is not None and self.bias.data_ptr() == bias.data_ptr():
+            self.bias = self.bias.clone()                   # the layer's own, as its codes are
+        codes, ld, scales = self.weight._args()
+        self._args = codes, ld, scales, self.channels, self.d, _ptr(self.bias)
+
+    def __call__(self, x: torch.Tensor, out: torch.Tensor = None, workspace: torch.Tensor = None) -> torch.Tensor:
+        """x [..., d] of float32, float16 or bfloat16 -> [..., channels] of its type."""
+        assert not (x.requires_grad and torch.is_grad_enabled()), "codes have no gradient: use torch.no_grad() or x.detach()"
+        assert x.dim() >= 1 and x.shape[-1] == self.d and x.device == self.device, f"need [..., {self.d}] on {self.device}"
+        rows = x if x.dim() == 2 else x.reshape(-1, self.d)
+        m, _, ldx = _typed_matrix(rows, "rows")
+        if out is None:
+            out = torch.empty((*x.shape[:-1], self.channels), dtype=x.dtype, device=x.device)
+            ldo = self.channels
+        else:
+            assert out.shape == (*x.shape[:-1], self.channels) and out.dtype is x.dtype and out.device == x.device, "need an output of x's type and rows"
+            _, _, ldo = _typed_matrix(out if out.dim() == 2 else out.view(-1, self.channels), "an output")
+        if torch.cuda.current_device() != x.get_device():
+            with torch.cuda.device(x.device):
+                return self._run(rows, m, ldx, out, ldo, workspace)
+        return self._run(rows, m, ldx, out, ldo, workspace)
+
+    def _run(self, x, m, ldx, out, ldo, workspace):
+        workspace, ws, size = KVCache._workspace(workspace, _lib.lpq_linear8_workspace_bytes(m, self.channels, self.d), x.device)
+        _check(_lib.lpq_linear8(x.data_ptr(), ldx, _TYPE[x.dtype], m, *self._args, out.data_ptr(), ldo, ws, size, _stream_of(x)))
+        return out
 
 
 def rerank_f32(x: torch.Tensor, q: torch.Tensor, cand_ids: torch.Tensor, k: int, metric="l2sq"):
