@@ -375,31 +375,31 @@ int lpq_kv_attend_masked(const lpq_kv *kv, const void *q_dev, int64_t ldq_seq, i
  * exactly); a row of zeros has the scale 0.  A row that holds an infinity or a NaN has the codes 0 and the scale NaN, and all its
  * products are NaN.
  *
- * lpq_row_codes_stride: bytes that a row of d codes takes, d rounded up to a multiple of 128 (0: d out of range).
- * lpq_encode_rows: x_dev [n][d] of `type`, rows ldx elements apart, to codes_dev [n], rows ld_codes >= that stride apart; the bytes from d up to
- * the stride are set to 0, those behind it are not touched.  scales_dev float [n].
+ * Codes are kept in blocks of 16 rows x 64 features, the shape in which the matrix instructions take them: row i, feature k is byte
+ * ((i / 16) B + k / 64) 1024 + (k % 64 / 16) 256 + (i % 16) 16 + k % 16, with B = 2 ceil(d / 128) blocks to a row.
+ * lpq_row_codes_bytes: what n rows take, the last block's rows behind n included (0: out of range).
+ * lpq_encode_rows: x_dev [n][d] of `type`, rows ldx elements apart, to codes and scales_dev float [n].  Features from d to the end of the last
+ * block are set to 0; rows of it behind n are not touched.
  * lpq_matmul_i8: out[i][c] = (sum_k a[i][k] b[c][k]) * a_scale[i] * b_scale[c] + bias[c] for m rows and n channels, with exact sums, the
  * products with the scales (in this order) and the sum with the bias each rounded to binary32, the result to `type`; no scale makes a
  * product leave binary32's range on the way.  bias_dev float [n] or null; rows of the output ldo elements apart.  Codes are -127 .. 127 as
- * lpq_encode_rows leaves them: bytes between d and the stride are read and must be 0 in a or in b.  One set of codes can go
- * through several products.
+ * lpq_encode_rows leaves them: features behind d are read and must be 0 in a or in b; what rows behind m or n hold does not matter.  One set of
+ * codes can go through several products.
  * lpq_linear8: both for rows x_dev [m][d] of `type`, which the output has too.  Rows x_dev may overlap (ldx 0: one row n times).  A row's results do not depend on the rows beside it.
- * Codes: start and stride 16-byte aligned.  Workspace: 256-byte aligned, for the one call (null where 0 bytes are needed); one that
+ * Codes: 256-byte aligned.  Workspace: 256-byte aligned, for the one call (null where 0 bytes are needed); one that
  * was captured into a graph belongs to the graph.  Output and workspace must not overlap the inputs.
- * LPQ_EINVAL: null argument, negative size, unknown type, strides below 0, beyond 2^40 elements or with which codes or
+ * LPQ_EINVAL: null argument, negative size, unknown type, strides below 0, beyond 2^40 elements or with which
  * outputs overlap, misaligned codes or workspace;
- * LPQ_ERANGE: d > 131072 (its sums would not fit 32 bits), m or n >= 2^31, codes more than 2^20 bytes apart, more than 2^22 tiles of 128 rows x 128
+ * LPQ_ERANGE: d > 131072 (its sums would not fit 32 bits), m or n >= 2^31, more than 2^22 tiles of 128 rows x 128
  * channels, too small a workspace. */
-int64_t lpq_row_codes_stride(int d);
-int lpq_encode_rows(const void *x_dev, int64_t ldx, int type, int64_t n, int d, int8_t *codes_dev, int64_t ld_codes, float *scales_dev,
-                    void *stream);
+size_t lpq_row_codes_bytes(int64_t n, int d);
+int lpq_encode_rows(const void *x_dev, int64_t ldx, int type, int64_t n, int d, int8_t *codes_dev, float *scales_dev, void *stream);
 size_t lpq_matmul_i8_workspace_bytes(int64_t m, int64_t n, int d);
-int lpq_matmul_i8(const int8_t *a_dev, int64_t lda, const float *a_scales_dev, int64_t m, const int8_t *b_dev, int64_t ldb,
-                  const float *b_scales_dev, int64_t n, int d, const float *bias_dev, void *out_dev, int64_t ldo, int type,
-                  void *workspace_dev, size_t workspace_bytes, void *stream);
+int lpq_matmul_i8(const int8_t *a_dev, const float *a_scales_dev, int64_t m, const int8_t *b_dev, const float *b_scales_dev, int64_t n, int d,
+                  const float *bias_dev, void *out_dev, int64_t ldo, int type, void *workspace_dev, size_t workspace_bytes, void *stream);
 size_t lpq_linear8_workspace_bytes(int64_t m, int64_t n, int d);
-int lpq_linear8(const void *x_dev, int64_t ldx, int type, int64_t m, const int8_t *codes_dev, int64_t ld_codes, const float *scales_dev,
-                int64_t n, int d, const float *bias_dev, void *out_dev, int64_t ldo, void *workspace_dev, size_t workspace_bytes,
+int lpq_linear8(const void *x_dev, int64_t ldx, int type, int64_t m, const int8_t *codes_dev, const float *scales_dev, int64_t n,
+                int d, const float *bias_dev, void *out_dev, int64_t ldo, void *workspace_dev, size_t workspace_bytes,
                 void *stream);
 
 /* ---------------------------------------------------------------- diagnostics ---- */

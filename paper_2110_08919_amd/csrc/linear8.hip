@@ -4,6 +4,7 @@
 //   y[i][c]    = (sum_k a[i][k] b[c][k]) sa[i] sb[c] + bias[c],      the sums exact in 32 bits
 #include <algorithm>
 #include <type_traits>
+#include <stdlib.h>
 
 #include "kv_internal.h"
 #include "linear8_internal.h"
@@ -15,8 +16,7 @@ namespace lpq {
 namespace {
 
 // ------------------------------------------------------------------ rows to codes ----
-constexpr int ROW_THREADS = 256;
-constexpr int ROW_UNITS = 8;        // units of 8 values that a thread keeps in registers
+constexpr int ROW_THREADS = 1024;
 
 __device__ __forceinline__ uint32_t magnitude8(const float *v)
 {
@@ -55,31 +55,44 @@ __device__ __forceinline__ uint2 row_codes8(const float *v, const RowFactor &f)
     return make_uint2(lo, hi);
 }
 
-// Rows of up to THREADS * UNITS * 8 values are read once, by THREADS threads each, longer ones twice (the second time from a cache).
-template <int type, int THREADS, int UNITS>
-__global__ __launch_bounds__(ROW_THREADS) void encode_rows_kernel(const void *__restrict__ x, int64_t ldx, int64_t n, int d, int units,
-                                                                  int8_t *__restrict__ codes, int64_t ld, float *__restrict__ scales)
+// Codes lie in blocks of 16 rows x 64 features, 1 KB each: [row / 16][feature / 64][feature % 64 / 16][row % 16][feature % 16].  A block is what a
+// wave's matrix instruction takes, 16 bytes a lane, so that every load of codes is one run of memory.
+__host__ __device__ __forceinline__ int64_t block_of(int64_t row16, int64_t feature64, int blocks) { return (row16 * blocks + feature64) << 10; }
+
+// A workgroup has ROWS rows at a time, THREADS threads each.  Rows of up to THREADS * UNITS * 16 values are read once, longer ones twice (the second
+// time from a cache).  Bound by memory; ROWS is large where there are many rows, so that what neighbours write makes whole lines.
+template <int type, int ROWS, int UNITS>
+__global__ __launch_bounds__(ROW_THREADS) void encode_rows_kernel(const void *__restrict__ x, int64_t ldx, int64_t n, int d, int blocks,
+                                                                  int8_t *__restrict__ codes, float *__restrict__ scales)
 {
-    constexpr int ROWS = ROW_THREADS / THREADS;
-    const int t = threadIdx.x % THREADS;
-    const int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / THREADS;
-    if (ROWS > 1 && row >= n) return;
-    const int64_t at = row * ldx;
-    Raw8 raw[UNITS];
+    constexpr int THREADS = ROW_THREADS / ROWS;
+    const int t = threadIdx.x % THREADS, mine = threadIdx.x / THREADS;
+    const int64_t row = (int64_t)blockIdx.x * ROWS + mine, from = row < n ? row : n - 1;
+    const int64_t at = from * ldx;
+    const int units = 4 * blocks;
+    Raw8 raw[UNITS][2];
     float v[8];
-    uint32_t most = 0;
+    uint32_t most = 0, c[4];
+    const auto load = [&](int u, Raw8 *r) {
+        r[0] = kv_load8(x, type, at + 16 * u, d - 16 * u);
+        r[1] = kv_load8(x, type, at + 16 * u + 8, d - 16 * u - 8);
+    };
+    const auto look = [&](int u, const Raw8 *r) {
 #pragma unroll
-    for (int i = 0; i < UNITS; ++i) raw[i] = kv_load8(x, type, at + 8 * (t + i * THREADS), d - 8 * (t + i * THREADS));
+        for (int h = 0; h < 2; ++h) {
+            kv_floats8(r[h], type, d - 16 * u - 8 * h, v);
+            const uint32_t b = magnitude8(v);
+            most = b > most ? b : most;
+        }
+    };
 #pragma unroll
-    for (int i = 0; i < UNITS; ++i) {
-        kv_floats8(raw[i], type, d - 8 * (t + i * THREADS), v);
-        const uint32_t b = magnitude8(v);
-        most = b > most ? b : most;
-    }
+    for (int i = 0; i < UNITS; ++i) load(t + i * THREADS, raw[i]);
+#pragma unroll
+    for (int i = 0; i < UNITS; ++i) look(t + i * THREADS, raw[i]);
     for (int u = t + UNITS * THREADS; u < units; u += THREADS) {
-        kv_floats8(kv_load8(x, type, at + 8 * u, d - 8 * u), type, d - 8 * u, v);
-        const uint32_t b = magnitude8(v);
-        most = b > most ? b : most;
+        Raw8 r[2];
+        load(u, r);
+        look(u, r);
     }
     most = (uint32_t)wave_max_i32((int)most);
     if (THREADS > 64) {
@@ -87,21 +100,32 @@ __global__ __launch_bounds__(ROW_THREADS) void encode_rows_kernel(const void *__
         if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = most;
         __syncthreads();
 #pragma unroll
-        for (int w = 0; w < THREADS / 64; ++w) most = waves[w] > most ? waves[w] : most;
+        for (int w = 0; w < THREADS / 64; ++w) {
+            const uint32_t o = waves[mine * (THREADS / 64) + w];
+            most = o > most ? o : most;
+        }
     }
+    if (row >= n) return;
     const RowFactor f = row_factor(most);
     if (t == 0) scales[row] = f.scale;
-    int8_t *const out = codes + row * ld;
+    int8_t *const out = codes + block_of(row >> 4, 0, blocks) + 16 * (row & 15);
+    const auto store = [&](int u, const Raw8 *r) {
 #pragma unroll
-    for (int i = 0; i < UNITS; ++i) {
-        const int u = t + i * THREADS;
-        if (u >= units) break;
-        kv_floats8(raw[i], type, d - 8 * u, v);
-        *reinterpret_cast<uint2 *>(out + 8 * u) = row_codes8(v, f);
-    }
+        for (int h = 0; h < 2; ++h) {
+            kv_floats8(r[h], type, d - 16 * u - 8 * h, v);
+            const uint2 w = row_codes8(v, f);
+            c[2 * h] = w.x;
+            c[2 * h + 1] = w.y;
+        }
+        *reinterpret_cast<uint4 *>(out + 256 * (int64_t)u) = make_uint4(c[0], c[1], c[2], c[3]);
+    };
+#pragma unroll
+    for (int i = 0; i < UNITS; ++i)
+        if (t + i * THREADS < units) store(t + i * THREADS, raw[i]);
     for (int u = t + UNITS * THREADS; u < units; u += THREADS) {
-        kv_floats8(kv_load8(x, type, at + 8 * u, d - 8 * u), type, d - 8 * u, v);
-        *reinterpret_cast<uint2 *>(out + 8 * u) = row_codes8(v, f);
+        Raw8 r[2];
+        load(u, r);
+        store(u, r);
     }
 }
 
@@ -115,51 +139,251 @@ struct Scale {
 __device__ __forceinline__ Scale split_scale(float s) { return {__builtin_amdgcn_frexp_mantf(s), __builtin_amdgcn_frexp_expf(s)}; }
 __device__ __forceinline__ float scaled(int sum, const Scale &a, const Scale &b) { return ldexpf(((float)sum * a.m) * b.m, a.e + b.e); }
 
+// Few rows.  Bound by reading the weights, which go from memory to registers, each byte to one wave: a workgroup's eight waves share CT tiles
+// of 16 channels and take every eighth run of 128 features of them (v_mfma_i32_16x16x64_i8, channels as rows of the result), and the
+// eight sums come together through LDS.  The tokens' codes, MT tiles of 16, come from the cache of their chiplet with each run.  FUSED (few rows):
+// the workgroup makes the codes itself, in LDS, while its first weights are under way: one launch, and no round trip through memory.
+// A barrier for what the waves write to and read from LDS; loads from memory stay under way.
+__device__ __forceinline__ void lds_barrier()
+{
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0xC07F);      // lgkmcnt(0); known to the compiler, which then counts only what comes after
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+constexpr int STREAM_WAVES = 8, STREAM_THREADS = 64 * STREAM_WAVES, STREAM_K = 128;
+constexpr int FUSED_VALUES = 16384;           // values of x that a workgroup makes codes of: 32 a thread
+constexpr int FUSED_ROWS = 8, FUSED_PAD = 16;
+constexpr int STREAM_ROWS = 128;
+
+struct StreamWork {
+    const int8_t *x, *w;
+    const float *sx, *sw;
+    int m;
+    int64_t n;
+    int runs;                    // of STREAM_K features
+    Linear8Out out;
+    const void *raw;             // FUSED: rows of `out.type`
+    int64_t ld_raw;
+    int d, rows;                 // FUSED: m rounded up to a power of two
+};
+
+// Loads past the end of a buffer give zeros and ask for nothing, so that the loop's loads need no branches: behind a branch the compiler
+// would wait for all that is under way at every use.
+typedef __amdgpu_buffer_rsrc_t Buffer;
+__device__ __forceinline__ Buffer codes_buffer(const int8_t *p, int64_t bytes)
+{
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<int8_t *>(p), 0, (int)bytes, 0x00020000);
+}
+__device__ __forceinline__ v4i load16(Buffer b, int at) { return __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(b, at, 0, 0)); }
+
+constexpr int stream_waves_per_simd(int mt, int ct, bool wide) { return mt + ct <= 5 && !wide ? 4 : 2; }
+constexpr int stream_depth(int mt, int ct) { return mt + ct <= 3 ? 4 : 2; }
+
+template <int MT, int CT, bool FUSED, int type>
+__global__ __launch_bounds__(STREAM_THREADS, stream_waves_per_simd(MT, CT, FUSED && type == LPQ_TYPE_F32 && CT > 1)) void linear8_stream_kernel(StreamWork g)
+{
+    static_assert(!FUSED || MT == 1);
+    constexpr int DEPTH = stream_depth(MT, CT), ENDS = (CT * MT + STREAM_WAVES - 1) / STREAM_WAVES;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int in_tile = lane & 15, chunk = 16 * (lane >> 4);
+    const int64_t ch0 = (int64_t)blockIdx.x * 16 * CT;
+    __shared__ __align__(16) int4 sums[STREAM_WAVES * CT * MT * 64];
+    __shared__ __align__(16) int8_t own[FUSED ? FUSED_VALUES + FUSED_ROWS * FUSED_PAD : 16];
+    __shared__ uint32_t magnitude[STREAM_WAVES];
+    __shared__ Scale own_scale[FUSED_ROWS];
+
+    // FUSED: the rows' values first, so that waiting for them is not waiting for the weights
+    constexpr int UNITS = FUSED ? FUSED_VALUES / (8 * STREAM_THREADS) : 1;
+    Raw8 raw[UNITS];
+    const int row_threads = FUSED ? STREAM_THREADS / g.rows : 1, row = FUSED ? (int)threadIdx.x / row_threads : 0;
+    const int me = threadIdx.x - row * row_threads;
+    if (FUSED) {
+        const int from = row < g.m ? row : g.m - 1;
+#pragma unroll
+        for (int i = 0; i < UNITS; ++i) {
+            const int u = 8 * (me + i * row_threads);
+            raw[i] = kv_load8(g.raw, type, from * g.ld_raw + u, g.d - u);
+        }
+    }
+
+    const int bytes = g.runs * STREAM_K, tile_bytes = 16 * bytes;
+    const int64_t tiles = (g.n - ch0 + 15) >> 4;
+    const Buffer wb = codes_buffer(g.w + (ch0 >> 4) * tile_bytes, (tiles < CT ? tiles : CT) * tile_bytes);
+    const Buffer xb = FUSED ? wb : codes_buffer(g.x, (int64_t)((g.m + 15) >> 4) * tile_bytes);
+    const int own_at = FUSED ? (in_tile < g.m ? in_tile : g.m - 1) * (bytes + FUSED_PAD) + chunk : 0;
+    v4i fw[DEPTH][CT][2], fx[DEPTH][MT][2];
+    const auto load = [&](int slot, int run) {
+        const int at = (run < g.runs ? run * (16 * STREAM_K) : 1 << 30) + 16 * lane;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            if (!FUSED) {
+#pragma unroll
+                for (int j = 0; j < MT; ++j) fx[slot][j][k] = load16(xb, at + j * tile_bytes + 1024 * k);
+            }
+#pragma unroll
+            for (int i = 0; i < CT; ++i) fw[slot][i][k] = load16(wb, at + i * tile_bytes + 1024 * k);
+        }
+    };
+#pragma unroll
+    for (int i = 0; i < DEPTH; ++i) load(i, wave + i * STREAM_WAVES);
+
+    // what the results are multiplied by, long before it is needed
+    float end_w[4], end_bias[4], end_x;
+    const float *const bias = g.out.bias ? g.out.bias : g.sw;
+    const auto ends = [&](int u) {
+        const int token = 16 * (u % MT) + in_tile;
+        end_x = FUSED ? 0.0f : g.sx[token < g.m ? token : 0];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int64_t c = ch0 + 16 * (u / MT) + 4 * (lane >> 4) + e, at = c < g.n ? c : g.n - 1;
+            end_w[e] = g.sw[at];
+            end_bias[e] = bias[at];
+        }
+    };
+    ends(wave < CT * MT ? wave : 0);
+
+    if (FUSED) {
+        uint32_t most = 0;
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < UNITS; ++i) {
+            kv_floats8(raw[i], type, g.d - 8 * (me + i * row_threads), v);
+            const uint32_t b = magnitude8(v);
+            most = b > most ? b : most;
+        }
+        most = (uint32_t)wave_max_i32((int)most);
+        if (lane == 0) magnitude[wave] = most;
+        lds_barrier();
+        const int waves = STREAM_WAVES / g.rows, first = wave / waves * waves;
+        for (int i = 0; i < waves; ++i) most = magnitude[first + i] > most ? magnitude[first + i] : most;
+        const RowFactor f = row_factor(most);
+        if (me == 0) own_scale[row] = split_scale(f.scale);
+        int8_t *const to = own + row * (bytes + FUSED_PAD);
+#pragma unroll
+        for (int i = 0; i < UNITS; ++i) {
+            const int u = 8 * (me + i * row_threads);
+            if (u < bytes) {
+                kv_floats8(raw[i], type, g.d - u, v);
+                *reinterpret_cast<uint2 *>(to + u) = row_codes8(v, f);
+            }
+        }
+        lds_barrier();
+    }
+
+    v4i acc[CT][MT];
+#pragma unroll
+    for (int i = 0; i < CT; ++i)
+#pragma unroll
+        for (int j = 0; j < MT; ++j) acc[i][j] = v4i{0, 0, 0, 0};
+    for (int run0 = wave; run0 < g.runs; run0 += DEPTH * STREAM_WAVES) {
+#pragma unroll
+        for (int s = 0; s < DEPTH; ++s) {
+            const int run = run0 + s * STREAM_WAVES;
+            if (FUSED) {                   // past the end: any codes, times weights of zero
+                const int at = run < g.runs ? run * STREAM_K : 0;
+#pragma unroll
+                for (int k = 0; k < 2; ++k) fx[s][0][k] = *reinterpret_cast<const v4i *>(own + own_at + at + 64 * k);
+            }
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+                for (int i = 0; i < CT; ++i)
+#pragma unroll
+                    for (int j = 0; j < MT; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fw[s][i][k], fx[s][j][k], acc[i][j], 0, 0, 0);
+            load(s, run + DEPTH * STREAM_WAVES);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < CT; ++i)
+#pragma unroll
+        for (int j = 0; j < MT; ++j)
+            sums[(wave * CT * MT + i * MT + j) * 64 + lane] = make_int4(acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]);
+    lds_barrier();
+#pragma unroll
+    for (int i = 0; i < ENDS; ++i) {
+        const int u = wave + i * STREAM_WAVES, token = 16 * (u % MT) + in_tile;
+        if (u >= CT * MT) break;
+        int t[4] = {0, 0, 0, 0};
+#pragma unroll
+        for (int v = 0; v < STREAM_WAVES; ++v) {
+            const int4 o = sums[(v * CT * MT + u) * 64 + lane];
+            t[0] += o.x; t[1] += o.y; t[2] += o.z; t[3] += o.w;
+        }
+        const int64_t c = ch0 + 16 * (u / MT) + 4 * (lane >> 4);
+        if (token >= g.m || c >= g.n) continue;
+        if (i > 0) ends(u);
+        const Scale a = FUSED ? own_scale[token] : split_scale(end_x);
+        float y[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            y[e] = scaled(t[e], a, split_scale(end_w[e]));
+            if (g.out.bias) y[e] += end_bias[e];
+        }
+        kv_store<4>(g.out.p, FUSED ? type : g.out.type, token * g.out.ld + c, (int)(g.n - c < 4 ? g.n - c : 4), y);
+    }
+}
+
 // Tiles.  The workgroup's four waves stand 2 x 2; a wave has TC x TT tiles of 32 channels x 32 tokens (v_mfma_i32_32x32x32_i8, channels as rows of
 // the result, so that a lane holds 4 neighbouring channels of a token).  Stages of 64 features of all the workgroup's channels and tokens come
-// into a ring in LDS by asynchronous copies of 16 bytes a lane.
+// into a ring in LDS by asynchronous copies of 16 bytes a lane, a block at a time, three stages ahead; the operands of the next half of a
+// stage are read from there while the matrix instructions of this half run.
 constexpr int TILE_THREADS = 256, TILE_K = 64, TILE_STAGES = 4;
 
 struct TileWork {
     const int8_t *x, *w;
     const float *sx, *sw;
-    int64_t ldx, ldw, m, n;
-    int stages;                  // of TILE_K features
-    int per_part;                // stages of a part
+    int64_t m, n;
+    int blocks;                  // of 64 features in a row: a stage each
+    int stages, per_part;        // of them with features, of a part
     int tiles_m, tiles_n, parts;
     Linear8Out out;
     int *sums;                   // parts > 1: [parts][m][n rounded up to 4]
 };
 
+// Copies of one wave: every fourth block of a stage, channels first, then tokens.
 template <int TT, int TC>
-__device__ __forceinline__ void tile_copy(const TileWork &g, int64_t row0, int64_t ch0, int stage, char *ring, int wave, int lane)
-{
-    constexpr int BM = 64 * TT, BN = 64 * TC, RUNS = (BM + BN) / 16;      // runs of 16 rows, 1 KB
-    const unsigned base = lds_offset(ring) + (stage % TILE_STAGES) * (BM + BN) * TILE_K;
+struct TileCopies {
+    static constexpr int BM = 64 * TT, BN = 64 * TC, COUNT = (BM + BN) / 64;
+    const int8_t *from[COUNT];
+    unsigned to;
+    __device__ __forceinline__ void setup(const TileWork &g, int64_t row0, int64_t ch0, int stage, const char *ring, int wave, int lane)
+    {
+        to = lds_offset(ring) + 1024 * wave;
 #pragma unroll
-    for (int i = 0; i < RUNS / 4; ++i) {
-        const int run = wave + 4 * i, r = 16 * run + (lane >> 2), slot = lane & 3;      // channels first, then tokens
-        const bool channel = r < BN;
-        const int in = channel ? r : r - BN;
-        const int chunk = slot ^ swz<4>(in);
-        int64_t row = (channel ? ch0 : row0) + in;
-        const int64_t last = (channel ? g.n : g.m) - 1;
-        row = row < last ? row : last;
-        async_copy16((channel ? g.w + row * g.ldw : g.x + row * g.ldx) + (int64_t)stage * TILE_K + 16 * chunk, base + 1024 * run);
+        for (int i = 0; i < COUNT; ++i) {
+            const int block = wave + 4 * i;
+            const bool channel = block < BN / 16;
+            const int64_t last = ((channel ? g.n : g.m) - 1) >> 4;
+            int64_t row16 = channel ? (ch0 >> 4) + block : (row0 >> 4) + block - BN / 16;
+            row16 = row16 < last ? row16 : last;
+            from[i] = (channel ? g.w : g.x) + block_of(row16, stage, g.blocks) + 16 * lane;
+        }
     }
-}
+    __device__ __forceinline__ void next(int slot)
+    {
+#pragma unroll
+        for (int i = 0; i < COUNT; ++i) {
+            async_copy16(from[i], to + slot * (BM + BN) * TILE_K + 4096 * i);
+            from[i] += 1024;
+        }
+    }
+};
 
 template <int TT, int TC, int TYPE, bool PARTS>
 __global__ __launch_bounds__(TILE_THREADS) void linear8_tile_kernel(TileWork g)
 {
-    constexpr int BM = 64 * TT, BN = 64 * TC, STAGE = (BM + BN) * TILE_K, COPIES = (BM + BN) / 64;
+    typedef TileCopies<TT, TC> Copies;
+    constexpr int BM = 64 * TT, BN = 64 * TC, STAGE = (BM + BN) * TILE_K;
     __shared__ __align__(1024) char ring[TILE_STAGES * STAGE];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int part = PARTS ? blockIdx.x / (g.tiles_m * g.tiles_n) : 0, tile = PARTS ? blockIdx.x - part * (g.tiles_m * g.tiles_n) : blockIdx.x;
+    const int tiles = g.tiles_m * g.tiles_n;
+    const int part = PARTS ? blockIdx.x / tiles : 0, tile = PARTS ? blockIdx.x - part * tiles : blockIdx.x;
     const int tm = tile % g.tiles_m, tn = tile / g.tiles_m;
     const int64_t row0 = (int64_t)tm * BM, ch0 = (int64_t)tn * BN;
     const int wt = (wave & 1) * 32 * TT, wc = (wave >> 1) * 32 * TC;
-    const int begin = part * g.per_part, end = PARTS ? min(begin + g.per_part, g.stages) : g.stages;
+    const int begin = part * g.per_part, stages = min(g.per_part, g.stages - begin);
 
     v16i acc[TC][TT];
 #pragma unroll
@@ -169,77 +393,128 @@ __global__ __launch_bounds__(TILE_THREADS) void linear8_tile_kernel(TileWork g)
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[i][j][e] = 0;
 
-    for (int s = begin; s < begin + TILE_STAGES - 1 && s < end; ++s) tile_copy<TT, TC>(g, row0, ch0, s, ring, wave, lane);
-    for (int s = begin; s < end; ++s) {
-        const int ahead = min(end - 1 - s, TILE_STAGES - 2);
-        wait_vmcnt(ahead * COPIES);
-        __syncthreads();                         // the stage is there for all, and nobody reads the one before it any more
-        if (s + TILE_STAGES - 1 < end) tile_copy<TT, TC>(g, row0, ch0, s + TILE_STAGES - 1, ring, wave, lane);
-        const char *const here = ring + (s % TILE_STAGES) * STAGE;
+    // what the results are multiplied by, long before it is needed
+    float end_w = 0.0f, end_x = 0.0f, end_bias = 0.0f;
+    if (!PARTS) {
+        const int64_t c = ch0 + threadIdx.x < g.n ? ch0 + threadIdx.x : g.n - 1, t = row0 + threadIdx.x < g.m ? row0 + threadIdx.x : g.m - 1;
+        end_w = g.sw[c];
+        end_x = g.sx[t];
+        if (g.out.bias) end_bias = g.out.bias[c];
+        asm volatile("" : "+v"(end_w), "+v"(end_x), "+v"(end_bias));      // now: the copies below are counted
+    }
+    Copies copies;
+    copies.setup(g, row0, ch0, begin, ring, wave, lane);
+    const int at = (lane >> 5) * 256 + (lane & 15) * 16 + ((lane >> 4) & 1) * 1024;
+    v4i fc[2][TC], ft[2][TT];
+    const auto operands = [&](int slot, int half) {
+        const char *const here = ring + slot * STAGE + 512 * half + at;
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            v4i fc[TC], ft[TT];
-            const int chunk = 2 * k + (lane >> 5);
+        for (int i = 0; i < TC; ++i) fc[half][i] = *reinterpret_cast<const v4i *>(here + 64 * (wc + 32 * i));
 #pragma unroll
-            for (int i = 0; i < TC; ++i) {
-                const int r = wc + 32 * i + (lane & 31);
-                fc[i] = *reinterpret_cast<const v4i *>(here + r * TILE_K + 16 * (chunk ^ swz<4>(r)));
-            }
+        for (int j = 0; j < TT; ++j) ft[half][j] = *reinterpret_cast<const v4i *>(here + 64 * (BN + wt + 32 * j));
+    };
+    const auto multiply = [&](int half) {
+        __builtin_amdgcn_sched_barrier(0);           // the reads that were asked for go ahead of these, not behind
 #pragma unroll
-            for (int j = 0; j < TT; ++j) {
-                const int r = wt + 32 * j + (lane & 31);
-                ft[j] = *reinterpret_cast<const v4i *>(here + BN * TILE_K + r * TILE_K + 16 * (chunk ^ swz<4>(r)));
-            }
+        for (int i = 0; i < TC; ++i)
+#pragma unroll
+            for (int j = 0; j < TT; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fc[half][i], ft[half][j], acc[i][j], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    for (int s = 0; s < TILE_STAGES && s < stages; ++s) copies.next(s);
+    wait_vmcnt(min(stages - 1, TILE_STAGES - 1) * Copies::COUNT);
+    lds_barrier();
+    operands(0, 0);
+    for (int s = 0; s < stages; ++s) {
+        operands(s % TILE_STAGES, 1);
+        multiply(0);
+        // the next stage is there for all, and nobody reads this one any more: its place is filled again
+        if (s + TILE_STAGES <= stages) __builtin_amdgcn_s_waitcnt(vmcnt_imm((TILE_STAGES - 2) * Copies::COUNT));
+        else __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
+        lds_barrier();
+        if (s + TILE_STAGES < stages) copies.next(s % TILE_STAGES);
+        operands((s + 1) % TILE_STAGES, 0);          // (after the last stage: of one gone by, for nothing)
+        multiply(1);
+    }
+
+    if (PARTS) {
+        const int64_t wide = (g.n + 3) & ~int64_t(3);
+#pragma unroll
+        for (int j = 0; j < TT; ++j) {
+            const int64_t token = row0 + wt + 32 * j + (lane & 31);
 #pragma unroll
             for (int i = 0; i < TC; ++i)
 #pragma unroll
-                for (int j = 0; j < TT; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fc[i], ft[j], acc[i][j], 0, 0, 0);
+                for (int q = 0; q < 4; ++q) {
+                    const int64_t c = ch0 + wc + 32 * i + 8 * q + 4 * (lane >> 5);
+                    if (token < g.m && c < g.n)
+                        *reinterpret_cast<int4 *>(g.sums + ((int64_t)part * g.m + token) * wide + c) =
+                            make_int4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
+                }
         }
+        return;
     }
-
+    // The ring's memory turns each wave's tiles over, 32 tokens at a time: in by channels of a token, out in whole lines of a token's row.
+    constexpr int WIDTH = 32 * TC, SIZE = TYPE == LPQ_TYPE_F32 ? 4 : 2, PITCH = WIDTH * SIZE + 16, LANES = WIDTH / 8;
+    static_assert(4 * 32 * PITCH + 8 * (BM + 2 * BN) <= TILE_STAGES * STAGE);
+    char *const own = ring + wave * 32 * PITCH;
+    Scale *const scales_w = reinterpret_cast<Scale *>(ring + 4 * 32 * PITCH), *const scales_x = scales_w + BN;
+    float *const biases = reinterpret_cast<float *>(scales_x + BM);
+    lds_barrier();
+    if (BN == TILE_THREADS || threadIdx.x < BN) {
+        scales_w[threadIdx.x] = split_scale(end_w);
+        biases[threadIdx.x] = end_bias;
+    }
+    if (BM == TILE_THREADS || threadIdx.x < BM) scales_x[threadIdx.x] = split_scale(end_x);
+    lds_barrier();
 #pragma unroll
     for (int j = 0; j < TT; ++j) {
-        const int64_t token = row0 + wt + 32 * j + (lane & 31);
-        if (token >= g.m) continue;
-        Scale a = {0.0f, 0};
-        if (!PARTS) a = split_scale(g.sx[token]);
+        const Scale a = scales_x[wt + 32 * j + (lane & 31)];
 #pragma unroll
         for (int i = 0; i < TC; ++i)
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                const int64_t c = ch0 + wc + 32 * i + 8 * q + 4 * (lane >> 5);
-                const int left = (int)(g.n - c < 4 ? g.n - c : 4);
-                if (left <= 0) continue;
-                if (PARTS) {
-                    const int64_t wide = (g.n + 3) & ~int64_t(3);
-                    *reinterpret_cast<int4 *>(g.sums + ((int64_t)part * g.m + token) * wide + c) =
-                        make_int4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
-                } else {
-                    float y[4];
+                const int c = 32 * i + 8 * q + 4 * (lane >> 5);
+                float y[4];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int64_t ce = c + (e < left ? e : 0);
-                        y[e] = scaled(acc[i][j][4 * q + e], a, split_scale(g.sw[ce]));
-                        if (g.out.bias) y[e] += g.out.bias[ce];
-                    }
-                    kv_store<4>(g.out.p, TYPE, token * g.out.ld + c, left, y);
+                for (int e = 0; e < 4; ++e) {
+                    y[e] = scaled(acc[i][j][4 * q + e], a, scales_w[wc + c + e]);
+                    if (g.out.bias) y[e] += biases[wc + c + e];
                 }
+                kv_store<4>(own, TYPE, (lane & 31) * (PITCH / SIZE) + c, 4, y);
             }
+        wave_lds_sync();
+#pragma unroll
+        for (int r0 = 0; r0 < 32; r0 += 64 / LANES) {
+            const int r = r0 + lane / LANES, c = 8 * (lane % LANES);
+            const int64_t token = row0 + wt + 32 * j + r, channel = ch0 + wc + c;
+            const int left = (int)(g.n - channel < 8 ? g.n - channel : 8);
+            if (token >= g.m || left <= 0) continue;
+            if (TYPE == LPQ_TYPE_F32) {
+                float y[8];
+                __builtin_memcpy(y, own + r * PITCH + c * SIZE, 32);
+                kv_store_pieces<8>(static_cast<float *>(g.out.p) + token * g.out.ld + channel, left, y);
+            } else {
+                uint16_t y[8];
+                __builtin_memcpy(y, own + r * PITCH + c * SIZE, 16);
+                kv_store_pieces<8>(static_cast<uint16_t *>(g.out.p) + token * g.out.ld + channel, left, y);
+            }
+        }
+        wave_lds_sync();
     }
 }
 
 }  // namespace
 
-hipError_t launch_encode_rows(const void *x, int64_t ldx, int type, int64_t n, int d, int8_t *codes, int64_t ld, float *scales, hipStream_t st)
+hipError_t launch_encode_rows(const void *x, int64_t ldx, int type, int64_t n, int d, int8_t *codes, float *scales, hipStream_t st)
 {
     if (n == 0) return hipSuccess;
-    const int units = (int)round_up(d, ROW_CODES_ALIGN) / 8;
+    const int blocks = row_blocks(d);
     const auto go = [&](auto t) {
-        constexpr int T = decltype(t)::value;
-        if (units <= 64) encode_rows_kernel<T, 64, 1><<<dim3((unsigned)ceil_div(n, (int64_t)4)), ROW_THREADS, 0, st>>>(x, ldx, n, d, units, codes, ld, scales);
-        else if (units <= 256) encode_rows_kernel<T, 256, 1><<<dim3((unsigned)n), ROW_THREADS, 0, st>>>(x, ldx, n, d, units, codes, ld, scales);
-        else if (units <= 1024) encode_rows_kernel<T, 256, 4><<<dim3((unsigned)n), ROW_THREADS, 0, st>>>(x, ldx, n, d, units, codes, ld, scales);
-        else encode_rows_kernel<T, 256, ROW_UNITS><<<dim3((unsigned)n), ROW_THREADS, 0, st>>>(x, ldx, n, d, units, codes, ld, scales);
+        constexpr int T = decltype(t)::value, WIDE = T == LPQ_TYPE_F32 ? 2 : 1;
+        if (n >= 4096) encode_rows_kernel<T, 16, 8 / WIDE><<<dim3((unsigned)ceil_div(n, (int64_t)16)), ROW_THREADS, 0, st>>>(x, ldx, n, d, blocks, codes, scales);
+        else if (n >= 1024 || d <= 4096) encode_rows_kernel<T, 4, 4 / WIDE><<<dim3((unsigned)ceil_div(n, (int64_t)4)), ROW_THREADS, 0, st>>>(x, ldx, n, d, blocks, codes, scales);
+        else encode_rows_kernel<T, 1, 2><<<dim3((unsigned)n), ROW_THREADS, 0, st>>>(x, ldx, n, d, blocks, codes, scales);
     };
     if (type == LPQ_TYPE_F32) go(std::integral_constant<int, LPQ_TYPE_F32>());
     else if (type == LPQ_TYPE_F16) go(std::integral_constant<int, LPQ_TYPE_F16>());
@@ -247,17 +522,90 @@ hipError_t launch_encode_rows(const void *x, int64_t ldx, int type, int64_t n, i
     return hipGetLastError();
 }
 
-Linear8Plan linear8_plan(int64_t m, int64_t n, int d) { return {128, 128, 1, 0}; }
+Linear8Plan linear8_plan(int64_t m, int64_t n, int d)
+{
+    if (getenv("LIN_CT") && m <= STREAM_ROWS) { const int tiles = (int)ceil_div(m, (int64_t)16), rows = 16 * (tiles == 5 ? 6 : tiles == 7 ? 8 : tiles);
+        return {rows, 16 * std::min(atoi(getenv("LIN_CT")), rows <= 32 ? 4 : 2), 0, 0}; }
+    if (m <= STREAM_ROWS) {
+        const int tiles = (int)ceil_div(m, (int64_t)16), rows = 16 * (tiles == 5 ? 6 : tiles == 7 ? 8 : tiles);
+        const int64_t groups = ceil_div(n, (int64_t)16);
+        return {rows, rows > 16 && groups >= 512 ? 32 : 16, 0, 0};
+    }
+    if (getenv("LIN_T") ? atoi(getenv("LIN_T")) == 4 : m >= 2048 && n >= 2048) return {256, 256, 1, 0};
+    return {128, 128, 1, 0};
+}
+
+bool linear8_fused(int64_t m, int d) { return m <= FUSED_ROWS && next_pow2((int)m) * 64 * row_blocks(d) <= FUSED_VALUES; }
+
+template <int MT, int CT>
+static void stream(const StreamWork &g, dim3 grid, hipStream_t st)
+{
+    linear8_stream_kernel<MT, CT, false, 0><<<grid, STREAM_THREADS, 0, st>>>(g);
+}
+template <int MT>
+static void stream_channels(const StreamWork &g, int channels, dim3 grid, hipStream_t st)
+{
+    if (channels == 16) stream<MT, 1>(g, grid, st);
+    else if (channels == 32) stream<MT, 2>(g, grid, st);
+    else stream<MT, 4>(g, grid, st);
+}
+
+template <int MT>
+static void stream_two(const StreamWork &g, int channels, dim3 grid, hipStream_t st)
+{
+    if (channels == 16) stream<MT, 1>(g, grid, st);
+    else stream<MT, 2>(g, grid, st);
+}
+
+static hipError_t launch_stream(const StreamWork &g, const Linear8Plan &plan, hipStream_t st)
+{
+    const dim3 grid((unsigned)ceil_div(g.n, (int64_t)plan.channels));
+    switch (plan.rows) {
+    case 16: stream_channels<1>(g, plan.channels, grid, st); break;
+    case 32: stream_channels<2>(g, plan.channels, grid, st); break;
+    case 48: stream_two<3>(g, plan.channels, grid, st); break;
+    case 64: stream_two<4>(g, plan.channels, grid, st); break;
+    case 96: stream_two<6>(g, plan.channels, grid, st); break;
+    default: stream_two<8>(g, plan.channels, grid, st); break;
+    }
+    return hipGetLastError();
+}
+
+template <int TYPE>
+static void fused(const StreamWork &g, int channels, dim3 grid, hipStream_t st)
+{
+    if (channels == 16) linear8_stream_kernel<1, 1, true, TYPE><<<grid, STREAM_THREADS, 0, st>>>(g);
+    else if (channels == 32) linear8_stream_kernel<1, 2, true, TYPE><<<grid, STREAM_THREADS, 0, st>>>(g);
+    else linear8_stream_kernel<1, 4, true, TYPE><<<grid, STREAM_THREADS, 0, st>>>(g);
+}
+
+hipError_t launch_linear8_fused(const void *x, int64_t ldx, int64_t m, const RowCodes &w, int d, const Linear8Out &out, const Linear8Plan &plan,
+                                hipStream_t st)
+{
+    const StreamWork g = {nullptr, w.codes, nullptr, w.scales, (int)m, w.n, row_blocks(d) / 2, out, x, ldx, d, next_pow2((int)m)};
+    const dim3 grid((unsigned)ceil_div(w.n, (int64_t)plan.channels));
+    if (out.type == LPQ_TYPE_F32) fused<LPQ_TYPE_F32>(g, plan.channels, grid, st);
+    else if (out.type == LPQ_TYPE_F16) fused<LPQ_TYPE_F16>(g, plan.channels, grid, st);
+    else fused<LPQ_TYPE_BF16>(g, plan.channels, grid, st);
+    return hipGetLastError();
+}
 
 hipError_t launch_linear8(const RowCodes &x, const RowCodes &w, int d, const Linear8Out &out, const Linear8Plan &plan, void *workspace, hipStream_t st)
 {
+    if (plan.parts == 0)
+        return launch_stream({x.codes, w.codes, x.scales, w.scales, (int)x.n, w.n, row_blocks(d) / 2, out, nullptr, 0, d, 0}, plan, st);
     const int stages = (int)ceil_div(d, TILE_K);
-    const TileWork g = {x.codes, w.codes, x.scales, w.scales, x.ld, w.ld, x.n, w.n, stages, stages, (int)ceil_div(x.n, (int64_t)plan.rows),
-                        (int)ceil_div(w.n, (int64_t)plan.channels), plan.parts, out, static_cast<int *>(workspace)};
+    const TileWork g = {x.codes, w.codes, x.scales, w.scales, x.n, w.n, row_blocks(d), stages, stages, (int)ceil_div(x.n, (int64_t)plan.rows),
+                  (int)ceil_div(w.n, (int64_t)plan.channels), plan.parts, out, static_cast<int *>(workspace)};
     const dim3 grid((unsigned)(g.tiles_m * g.tiles_n * plan.parts));
-    if (out.type == LPQ_TYPE_F32) linear8_tile_kernel<2, 2, LPQ_TYPE_F32, false><<<grid, TILE_THREADS, 0, st>>>(g);
-    else if (out.type == LPQ_TYPE_F16) linear8_tile_kernel<2, 2, LPQ_TYPE_F16, false><<<grid, TILE_THREADS, 0, st>>>(g);
-    else linear8_tile_kernel<2, 2, LPQ_TYPE_BF16, false><<<grid, TILE_THREADS, 0, st>>>(g);
+    const auto go = [&](auto t) {
+        constexpr int T = decltype(t)::value;
+        if (plan.rows == 256) linear8_tile_kernel<4, 4, T, false><<<grid, TILE_THREADS, 0, st>>>(g);
+        else linear8_tile_kernel<2, 2, T, false><<<grid, TILE_THREADS, 0, st>>>(g);
+    };
+    if (out.type == LPQ_TYPE_F32) go(std::integral_constant<int, LPQ_TYPE_F32>());
+    else if (out.type == LPQ_TYPE_F16) go(std::integral_constant<int, LPQ_TYPE_F16>());
+    else go(std::integral_constant<int, LPQ_TYPE_BF16>());
     return hipGetLastError();
 }
 

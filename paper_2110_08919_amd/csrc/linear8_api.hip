@@ -25,7 +25,10 @@ static int element_bytes(int type) { return type == LPQ_TYPE_F32 ? 4 : type == L
 
 constexpr int64_t MAX_STRIDE = int64_t(1) << 40;
 
-extern "C" int64_t lpq_row_codes_stride(int d) { return d < 1 || d > LINEAR8_MAX_D ? 0 : round_up(d, ROW_CODES_ALIGN); }
+extern "C" size_t lpq_row_codes_bytes(int64_t n, int d)
+{
+    return n < 0 || n >= (int64_t(1) << 31) || d < 1 || d > LINEAR8_MAX_D ? 0 : (size_t)ceil_div(n, (int64_t)16) * row_blocks(d) * 1024;
+}
 
 static int check_features(int d)
 {
@@ -45,26 +48,22 @@ static int check_rows(const char *what, const void *p, int64_t ld, int type, int
     return LPQ_OK;
 }
 
-static int check_codes(const char *what, const void *codes, int64_t ld, const float *scales, int64_t n, int d)
+static int check_codes(const char *what, const void *codes, const float *scales, int64_t n)
 {
     if (n < 0) return fail(LPQ_EINVAL, "%lld %s", (long long)n, what);
     if (n >= (int64_t(1) << 31)) return fail(LPQ_ERANGE, "%lld %s, must stay below 2^31", (long long)n, what);
     if (n > 0 && (!codes || !scales)) return fail(LPQ_EINVAL, "null %s", what);
-    if ((uintptr_t)codes % 16 || ld % 16 || ld < lpq_row_codes_stride(d))
-        return fail(LPQ_EINVAL, "%s of %d codes, %lld bytes apart: need a 16-byte aligned start and stride of at least %lld", what, d, (long long)ld,
-                    (long long)lpq_row_codes_stride(d));
-    if (ld > LINEAR8_MAX_STRIDE) return fail(LPQ_ERANGE, "%s %lld bytes apart, at most %d", what, (long long)ld, (int)LINEAR8_MAX_STRIDE);
+    if ((uintptr_t)codes % 256) return fail(LPQ_EINVAL, "%s must be 256-byte aligned", what);
     return LPQ_OK;
 }
 
-extern "C" int lpq_encode_rows(const void *x_dev, int64_t ldx, int type, int64_t n, int d, int8_t *codes_dev, int64_t ld_codes, float *scales_dev,
-                               void *stream)
+extern "C" int lpq_encode_rows(const void *x_dev, int64_t ldx, int type, int64_t n, int d, int8_t *codes_dev, float *scales_dev, void *stream)
 {
     int rc = check_features(d);
     if (!rc) rc = check_rows("rows", x_dev, ldx, type, n, d, false);
-    if (!rc) rc = check_codes("rows", codes_dev, ld_codes, scales_dev, n, d);
+    if (!rc) rc = check_codes("codes", codes_dev, scales_dev, n);
     if (rc) return rc;
-    const hipError_t e = launch_encode_rows(x_dev, ldx, type, n, d, codes_dev, ld_codes, scales_dev, (hipStream_t)stream);
+    const hipError_t e = launch_encode_rows(x_dev, ldx, type, n, d, codes_dev, scales_dev, (hipStream_t)stream);
     return e == hipSuccess ? LPQ_OK : hip_fail(e, "lpq_encode_rows");
 }
 
@@ -88,18 +87,17 @@ static int check_workspace(const void *workspace_dev, size_t bytes, size_t need)
     return LPQ_OK;
 }
 
-extern "C" int lpq_matmul_i8(const int8_t *a_dev, int64_t lda, const float *a_scales_dev, int64_t m, const int8_t *b_dev, int64_t ldb,
-                             const float *b_scales_dev, int64_t n, int d, const float *bias_dev, void *out_dev, int64_t ldo, int type,
-                             void *workspace_dev, size_t workspace_bytes, void *stream)
+extern "C" int lpq_matmul_i8(const int8_t *a_dev, const float *a_scales_dev, int64_t m, const int8_t *b_dev, const float *b_scales_dev, int64_t n, int d,
+                             const float *bias_dev, void *out_dev, int64_t ldo, int type, void *workspace_dev, size_t workspace_bytes, void *stream)
 {
     int rc = check_features(d);
-    if (!rc) rc = check_codes("rows", a_dev, lda, a_scales_dev, m, d);
-    if (!rc) rc = check_codes("channels", b_dev, ldb, b_scales_dev, n, d);
+    if (!rc) rc = check_codes("rows", a_dev, a_scales_dev, m);
+    if (!rc) rc = check_codes("channels", b_dev, b_scales_dev, n);
     if (!rc) rc = check_rows("outputs", out_dev, ldo, type, n > 0 ? m : 0, n, true);
     if (!rc) rc = check_product(m, n);
     if (!rc && m > 0 && n > 0) rc = check_workspace(workspace_dev, workspace_bytes, lpq_matmul_i8_workspace_bytes(m, n, d));
     if (rc || m == 0 || n == 0) return rc;
-    const hipError_t e = launch_linear8({a_dev, a_scales_dev, lda, m}, {b_dev, b_scales_dev, ldb, n}, d, {out_dev, ldo, type, bias_dev},
+    const hipError_t e = launch_linear8({a_dev, a_scales_dev, m}, {b_dev, b_scales_dev, n}, d, {out_dev, ldo, type, bias_dev},
                                         linear8_plan(m, n, d), workspace_dev, (hipStream_t)stream);
     return e == hipSuccess ? LPQ_OK : hip_fail(e, "lpq_matmul_i8");
 }
@@ -110,8 +108,9 @@ struct Linear8Space {
 };
 static Linear8Space linear8_space(int64_t m, int64_t n, int d)
 {
+    if (linear8_fused(m, d)) return {0, 0, 0};
     Linear8Space s;
-    s.scales = (size_t)m * lpq_row_codes_stride(d);      // a multiple of 128
+    s.scales = lpq_row_codes_bytes(m, d);
     s.parts = (size_t)round_up(s.scales + 4 * m, 256);
     s.bytes = s.parts + lpq_matmul_i8_workspace_bytes(m, n, d);
     return s;
@@ -123,26 +122,31 @@ extern "C" size_t lpq_linear8_workspace_bytes(int64_t m, int64_t n, int d)
     return linear8_space(m, n, d).bytes;
 }
 
-extern "C" int lpq_linear8(const void *x_dev, int64_t ldx, int type, int64_t m, const int8_t *codes_dev, int64_t ld_codes, const float *scales_dev,
-                           int64_t n, int d, const float *bias_dev, void *out_dev, int64_t ldo, void *workspace_dev, size_t workspace_bytes,
+extern "C" int lpq_linear8(const void *x_dev, int64_t ldx, int type, int64_t m, const int8_t *codes_dev, const float *scales_dev, int64_t n,
+                           int d, const float *bias_dev, void *out_dev, int64_t ldo, void *workspace_dev, size_t workspace_bytes,
                            void *stream)
 {
     int rc = check_features(d);
     if (!rc) rc = check_rows("rows", x_dev, ldx, type, m, d, false);
-    if (!rc) rc = check_codes("channels", codes_dev, ld_codes, scales_dev, n, d);
+    if (!rc) rc = check_codes("channels", codes_dev, scales_dev, n);
     if (!rc) rc = check_rows("outputs", out_dev, ldo, type, n > 0 ? m : 0, n, true);
     if (!rc) rc = check_product(m, n);
     if (rc || m == 0 || n == 0) return rc;
     const Linear8Space s = linear8_space(m, n, d);
     rc = check_workspace(workspace_dev, workspace_bytes, s.bytes);
     if (rc) return rc;
+    const Linear8Out out = {out_dev, ldo, type, bias_dev};
+    const RowCodes weights = {codes_dev, scales_dev, n};
+    const Linear8Plan plan = linear8_plan(m, n, d);
+    if (linear8_fused(m, d)) {
+        const hipError_t e = launch_linear8_fused(x_dev, ldx, m, weights, d, out, plan, (hipStream_t)stream);
+        return e == hipSuccess ? LPQ_OK : hip_fail(e, "lpq_linear8");
+    }
     char *const space = static_cast<char *>(workspace_dev);
-    const int64_t ld = lpq_row_codes_stride(d);
     int8_t *const rows = reinterpret_cast<int8_t *>(space);
     float *const row_scales = reinterpret_cast<float *>(space + s.scales);
-    hipError_t e = launch_encode_rows(x_dev, ldx, type, m, d, rows, ld, row_scales, (hipStream_t)stream);
+    hipError_t e = launch_encode_rows(x_dev, ldx, type, m, d, rows, row_scales, (hipStream_t)stream);
     if (e == hipSuccess)
-        e = launch_linear8({rows, row_scales, ld, m}, {codes_dev, scales_dev, ld_codes, n}, d, {out_dev, ldo, type, bias_dev}, linear8_plan(m, n, d),
-                           space + s.parts, (hipStream_t)stream);
+        e = launch_linear8({rows, row_scales, m}, weights, d, out, plan, space + s.parts, (hipStream_t)stream);
     return e == hipSuccess ? LPQ_OK : hip_fail(e, "lpq_linear8");
 }

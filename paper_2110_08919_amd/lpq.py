@@ -95,12 +95,12 @@ def lib() -> C.CDLL:
             "lpq_kv_attend_masked_workspace_bytes": (C.c_size_t, [vp, i64, i32, i32, i64, i32, i64, i32, i32]),
             "lpq_kv_attend_masked": (i32, [vp, vp, i64, i64, i64, i32, i64, i32, i32, f32, vp, vp, i64, i64, vp, i32, i64, i32, vp, i64, i64,
                                            vp, i64, i64, i64, vp, vp, C.c_size_t, vp]),
-            "lpq_row_codes_stride": (i64, [i32]),
-            "lpq_encode_rows": (i32, [vp, i64, i32, i64, i32, vp, i64, vp, vp]),
+            "lpq_row_codes_bytes": (C.c_size_t, [i64, i32]),
+            "lpq_encode_rows": (i32, [vp, i64, i32, i64, i32, vp, vp, vp]),
             "lpq_matmul_i8_workspace_bytes": (C.c_size_t, [i64, i64, i32]),
-            "lpq_matmul_i8": (i32, [vp, i64, vp, i64, vp, i64, vp, i64, i32, vp, vp, i64, i32, vp, C.c_size_t, vp]),
+            "lpq_matmul_i8": (i32, [vp, vp, i64, vp, vp, i64, i32, vp, vp, i64, i32, vp, C.c_size_t, vp]),
             "lpq_linear8_workspace_bytes": (C.c_size_t, [i64, i64, i32]),
-            "lpq_linear8": (i32, [vp, i64, i32, i64, vp, i64, vp, i64, i32, vp, vp, i64, vp, C.c_size_t, vp]),
+            "lpq_linear8": (i32, [vp, i64, i32, i64, vp, vp, i64, i32, vp, vp, i64, vp, C.c_size_t, vp]),
             "lpq_last_error": (C.c_char_p, []),
         }
         for name, (res, args) in sig.items():
@@ -576,26 +576,30 @@ def _typed_matrix(t: torch.Tensor, what: str):
 
 
 class RowCodes:
-    """Rows [n, d] as 8-bit codes with a scale each: what encode_rows() makes and matmul_i8() takes.  `codes` int8 [n, stride] (features d on are
-    0) and `scales` float32 [n]; a row reads back as codes * scale."""
+    """Rows [n, d] as 8-bit codes with a scale each: what encode_rows() makes and matmul_i8() takes.  `blocks` int8 [ceil(n / 16), 2 ceil(d / 128), 4,
+    16, 16] holds code k of row i at [i // 16, k // 64, k % 64 // 16, i % 16, k % 16] (features d on are 0), `scales` float32 [n]; a row reads
+    back as codes * scale."""
 
-    def __init__(self, codes: torch.Tensor, scales: torch.Tensor, d: int):
-        assert codes.is_cuda and codes.dtype is torch.int8 and codes.dim() == 2 and codes.stride(1) == 1, "need rows of device codes"
-        assert scales.is_cuda and scales.dtype is torch.float32 and scales.is_contiguous() and scales.shape == codes.shape[:1] \
-            and scales.device == codes.device, "need a float32 scale for each row, on the codes' device"
-        assert 1 <= d <= codes.shape[1] and codes.shape[1] >= lib().lpq_row_codes_stride(d) > 0, "rows are as long as their stride"
-        self.codes, self.scales, self.d = codes, scales, d
+    def __init__(self, blocks: torch.Tensor, scales: torch.Tensor, d: int):
+        assert blocks.is_cuda and blocks.dtype is torch.int8 and blocks.is_contiguous(), "need blocks of device codes"
+        assert scales.is_cuda and scales.dtype is torch.float32 and scales.is_contiguous() and scales.dim() == 1 and scales.device == blocks.device, \
+            "need a float32 scale for each row, on the codes' device"
+        assert d >= 1 and blocks.shape == self.shape(scales.shape[0], d), f"need blocks {self.shape(scales.shape[0], d)}"
+        self.blocks, self.scales, self.d, self.n = blocks, scales, d, scales.shape[0]
+
+    @staticmethod
+    def shape(n: int, d: int):
+        return -(-n // 16), 2 * -(-d // 128), 4, 16, 16
 
     @property
-    def n(self) -> int:
-        return self.codes.shape[0]
+    def codes(self) -> torch.Tensor:
+        """int8 [n, d], a copy."""
+        rows = self.blocks.permute(0, 3, 1, 2, 4).reshape(16 * self.blocks.shape[0], -1)
+        return rows[:self.n, :self.d].contiguous()
 
     def float(self) -> torch.Tensor:
         """The rows as they read back, float32 [n, d]."""
-        return self.codes[:, :self.d].float() * self.scales[:, None]
-
-    def _args(self):
-        return self.codes.data_ptr(), max(self.codes.stride(0), self.codes.shape[1]), self.scales.data_ptr()
+        return self.codes.float() * self.scales[:, None]
 
 
 def encode_rows(x: torch.Tensor) -> RowCodes:
@@ -603,11 +607,10 @@ def encode_rows(x: torch.Tensor) -> RowCodes:
     the codes: rows that require a gradient are refused."""
     assert not (x.requires_grad and torch.is_grad_enabled()), "codes have no gradient: use torch.no_grad() or x.detach()"
     n, d, ld = _typed_matrix(x, "rows")
-    stride = lib().lpq_row_codes_stride(d)
-    assert stride > 0, f"rows of 1 to 131072 values, not {d}"
+    assert lib().lpq_row_codes_bytes(n, d) > 0 or n == 0, f"rows of 1 to 131072 values, not {d}"
     with torch.cuda.device(x.device):
-        out = RowCodes(torch.empty((n, stride), dtype=torch.int8, device=x.device), torch.empty(n, dtype=torch.float32, device=x.device), d)
-        _check(lib().lpq_encode_rows(x.data_ptr(), ld, _TYPE[x.dtype], n, d, out.codes.data_ptr(), stride, out.scales.data_ptr(), _stream_of(x)))
+        out = RowCodes(torch.empty(RowCodes.shape(n, d), dtype=torch.int8, device=x.device), torch.empty(n, dtype=torch.float32, device=x.device), d)
+        _check(lib().lpq_encode_rows(x.data_ptr(), ld, _TYPE[x.dtype], n, d, out.blocks.data_ptr(), out.scales.data_ptr(), _stream_of(x)))
     return out
 
 
@@ -621,17 +624,16 @@ def _bias(bias: torch.Tensor, n: int, device):
 def matmul_i8(a: RowCodes, b: RowCodes, bias: torch.Tensor = None, dtype=torch.bfloat16, out: torch.Tensor = None) -> torch.Tensor:
     """[rows of a, rows of b] of `dtype`: the products of all rows of a with all rows of b (and bias, one for each row of b)."""
     assert a.d == b.d, f"rows of {a.d} and of {b.d} codes"
-    assert a.codes.device == b.codes.device, "both on one device"
+    assert a.blocks.device == b.blocks.device, "both on one device"
     if out is None:
-        out = torch.empty((a.n, b.n), dtype=dtype, device=a.codes.device)
+        out = torch.empty((a.n, b.n), dtype=dtype, device=a.blocks.device)
     m, n, ldo = _typed_matrix(out, "an output")
-    assert (m, n) == (a.n, b.n) and out.device == a.codes.device, f"need an output [{a.n}, {b.n}] on the codes' device"
-    bias = _bias(bias, n, a.codes.device)
-    pa, lda, sa = a._args()
-    pb, ldb, sb = b._args()
+    assert (m, n) == (a.n, b.n) and out.device == a.blocks.device, f"need an output [{a.n}, {b.n}] on the codes' device"
+    bias = _bias(bias, n, a.blocks.device)
     with torch.cuda.device(out.device):
         ws, size = _scratch(lib().lpq_matmul_i8_workspace_bytes(m, n, a.d), out.device)
-        _check(lib().lpq_matmul_i8(pa, lda, sa, m, pb, ldb, sb, n, a.d, _ptr(bias), out.data_ptr(), ldo, _TYPE[out.dtype], _ptr(ws), size, _stream_of(out)))
+        _check(lib().lpq_matmul_i8(a.blocks.data_ptr(), a.scales.data_ptr(), m, b.blocks.data_ptr(), b.scales.data_ptr(), n, a.d, _ptr(bias),
+                                   out.data_ptr(), ldo, _TYPE[out.dtype], _ptr(ws), size, _stream_of(out)))
     return out
 
 
@@ -649,8 +651,7 @@ class Linear8:
         self.bias = _bias(bias, self.channels, self.device)
         if bias is not None and self.bias.data_ptr() == bias.data_ptr():
             self.bias = self.bias.clone()                   # the layer's own, as its codes are
-        codes, ld, scales = self.weight._args()
-        self._args = codes, ld, scales, self.channels, self.d, _ptr(self.bias)
+        self._args = self.weight.blocks.data_ptr(), self.weight.scales.data_ptr(), self.channels, self.d, _ptr(self.bias)
 
     def __call__(self, x: torch.Tensor, out: torch.Tensor = None, workspace: torch.Tensor = None) -> torch.Tensor:
         """x [..., d] of float32, float16 or bfloat16 -> [..., channels] of its type."""

@@ -30,6 +30,11 @@ def codes_of(x):
     return torch.from_numpy(codes.astype(np.int64)), torch.from_numpy(scales.astype(np.float32))
 
 
+def rows_of(codes):
+    """Rows with their ends behind feature d."""
+    return codes.blocks.permute(0, 3, 1, 2, 4).flatten(2).flatten(0, 1)[:codes.n]
+
+
 def product_of(a, sa, b, sb, bias, dtype):
     """fl(fl(fl(sum) sa) sb) [+ bias] to dtype."""
     sums = a.double() @ b.double().t()                       # exact: below 2^53
@@ -53,9 +58,13 @@ def test_rows_to_codes(kind, n, d):
     got = lpq.encode_rows(x.cuda())
     codes, scales = codes_of(x)
     stride = (d + 127) // 128 * 128
-    assert got.codes.shape == (n, stride) and got.n == n and got.d == d
-    assert torch.equal(got.codes[:, :d].cpu().long(), codes)
-    assert not got.codes[:, d:].any()
+    assert got.codes.shape == (n, d) and got.n == n and got.d == d
+    assert torch.equal(got.codes.cpu().long(), codes)
+    blocks = got.blocks.cpu()
+    assert blocks.shape == ((n + 15) // 16, stride // 64, 4, 16, 16)
+    for i, k in ((0, 0), (n - 1, d - 1), (n // 2, d // 3)):
+        assert blocks.flatten()[(i // 16 * (stride // 64) + k // 64) * 1024 + k % 64 // 16 * 256 + i % 16 * 16 + k % 16] == codes[i, k]
+    assert not rows_of(got)[:, d:].any()
     assert torch.equal(got.scales.cpu(), scales)
     assert torch.equal(got.float().cpu(), codes.float() * scales[:, None])
 
@@ -70,7 +79,7 @@ def test_rows_of_any_size_and_rows_that_are_not_finite(kind):
     x = x.to(TYPES[kind])
     got = lpq.encode_rows(x.cuda())
     codes, scales = codes_of(x)
-    assert torch.equal(got.codes[:, :300].cpu().long(), codes)
+    assert torch.equal(got.codes.cpu().long(), codes)
     same(got.scales, scales)
     assert codes[1].abs().max() == 127 and torch.isnan(scales[8:11]).all() and scales[0] == 0
     w = make(40, 300, kind, 4)
@@ -181,7 +190,10 @@ def test_codes_whose_rest_of_a_row_is_not_zero():
         x, w = make(m, 200, "f32", 8), make(150, 200, "f32", 9)
         a, b = lpq.encode_rows(x.cuda()), lpq.encode_rows(w.cuda())
         want = lpq.matmul_i8(a, b, dtype=torch.float32)
-        b.codes[:, 200:] = 99
+        b.blocks[:, 3, 0, :, 8:] = 99
+        b.blocks[:, 3, 1:] = -99
+        a.blocks[m // 16:, :, :, m % 16:] = 77               # rows behind the last
+        b.blocks[150 // 16:, :, :, 150 % 16:] = 55
         assert torch.equal(lpq.matmul_i8(a, b, dtype=torch.float32), want)
 
 
@@ -245,7 +257,7 @@ def test_refusals():
     with pytest.raises(lpq.LpqError):
         layer(x, out=torch.empty(1, 5, device="cuda").expand(3, 5))
     with pytest.raises(lpq.LpqError):
-        layer(x, workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))
+        layer(x.repeat(10, 1), workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))
     with pytest.raises(AssertionError):
         lpq.matmul_i8(lpq.encode_rows(x), lpq.encode_rows(x[:, :60]))
     bias = torch.ones(5, device="cuda")

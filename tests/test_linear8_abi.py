@@ -14,8 +14,9 @@ def L():
     return lpq.lib()
 
 
-def test_strides_and_workspaces(L):
-    assert [L.lpq_row_codes_stride(d) for d in (-1, 0, 1, 128, 129, 131072, 131073)] == [0, 0, 128, 128, 256, 131072, 0]
+def test_sizes_of_codes_and_workspaces(L):
+    assert [L.lpq_row_codes_bytes(1, d) for d in (-1, 0, 1, 128, 129, 131072, 131073)] == [0, 0, 2048, 2048, 4096, 16 * 131072, 0]
+    assert [L.lpq_row_codes_bytes(n, 1) for n in (-1, 0, 16, 17, 1 << 31)] == [0, 0, 2048, 4096, 0]
     for m, n, d in ((0, 5, 5), (5, 0, 5), (5, 5, 0), (5, 5, 1 << 20), (1 << 31, 5, 5), (5, 1 << 31, 5), (-1, 5, 5)):
         assert L.lpq_linear8_workspace_bytes(m, n, d) == 0 and L.lpq_matmul_i8_workspace_bytes(m, n, d) == 0
     for m, n, d in ((1, 1, 1), (300, 700, 1000), (48, 11_111, 4100)):
@@ -28,20 +29,20 @@ def test_refusals(L):
     a = C.create_string_buffer(4096)
     p = (C.addressof(a) + 255) // 256 * 256
 
-    def encode(x=p, ldx=64, kind=0, n=2, d=64, codes=p, ld=128, scales=p):
-        return L.lpq_encode_rows(x, ldx, kind, n, d, codes, ld, scales, None)
+    def encode(x=p, ldx=64, kind=0, n=2, d=64, codes=p, scales=p):
+        return L.lpq_encode_rows(x, ldx, kind, n, d, codes, scales, None)
 
-    def product(pa=p, lda=128, sa=p, m=2, pb=p, ldb=128, sb=p, n=2, d=64, out=p, ldo=2, kind=0, ws=None, size=0):
-        return L.lpq_matmul_i8(pa, lda, sa, m, pb, ldb, sb, n, d, None, out, ldo, kind, ws, size, None)
+    def product(pa=p, sa=p, m=2, pb=p, sb=p, n=2, d=64, out=p, ldo=2, kind=0, ws=None, size=0):
+        return L.lpq_matmul_i8(pa, sa, m, pb, sb, n, d, None, out, ldo, kind, ws, size, None)
 
-    def linear(x=p, ldx=64, kind=0, m=2, codes=p, ld=128, scales=p, n=2, d=64, out=p, ldo=2, ws=p, size=1 << 30):
-        return L.lpq_linear8(x, ldx, kind, m, codes, ld, scales, n, d, None, out, ldo, ws, size, None)
+    def linear(x=p, ldx=64, kind=0, m=2, codes=p, scales=p, n=2, d=64, out=p, ldo=2, ws=p, size=1 << 30):
+        return L.lpq_linear8(x, ldx, kind, m, codes, scales, n, d, None, out, ldo, ws, size, None)
 
     for call, more in ((encode, {}), (linear, {"m": 2})):
-        assert call(d=0) == lpq.EINVAL and call(d=131_073, ldx=1 << 20, ld=1 << 18) == lpq.ERANGE
+        assert call(d=0) == lpq.EINVAL and call(d=131_073, ldx=1 << 20) == lpq.ERANGE
         assert call(kind=3) == lpq.EINVAL and call(x=None) == lpq.EINVAL and call(codes=None) == lpq.EINVAL and call(scales=None) == lpq.EINVAL
         assert call(ldx=-1) == lpq.EINVAL and call(ldx=(1 << 40) + 1) == lpq.EINVAL
-        assert call(ld=112) == lpq.EINVAL and call(ld=136) == lpq.EINVAL and call(ld=(1 << 20) + 16) == lpq.ERANGE and call(codes=p + 8) == lpq.EINVAL
+        assert call(codes=p + 128) == lpq.EINVAL
         assert call(n=-1) == lpq.EINVAL and call(n=1 << 31) == lpq.ERANGE
     assert encode(n=0, x=None, codes=None, scales=None) == lpq.OK
     for call in (product, linear):
@@ -49,8 +50,8 @@ def test_refusals(L):
         assert call(m=1 << 31) == lpq.ERANGE and call(m=-1) == lpq.EINVAL
         assert call(m=1 << 30, n=1 << 20, ldo=1 << 20) == lpq.ERANGE       # more tiles than a launch has
         assert call(m=0, out=None) == lpq.OK and call(n=0) == lpq.OK
-    assert product(lda=64) == lpq.EINVAL and product(ldb=64) == lpq.EINVAL and product(sa=None) == lpq.EINVAL and product(sb=None) == lpq.EINVAL
-    assert linear(ws=None) == lpq.EINVAL and linear(ws=p + 128) == lpq.EINVAL and linear(size=16) == lpq.ERANGE
+    assert product(pa=p + 16) == lpq.EINVAL and product(pb=p + 64) == lpq.EINVAL and product(pa=None) == lpq.EINVAL and product(sa=None) == lpq.EINVAL and product(sb=None) == lpq.EINVAL
+    assert linear(m=9, ws=None) == lpq.EINVAL and linear(m=9, ws=p + 128) == lpq.EINVAL and linear(m=9, size=16) == lpq.ERANGE
     assert b"workspace" in L.lpq_last_error()
 
 
@@ -62,4 +63,4 @@ def test_binding_takes_device_rows_only():
     with pytest.raises(AssertionError):
         lpq.Linear8(torch.zeros(2, 4))
     with pytest.raises(AssertionError):
-        lpq.RowCodes(torch.zeros(2, 128, dtype=torch.int8), torch.zeros(2), 4)
+        lpq.RowCodes(torch.zeros(1, 2, 4, 16, 16, dtype=torch.int8), torch.zeros(2), 4)
