@@ -361,13 +361,10 @@ struct TileCopies {
             from[i] = (channel ? g.w : g.x) + block_of(row16, stage, g.blocks) + 16 * lane;
         }
     }
-    __device__ __forceinline__ void next(int slot)
+    __device__ __forceinline__ void one(int i, int slot)
     {
-#pragma unroll
-        for (int i = 0; i < COUNT; ++i) {
-            async_copy16(from[i], to + slot * (BM + BN) * TILE_K + 4096 * i);
-            from[i] += 1024;
-        }
+        async_copy16(from[i], to + slot * (BM + BN) * TILE_K + 4096 * i);
+        from[i] += 1024;
     }
 };
 
@@ -406,35 +403,51 @@ __global__ __launch_bounds__(TILE_THREADS) void linear8_tile_kernel(TileWork g)
     copies.setup(g, row0, ch0, begin, ring, wave, lane);
     const int at = (lane >> 5) * 256 + (lane & 15) * 16 + ((lane >> 4) & 1) * 1024;
     v4i fc[2][TC], ft[2][TT];
-    const auto operands = [&](int slot, int half) {
+    const auto operand = [&](int slot, int half, int k) {
         const char *const here = ring + slot * STAGE + 512 * half + at;
-#pragma unroll
-        for (int i = 0; i < TC; ++i) fc[half][i] = *reinterpret_cast<const v4i *>(here + 64 * (wc + 32 * i));
-#pragma unroll
-        for (int j = 0; j < TT; ++j) ft[half][j] = *reinterpret_cast<const v4i *>(here + 64 * (BN + wt + 32 * j));
+        if (k < TC) fc[half][k] = *reinterpret_cast<const v4i *>(here + 64 * (wc + 32 * k));
+        else ft[half][k - TC] = *reinterpret_cast<const v4i *>(here + 64 * (BN + wt + 32 * (k - TC)));
     };
-    const auto multiply = [&](int half) {
-        __builtin_amdgcn_sched_barrier(0);           // the reads that were asked for go ahead of these, not behind
+    // The matrix instructions of a half, and between them the reads of the next half's operands and half of a stage's copies: a wave that
+    // asks for these in one go is held up by their queues for as long as the matrix pipe then has nothing to do.
+    const auto multiply = [&](int half, int next_slot, bool copy, int copy_slot) {
+        constexpr int STEPS = TT * TC, READS = TT + TC, COPIES = Copies::COUNT / 2;
 #pragma unroll
-        for (int i = 0; i < TC; ++i)
+        for (int k = 0; k < STEPS; ++k) {
+            const int i = k / TT, j = k % TT;
+            __builtin_amdgcn_sched_barrier(0);
+            acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fc[half][i], ft[half][j], acc[i][j], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+            // reads in the first half of them, so that none is waited for
 #pragma unroll
-            for (int j = 0; j < TT; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fc[half][i], ft[half][j], acc[i][j], 0, 0, 0);
+            for (int r = 2 * k * READS / STEPS; r < 2 * (k + 1) * READS / STEPS && r < READS; ++r) operand(next_slot, half ^ 1, r);
+            if (copy && 2 * k >= STEPS) {
+                constexpr int FROM = STEPS / 2;
+#pragma unroll
+                for (int c = (k - FROM) * COPIES / FROM; c < (k - FROM + 1) * COPIES / FROM; ++c) copies.one(c + (half ? 0 : COPIES), copy_slot);
+            }
+        }
         __builtin_amdgcn_sched_barrier(0);
     };
-    for (int s = 0; s < TILE_STAGES && s < stages; ++s) copies.next(s);
-    wait_vmcnt(min(stages - 1, TILE_STAGES - 1) * Copies::COUNT);
+    // In flight: stages 0 to 2 and half of 3 ahead of the loop, whose first half completes it.
+    for (int s = 0; s < TILE_STAGES - 1 && s < stages; ++s)
+#pragma unroll
+        for (int i = 0; i < Copies::COUNT; ++i) copies.one(i, s);
+    wait_vmcnt(min(stages - 1, TILE_STAGES - 2) * Copies::COUNT);
     lds_barrier();
-    operands(0, 0);
+#pragma unroll
+    for (int r = 0; r < TT + TC; ++r) operand(0, 0, r);
+    if (TILE_STAGES - 1 < stages) {
+#pragma unroll
+        for (int i = 0; i < Copies::COUNT / 2; ++i) copies.one(i, TILE_STAGES - 1);
+    }
     for (int s = 0; s < stages; ++s) {
-        operands(s % TILE_STAGES, 1);
-        multiply(0);
+        multiply(0, s % TILE_STAGES, s + TILE_STAGES - 1 < stages, (s + TILE_STAGES - 1) % TILE_STAGES);
         // the next stage is there for all, and nobody reads this one any more: its place is filled again
         if (s + TILE_STAGES <= stages) __builtin_amdgcn_s_waitcnt(vmcnt_imm((TILE_STAGES - 2) * Copies::COUNT));
         else __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
         lds_barrier();
-        if (s + TILE_STAGES < stages) copies.next(s % TILE_STAGES);
-        operands((s + 1) % TILE_STAGES, 0);          // (after the last stage: of one gone by, for nothing)
-        multiply(1);
+        multiply(1, (s + 1) % TILE_STAGES, s + TILE_STAGES < stages, s % TILE_STAGES);      // (behind the last stage: reads for nothing)
     }
 
     if (PARTS) {
