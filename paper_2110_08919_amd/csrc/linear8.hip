@@ -18,16 +18,62 @@ namespace {
 // ------------------------------------------------------------------ rows to codes ----
 constexpr int ROW_THREADS = 1024;
 
-__device__ __forceinline__ uint32_t magnitude8(const float *v)
-{
-    uint32_t most = 0;
+// 16 neighbouring values of a row as they lie in memory; those behind its end are 0.  Wide loads whatever the alignment, but for the row's
+// last ones, which come one at a time.
+template <int type>
+struct Run16 {
+    static constexpr int WORDS = type == LPQ_TYPE_F32 ? 16 : 8;
+    uint32_t w[WORDS];
+    __device__ __forceinline__ void load(const void *base, int64_t at, int left)
+    {
+        constexpr int SIZE = type == LPQ_TYPE_F32 ? 4 : 2;
+        const char *const p = static_cast<const char *>(base) + SIZE * at;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const uint32_t b = __builtin_bit_cast(uint32_t, v[e]) & 0x7fffffffu;      // ordered as the magnitudes, infinity and NaN on top
-        most = b > most ? b : most;
+        for (int i = 0; i < WORDS; ++i) w[i] = 0;
+        if (left >= 16) {
+            uint4 t[WORDS / 4];
+            __builtin_memcpy(t, p, sizeof(t));
+#pragma unroll
+            for (int i = 0; i < WORDS / 4; ++i) {
+                w[4 * i] = t[i].x; w[4 * i + 1] = t[i].y; w[4 * i + 2] = t[i].z; w[4 * i + 3] = t[i].w;
+            }
+        } else if (left > 0) {
+#pragma unroll
+            for (int e = 0; e < 15; ++e)
+                if (e < left) {
+                    if (type == LPQ_TYPE_F32) w[e] = reinterpret_cast<const uint32_t *>(p)[e];
+                    else w[e >> 1] |= (uint32_t) reinterpret_cast<const uint16_t *>(p)[e] << (16 * (e & 1));
+                }
+        }
     }
-    return most;
-}
+    // Magnitudes compare as their bits do, infinity and NaN on top; of a 16-bit type two at a time, whose larger one magnitude() takes.
+    __device__ __forceinline__ void most(uint32_t &m) const
+    {
+#pragma unroll
+        for (int i = 0; i < WORDS; ++i) {
+            if (type == LPQ_TYPE_F32) {
+                const uint32_t b = w[i] & 0x7fffffffu;
+                m = b > m ? b : m;
+            } else {
+                typedef uint16_t Two __attribute__((ext_vector_type(2)));
+                m = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(Two, w[i] & 0x7fff7fffu), __builtin_bit_cast(Two, m)));
+            }
+        }
+    }
+    static __device__ __forceinline__ uint32_t magnitude(uint32_t m)
+    {
+        if (type == LPQ_TYPE_F32) return m;
+        const uint32_t a = m & 0xffffu, b = m >> 16, c = a > b ? a : b;
+        return type == LPQ_TYPE_BF16 ? c << 16 : __builtin_bit_cast(uint32_t, (float)__builtin_bit_cast(_Float16, (uint16_t)c));
+    }
+    __device__ __forceinline__ float value(int e) const
+    {
+        if (type == LPQ_TYPE_F32) return __builtin_bit_cast(float, w[e % WORDS]);
+        const uint32_t u = w[e >> 1];
+        if (type == LPQ_TYPE_BF16) return __builtin_bit_cast(float, e & 1 ? u & 0xffff0000u : u << 16);
+        return (float)__builtin_bit_cast(_Float16, (uint16_t)(u >> (16 * (e & 1))));
+    }
+};
 
 // What a row is multiplied by to become codes.  A row below 2^-100 is taken times 2^60 first, exactly, so that 127 / A stays finite; one that
 // holds an infinity or a NaN has the codes 0 and the scale NaN, so that whatever it goes into is NaN.
@@ -42,25 +88,32 @@ __device__ __forceinline__ RowFactor row_factor(uint32_t magnitude)
     else if (magnitude) f.by = 127.0f / (most * f.up);
     return f;
 }
-__device__ __forceinline__ uint2 row_codes8(const float *v, const RowFactor &f)
+// Codes of 16 values; all of a wave's are of one row.  Adding 1.5 x 2^23 rounds to a whole number, to nearest even, and leaves it in the low byte.
+template <int type>
+__device__ __forceinline__ uint4 row_codes16(const Run16<type> &r, const RowFactor &f)
 {
-    uint32_t c[8];
+    uint32_t c[4];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const float t = rintf((v[e] * f.up) * f.by);
-        c[e] = f.by == 0.0f ? 0u : (uint32_t)(int)t;
+    for (int g = 0; g < 4; ++g) {
+        uint32_t b[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            float v = r.value(4 * g + e);
+            if (type != LPQ_TYPE_F16) v *= f.up;
+            b[e] = __builtin_bit_cast(uint32_t, v * f.by + 0x1.8p23f);
+        }
+        const uint32_t lo = __builtin_amdgcn_perm(b[1], b[0], 0x0c0c0400u), hi = __builtin_amdgcn_perm(b[3], b[2], 0x04000c0cu);
+        c[g] = f.by == 0.0f ? 0u : lo | hi;
     }
-    const uint32_t lo = __builtin_amdgcn_perm(c[1], c[0], 0x0c0c0400u) | __builtin_amdgcn_perm(c[3], c[2], 0x04000c0cu);
-    const uint32_t hi = __builtin_amdgcn_perm(c[5], c[4], 0x0c0c0400u) | __builtin_amdgcn_perm(c[7], c[6], 0x04000c0cu);
-    return make_uint2(lo, hi);
+    return make_uint4(c[0], c[1], c[2], c[3]);
 }
 
 // Codes lie in blocks of 16 rows x 64 features, 1 KB each: [row / 16][feature / 64][feature % 64 / 16][row % 16][feature % 16].  A block is what a
 // wave's matrix instruction takes, 16 bytes a lane, so that every load of codes is one run of memory.
 __host__ __device__ __forceinline__ int64_t block_of(int64_t row16, int64_t feature64, int blocks) { return (row16 * blocks + feature64) << 10; }
 
-// A workgroup has ROWS rows at a time, THREADS threads each.  Rows of up to THREADS * UNITS * 16 values are read once, longer ones twice (the second
-// time from a cache).  Bound by memory; ROWS is large where there are many rows, so that what neighbours write makes whole lines.
+// A workgroup has ROWS rows, THREADS threads each.  Rows of up to THREADS * UNITS * 16 values are read once, longer ones twice (the second
+// time from a cache).  Bound by the round trips to memory.
 template <int type, int ROWS, int UNITS>
 __global__ __launch_bounds__(ROW_THREADS) void encode_rows_kernel(const void *__restrict__ x, int64_t ldx, int64_t n, int d, int blocks,
                                                                   int8_t *__restrict__ codes, float *__restrict__ scales)
@@ -70,30 +123,17 @@ __global__ __launch_bounds__(ROW_THREADS) void encode_rows_kernel(const void *__
     const int64_t row = (int64_t)blockIdx.x * ROWS + mine, from = row < n ? row : n - 1;
     const int64_t at = from * ldx;
     const int units = 4 * blocks;
-    Raw8 raw[UNITS][2];
-    float v[8];
-    uint32_t most = 0, c[4];
-    const auto load = [&](int u, Raw8 *r) {
-        r[0] = kv_load8(x, type, at + 16 * u, d - 16 * u);
-        r[1] = kv_load8(x, type, at + 16 * u + 8, d - 16 * u - 8);
-    };
-    const auto look = [&](int u, const Raw8 *r) {
+    Run16<type> raw[UNITS], r;
+    uint32_t most = 0;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            kv_floats8(r[h], type, d - 16 * u - 8 * h, v);
-            const uint32_t b = magnitude8(v);
-            most = b > most ? b : most;
-        }
-    };
+    for (int i = 0; i < UNITS; ++i) raw[i].load(x, at + 16 * (t + i * THREADS), d - 16 * (t + i * THREADS));
 #pragma unroll
-    for (int i = 0; i < UNITS; ++i) load(t + i * THREADS, raw[i]);
-#pragma unroll
-    for (int i = 0; i < UNITS; ++i) look(t + i * THREADS, raw[i]);
+    for (int i = 0; i < UNITS; ++i) raw[i].most(most);
     for (int u = t + UNITS * THREADS; u < units; u += THREADS) {
-        Raw8 r[2];
-        load(u, r);
-        look(u, r);
+        r.load(x, at + 16 * u, d - 16 * u);
+        r.most(most);
     }
+    most = Run16<type>::magnitude(most);
     most = (uint32_t)wave_max_i32((int)most);
     if (THREADS > 64) {
         __shared__ uint32_t waves[ROW_THREADS / 64];
@@ -109,23 +149,53 @@ __global__ __launch_bounds__(ROW_THREADS) void encode_rows_kernel(const void *__
     const RowFactor f = row_factor(most);
     if (t == 0) scales[row] = f.scale;
     int8_t *const out = codes + block_of(row >> 4, 0, blocks) + 16 * (row & 15);
-    const auto store = [&](int u, const Raw8 *r) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            kv_floats8(r[h], type, d - 16 * u - 8 * h, v);
-            const uint2 w = row_codes8(v, f);
-            c[2 * h] = w.x;
-            c[2 * h + 1] = w.y;
-        }
-        *reinterpret_cast<uint4 *>(out + 256 * (int64_t)u) = make_uint4(c[0], c[1], c[2], c[3]);
+    for (int i = 0; i < UNITS; ++i)
+        if (t + i * THREADS < units) *reinterpret_cast<uint4 *>(out + 256 * (int64_t)(t + i * THREADS)) = row_codes16(raw[i], f);
+    for (int u = t + UNITS * THREADS; u < units; u += THREADS) {
+        r.load(x, at + 16 * u, d - 16 * u);
+        *reinterpret_cast<uint4 *>(out + 256 * (int64_t)u) = row_codes16(r, f);
+    }
+}
+
+// Many rows: a wave to each of a workgroup's 8, two workgroups to a CU, so that one reads while the other writes.  The codes of 1024 features at a time
+// are turned over in LDS and leave as whole lines (8 rows x 16 features are 128 bytes of a block).
+constexpr int MANY_ROWS = 8, MANY_THREADS = 64 * MANY_ROWS;
+template <int type, int UNITS>
+__global__ __launch_bounds__(MANY_THREADS, 4) void encode_many_kernel(const void *__restrict__ x, int64_t ldx, int64_t n, int d, int blocks,
+                                                                      int8_t *__restrict__ codes, float *__restrict__ scales)
+{
+    __shared__ uint4 turn[2][64 * MANY_ROWS];
+    const int lane = threadIdx.x & 63, mine = threadIdx.x >> 6, units = 4 * blocks;
+    const int64_t row0 = (int64_t)blockIdx.x * MANY_ROWS, row = row0 + mine;
+    const int64_t at = (row < n ? row : n - 1) * ldx;
+    Run16<type> raw[UNITS], r;
+    uint32_t most = 0;
+#pragma unroll
+    for (int i = 0; i < UNITS; ++i) raw[i].load(x, at + 16 * (lane + 64 * i), d - 16 * (lane + 64 * i));
+#pragma unroll
+    for (int i = 0; i < UNITS; ++i) raw[i].most(most);
+    for (int u = lane + 64 * UNITS; u < units; u += 64) {
+        r.load(x, at + 16 * u, d - 16 * u);
+        r.most(most);
+    }
+    const RowFactor f = row_factor((uint32_t)wave_max_i32((int)Run16<type>::magnitude(most)));
+    if (lane == 0 && row < n) scales[row] = f.scale;
+    int8_t *const out = codes + block_of(row0 >> 4, 0, blocks) + 16 * (row0 & 8);
+    const int to_unit = threadIdx.x / MANY_ROWS, to_row = threadIdx.x % MANY_ROWS;
+    const auto store = [&](int i, const Run16<type> &from) {
+        uint4 *const t = turn[i & 1];
+        t[lane * MANY_ROWS + (mine ^ (lane & 7))] = row_codes16(from, f);
+        __syncthreads();
+        if (64 * i + to_unit < units && row0 + to_row < n)
+            *reinterpret_cast<uint4 *>(out + 256 * (int64_t)(64 * i + to_unit) + 16 * to_row) = t[to_unit * MANY_ROWS + (to_row ^ (to_unit & 7))];
     };
 #pragma unroll
     for (int i = 0; i < UNITS; ++i)
-        if (t + i * THREADS < units) store(t + i * THREADS, raw[i]);
-    for (int u = t + UNITS * THREADS; u < units; u += THREADS) {
-        Raw8 r[2];
-        load(u, r);
-        store(u, r);
+        if (64 * i < units) store(i, raw[i]);
+    for (int i = UNITS; 64 * i < units; ++i) {
+        r.load(x, at + 16 * (lane + 64 * i), d - 16 * (lane + 64 * i));
+        store(i, r);
     }
 }
 
@@ -195,16 +265,16 @@ __global__ __launch_bounds__(STREAM_THREADS, stream_waves_per_simd(MT, CT, FUSED
     __shared__ Scale own_scale[FUSED_ROWS];
 
     // FUSED: the rows' values first, so that waiting for them is not waiting for the weights
-    constexpr int UNITS = FUSED ? FUSED_VALUES / (8 * STREAM_THREADS) : 1;
-    Raw8 raw[UNITS];
+    constexpr int UNITS = FUSED ? FUSED_VALUES / (16 * STREAM_THREADS) : 1;
+    Run16<type> raw[UNITS];
     const int row_threads = FUSED ? STREAM_THREADS / g.rows : 1, row = FUSED ? (int)threadIdx.x / row_threads : 0;
     const int me = threadIdx.x - row * row_threads;
     if (FUSED) {
         const int from = row < g.m ? row : g.m - 1;
 #pragma unroll
         for (int i = 0; i < UNITS; ++i) {
-            const int u = 8 * (me + i * row_threads);
-            raw[i] = kv_load8(g.raw, type, from * g.ld_raw + u, g.d - u);
+            const int u = 16 * (me + i * row_threads);
+            raw[i].load(g.raw, from * g.ld_raw + u, g.d - u);
         }
     }
 
@@ -246,14 +316,9 @@ __global__ __launch_bounds__(STREAM_THREADS, stream_waves_per_simd(MT, CT, FUSED
 
     if (FUSED) {
         uint32_t most = 0;
-        float v[8];
 #pragma unroll
-        for (int i = 0; i < UNITS; ++i) {
-            kv_floats8(raw[i], type, g.d - 8 * (me + i * row_threads), v);
-            const uint32_t b = magnitude8(v);
-            most = b > most ? b : most;
-        }
-        most = (uint32_t)wave_max_i32((int)most);
+        for (int i = 0; i < UNITS; ++i) raw[i].most(most);
+        most = (uint32_t)wave_max_i32((int)Run16<type>::magnitude(most));
         if (lane == 0) magnitude[wave] = most;
         lds_barrier();
         const int waves = STREAM_WAVES / g.rows, first = wave / waves * waves;
@@ -263,11 +328,8 @@ __global__ __launch_bounds__(STREAM_THREADS, stream_waves_per_simd(MT, CT, FUSED
         int8_t *const to = own + row * (bytes + FUSED_PAD);
 #pragma unroll
         for (int i = 0; i < UNITS; ++i) {
-            const int u = 8 * (me + i * row_threads);
-            if (u < bytes) {
-                kv_floats8(raw[i], type, g.d - u, v);
-                *reinterpret_cast<uint2 *>(to + u) = row_codes8(v, f);
-            }
+            const int u = 16 * (me + i * row_threads);
+            if (u < bytes) *reinterpret_cast<uint4 *>(to + u) = row_codes16(raw[i], f);
         }
         lds_barrier();
     }
@@ -525,7 +587,7 @@ hipError_t launch_encode_rows(const void *x, int64_t ldx, int type, int64_t n, i
     const int blocks = row_blocks(d);
     const auto go = [&](auto t) {
         constexpr int T = decltype(t)::value, WIDE = T == LPQ_TYPE_F32 ? 2 : 1;
-        if (n >= 4096) encode_rows_kernel<T, 16, 8 / WIDE><<<dim3((unsigned)ceil_div(n, (int64_t)16)), ROW_THREADS, 0, st>>>(x, ldx, n, d, blocks, codes, scales);
+        if (n >= 2048) encode_many_kernel<T, 8 / WIDE><<<dim3((unsigned)ceil_div(n, (int64_t)MANY_ROWS)), MANY_THREADS, 0, st>>>(x, ldx, n, d, blocks, codes, scales);
         else if (n >= 1024 || d <= 4096) encode_rows_kernel<T, 4, 4 / WIDE><<<dim3((unsigned)ceil_div(n, (int64_t)4)), ROW_THREADS, 0, st>>>(x, ldx, n, d, blocks, codes, scales);
         else encode_rows_kernel<T, 1, 2><<<dim3((unsigned)n), ROW_THREADS, 0, st>>>(x, ldx, n, d, blocks, codes, scales);
     };
