@@ -507,6 +507,12 @@ int lpq_probe_mfma_i8(const void *operands_dev, size_t operand_bytes, int iters,
 int lpq_probe_scan_core(const void *operands_dev, size_t operand_bytes, int stages, double *tops, void *stream);
 int lpq_probe_stream(const void *src_dev, size_t bytes, int mode, int reps, double *gbps, void *stream);
 
+/* How lpq_matmul_i8 goes about a product: [0] tokens and [1] channels of a workgroup, [2] parts that the features are dealt out in (0: few
+ * rows, whose weights go past LDS), [3] 1 where lpq_linear8 makes the codes in the same launch.  Needs no device.  LPQ_EINVAL /
+ * LPQ_ERANGE as lpq_matmul_i8; out_count < LPQ_LINEAR8_INFO_COUNT. */
+#define LPQ_LINEAR8_INFO_COUNT 4
+int lpq_linear8_plan_info(int64_t m, int64_t n, int d, int64_t *out, int out_count);
+
 /* Diagnostics of the collecting variant: after a search with the same (idx, nq, k, metric) and
  * workspace has finished, the number of queries whose candidates did not fit and that were
  * searched again (0 when the search did not use the collecting variant) and the

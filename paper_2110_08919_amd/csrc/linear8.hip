@@ -3,8 +3,8 @@
 //   code[i][k] = rint(x[i][k] (127 / A_i)),  scale[i] = A_i / 127,  A_i = max_k |x[i][k]|
 //   y[i][c]    = (sum_k a[i][k] b[c][k]) sa[i] sb[c] + bias[c],      the sums exact in 32 bits
 #include <algorithm>
+#include <cmath>
 #include <type_traits>
-#include <stdlib.h>
 
 #include "kv_internal.h"
 #include "linear8_internal.h"
@@ -225,7 +225,7 @@ __device__ __forceinline__ void lds_barrier()
 constexpr int STREAM_WAVES = 8, STREAM_THREADS = 64 * STREAM_WAVES, STREAM_K = 128;
 constexpr int FUSED_VALUES = 16384;           // values of x that a workgroup makes codes of: 32 a thread
 constexpr int FUSED_ROWS = 8, FUSED_PAD = 16;
-constexpr int STREAM_ROWS = 128;
+constexpr int STREAM_ROWS = 128, CUS = 256;
 
 struct StreamWork {
     const int8_t *x, *w;
@@ -248,14 +248,17 @@ __device__ __forceinline__ Buffer codes_buffer(const int8_t *p, int64_t bytes)
 }
 __device__ __forceinline__ v4i load16(Buffer b, int at) { return __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(b, at, 0, 0)); }
 
-constexpr int stream_waves_per_simd(int mt, int ct, bool wide) { return mt + ct <= 5 && !wide ? 4 : 2; }
-constexpr int stream_depth(int mt, int ct) { return mt + ct <= 3 ? 4 : 2; }
+constexpr int stream_waves_per_simd(int mt, int ct) { return (mt + ct <= 4 && mt < 3) || (ct == 1 && mt == 4) ? 4 : 2; }
+// Runs of weights and of codes in flight.
+constexpr int stream_depth(int mt, int ct) { return mt + ct <= 3 || ct == 1 ? 4 : 2; }
+constexpr int stream_depth_x(int mt, int ct) { return mt + ct <= 3 ? 4 : mt >= 4 ? 1 : 2; }
+constexpr int stream_channels(int mt) { return mt <= 4 ? 4 : mt <= 6 ? 3 : 2; }      // most tiles of 16 channels: the sums fit LDS
 
 template <int MT, int CT, bool FUSED, int type>
-__global__ __launch_bounds__(STREAM_THREADS, stream_waves_per_simd(MT, CT, FUSED && type == LPQ_TYPE_F32 && CT > 1)) void linear8_stream_kernel(StreamWork g)
+__global__ __launch_bounds__(STREAM_THREADS, stream_waves_per_simd(MT, CT)) void linear8_stream_kernel(StreamWork g)
 {
     static_assert(!FUSED || MT == 1);
-    constexpr int DEPTH = stream_depth(MT, CT), ENDS = (CT * MT + STREAM_WAVES - 1) / STREAM_WAVES;
+    constexpr int DEPTH = stream_depth(MT, CT), DEPTH_X = stream_depth_x(MT, CT), ENDS = (CT * MT + STREAM_WAVES - 1) / STREAM_WAVES;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int in_tile = lane & 15, chunk = 16 * (lane >> 4);
     const int64_t ch0 = (int64_t)blockIdx.x * 16 * CT;
@@ -283,21 +286,27 @@ __global__ __launch_bounds__(STREAM_THREADS, stream_waves_per_simd(MT, CT, FUSED
     const Buffer wb = codes_buffer(g.w + (ch0 >> 4) * tile_bytes, (tiles < CT ? tiles : CT) * tile_bytes);
     const Buffer xb = FUSED ? wb : codes_buffer(g.x, (int64_t)((g.m + 15) >> 4) * tile_bytes);
     const int own_at = FUSED ? (in_tile < g.m ? in_tile : g.m - 1) * (bytes + FUSED_PAD) + chunk : 0;
-    v4i fw[DEPTH][CT][2], fx[DEPTH][MT][2];
-    const auto load = [&](int slot, int run) {
+    v4i fw[DEPTH][CT][2], fx[DEPTH_X][MT][2];
+    const auto load_x = [&](int slot, int run) {
         const int at = (run < g.runs ? run * (16 * STREAM_K) : 1 << 30) + 16 * lane;
+        if (!FUSED) {
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            if (!FUSED) {
+            for (int k = 0; k < 2; ++k)
 #pragma unroll
                 for (int j = 0; j < MT; ++j) fx[slot][j][k] = load16(xb, at + j * tile_bytes + 1024 * k);
-            }
-#pragma unroll
-            for (int i = 0; i < CT; ++i) fw[slot][i][k] = load16(wb, at + i * tile_bytes + 1024 * k);
         }
     };
+    const auto load_w = [&](int slot, int run) {
+        const int at = (run < g.runs ? run * (16 * STREAM_K) : 1 << 30) + 16 * lane;
 #pragma unroll
-    for (int i = 0; i < DEPTH; ++i) load(i, wave + i * STREAM_WAVES);
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int i = 0; i < CT; ++i) fw[slot][i][k] = load16(wb, at + i * tile_bytes + 1024 * k);
+    };
+#pragma unroll
+    for (int i = 0; i < DEPTH; ++i) load_w(i, wave + i * STREAM_WAVES);
+#pragma unroll
+    for (int i = 0; i < DEPTH_X; ++i) load_x(i, wave + i * STREAM_WAVES);
 
     // what the results are multiplied by, long before it is needed
     float end_w[4], end_bias[4], end_x;
@@ -342,19 +351,20 @@ __global__ __launch_bounds__(STREAM_THREADS, stream_waves_per_simd(MT, CT, FUSED
     for (int run0 = wave; run0 < g.runs; run0 += DEPTH * STREAM_WAVES) {
 #pragma unroll
         for (int s = 0; s < DEPTH; ++s) {
-            const int run = run0 + s * STREAM_WAVES;
+            const int run = run0 + s * STREAM_WAVES, sx = s % DEPTH_X;
             if (FUSED) {                   // past the end: any codes, times weights of zero
                 const int at = run < g.runs ? run * STREAM_K : 0;
 #pragma unroll
-                for (int k = 0; k < 2; ++k) fx[s][0][k] = *reinterpret_cast<const v4i *>(own + own_at + at + 64 * k);
+                for (int k = 0; k < 2; ++k) fx[sx][0][k] = *reinterpret_cast<const v4i *>(own + own_at + at + 64 * k);
             }
 #pragma unroll
             for (int k = 0; k < 2; ++k)
 #pragma unroll
                 for (int i = 0; i < CT; ++i)
 #pragma unroll
-                    for (int j = 0; j < MT; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fw[s][i][k], fx[s][j][k], acc[i][j], 0, 0, 0);
-            load(s, run + DEPTH * STREAM_WAVES);
+                    for (int j = 0; j < MT; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fw[s][i][k], fx[sx][j][k], acc[i][j], 0, 0, 0);
+            load_x(sx, run + DEPTH_X * STREAM_WAVES);
+            load_w(s, run + DEPTH * STREAM_WAVES);
         }
     }
 #pragma unroll
@@ -483,10 +493,10 @@ __global__ __launch_bounds__(TILE_THREADS) void linear8_tile_kernel(TileWork g)
             // reads in the first half of them, so that none is waited for
 #pragma unroll
             for (int r = 2 * k * READS / STEPS; r < 2 * (k + 1) * READS / STEPS && r < READS; ++r) operand(next_slot, half ^ 1, r);
-            if (copy && 2 * k >= STEPS) {
-                constexpr int FROM = STEPS / 2;
+            constexpr int FROM = STEPS / 2, REST = STEPS - FROM;
+            if (copy && k >= FROM) {
 #pragma unroll
-                for (int c = (k - FROM) * COPIES / FROM; c < (k - FROM + 1) * COPIES / FROM; ++c) copies.one(c + (half ? 0 : COPIES), copy_slot);
+                for (int c = (k - FROM) * COPIES / REST; c < (k - FROM + 1) * COPIES / REST; ++c) copies.one(c + (half ? 0 : COPIES), copy_slot);
             }
         }
         __builtin_amdgcn_sched_barrier(0);
@@ -579,6 +589,31 @@ __global__ __launch_bounds__(TILE_THREADS) void linear8_tile_kernel(TileWork g)
     }
 }
 
+// Sums of parts, in order, to results: 4 channels of a token a thread.
+template <int TYPE>
+__global__ __launch_bounds__(TILE_THREADS) void linear8_join_kernel(TileWork g, unsigned groups)
+{
+    const int64_t u = (int64_t)blockIdx.x * TILE_THREADS + threadIdx.x, token = u / groups;
+    if (token >= g.m) return;
+    const int64_t c = 4 * (u - token * groups), each = g.m * (4 * (int64_t)groups);
+    const int *const from = g.sums + token * (4 * (int64_t)groups) + c;
+    int t[4] = {0, 0, 0, 0};
+#pragma unroll 4
+    for (int p = 0; p < g.parts; ++p) {
+        const int4 v = *reinterpret_cast<const int4 *>(from + p * each);
+        t[0] += v.x; t[1] += v.y; t[2] += v.z; t[3] += v.w;
+    }
+    const Scale a = split_scale(g.sx[token]);
+    float y[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const int64_t ce = c + e < g.n ? c + e : g.n - 1;
+        y[e] = scaled(t[e], a, split_scale(g.sw[ce]));
+        if (g.out.bias) y[e] += g.out.bias[ce];
+    }
+    kv_store<4>(g.out.p, TYPE, token * g.out.ld + c, (int)(g.n - c < 4 ? g.n - c : 4), y);
+}
+
 }  // namespace
 
 hipError_t launch_encode_rows(const void *x, int64_t ldx, int type, int64_t n, int d, int8_t *codes, float *scales, hipStream_t st)
@@ -597,71 +632,80 @@ hipError_t launch_encode_rows(const void *x, int64_t ldx, int type, int64_t n, i
     return hipGetLastError();
 }
 
+// What takes the shortest time by these estimates, in microseconds beside what all have in common (measured over 33 to 8192 rows, 1024 to 32 768
+// channels and 1024 to 16 384 features, within a fifth; k: workgroups to a CU).  The weights come at 4.5 TB/s at best.  Few rows: what a workgroup
+// reads at 60 GB/s; of tiles of 16 channels as many as leave one generation of workgroups (48 rows, 11 111 x 4100: 1, 2, 3, 4 tiles 23.7, 22.8,
+// 19.1, 20.4 us; 64 rows, 16 384 x 8192: 48, 42.8, 46.6, 36.1).  Tiles: a stage takes 0.21 us (64 x 64), 0.33 us (128 x 128) and 0.83 us (256 x
+// 256) alone on its CU, and more together with others.  Parts cost a launch and 0.42 us for a MB of sums (128 rows, 1024 x 16 384: tiles of 64 in 1, 2, 4, 8
+// parts 59.6, 37.5, 25.4, 21.1 us, few rows' way 40.5).
 Linear8Plan linear8_plan(int64_t m, int64_t n, int d)
 {
-    if (getenv("LIN_CT") && m <= STREAM_ROWS) { const int tiles = (int)ceil_div(m, (int64_t)16), rows = 16 * (tiles == 5 ? 6 : tiles == 7 ? 8 : tiles);
-        return {rows, 16 * std::min(atoi(getenv("LIN_CT")), rows <= 32 ? 4 : 2), 0, 0}; }
+    const double stages = (double)ceil_div(d, TILE_K);
+    Linear8Plan best = {0, 0, 0, 0};
+    const double weights = n * 64 * stages / 4.5e6;
+    double least = INFINITY;
     if (m <= STREAM_ROWS) {
-        const int tiles = (int)ceil_div(m, (int64_t)16), rows = 16 * (tiles == 5 ? 6 : tiles == 7 ? 8 : tiles);
-        const int64_t groups = ceil_div(n, (int64_t)16);
-        return {rows, rows > 16 && groups >= 512 ? 32 : 16, 0, 0};
+        const int tiles = (int)ceil_div(m, (int64_t)16), mt = tiles == 5 ? 6 : tiles == 7 ? 8 : tiles;
+        const int ct = (int)std::min<int64_t>(stream_channels(mt), std::max<int64_t>(1, ceil_div(n, 16 * CUS)));
+        const double k = std::max(1.0, (double)n / (16 * ct) / CUS);
+        best = {16 * mt, 16 * ct, 0, 0};
+        if (mt <= 2) return best;
+        least = std::max(k * 1024 * (mt + ct) * stages / 60e3, weights);
     }
-    if (getenv("LIN_T") ? atoi(getenv("LIN_T")) == 4 : m >= 2048 && n >= 2048) return {256, 256, 1, 0};
-    return {128, 128, 1, 0};
+    for (const int size : {64, 128, 256}) {
+        const double tiles = (double)ceil_div(m, (int64_t)size) * ceil_div(n, (int64_t)size);
+        for (int parts = 1; parts <= (size == 256 ? 1 : 16) && 4 * parts <= std::max(stages, 4.0); parts *= 2) {
+            const double k = tiles * parts / CUS, per_part = ceil(stages / parts);
+            double t = size == 64 ? per_part * std::max(0.21, 0.125 * k) : size == 128 ? per_part * std::max(0.33, 0.1 + 0.28 * k)
+                                                                                       : ceil(k) * (12 + per_part * 0.83);
+            t = std::max(t, weights);
+            const double sums = (double)parts * m * round_up(n, 4) * 4;
+            if (parts > 1) t += 3 + 0.42e-6 * sums;
+            if (t >= least) continue;
+            least = t;
+            best = {size, size, parts, parts > 1 ? (size_t)sums : 0};
+        }
+    }
+    if (best.parts > 1) {        // none of them empty
+        best.parts = (int)ceil_div((int)stages, (int)ceil_div((int)stages, best.parts));
+        best.bytes = (size_t)best.parts * m * round_up(n, 4) * 4;
+    }
+    return best;
 }
 
 bool linear8_fused(int64_t m, int d) { return m <= FUSED_ROWS && next_pow2((int)m) * 64 * row_blocks(d) <= FUSED_VALUES; }
 
-template <int MT, int CT>
-static void stream(const StreamWork &g, dim3 grid, hipStream_t st)
-{
-    linear8_stream_kernel<MT, CT, false, 0><<<grid, STREAM_THREADS, 0, st>>>(g);
-}
 template <int MT>
-static void stream_channels(const StreamWork &g, int channels, dim3 grid, hipStream_t st)
+static void stream(const StreamWork &g, int channels, dim3 grid, hipStream_t st)
 {
-    if (channels == 16) stream<MT, 1>(g, grid, st);
-    else if (channels == 32) stream<MT, 2>(g, grid, st);
-    else stream<MT, 4>(g, grid, st);
-}
-
-template <int MT>
-static void stream_two(const StreamWork &g, int channels, dim3 grid, hipStream_t st)
-{
-    if (channels == 16) stream<MT, 1>(g, grid, st);
-    else stream<MT, 2>(g, grid, st);
+    constexpr int MOST = stream_channels(MT);
+    if (channels == 16) linear8_stream_kernel<MT, 1, false, 0><<<grid, STREAM_THREADS, 0, st>>>(g);
+    else if (channels == 32) linear8_stream_kernel<MT, 2, false, 0><<<grid, STREAM_THREADS, 0, st>>>(g);
+    else if (channels == 48) linear8_stream_kernel<MT, MOST < 3 ? MOST : 3, false, 0><<<grid, STREAM_THREADS, 0, st>>>(g);
+    else linear8_stream_kernel<MT, MOST, false, 0><<<grid, STREAM_THREADS, 0, st>>>(g);
 }
 
 static hipError_t launch_stream(const StreamWork &g, const Linear8Plan &plan, hipStream_t st)
 {
     const dim3 grid((unsigned)ceil_div(g.n, (int64_t)plan.channels));
     switch (plan.rows) {
-    case 16: stream_channels<1>(g, plan.channels, grid, st); break;
-    case 32: stream_channels<2>(g, plan.channels, grid, st); break;
-    case 48: stream_two<3>(g, plan.channels, grid, st); break;
-    case 64: stream_two<4>(g, plan.channels, grid, st); break;
-    case 96: stream_two<6>(g, plan.channels, grid, st); break;
-    default: stream_two<8>(g, plan.channels, grid, st); break;
+    case 16: stream<1>(g, plan.channels, grid, st); break;
+    case 32: stream<2>(g, plan.channels, grid, st); break;
+    case 48: stream<3>(g, plan.channels, grid, st); break;
+    case 64: stream<4>(g, plan.channels, grid, st); break;
+    case 96: stream<6>(g, plan.channels, grid, st); break;
+    default: stream<8>(g, plan.channels, grid, st); break;
     }
     return hipGetLastError();
 }
 
-template <int TYPE>
-static void fused(const StreamWork &g, int channels, dim3 grid, hipStream_t st)
-{
-    if (channels == 16) linear8_stream_kernel<1, 1, true, TYPE><<<grid, STREAM_THREADS, 0, st>>>(g);
-    else if (channels == 32) linear8_stream_kernel<1, 2, true, TYPE><<<grid, STREAM_THREADS, 0, st>>>(g);
-    else linear8_stream_kernel<1, 4, true, TYPE><<<grid, STREAM_THREADS, 0, st>>>(g);
-}
-
-hipError_t launch_linear8_fused(const void *x, int64_t ldx, int64_t m, const RowCodes &w, int d, const Linear8Out &out, const Linear8Plan &plan,
-                                hipStream_t st)
+hipError_t launch_linear8_fused(const void *x, int64_t ldx, int64_t m, const RowCodes &w, int d, const Linear8Out &out, hipStream_t st)
 {
     const StreamWork g = {nullptr, w.codes, nullptr, w.scales, (int)m, w.n, row_blocks(d) / 2, out, x, ldx, d, next_pow2((int)m)};
-    const dim3 grid((unsigned)ceil_div(w.n, (int64_t)plan.channels));
-    if (out.type == LPQ_TYPE_F32) fused<LPQ_TYPE_F32>(g, plan.channels, grid, st);
-    else if (out.type == LPQ_TYPE_F16) fused<LPQ_TYPE_F16>(g, plan.channels, grid, st);
-    else fused<LPQ_TYPE_BF16>(g, plan.channels, grid, st);
+    const dim3 grid((unsigned)ceil_div(w.n, (int64_t)16));
+    if (out.type == LPQ_TYPE_F32) linear8_stream_kernel<1, 1, true, LPQ_TYPE_F32><<<grid, STREAM_THREADS, 0, st>>>(g);
+    else if (out.type == LPQ_TYPE_F16) linear8_stream_kernel<1, 1, true, LPQ_TYPE_F16><<<grid, STREAM_THREADS, 0, st>>>(g);
+    else linear8_stream_kernel<1, 1, true, LPQ_TYPE_BF16><<<grid, STREAM_THREADS, 0, st>>>(g);
     return hipGetLastError();
 }
 
@@ -670,13 +714,26 @@ hipError_t launch_linear8(const RowCodes &x, const RowCodes &w, int d, const Lin
     if (plan.parts == 0)
         return launch_stream({x.codes, w.codes, x.scales, w.scales, (int)x.n, w.n, row_blocks(d) / 2, out, nullptr, 0, d, 0}, plan, st);
     const int stages = (int)ceil_div(d, TILE_K);
-    const TileWork g = {x.codes, w.codes, x.scales, w.scales, x.n, w.n, row_blocks(d), stages, stages, (int)ceil_div(x.n, (int64_t)plan.rows),
-                  (int)ceil_div(w.n, (int64_t)plan.channels), plan.parts, out, static_cast<int *>(workspace)};
+    const TileWork g = {x.codes, w.codes, x.scales, w.scales, x.n, w.n, row_blocks(d), stages, (int)ceil_div(stages, plan.parts),
+                        (int)ceil_div(x.n, (int64_t)plan.rows), (int)ceil_div(w.n, (int64_t)plan.channels), plan.parts, out,
+                        static_cast<int *>(workspace)};
     const dim3 grid((unsigned)(g.tiles_m * g.tiles_n * plan.parts));
+    if (plan.parts > 1) {
+        if (plan.rows == 128) linear8_tile_kernel<2, 2, 0, true><<<grid, TILE_THREADS, 0, st>>>(g);
+        else linear8_tile_kernel<1, 1, 0, true><<<grid, TILE_THREADS, 0, st>>>(g);
+    }
     const auto go = [&](auto t) {
         constexpr int T = decltype(t)::value;
-        if (plan.rows == 256) linear8_tile_kernel<4, 4, T, false><<<grid, TILE_THREADS, 0, st>>>(g);
-        else linear8_tile_kernel<2, 2, T, false><<<grid, TILE_THREADS, 0, st>>>(g);
+        if (plan.parts > 1) {
+            const int64_t groups = ceil_div(w.n, (int64_t)4);
+            linear8_join_kernel<T><<<dim3((unsigned)ceil_div(x.n * groups, (int64_t)TILE_THREADS)), TILE_THREADS, 0, st>>>(g, (unsigned)groups);
+        } else if (plan.rows == 256) {
+            linear8_tile_kernel<4, 4, T, false><<<grid, TILE_THREADS, 0, st>>>(g);
+        } else if (plan.rows == 128) {
+            linear8_tile_kernel<2, 2, T, false><<<grid, TILE_THREADS, 0, st>>>(g);
+        } else {
+            linear8_tile_kernel<1, 1, T, false><<<grid, TILE_THREADS, 0, st>>>(g);
+        }
     };
     if (out.type == LPQ_TYPE_F32) go(std::integral_constant<int, LPQ_TYPE_F32>());
     else if (out.type == LPQ_TYPE_F16) go(std::integral_constant<int, LPQ_TYPE_F16>());

@@ -137,9 +137,8 @@ extern "C" int lpq_linear8(const void *x_dev, int64_t ldx, int type, int64_t m, 
     if (rc) return rc;
     const Linear8Out out = {out_dev, ldo, type, bias_dev};
     const RowCodes weights = {codes_dev, scales_dev, n};
-    const Linear8Plan plan = linear8_plan(m, n, d);
     if (linear8_fused(m, d)) {
-        const hipError_t e = launch_linear8_fused(x_dev, ldx, m, weights, d, out, plan, (hipStream_t)stream);
+        const hipError_t e = launch_linear8_fused(x_dev, ldx, m, weights, d, out, (hipStream_t)stream);
         return e == hipSuccess ? LPQ_OK : hip_fail(e, "lpq_linear8");
     }
     char *const space = static_cast<char *>(workspace_dev);
@@ -147,6 +146,22 @@ extern "C" int lpq_linear8(const void *x_dev, int64_t ldx, int type, int64_t m, 
     float *const row_scales = reinterpret_cast<float *>(space + s.scales);
     hipError_t e = launch_encode_rows(x_dev, ldx, type, m, d, rows, row_scales, (hipStream_t)stream);
     if (e == hipSuccess)
-        e = launch_linear8({rows, row_scales, m}, weights, d, out, plan, space + s.parts, (hipStream_t)stream);
+        e = launch_linear8({rows, row_scales, m}, weights, d, out, linear8_plan(m, n, d), space + s.parts, (hipStream_t)stream);
     return e == hipSuccess ? LPQ_OK : hip_fail(e, "lpq_linear8");
+}
+
+extern "C" int lpq_linear8_plan_info(int64_t m, int64_t n, int d, int64_t *out, int out_count)
+{
+    if (!out || out_count < LPQ_LINEAR8_INFO_COUNT) return fail(LPQ_EINVAL, "out must hold LPQ_LINEAR8_INFO_COUNT values");
+    int rc = check_features(d);
+    if (!rc && (m < 1 || n < 1)) rc = fail(LPQ_EINVAL, "%lld rows, %lld channels", (long long)m, (long long)n);
+    if (!rc && (m >= (int64_t(1) << 31) || n >= (int64_t(1) << 31))) rc = fail(LPQ_ERANGE, "%lld rows, %lld channels", (long long)m, (long long)n);
+    if (!rc) rc = check_product(m, n);
+    if (rc) return rc;
+    const Linear8Plan p = linear8_plan(m, n, d);
+    out[0] = p.rows;
+    out[1] = p.channels;
+    out[2] = p.parts;
+    out[3] = linear8_fused(m, d);
+    return LPQ_OK;
 }

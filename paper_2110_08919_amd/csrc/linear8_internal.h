@@ -35,8 +35,7 @@ Linear8Plan linear8_plan(int64_t m, int64_t n, int d);
 hipError_t launch_encode_rows(const void *x, int64_t ldx, int type, int64_t n, int d, int8_t *codes, float *scales, hipStream_t st);
 // Few rows, whose codes the product's own kernel makes.
 bool linear8_fused(int64_t m, int d);
-hipError_t launch_linear8_fused(const void *x, int64_t ldx, int64_t m, const RowCodes &w, int d, const Linear8Out &out, const Linear8Plan &plan,
-                                hipStream_t st);
+hipError_t launch_linear8_fused(const void *x, int64_t ldx, int64_t m, const RowCodes &w, int d, const Linear8Out &out, hipStream_t st);
 hipError_t launch_linear8(const RowCodes &x, const RowCodes &w, int d, const Linear8Out &out, const Linear8Plan &plan, void *workspace, hipStream_t st);
 
 }  // namespace lpq

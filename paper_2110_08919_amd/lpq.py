@@ -101,6 +101,7 @@ def lib() -> C.CDLL:
             "lpq_matmul_i8": (i32, [vp, vp, i64, vp, vp, i64, i32, vp, vp, i64, i32, vp, C.c_size_t, vp]),
             "lpq_linear8_workspace_bytes": (C.c_size_t, [i64, i64, i32]),
             "lpq_linear8": (i32, [vp, i64, i32, i64, vp, vp, i64, i32, vp, vp, i64, vp, C.c_size_t, vp]),
+            "lpq_linear8_plan_info": (i32, [i64, i64, i32, C.POINTER(i64), i32]),
             "lpq_last_error": (C.c_char_p, []),
         }
         for name, (res, args) in sig.items():
@@ -175,6 +176,16 @@ def search_maxima_info(d: int, bits: int, packed: bool, n_items: int, nq: int, k
     """lpq_search_maxima_info: how such a search goes by group maxima, MAXIMA_INFO_COUNT zeros where it does not (no device needed)."""
     out = (C.c_int64 * MAXIMA_INFO_COUNT)()
     _check(lib().lpq_search_maxima_info(d, bits, 1 if packed else 0, n_items, nq, k, out, MAXIMA_INFO_COUNT))
+    return list(out)
+
+
+LINEAR8_INFO_COUNT = 4
+
+
+def linear8_plan_info(m: int, n: int, d: int):
+    """lpq_linear8_plan_info: tokens and channels of a workgroup, parts of the features, whether codes are made on the way (no device needed)."""
+    out = (C.c_int64 * LINEAR8_INFO_COUNT)()
+    _check(lib().lpq_linear8_plan_info(m, n, d, out, LINEAR8_INFO_COUNT))
     return list(out)
 
 

@@ -139,6 +139,36 @@ def test_layer(m, n, d, kind, with_bias):
     same(lpq.matmul_i8(lpq.encode_rows(x.cuda()), layer.weight, layer.bias, TYPES[kind]), product_of(a, sa, b, sb, bias, TYPES[kind]))
 
 
+# One product for every way that they go: tokens and channels of a workgroup, parts.
+WAYS = [(16, 16, 0, 9, 70, 2100), (16, 32, 0, 13, 4200, 300), (16, 48, 0, 16, 11_003, 260), (16, 64, 0, 10, 13_000, 100),
+        (32, 16, 0, 20, 600, 1400), (32, 32, 0, 32, 5001, 520), (32, 48, 0, 17, 12_000, 130), (32, 64, 0, 30, 12_400, 64),
+        (48, 16, 0, 35, 500, 1100), (48, 32, 0, 48, 4500, 400), (48, 48, 0, 41, 9000, 770), (48, 64, 0, 33, 12_345, 500),
+        (64, 16, 0, 50, 3900, 1000), (64, 32, 0, 64, 8100, 1030), (64, 48, 0, 49, 12_000, 2000), (64, 64, 0, 63, 13_000, 2100),
+        (96, 16, 0, 96, 4090, 2000), (96, 32, 0, 66, 8000, 3000), (96, 48, 0, 90, 9000, 4100),
+        (128, 16, 0, 128, 4000, 2000), (128, 32, 0, 100, 8000, 3100),
+        (64, 64, 1, 129, 333, 200), (64, 64, 1, 500, 900, 64), (128, 128, 1, 2000, 2100, 300), (128, 128, 1, 1111, 4097, 70),
+        (256, 256, 1, 3900, 4001, 2600), (64, 64, 2, 4000, 130, 3000), (64, 64, 4, 130, 61, 1500), (64, 64, 7, 130, 60, 2100),
+        (64, 64, 16, 131, 59, 6000), (128, 128, 2, 2000, 1001, 16_400), (128, 128, 4, 200, 4099, 8200), (128, 128, 8, 1100, 300, 16_400)]
+
+
+@pytest.mark.parametrize("rows,channels,parts,m,n,d", WAYS)
+def test_every_way_a_product_goes(rows, channels, parts, m, n, d):
+    from paper_2110_08919_amd import lpq
+    assert lpq.linear8_plan_info(m, n, d)[:3] == [rows, channels, parts]
+    for kind in ("bf16", "f32"):
+        x, w = make(m, d, kind, m).cuda(), make(n, d, kind, n + 1, 0.1).cuda()
+        bias = torch.randn(n, generator=torch.Generator().manual_seed(d)).cuda()
+        a, b = lpq.encode_rows(x), lpq.encode_rows(w)
+        sums = a.codes.double() @ b.codes.double().t().contiguous()          # whole numbers below 2^53
+        want = ((sums.float() * a.scales[:, None]) * b.scales + bias).to(TYPES[kind])
+        got = lpq.matmul_i8(a, b, bias, TYPES[kind])
+        assert torch.equal(got, want)
+        if kind == "bf16":
+            out = torch.full((m, n + 3), 5.0, dtype=TYPES[kind], device="cuda")
+            assert torch.equal(lpq.Linear8(w, bias)(x, out=out[:, 1:-2]), want)
+            assert (out[:, :1] == 5).all() and (out[:, -2:] == 5).all()
+
+
 @pytest.mark.parametrize("m,n", [(1, 3), (2, 40), (70, 33), (140, 130)])
 def test_the_largest_sums(m, n):
     """131 072 products of 127 by 127, and of 127 by -127: the longest rows, near both ends of 32 bits."""

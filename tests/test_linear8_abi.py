@@ -55,6 +55,31 @@ def test_refusals(L):
     assert b"workspace" in L.lpq_last_error()
 
 
+def test_which_way_products_go(L):
+    """Few rows past LDS, up to 4 tiles of channels where there are many; tiles that grow with the product; parts only where workgroups are few."""
+    from paper_2110_08919_amd import lpq
+    info = lpq.linear8_plan_info
+    assert info(1, 4096, 4096) == [16, 16, 0, 1] and info(8, 4096, 4096)[3] == 0 and info(8, 4096, 2048)[3] == 1 and info(1, 8, 16_385)[3] == 0
+    assert info(48, 11_111, 4100) == [48, 48, 0, 0] and info(33, 4096, 4096)[:3] == [48, 16, 0]
+    assert info(8192, 8192, 8192) == [256, 256, 1, 0] and info(1024, 4096, 4096) == [128, 128, 1, 0]
+    assert info(300, 100, 100)[2] == 1 and info(128, 1024, 16_384)[2] > 1
+    for m in (1, 16, 17, 33, 64, 65, 128, 129, 1000, 30_000):
+        for n in (1, 16, 500, 5000, 70_000):
+            for d in (1, 64, 65, 1000, 16_384, 131_072):
+                rows, channels, parts, fused = info(m, n, d)
+                stages = -(-d // 64)
+                if parts == 0:
+                    assert rows >= m and rows in (16, 32, 48, 64, 96, 128) and channels in (16, 32, 48, 64) and rows // 16 * channels // 16 <= 18
+                else:
+                    assert m > 32 and rows == channels and rows in (64, 128, 256) and (parts == 1 or rows < 256)
+                    assert (parts - 1) * -(-stages // parts) < stages          # no part is empty
+                    need = L.lpq_matmul_i8_workspace_bytes(m, n, d)
+                    assert need == (0 if parts == 1 else parts * m * -(-n // 4) * 16)
+    out = (C.c_int64 * 4)()
+    assert L.lpq_linear8_plan_info(1, 1, 1, out, 3) == lpq.EINVAL and L.lpq_linear8_plan_info(0, 1, 1, out, 4) == lpq.EINVAL
+    assert L.lpq_linear8_plan_info(1, 1, 1 << 18, out, 4) == lpq.ERANGE
+
+
 def test_binding_takes_device_rows_only():
     from paper_2110_08919_amd import lpq
     lpq.lib()
