@@ -49,8 +49,12 @@ typedef _Float16 v8h __attribute__((ext_vector_type(8)));
 
 constexpr int THREADS = 256, WAVES = 4;
 constexpr float NEG = -INFINITY;
-constexpr float HEADROOM = 2.0f;     // how far scores may pass the maximum before it moves (powers of two)
-constexpr float LIFT = 13.0f;        // weights are exp2(t - m + LIFT): at most 2^15, and fp16 holds them to 2^-37 of the largest
+constexpr float WEIGHT_TOP = 15.0f;  // weights are exp2(t - m + lift): at most 2^15
+// How far scores may pass the maximum before it moves (powers of two), and what weights are lifted by: HEADROOM + LIFT = WEIGHT_TOP.  By 2, fp16
+// holds weights to 2^-37 of the largest; masked calls of the 16-bit types have 6 and 2^-33, and the maximum hardly moves after a pair's
+// first tiles: TODO.
+__host__ __device__ constexpr float headroom(bool masked, int type) { return masked && type != LPQ_TYPE_F32 ? 6.0f : 2.0f; }
+__host__ __device__ constexpr float lift(bool masked, int type) { return WEIGHT_TOP - headroom(masked, type); }
 constexpr float FAR = 1024.0f;       // maxima beyond it are subtracted from the scores before these are multiplied by their scale
 constexpr float MAXIMUM = 0x1p-48f;  // maxima that go from wave to wave and from part to part are times this: finite for any query and scale
 __device__ __forceinline__ float lag(float m, float top) { return top == NEG ? 1.0f : __builtin_amdgcn_exp2f((m - top) * (1.0f / MAXIMUM)); }
@@ -351,6 +355,7 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, TYPE, std::i
     typedef Tile<DP, PACKED> T;
     constexpr bool WINDOW = std::is_same<CALL, KvWindow>::value, TREE = std::is_same<CALL, KvTree>::value, MASKED = WINDOW || TREE;
     constexpr int TG = T::TG, NS = T::NS, NT = T::NT, TOK = 16 * TG;
+    constexpr float HEADROOM = headroom(MASKED, TYPE), LIFT = lift(MASKED, TYPE);
     constexpr int ND = query_digits(TYPE), NP = TYPE == LPQ_TYPE_F32 ? 2 : 1, RB = PACKED ? DP / 2 : DP;
     // what ND digits hold, less a rounding
     constexpr float QMAX = ND == 4 ? 2139061888.0f : ND == 3 ? 8355600.0f : 32639.0f;
@@ -952,7 +957,7 @@ __global__ __launch_bounds__(NT) void kv_join_kernel(KvView kv, KvQueries q, KvA
     kv_store<4>(a.out, q.type, out_row + c0, kv.dim - c0, v);
     if (a.lse && col == 0) {
         const int64_t lat = ((int64_t)b * q.new_tokens + r / q.group) * ((int64_t)kv.heads * q.group) + h * q.group + r % q.group;
-        a.lse[lat] = l == 0.0f ? NEG : (top * (1.0f / MAXIMUM) - LIFT + __log2f(l)) * 0.69314718055994531f + a.lse[lat];
+        a.lse[lat] = l == 0.0f ? NEG : (top * (1.0f / MAXIMUM) - lift(MASKED, q.type) + __log2f(l)) * 0.69314718055994531f + a.lse[lat];
     }
 }
 
