@@ -356,7 +356,8 @@ int lpq_kv_attend(const lpq_kv *kv, const void *q_dev, int64_t ldq_seq, int64_t 
  *                only.  New tokens whose own position is below 0 see nothing, as in lpq_kv_attend;
  * or neither: lpq_kv_attend.  Of chosen pages, the tokens that are seen.  Only pages that a row sees something of are read (chosen pages:
  * all of them).
- * A row's result depends neither on the rows beside it nor on what is stored at positions that it does not see.
+ * A row's result does not depend on what is stored at positions that it does not see, and on the rows beside it only within the roundings of its
+ * weights (where their common maximum stood).
  * LPQ_EINVAL beside what is named above: window or sinks below 0, sinks without a window, window and tree, strides of the
  * tree below 0 or beyond 2^40; LPQ_ERANGE: a tree of more than 4096 new tokens. */
 size_t lpq_kv_attend_masked_workspace_bytes(const lpq_kv *kv, int64_t nseq, int new_tokens, int q_heads,

@@ -52,7 +52,7 @@ constexpr float NEG = -INFINITY;
 constexpr float WEIGHT_TOP = 15.0f;  // weights are exp2(t - m + lift): at most 2^15
 // How far scores may pass the maximum before it moves (powers of two), and what weights are lifted by: HEADROOM + LIFT = WEIGHT_TOP.  By 2, fp16
 // holds weights to 2^-37 of the largest; masked calls of the 16-bit types have 6 and 2^-33, and the maximum hardly moves after a pair's
-// first tiles: TODO.
+// first tiles: 32 trees on 96 bfloat16 rows a head 161 us by 2, 154 by 6.
 __host__ __device__ constexpr float headroom(bool masked, int type) { return masked && type != LPQ_TYPE_F32 ? 6.0f : 2.0f; }
 __host__ __device__ constexpr float lift(bool masked, int type) { return WEIGHT_TOP - headroom(masked, type); }
 constexpr float FAR = 1024.0f;       // maxima beyond it are subtracted from the scores before these are multiplied by their scale
@@ -181,7 +181,7 @@ struct Parts {
 // hold the workgroup's first tile (or part) finds it.
 template <typename CALL>
 __device__ __forceinline__ bool first_place(const KvView &kv, const KvQueries &q, const CALL &a, RowTokens rows, unsigned me, unsigned of, int tile,
-                                            int least, Place &out)
+                                            int least, unsigned crossing, Place &out)
 {
     auto tiles_of = [&](int b) { return tiles_seen(kv, q, a, rows, a.lengths[b], tile); };
     const int lane = threadIdx.x & 63, pairs = kv.heads;      // of a sequence
@@ -192,7 +192,7 @@ __device__ __forceinline__ bool first_place(const KvView &kv, const KvQueries &q
     unsigned upto = wave_scan(mine);
     const unsigned total = (unsigned)__builtin_amdgcn_readlane((int)upto, 63) * pairs, all_pairs = (unsigned)a.nseq * pairs;
     unsigned run = (total + of - 1) / of;
-    const bool apart = run < CROSSING && all_pairs < of;
+    const bool apart = run < crossing && all_pairs < of;
     if (apart) {
         // The smallest run whose parts fit the grid, or nearly: at least total / of, and every pair rounds its number of parts up
         // by less than one, so that total / (of - all_pairs) is enough.
@@ -348,6 +348,114 @@ __device__ __forceinline__ int row_sum_of(int v)
     return v;
 }
 
+// A row of queries, 8 features a lane, LR lanes.
+//   What every token's score has: sum q (k + s / 2) scale.
+template <int LR>
+__device__ __forceinline__ float query_offset(const float *v, const float *step, const float *k, float scale)
+{
+    float offset = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) offset += v[e] * scale * (k[e] + 0.5f * step[e]);
+#pragma unroll
+    for (int o = 1; o < LR; o <<= 1) offset += __shfl_xor(offset, o, 64);
+    return offset;
+}
+//   x = q s in place, times 1 / back^2 where that leaves binary32's middle range (rare); returns its largest magnitude, infinite if one is not finite.
+template <int LR>
+__device__ __forceinline__ float query_steps(float *x, const float *step, float *back)
+{
+    float v[8], most;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = x[e];
+    auto with_steps = [&](float by) {
+        most = 0.0f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            x[e] = v[e] * by * by * step[e];
+            const float size = fabsf(x[e]);
+            most = fmaxf(most, size <= 3.402823466e38f ? size : INFINITY);     // a NaN counts as infinite
+        }
+        most = row_max<LR>(most);
+    };
+    with_steps(1.0f);
+    *back = 1.0f;
+    if (__any(most == INFINITY || (most > 0.0f && most <= 1e-30f))) {
+        *back = most == INFINITY ? 0x1p64f : most > 0.0f && most <= 1e-30f ? 0x1p-64f : 1.0f;
+        with_steps(1.0f / *back);
+    }
+    return most;
+}
+//   Rounded to most / QMAX, of the sign of the scores' scale, in ND signed digits, `apart` bytes from one to the next.
+template <int ND, bool PACKED>
+__device__ __forceinline__ void query_digits8(const float *x, float most, float scale, float qmax, int8_t *row, int apart, int qc)
+{
+    const bool use = most != INFINITY && most > 1e-30f;          // below 1e-30 now: scores are 0 at any scale
+    const float f = use ? __uint_as_float(__float_as_uint(qmax / most) | (__float_as_uint(scale) & 0x80000000u)) : 0.0f;
+    int8_t d[ND][8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        // packed rows have the even features of 16 first (low nibbles of 8 bytes), then the odd ones
+        const int to = PACKED ? (e >> 1) + 4 * (e & 1) : e;
+        int z = use ? (int)rintf(x[e] * f) : 0;
+#pragma unroll
+        for (int dd = ND - 1; dd > 0; --dd) {
+            const int up = (z + 128) >> 8;
+            d[dd][to] = (int8_t)(z - (up << 8));                 // -128 .. 127
+            z = up;
+        }
+        d[0][to] = (int8_t)z;
+    }
+#pragma unroll
+    for (int dd = 0; dd < ND; ++dd) {
+        uint32_t w[2];
+        __builtin_memcpy(w, d[dd], 8);
+        int8_t *const to = row + dd * apart;
+        if (PACKED) {
+            *reinterpret_cast<uint32_t *>(to + 16 * (qc >> 1) + 4 * (qc & 1)) = w[0];
+            *reinterpret_cast<uint32_t *>(to + 16 * (qc >> 1) + 8 + 4 * (qc & 1)) = w[1];
+        } else {
+            *reinterpret_cast<uint2 *>(to + 8 * qc) = make_uint2(w[0], w[1]);
+        }
+    }
+}
+//   What the integer scores are multiplied by, above 0 and finite.
+template <bool PACKED>
+__device__ __forceinline__ float score_scale(float most, float qmax, float back, float scale)
+{
+    const float by = most / qmax * (PACKED ? 1.44269504088896f / 16.0f : 1.44269504088896f) * back * fabsf(scale) * back;
+    return fminf(fmaxf(by, 1e-30f), 3.402823466e38f);
+}
+// The digits' products put together.
+template <int ND>
+__device__ __forceinline__ float score_of(const v4i *sum, int j)
+{
+    const float low = (float)(sum[ND - 2][j] * 256 + sum[ND - 1][j]);
+    if constexpr (ND == 4) return __builtin_fmaf((float)(sum[0][j] * 256 + sum[1][j]), 65536.0f, low);
+    else if constexpr (ND == 3) return __builtin_fmaf((float)sum[0][j], 65536.0f, low);
+    else return low;
+}
+// The same without conversions, which take four times an addition's time: a sum that begins at the bits of 1.5 x 2^23 has, read as binary32, that much more
+// than its value (sums of a digit's products stay within 2^22).  The score comes out SCORE_SHIFT too large, which drops out of the softmax.
+constexpr float SCORE_SHIFT = 12582912.0f;
+constexpr int INT_AS_FLOAT = 0x4b400000;
+template <int ND>
+__device__ __forceinline__ float shifted_score(const v4i *sum, int j)
+{
+    auto of = [&](int dd) { const int bits = sum[dd][j]; return __builtin_bit_cast(float, bits); };
+    const float low = __builtin_fmaf(of(ND - 2) - SCORE_SHIFT, 256.0f, of(ND - 1));
+    if constexpr (ND == 4) return __builtin_fmaf(__builtin_fmaf(of(0) - SCORE_SHIFT, 256.0f, of(1) - SCORE_SHIFT), 65536.0f, low);
+    else if constexpr (ND == 3) return __builtin_fmaf(of(0) - SCORE_SHIFT, 65536.0f, low);
+    else return low;
+}
+// Orders what the lanes of one wave write to and read from LDS.
+__device__ __forceinline__ void wave_order()
+{
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0xC07F);        // lgkmcnt(0)
+    __builtin_amdgcn_wave_barrier();
+    asm volatile("" ::: "memory");
+}
+
 template <int DP, bool PACKED, int RT, int TYPE, typename CALL>
 __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, TYPE, std::is_same<CALL, KvWindow>::value)) void kv_attend_kernel(KvView kv, KvQueries q, CALL a, int row_tiles,
                                                                                        int least)
@@ -385,7 +493,7 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, TYPE, std::i
         const unsigned eights = __builtin_amdgcn_readfirstlane(blockIdx.x / (8 * row_tiles)), in = blockIdx.x - eights * 8 * row_tiles;
         row_tile = in >> 3;
         share = eights * 8 + (in & 7);
-        if (!first_place(kv, q, a, row_tokens(q, row_tile * 16 * RT, 16 * RT), share, gridDim.x / row_tiles, TOK, least, at)) return;
+        if (!first_place(kv, q, a, row_tokens(q, row_tile * 16 * RT, 16 * RT), share, gridDim.x / row_tiles, TOK, least, CROSSING, at)) return;
     }
     const int row0 = row_tile * 16 * RT;
     int left = at.run, b = at.b, pair = at.pair, start = at.tile, tiles = at.tiles;
@@ -500,71 +608,19 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, TYPE, std::i
 #pragma unroll 1
         for (int i = 0; i < PASSES; ++i) {
             const int r16 = i * PASS + tid / LR;
-            float v[8], most;
-            kv_floats8(raw, TYPE, kv.dim - qc0, v);
+            float x[8], back;
+            kv_floats8(raw, TYPE, kv.dim - qc0, x);
             if (i + 1 < PASSES) raw = load_queries(i + 1);
             if (a.lse) {
-                float offset = 0.0f;
-                const float *k = kv.key.k + h * DP + qc0;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) offset += v[e] * a.scale * (k[e] + 0.5f * step[e]);
-#pragma unroll
-                for (int o = 1; o < LR; o <<= 1) offset += __shfl_xor(offset, o, 64);
+                const float offset = query_offset<LR>(x, step, kv.key.k + h * DP + qc0, a.scale);
                 if (qc == 0 && r16 < 16 * RT) row_shift[r16] = offset;
             }
-            float x[8];
-            auto with_steps = [&](float by) {
-                most = 0.0f;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    x[e] = v[e] * by * by * step[e];
-                    const float size = fabsf(x[e]);
-                    most = fmaxf(most, size <= 3.402823466e38f ? size : INFINITY);     // a NaN counts as infinite
-                }
-                most = row_max<LR>(most);
-            };
-            with_steps(1.0f);
-            float back = 1.0f;
-            if (__any(most == INFINITY || (most > 0.0f && most <= 1e-30f))) {     // rare: by a power of two into the middle of binary32's range
-                back = most == INFINITY ? 0x1p64f : most > 0.0f && most <= 1e-30f ? 0x1p-64f : 1.0f;
-                with_steps(1.0f / back);
-            }
-            const bool bad = most == INFINITY, use = !bad && most > 1e-30f;  // below 1e-30 now: scores are 0 at any scale
-            const float f = use ? __uint_as_float(__float_as_uint(QMAX / most) | (__float_as_uint(a.scale) & 0x80000000u)) : 0.0f;      // of scale's sign
-            int8_t d[ND][8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                // packed rows have the even features of 16 first (low nibbles of 8 bytes), then the odd ones
-                const int to = PACKED ? (e >> 1) + 4 * (e & 1) : e;
-                int z = use ? (int)rintf(x[e] * f) : 0;
-#pragma unroll
-                for (int dd = ND - 1; dd > 0; --dd) {
-                    const int up = (z + 128) >> 8;
-                    d[dd][to] = (int8_t)(z - (up << 8));                     // -128 .. 127
-                    z = up;
-                }
-                d[0][to] = (int8_t)z;
-            }
-            if (8 * qc < DP && r16 < 16 * RT) {
-#pragma unroll
-                for (int dd = 0; dd < ND; ++dd) {
-                    uint32_t w[2];
-                    __builtin_memcpy(w, d[dd], 8);
-                    int8_t *row = digits[dd][r16];
-                    if (PACKED) {
-                        *reinterpret_cast<uint32_t *>(row + 16 * (qc >> 1) + 4 * (qc & 1)) = w[0];
-                        *reinterpret_cast<uint32_t *>(row + 16 * (qc >> 1) + 8 + 4 * (qc & 1)) = w[1];
-                    } else {
-                        *reinterpret_cast<uint2 *>(row + 8 * qc) = make_uint2(w[0], w[1]);
-                    }
-                }
-                // above 0 and finite, so that -inf in the place of a masked score stays that and equal scores stay equal (below 1e-30 scores are 0
-                // in any case, at the other end the largest take all); negative: the row is not finite
-                if (qc == 0) {
-                    const float by = most / QMAX * (PACKED ? 1.44269504088896f / 16.0f : 1.44269504088896f) * back * fabsf(a.scale) * back;
-                    row_scale[r16] = bad ? -1.0f : fminf(fmaxf(by, 1e-30f), 3.402823466e38f);
-                }
-            }
+            const float most = query_steps<LR>(x, step, &back);
+            if (r16 >= 16 * RT) continue;
+            if (8 * qc < DP) query_digits8<ND, PACKED>(x, most, a.scale, QMAX, digits[0][r16], 16 * RT * (DP + 16), qc);
+            // equal scores stay equal, and -inf in the place of a masked one stays that (below 1e-30 scores are 0 in any case, at the other end the
+            // largest take all); negative: the row is not finite
+            if (qc == 0) row_scale[r16] = most == INFINITY ? -1.0f : score_scale<PACKED>(most, QMAX, back, a.scale);
         }
         // Of a window: a row sees .x positions from .y on, and those below .z.  Of a tree: positions up to .x (-1: none) that are below .y, or
         // whose bits are set in its token's words, bit p & 31 of word .z + (p >> 5); .y is a multiple of 32 at or ahead of the first new token, so
@@ -678,12 +734,7 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, TYPE, std::i
                         for (int dd = 0; dd < ND; ++dd) sum[dd] = __builtin_amdgcn_mfma_i32_16x16x64_i8(kf, qd[rt][dd][st], sum[dd], 0, 0, 0);
                     }
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const float low = (float)(sum[ND - 2][j] * 256 + sum[ND - 1][j]);
-                        if constexpr (ND == 4) s[rt][tg][j] = __builtin_fmaf((float)(sum[0][j] * 256 + sum[1][j]), 65536.0f, low);
-                        else if constexpr (ND == 3) s[rt][tg][j] = __builtin_fmaf((float)sum[0][j], 65536.0f, low);
-                        else s[rt][tg][j] = low;
-                    }
+                    for (int j = 0; j < 4; ++j) s[rt][tg][j] = score_of<ND>(sum, j);
                 }
             load_keys(next);
             v2h off = {(_Float16)(PACKED ? -8.0f / VALUE_SCALE : -128.0f / VALUE_SCALE), (_Float16)(PACKED ? -8.0f / VALUE_SCALE : -128.0f / VALUE_SCALE)};
@@ -878,6 +929,328 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, TYPE, std::i
     }
 }
 
+// Calls with a window and query rows enough to fill the chip, as the parts of prompts have.  The same mathematics, digits, weights and masks as
+// kv_attend_kernel, shared out the other way: a wave has 16 rows of its own, and all eight go through the same tokens, 64 at a time.  Waves 0
+// to 3 bring the keys of a group of 16 each into LDS, as the first product's operands, waves 4 to 7 the values, as fp16 in the second's, so that
+// codes are fetched, unpacked and made fp16 once for 128 rows; two buffers take turns, with one barrier to a tile, and the next tile's codes are under
+// way in registers meanwhile.  No row is another wave's concern: nothing is joined, and what a workgroup costs before its first tile and
+// behind its last, 9 us there, is shared by eight times the rows.
+// us, kv_attend_kernel and this one: 4 sequences of up to 9000 tokens, windows of 600 for 6000 rows a head, 4 heads of 96 on 4-bit codes, float16 113, 67; 8 of
+// 128 on 8-bit codes, bfloat16 265, 146, windows of 4000 1114, 532; 2800 float32 rows, windows of 1000, heads of 128 224, 149, of 256 575, 277; 128
+// sequences, 48 rows, windows of 1000 141, 102.  Where its workgroups do not fill the chip it loses: 32 sequences of 96 rows, windows of 2000, 87, 89,
+// 720 float32 rows on one head of 192 25, 41.  Bound by the vector pipe: of 64 tokens a row tile has 16 scores a lane, each joined from its digits,
+// compared, scaled, raised and rounded.
+constexpr int ROWS_TOKENS = 64, ROWS_WAVES = 8, ROWS_THREADS = 64 * ROWS_WAVES, ROWS_TILE = 16 * ROWS_WAVES;
+__host__ __device__ constexpr int rows_digits(int type, int dpad) { return query_digits(type) * 8 * (dpad + 16); }      // bytes, of 8 rows
+__host__ __device__ constexpr int rows_stage(int dpad) { return ROWS_TOKENS * dpad * 3; }
+__host__ __device__ constexpr int rows_blocks_per_cu(int dpad) { return dpad <= 128 ? 2 : 1; }
+
+template <int DP, bool PACKED, int TYPE>
+__global__ __launch_bounds__(ROWS_THREADS, 2 * rows_blocks_per_cu(DP)) void kv_rows_kernel(KvView kv, KvQueries q, KvWindow a, int row_tiles)
+{
+    constexpr float HEADROOM = headroom(true, TYPE), LIFT = lift(true, TYPE);
+    constexpr int NS = DP / 64, NT = DP / 16, RB = PACKED ? DP / 2 : DP, VW = ((PACKED ? NT / 2 : NT) + 3) / 4;
+    constexpr int ND = query_digits(TYPE), NP = TYPE == LPQ_TYPE_F32 ? 2 : 1, TILE_ROWS = ROWS_TILE;
+    constexpr float QMAX = ND == 4 ? 2139061888.0f : ND == 3 ? 8355600.0f : 32639.0f;
+    constexpr int KEYS = ROWS_TOKENS * DP, STAGE = rows_stage(DP);      // bytes: keys, keys and values
+    static_assert(ROWS_WAVES * rows_digits(TYPE, DP) <= 2 * STAGE, "the queries' digits go through the buffers' memory");
+    __shared__ __align__(16) char stage[2 * STAGE];
+    __shared__ int group_at[2][4];
+    __shared__ int4 row_sees[TILE_ROWS];
+    __shared__ float row_scale[TILE_ROWS], row_shift[TILE_ROWS];
+
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
+    const int rows = q.new_tokens * q.group;
+    const int64_t head_bytes = (int64_t)kv.page * RB;
+    // Neighbouring row tiles of a pair, which see nearly the same tokens, on one XCD.
+    const int work = (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3);      // (the grid: a multiple of 8)
+    if (work >= a.nseq * kv.heads * row_tiles) return;
+    const int pair = __builtin_amdgcn_readfirstlane(work / row_tiles), row_tile = work - pair * row_tiles;
+    const int b = __builtin_amdgcn_readfirstlane(pair / kv.heads), h = pair - b * kv.heads;
+    const int group = wave & 3;
+    const bool brings_keys = wave < 4;
+    const int tile0 = row_tile * TILE_ROWS, row0 = tile0 + 16 * wave;
+    const RowTokens tile_rows = row_tokens(q, tile0, TILE_ROWS);
+    const bool working = row0 < rows;      // a wave behind the last row brings tokens in, and has none of its own to see
+    const int len = length_of(kv, a, kv_uniform(a.lengths)[b]);
+    const int32_t *table = a.table + (int64_t)b * a.ld_table, *chosen = a.chosen + ((int64_t)b * kv.heads + h) * a.n_select;
+
+    // Pages, as in kv_attend_kernel: a lane looks up the wave's group of one of the next 64 tiles.
+    int gap_from = 0, gap_width = 0;
+    if (!a.chosen) {
+        const Span span = span_of(a, q, tile_rows, len);
+        gap_from = 16 * span.sink;
+        gap_width = 16 * (span.low - span.sink);
+    }
+    const int columns = a.chosen ? a.n_select : a.table_pages, pool_pages = (int)kv.pages, turns = tiles_seen(kv, q, a, tile_rows, kv_uniform(a.lengths)[b], ROWS_TOKENS);
+    int pages, positions;
+    auto look_up = [&](int turn) {
+        unsigned token = 64u * (unsigned)(turn + lane) + 16u * group;
+        if (token >= (unsigned)gap_from) token += gap_width;      // (the last tile may reach beyond what the rows see)
+        const int want = (int)(token >> kv.page_shift), inside = (int)token & (kv.page - 1);
+        bool there = turn + lane < turns && want < columns;
+        int column = there ? want : 0;
+        if (a.chosen) {
+            column = chosen[column];
+            there = there && (unsigned)column < (unsigned)a.table_pages;
+            column = there ? column : 0;
+        }
+        const int p = (column << kv.page_shift) + inside, id = table[column];
+        there = there && p < len && (unsigned)id < (unsigned)pool_pages;
+        pages = there ? id : 0;
+        positions = there ? p : INT32_MAX;
+    };
+    constexpr int KW = NS * (PACKED ? 2 : 4);
+    uint32_t raw_codes[KW > 4 * VW ? KW : 4 * VW];
+    int position;
+    auto load = [&](int turn) {
+        const int page = __builtin_amdgcn_readlane(pages, turn & 63);
+        position = __builtin_amdgcn_readlane(positions, turn & 63);
+        const int64_t base = ((int64_t)page * kv.heads + h) * head_bytes + (int64_t)((position & (kv.page - 1) & ~15) * RB);
+        const Stretch rows16 = stretch((brings_keys ? kv.k : kv.v) + base, position == INT32_MAX ? 0 : 16 * RB);
+        if (brings_keys) {
+#pragma unroll
+            for (int st = 0; st < NS; ++st) {
+                if constexpr (PACKED) {
+                    const v2u x = __builtin_amdgcn_raw_buffer_load_b64(rows16, n * RB + g * 8 + 32 * st, 0, 0);
+                    raw_codes[2 * st] = x.x; raw_codes[2 * st + 1] = x.y;
+                } else {
+                    const v4u x = __builtin_amdgcn_raw_buffer_load_b128(rows16, n * RB + g * 16 + 64 * st, 0, 0);
+                    raw_codes[4 * st] = x.x; raw_codes[4 * st + 1] = x.y; raw_codes[4 * st + 2] = x.z; raw_codes[4 * st + 3] = x.w;
+                }
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                uint32_t w[VW];
+                load_share<DP, PACKED>(rows16, (4 * g + j) * RB, n, w);
+                asm volatile("");          // (else the compiler makes one store of both branches' and keeps the array in memory)
+#pragma unroll
+                for (int i = 0; i < VW; ++i) raw_codes[j * VW + i] = w[i];
+            }
+        }
+    };
+    // Keys [group][64 features][lane] 16 bytes, values [two groups][feature of a lane's][lane] 8 tokens, of which this wave has 4.
+    auto keep = [&](int buffer) {
+        char *const to = stage + buffer * STAGE;
+        if (brings_keys) {
+#pragma unroll
+            for (int st = 0; st < NS; ++st) {
+                uint4 x;
+                if constexpr (PACKED) {       // nibbles c + 8 -> bytes 16 c
+                    const uint32_t u = raw_codes[2 * st] ^ 0x88888888u, w = raw_codes[2 * st + 1] ^ 0x88888888u;
+                    x = make_uint4(u << 4 & 0xf0f0f0f0u, w << 4 & 0xf0f0f0f0u, u & 0xf0f0f0f0u, w & 0xf0f0f0f0u);
+                } else {
+                    x = make_uint4(raw_codes[4 * st], raw_codes[4 * st + 1], raw_codes[4 * st + 2], raw_codes[4 * st + 3]);
+                }
+                *reinterpret_cast<uint4 *>(to + ((group * NS + st) * 64 + lane) * 16) = x;
+            }
+            if (lane == 0) group_at[buffer][group] = position;
+            return;
+        }
+        v2h off = {(_Float16)(PACKED ? -8.0f / VALUE_SCALE : -128.0f / VALUE_SCALE), (_Float16)(PACKED ? -8.0f / VALUE_SCALE : -128.0f / VALUE_SCALE)};
+        asm("" : "+v"(off));
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int i = 0; i < VW; ++i) raw_codes[j * VW + i] = value_word(PACKED, raw_codes[j * VW + i]);
+#pragma unroll
+        for (int f = 0; f < NT; ++f) {
+            const int word = PACKED ? f >> 3 : f >> 2;
+            *reinterpret_cast<uint2 *>(to + KEYS + (((group >> 1) * NT + f) * 64 + lane) * 16 + 8 * (group & 1)) =
+                make_uint2(value_pair<PACKED>(raw_codes[word], raw_codes[VW + word], f, off),
+                           value_pair<PACKED>(raw_codes[2 * VW + word], raw_codes[3 * VW + word], f, off));
+        }
+    };
+
+    look_up(0);
+    load(0);
+
+    // ---- queries: steps folded in, digits, 8 rows at a time through memory of the wave's own
+    constexpr int LR = DP <= 64 ? 8 : DP <= 128 ? 16 : 32, PASS = 64 / LR, PASSES = 16 / PASS;
+    const int qc = lane % LR, qc0 = 8 * qc < DP ? 8 * qc : 0;
+    int8_t *const digits = reinterpret_cast<int8_t *>(stage) + wave * rows_digits(TYPE, DP);
+    float step[8];
+    kv_load_floats8(kv.key.s + h * DP + qc0, step);
+    auto load_queries = [&](int i) {
+        const int r = row0 + i * PASS + lane / LR;
+        const bool on = i < PASSES && r < rows && 8 * qc < DP;
+        const int64_t qat = (int64_t)b * q.ld_seq + (int64_t)(r / q.group) * q.ld_token + (int64_t)(h * q.group + r % q.group) * q.ld_head;
+        return kv_load8(q.p, TYPE, qat + qc0, on ? kv.dim - qc0 : 0);
+    };
+    v4i qd[ND][NS];          // lane (n, g): features 64 st + 16 g .. + 15 of row n
+    Raw8 raw = load_queries(0);
+#pragma unroll
+    for (int eight = 0; eight < 2; ++eight) {
+#pragma unroll 1
+        for (int i = eight * PASSES / 2; i < (eight + 1) * PASSES / 2; ++i) {
+            const int r16 = i * PASS + lane / LR;
+            float x[8], back;
+            kv_floats8(raw, TYPE, kv.dim - qc0, x);
+            raw = load_queries(i + 1);
+            if (a.lse) {
+                const float offset = query_offset<LR>(x, step, kv.key.k + h * DP + qc0, a.scale);
+                if (qc == 0) row_shift[16 * wave + r16] = offset;
+            }
+            const float most = query_steps<LR>(x, step, &back);
+            if (8 * qc < DP) query_digits8<ND, PACKED>(x, most, a.scale, QMAX, digits + (r16 & 7) * (DP + 16), 8 * (DP + 16), qc);
+            if (qc == 0) row_scale[16 * wave + r16] = most == INFINITY ? -1.0f : score_scale<PACKED>(most, QMAX, back, a.scale);
+        }
+        wave_order();
+        if (n >> 3 == eight) {
+#pragma unroll
+            for (int dd = 0; dd < ND; ++dd)
+#pragma unroll
+                for (int st = 0; st < NS; ++st) qd[dd][st] = *reinterpret_cast<const v4i *>(digits + (dd * 8 + (n & 7)) * (DP + 16) + 64 * st + 16 * g);
+        }
+        wave_order();
+    }
+    const float rs = row_scale[16 * wave + n], scale = fabsf(rs);      // of the scores (integers so far)
+    float m = NEG;           // their maximum, as an integer
+    // What rows see: .x positions from .y on, and those below .z.
+    if (threadIdx.x < TILE_ROWS) {
+        const int r = tile0 + threadIdx.x, me = r < rows ? len - q.new_tokens + r / q.group : -1;
+        const int first = window_from(a, me), sinks = me < a.sinks ? me + 1 : a.sinks;
+        row_sees[threadIdx.x] = me < 0 ? make_int4(0, 0, 0, 0) : make_int4(me + 1 - first, first, sinks, 0);
+    }
+    // A group that ends at or before `seen` and begins at or behind `windows` is seen by all of the wave's rows.
+    const RowTokens mine = row_tokens(q, working ? row0 : tile0, 16);
+    const int seen = len - q.new_tokens + mine.from, windows = window_from(a, len - q.new_tokens + mine.to);
+
+    v4f l = {0.f, 0.f, 0.f, 0.f}, acc[NT];
+    v8h ones;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) ones[e] = (_Float16)1.0f;
+#pragma unroll
+    for (int t = 0; t < NT; ++t) acc[t] = v4f{0.f, 0.f, 0.f, 0.f};
+    __syncthreads();               // the digits are read: the buffers are free
+    keep(0);
+    if (turns > 1) load(1);
+    __syncthreads();
+
+    for (int turn = 0; turn < turns; ++turn) {
+        const char *const here = stage + (turn & 1) * STAGE;
+        if (working) {
+            int pos[4];
+            {
+                const int4 p = *reinterpret_cast<const int4 *>(group_at[turn & 1]);
+                pos[0] = __builtin_amdgcn_readfirstlane(p.x); pos[1] = __builtin_amdgcn_readfirstlane(p.y);
+                pos[2] = __builtin_amdgcn_readfirstlane(p.z); pos[3] = __builtin_amdgcn_readfirstlane(p.w);
+            }
+            // 32 tokens at a time
+#pragma unroll 1
+            for (int half = 0; half < 2; ++half) {
+                const int first = half ? pos[2] : pos[0], second = half ? pos[3] : pos[1];
+                const bool part = first > seen - 15 || second > seen - 15 || first < windows || second < windows;
+                float s[2][4];
+#pragma unroll
+                for (int tg = 0; tg < 2; ++tg) {
+                    v4i sum[ND];
+#pragma unroll
+                    for (int dd = 0; dd < ND; ++dd) sum[dd] = v4i{INT_AS_FLOAT, INT_AS_FLOAT, INT_AS_FLOAT, INT_AS_FLOAT};
+#pragma unroll
+                    for (int st = 0; st < NS; ++st) {
+                        const v4i kf = *reinterpret_cast<const v4i *>(here + (((2 * half + tg) * NS + st) * 64 + lane) * 16);
+#pragma unroll
+                        for (int dd = 0; dd < ND; ++dd) sum[dd] = __builtin_amdgcn_mfma_i32_16x16x64_i8(kf, qd[dd][st], sum[dd], 0, 0, 0);
+                    }
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) s[tg][j] = shifted_score<ND>(sum, j);
+                }
+                if (part) {
+                    asm volatile("");      // a branch: few tiles need it
+                    const int4 row = row_sees[16 * wave + n];
+#pragma unroll
+                    for (int tg = 0; tg < 2; ++tg) {
+                        const int at16 = tg ? second : first;
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const int e = 4 * g + j;
+                            const bool sees = (unsigned)(at16 - row.y) + e < (unsigned)row.x || at16 < row.z - e;
+                            if (!sees) s[tg][j] = NEG;
+                        }
+                    }
+                }
+                float top = s[0][0];
+#pragma unroll
+                for (int tg = 0; tg < 2; ++tg)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) top = fmaxf(top, s[tg][j]);
+                if (__any((top - m) * scale > HEADROOM)) {
+                    top = fmaxf(top, __shfl_xor(top, 16, 64));
+                    top = fmaxf(top, __shfl_xor(top, 32, 64));
+                    const float next = fmaxf(m, top);
+                    const float f = next == NEG ? 1.0f : __builtin_amdgcn_exp2f((m - next) * scale);
+                    m = next;
+                    l *= f;
+#pragma unroll
+                    for (int t = 0; t < NT; ++t)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) acc[t][j] *= f;
+                }
+                const float most = m == NEG ? 0.0f : m;
+                float up = LIFT - most * scale;
+                if (NP == 2 || __any(fabsf(up) > FAR)) {       // a difference of numbers this large keeps too little of it
+                    asm volatile("");
+#pragma unroll
+                    for (int tg = 0; tg < 2; ++tg)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) s[tg][j] -= most;
+                    up = LIFT;
+                }
+                v8h w[NP];
+#pragma unroll
+                for (int tg = 0; tg < 2; ++tg)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[tg][j], scale, up));
+                        const _Float16 p0 = (_Float16)p;
+                        w[0][tg * 4 + j] = p0;
+                        if constexpr (NP == 2) w[1][tg * 4 + j] = (_Float16)(p - (float)p0);
+                    }
+#pragma unroll
+                for (int p = 0; p < NP; ++p) l = __builtin_amdgcn_mfma_f32_16x16x32_f16(ones, w[p], l, 0, 0, 0);
+#pragma unroll
+                for (int f = 0; f < NT; ++f) {
+                    const v8h vf = *reinterpret_cast<const v8h *>(here + KEYS + ((half * NT + f) * 64 + lane) * 16);
+#pragma unroll
+                    for (int p = 0; p < NP; ++p) acc[f] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, w[p], acc[f], 0, 0, 0);
+                }
+            }
+        }
+        if (turn + 1 < turns) {
+            keep((turn + 1) & 1);
+            if (((turn + 2) & 63) == 0) look_up(turn + 2);
+            if (turn + 2 < turns) load(turn + 2);
+        }
+        __syncthreads();
+    }
+    asm volatile("s_nop 15");      // the last matrix results are read in other blocks of code
+
+    // ---- results
+    const int r = row0 + n;
+    if (r >= rows) return;
+    // a row that is not finite is not a number from the first token on that it sees
+    const float sum = rs < 0.0f && l[0] > 0.0f ? NAN : l[0], inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+    const int64_t out_row = (int64_t)b * a.ldo_seq + (int64_t)(r / q.group) * a.ldo_token + (int64_t)(h * q.group + r % q.group) * a.ldo_head;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int f = 0; f < NT; f += 4) {
+            const int c0 = feature_of<DP, PACKED>(4 * g + j, f);
+            const float4 vs = *reinterpret_cast<const float4 *>(kv.value.s + h * DP + c0), vk = *reinterpret_cast<const float4 *>(kv.value.k + h * DP + c0);
+            const float by[4] = {vs.x, vs.y, vs.z, vs.w}, from[4] = {vk.x, vk.y, vk.z, vk.w};
+            float x[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] = sum == 0.0f ? 0.0f : (acc[f + e][j] * VALUE_SCALE * inv + 0.5f) * by[e] + from[e];
+            kv_store<4>(a.out, TYPE, out_row + c0, kv.dim - c0, x);
+        }
+    if (a.lse && g == 0) {
+        const int64_t at = ((int64_t)b * q.new_tokens + r / q.group) * ((int64_t)kv.heads * q.group) + h * q.group + r % q.group;
+        a.lse[at] = sum == 0.0f ? NEG : ((m - SCORE_SHIFT) * scale - LIFT + __log2f(sum)) * 0.69314718055994531f + row_shift[16 * wave + n];
+    }
+}
+
 // Parts of a row joined, o = sum_u o_u 2^(m_u - m) / sum_u l_u 2^(m_u - m): a workgroup of NT threads per row, dpad / 4 of them side by
 // side per part.  Bound by two round trips to memory (which parts, then the parts, all asked for at once up to 4 per thread): 1024 rows
 // of 2 to 8 parts 4.7 us, 4096 rows 6.4, 32 rows of 32 parts 4.0.
@@ -964,6 +1337,12 @@ __global__ __launch_bounds__(NT) void kv_join_kernel(KvView kv, KvQueries q, KvA
 template <int DP, bool PACKED, int TYPE, typename CALL>
 void launch_rows(const KvView &kv, const KvQueries &q, const CALL &a, const KvAttendPlan &p, hipStream_t st)
 {
+    if constexpr (std::is_same<CALL, KvWindow>::value) {
+        if (p.rows == ROWS_TILE) {
+            kv_rows_kernel<DP, PACKED, TYPE><<<p.grid, ROWS_THREADS, 0, st>>>(kv, q, a, p.row_tiles);
+            return;
+        }
+    }
     if constexpr (two_row_tiles(DP, PACKED, TYPE, std::is_same<CALL, KvTree>::value)) {
         if (p.rows == 32) {
             kv_attend_kernel<DP, PACKED, 2, TYPE><<<p.grid, THREADS, 0, st>>>(kv, q, a, p.row_tiles, p.least);
@@ -1020,7 +1399,9 @@ KvAttendPlan kv_attend_plan(const KvView &kv, int64_t nseq, int new_tokens, int 
     const int64_t rows = (int64_t)new_tokens * group;
     const int64_t pairs = nseq * kv.heads;
     // What a row tile has to go through at most, of tokens that lie side by side: the sinks, and the windows of its new tokens.
-    if (mask.window) tokens = std::min<int64_t>(tokens, round_up((int64_t)mask.sinks, 16) + mask.window + std::min<int64_t>(new_tokens, 32 / group + 2) + 30);
+    if (mask.window) tokens = std::min<int64_t>(tokens, round_up((int64_t)mask.sinks, 16) + mask.window + std::min<int64_t>(new_tokens, 128 / group + 2) + 30);
+    const int64_t row_tiles = ceil_div(rows, (int64_t)ROWS_TILE);
+    if (mask.window && rows > 32 && row_tiles * pairs >= 256 * rows_blocks_per_cu(kv.dpad)) return {(int)row_tiles, ROWS_TILE, 0, (unsigned)round_up(row_tiles * pairs, 8), 0};
     p.rows = rows > 16 && pairs * tokens > TWO_ROW_TOKENS && two_row_tiles(kv.dpad, kv.packed, type, mask.tree != nullptr) ? 32 : 16;
     p.row_tiles = (int)ceil_div(rows, (int64_t)p.rows);
     const int64_t tile = tile_tokens(kv.dpad, kv.packed);
@@ -1036,7 +1417,7 @@ KvAttendPlan kv_attend_plan(const KvView &kv, int64_t nseq, int new_tokens, int 
         const int64_t room = ceil_div(chip, (int64_t)p.row_tiles);
         int64_t shares = most < room ? most : room;
         // Not a workgroup more than the chip holds at once, which would be a second generation of them: 96 bfloat16 rows on 8 heads of 128, 32
-        // sequences of 900 to 8000 tokens, 528 workgroups 181 us, 504 TODO.
+        // sequences of 900 to 8000 tokens, 528 workgroups 181 us, 504 161; 720 float32 rows on one of 192 31.6, 25.5.
         if (p.row_tiles > 1) shares = (mask.window || mask.tree) && room > 8 && shares > room / 8 * 8 ? room / 8 * 8 : round_up(shares, 8);
         p.grid = (unsigned)(shares * p.row_tiles);
         p.bytes = ((size_t)2 * p.grid * p.rows * (kv.dpad + 2) + (size_t)2 * pairs * (mask.window || mask.tree ? p.row_tiles : 1)) * sizeof(float);
