@@ -51,9 +51,10 @@ constexpr int THREADS = 256, WAVES = 4;
 constexpr float NEG = -INFINITY;
 constexpr float WEIGHT_TOP = 15.0f;  // weights are exp2(t - m + lift): at most 2^15
 // How far scores may pass the maximum before it moves (powers of two), and what weights are lifted by: HEADROOM + LIFT = WEIGHT_TOP.  By 2, fp16
-// holds weights to 2^-37 of the largest; masked calls of the 16-bit types have 6 and 2^-33, and the maximum hardly moves after a pair's
-// first tiles: 32 trees on 96 bfloat16 rows a head 161 us by 2, 154 by 6.
-__host__ __device__ constexpr float headroom(bool masked, int type) { return masked && type != LPQ_TYPE_F32 ? 6.0f : 2.0f; }
+// holds weights to 2^-37 of the largest; masked calls of bfloat16 have 6 and 2^-33, and the maximum hardly moves after a pair's first
+// tiles: 32 trees on 96 rows a head 161 us by 2, 154 by 6.  Not so for float16, whose error grows with it by a tenth: the largest weight is then
+// not a power of two as a rule.
+__host__ __device__ constexpr float headroom(bool masked, int type) { return masked && type == LPQ_TYPE_BF16 ? 6.0f : 2.0f; }
 __host__ __device__ constexpr float lift(bool masked, int type) { return WEIGHT_TOP - headroom(masked, type); }
 constexpr float FAR = 1024.0f;       // maxima beyond it are subtracted from the scores before these are multiplied by their scale
 constexpr float MAXIMUM = 0x1p-48f;  // maxima that go from wave to wave and from part to part are times this: finite for any query and scale

@@ -11,6 +11,10 @@
 // Measured (write, read): one row of 8 heads of 128, bfloat16: 5.1, 3.6 us; 64 rows of 64 sequences 6.7, 4.2; 26 244 rows of 6 x 100
 // float16 features of 12 prompts to packed codes 31.8 (vector instructions for 20 of them, 133 to a thread's 8 values, memory for 11;
 // float32 rows 42) and back 22.6; 151 419 rows of 8 x 128 back to bfloat16: 188 us, 4.9 TB/s of codes and rows (a copy of memory: 4.7).
+// Turned on the way, with four query heads to a key head: one row of 8 heads of 128, bfloat16: 6.6 us; 320 float32 rows of 2 x 80, 64 of them turned, and
+// 12 query heads: 12.4; 26 244 float16 rows of 6 x 100 to packed codes, 52 turned in pairs of neighbours, and 18 query heads: 113 where a copy of
+// as many bytes takes 57 (vector instructions for 58: Eq. 1, the turns, pieces of odd units; as they are, loads and instructions of a
+// workgroup follow each other); 23 140 bfloat16 rows of 8 x 128 and 32 query heads: 157 where a copy takes 108.
 #include <algorithm>
 #include <type_traits>
 
@@ -346,6 +350,10 @@ __device__ __forceinline__ void turn_queries(const KvView &kv, const KvPlaces &p
             const int first = NEIGHBOURS ? c0 >> 1 : c0, angles = !pairs || position < 0 ? 0 : a.half - first;
             float c[N], s[N];
             if (angles > 0) load_angles<N>(a, at, first, angles, c, s);
+            if (NEIGHBOURS && off) {       // (pairs that lie apart: each result; so each way takes less time)
+#pragma unroll
+                for (int e = 0; e < N; ++e) c[e] = s[e] = NAN;
+            }
 #pragma unroll
             for (int h = 0; h < TURN_HEADS; ++h) {
                 if (h0 + h >= a.q_heads) continue;
@@ -356,8 +364,8 @@ __device__ __forceinline__ void turn_queries(const KvView &kv, const KvPlaces &p
                     for (int e = 0; e < 4; ++e)
                         if (e < angles) {
                             const float p = u[2 * e], o = u[2 * e + 1];
-                            u[2 * e] = off ? NAN : __fsub_rn(__fmul_rn(p, c[e]), __fmul_rn(o, s[e]));
-                            u[2 * e + 1] = off ? NAN : __fadd_rn(__fmul_rn(o, c[e]), __fmul_rn(p, s[e]));
+                            u[2 * e] = __fsub_rn(__fmul_rn(p, c[e]), __fmul_rn(o, s[e]));
+                            u[2 * e + 1] = __fadd_rn(__fmul_rn(o, c[e]), __fmul_rn(p, s[e]));
                         }
                 } else if (pairs) {
                     kv_floats8(y[h], type, left, w);
