@@ -391,7 +391,7 @@ int lpq_kv_attend_masked(const lpq_kv *kv, const void *q_dev, int64_t ldq_seq, i
  * was captured into a graph belongs to the graph.  Output and workspace must not overlap the inputs.
  * LPQ_EINVAL: null argument, negative size, unknown type, strides below 0, beyond 2^40 elements or with which
  * outputs overlap, misaligned codes or workspace;
- * LPQ_ERANGE: d > 131072 (its sums would not fit 32 bits), m or n >= 2^31, more than 2^22 tiles of 128 rows x 128
+ * LPQ_ERANGE: d > 131072 (its sums would not fit 32 bits), more than 2^25 rows or channels, more than 2^22 tiles of 128 rows x 128
  * channels, too small a workspace. */
 size_t lpq_row_codes_bytes(int64_t n, int d);
 int lpq_encode_rows(const void *x_dev, int64_t ldx, int type, int64_t n, int d, int8_t *codes_dev, float *scales_dev, void *stream);

@@ -218,8 +218,8 @@ __device__ __forceinline__ float scaled(int sum, const Scale &a, const Scale &b)
 // Few rows.  Bound by reading the weights, which go from memory to registers, each byte to one wave: a workgroup's eight waves share CT tiles
 // of 16 channels and take every eighth run of 128 features of them (v_mfma_i32_16x16x64_i8, channels as rows of the result), and the
 // eight sums come together through LDS.  The tokens' codes, MT tiles of 16, come from the cache of their chiplet with each run.  FUSED (few rows):
-// the workgroup makes the codes itself, in LDS, while its first weights are under way: one launch, and no round trip through memory (4 rows, 4096 x 4096: 6.4
-// us, in two launches 9.5).
+// the workgroup makes the codes itself, in LDS, while its first weights are under way: one launch, and no round trip through memory (4096 x 4096: 4 rows 6.4 us,
+// 16 in two launches 10.1).
 // A barrier for what the waves write to and read from LDS; loads from memory stay under way.
 __device__ __forceinline__ void lds_barrier()
 {

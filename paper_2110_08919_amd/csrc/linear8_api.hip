@@ -27,7 +27,7 @@ constexpr int64_t MAX_STRIDE = int64_t(1) << 40;
 
 extern "C" size_t lpq_row_codes_bytes(int64_t n, int d)
 {
-    return n < 0 || n >= (int64_t(1) << 31) || d < 1 || d > LINEAR8_MAX_D ? 0 : (size_t)ceil_div(n, (int64_t)16) * row_blocks(d) * 1024;
+    return n < 0 || n > LINEAR8_MAX_ROWS || d < 1 || d > LINEAR8_MAX_D ? 0 : (size_t)ceil_div(n, (int64_t)16) * row_blocks(d) * 1024;
 }
 
 static int check_features(int d)
@@ -41,7 +41,7 @@ static int check_features(int d)
 static int check_rows(const char *what, const void *p, int64_t ld, int type, int64_t n, int64_t d, bool written)
 {
     if (n < 0) return fail(LPQ_EINVAL, "%lld %s", (long long)n, what);
-    if (n >= (int64_t(1) << 31)) return fail(LPQ_ERANGE, "%lld %s, must stay below 2^31", (long long)n, what);
+    if (n > LINEAR8_MAX_ROWS) return fail(LPQ_ERANGE, "%lld %s, at most %d", (long long)n, what, (int)LINEAR8_MAX_ROWS);
     if (!element_bytes(type)) return fail(LPQ_EINVAL, "unknown type %d", type);
     if (n > 0 && !p) return fail(LPQ_EINVAL, "null %s", what);
     if (ld < (written && n > 1 ? d : 0) || ld > MAX_STRIDE) return fail(LPQ_EINVAL, "%s of %lld elements, %lld apart", what, (long long)d, (long long)ld);
@@ -51,7 +51,7 @@ static int check_rows(const char *what, const void *p, int64_t ld, int type, int
 static int check_codes(const char *what, const void *codes, const float *scales, int64_t n)
 {
     if (n < 0) return fail(LPQ_EINVAL, "%lld %s", (long long)n, what);
-    if (n >= (int64_t(1) << 31)) return fail(LPQ_ERANGE, "%lld %s, must stay below 2^31", (long long)n, what);
+    if (n > LINEAR8_MAX_ROWS) return fail(LPQ_ERANGE, "%lld %s, at most %d", (long long)n, what, (int)LINEAR8_MAX_ROWS);
     if (n > 0 && (!codes || !scales)) return fail(LPQ_EINVAL, "null %s", what);
     if ((uintptr_t)codes % 256) return fail(LPQ_EINVAL, "%s must be 256-byte aligned", what);
     return LPQ_OK;
@@ -76,7 +76,7 @@ static int check_product(int64_t m, int64_t n)
 
 extern "C" size_t lpq_matmul_i8_workspace_bytes(int64_t m, int64_t n, int d)
 {
-    if (m < 1 || n < 1 || m >= (int64_t(1) << 31) || n >= (int64_t(1) << 31) || d < 1 || d > LINEAR8_MAX_D) return 0;
+    if (m < 1 || n < 1 || m > LINEAR8_MAX_ROWS || n > LINEAR8_MAX_ROWS || d < 1 || d > LINEAR8_MAX_D) return 0;
     return linear8_plan(m, n, d).bytes;
 }
 
@@ -118,7 +118,7 @@ static Linear8Space linear8_space(int64_t m, int64_t n, int d)
 
 extern "C" size_t lpq_linear8_workspace_bytes(int64_t m, int64_t n, int d)
 {
-    if (m < 1 || n < 1 || m >= (int64_t(1) << 31) || n >= (int64_t(1) << 31) || d < 1 || d > LINEAR8_MAX_D) return 0;
+    if (m < 1 || n < 1 || m > LINEAR8_MAX_ROWS || n > LINEAR8_MAX_ROWS || d < 1 || d > LINEAR8_MAX_D) return 0;
     return linear8_space(m, n, d).bytes;
 }
 
@@ -155,7 +155,7 @@ extern "C" int lpq_linear8_plan_info(int64_t m, int64_t n, int d, int64_t *out, 
     if (!out || out_count < LPQ_LINEAR8_INFO_COUNT) return fail(LPQ_EINVAL, "out must hold LPQ_LINEAR8_INFO_COUNT values");
     int rc = check_features(d);
     if (!rc && (m < 1 || n < 1)) rc = fail(LPQ_EINVAL, "%lld rows, %lld channels", (long long)m, (long long)n);
-    if (!rc && (m >= (int64_t(1) << 31) || n >= (int64_t(1) << 31))) rc = fail(LPQ_ERANGE, "%lld rows, %lld channels", (long long)m, (long long)n);
+    if (!rc && (m > LINEAR8_MAX_ROWS || n > LINEAR8_MAX_ROWS)) rc = fail(LPQ_ERANGE, "%lld rows, %lld channels", (long long)m, (long long)n);
     if (!rc) rc = check_product(m, n);
     if (rc) return rc;
     const Linear8Plan p = linear8_plan(m, n, d);

@@ -6,7 +6,8 @@
 
 namespace lpq {
 
-enum { LINEAR8_MAX_D = 1 << 17 };      // sums of this many products of two codes stay below 2^31
+enum { LINEAR8_MAX_D = 1 << 17,        // sums of this many products of two codes stay below 2^31
+       LINEAR8_MAX_ROWS = 1 << 25 };   // of a launch: 64 threads for a row of codes, 32 for a channel, fewer than 2^32 in all
 
 // Blocks of 64 features that a row takes, an even number.
 static inline int row_blocks(int d) { return (int)round_up(d, 128) / 64; }

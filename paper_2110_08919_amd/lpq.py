@@ -462,7 +462,7 @@ class KVCache:
         if q is not None:
             assert not (q.requires_grad and torch.is_grad_enabled()), "rotated queries have no gradient here: use torch.no_grad() or q.detach()"
             if out is None:
-                out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+                out = q.new_empty(q.shape)
             q_heads, queries = self._query_rows(q, n, k.dtype)
             more, into = self._query_rows(out, n, k.dtype)
             assert more == q_heads, "as many heads in the output"
@@ -540,7 +540,7 @@ class KVCache:
         nseq, tab = self._table(table)
         new, q_heads, queries = self._queries(q, nseq)
         if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            out = q.new_empty(q.shape)
             outputs = (out.data_ptr(), new * q_heads * self.dim, q_heads * self.dim, self.dim)
         else:
             assert out.shape == q.shape and out.dtype is q.dtype
@@ -662,6 +662,7 @@ class Linear8:
         self.bias = _bias(bias, self.channels, self.device)
         if bias is not None and self.bias.data_ptr() == bias.data_ptr():
             self.bias = self.bias.clone()                   # the layer's own, as its codes are
+        torch.cuda.current_stream(self.device).synchronize()     # calls on any stream find the codes written
         self._args = self.weight.blocks.data_ptr(), self.weight.scales.data_ptr(), self.channels, self.d, _ptr(self.bias)
 
     def __call__(self, x: torch.Tensor, out: torch.Tensor = None, workspace: torch.Tensor = None) -> torch.Tensor:
@@ -671,7 +672,7 @@ class Linear8:
         rows = x if x.dim() == 2 else x.reshape(-1, self.d)
         m, _, ldx = _typed_matrix(rows, "rows")
         if out is None:
-            out = torch.empty((*x.shape[:-1], self.channels), dtype=x.dtype, device=x.device)
+            out = x.new_empty((*x.shape[:-1], self.channels))
             ldo = self.channels
         else:
             assert out.shape == (*x.shape[:-1], self.channels) and out.dtype is x.dtype and out.device == x.device, "need an output of x's type and rows"

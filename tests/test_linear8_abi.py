@@ -16,8 +16,8 @@ def L():
 
 def test_sizes_of_codes_and_workspaces(L):
     assert [L.lpq_row_codes_bytes(1, d) for d in (-1, 0, 1, 128, 129, 131072, 131073)] == [0, 0, 2048, 2048, 4096, 16 * 131072, 0]
-    assert [L.lpq_row_codes_bytes(n, 1) for n in (-1, 0, 16, 17, 1 << 31)] == [0, 0, 2048, 4096, 0]
-    for m, n, d in ((0, 5, 5), (5, 0, 5), (5, 5, 0), (5, 5, 1 << 20), (1 << 31, 5, 5), (5, 1 << 31, 5), (-1, 5, 5)):
+    assert [L.lpq_row_codes_bytes(n, 1) for n in (-1, 0, 16, 17, 1 << 25, (1 << 25) + 1)] == [0, 0, 2048, 4096, 1 << 32, 0]
+    for m, n, d in ((0, 5, 5), (5, 0, 5), (5, 5, 0), (5, 5, 1 << 20), ((1 << 25) + 1, 5, 5), (5, (1 << 25) + 1, 5), (-1, 5, 5)):
         assert L.lpq_linear8_workspace_bytes(m, n, d) == 0 and L.lpq_matmul_i8_workspace_bytes(m, n, d) == 0
     for m, n, d in ((1, 1, 1), (300, 700, 1000), (48, 11_111, 4100)):
         both, product = L.lpq_linear8_workspace_bytes(m, n, d), L.lpq_matmul_i8_workspace_bytes(m, n, d)
@@ -38,17 +38,18 @@ def test_refusals(L):
     def linear(x=p, ldx=64, kind=0, m=2, codes=p, scales=p, n=2, d=64, out=p, ldo=2, ws=p, size=1 << 30):
         return L.lpq_linear8(x, ldx, kind, m, codes, scales, n, d, None, out, ldo, ws, size, None)
 
-    for call, more in ((encode, {}), (linear, {"m": 2})):
+    for call in (encode, linear):
         assert call(d=0) == lpq.EINVAL and call(d=131_073, ldx=1 << 20) == lpq.ERANGE
         assert call(kind=3) == lpq.EINVAL and call(x=None) == lpq.EINVAL and call(codes=None) == lpq.EINVAL and call(scales=None) == lpq.EINVAL
         assert call(ldx=-1) == lpq.EINVAL and call(ldx=(1 << 40) + 1) == lpq.EINVAL
         assert call(codes=p + 128) == lpq.EINVAL
-        assert call(n=-1) == lpq.EINVAL and call(n=1 << 31) == lpq.ERANGE
+        assert call(n=-1) == lpq.EINVAL
+    assert encode(n=(1 << 25) + 1) == lpq.ERANGE and linear(n=(1 << 25) + 1, ldo=1 << 26) == lpq.ERANGE
     assert encode(n=0, x=None, codes=None, scales=None) == lpq.OK
     for call in (product, linear):
         assert call(out=None) == lpq.EINVAL and call(ldo=1) == lpq.EINVAL and call(kind=-1) == lpq.EINVAL
-        assert call(m=1 << 31) == lpq.ERANGE and call(m=-1) == lpq.EINVAL
-        assert call(m=1 << 30, n=1 << 20, ldo=1 << 20) == lpq.ERANGE       # more tiles than a launch has
+        assert call(m=(1 << 25) + 1) == lpq.ERANGE and call(m=-1) == lpq.EINVAL
+        assert call(m=1 << 25, n=1 << 20, ldo=1 << 20) == lpq.ERANGE       # more tiles than a launch has
         assert call(m=0, out=None) == lpq.OK and call(n=0) == lpq.OK
     assert product(pa=p + 16) == lpq.EINVAL and product(pb=p + 64) == lpq.EINVAL and product(pa=None) == lpq.EINVAL and product(sa=None) == lpq.EINVAL and product(sb=None) == lpq.EINVAL
     assert linear(m=9, ws=None) == lpq.EINVAL and linear(m=9, ws=p + 128) == lpq.EINVAL and linear(m=9, size=16) == lpq.ERANGE
