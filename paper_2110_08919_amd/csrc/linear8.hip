@@ -4,10 +4,10 @@
 //   y[i][c]    = (sum_k a[i][k] b[c][k]) sa[i] sb[c] + bias[c],      the sums exact in 32 bits
 //
 // Measured with the rows' codes, bfloat16 unless said otherwise, weights not in a cache: 1 row, 4096 x 4096 5.8 us (4.3 where the weights are in the
-// memory-side cache), 32 768 x 16 384 91 us, 5.9 TB/s; 48 float16 rows, 11 111 x 4100 19.5; 64 rows, 16 384 x 8192 36; 128 rows, 32 768 x 16 384
-// 125; 1024 rows, 4096 x 4096 34; 8192 rows, 8192 x 8192 527, of these 43 for the codes (4.7 TB/s, as a copy of memory) and 484 for the product,
-// 2.27 POP/s, where a register-resident loop of the instruction sustains 3.46 on random bytes.  What is left there: a stage takes 0.81 us, 0.68
-// without its copies (0.62 at that loop's rate), and 12 us go before a tile's first stage and behind its last.
+// memory-side cache), 32 768 x 16 384 91 us, 5.9 TB/s; 48 float16 rows, 11 111 x 4100 19.1; 64 rows, 16 384 x 8192 36; 128 rows, 32 768 x 16 384
+// 124; 1024 rows, 4096 x 4096 34; 8192 rows, 8192 x 8192 513, of these 43 for the codes (4.7 TB/s, as a copy of memory) and 470 for the product,
+// 2.34 POP/s, where a register-resident loop of the instruction sustains 3.46 on random bytes.  What is left there: a stage takes 0.81 us, 0.68
+// without its copies (0.62 at that loop's rate), and 10 us go before a tile's first stage and behind its last.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -455,9 +455,14 @@ __global__ __launch_bounds__(TILE_THREADS) void linear8_tile_kernel(TileWork g)
     constexpr int BM = 64 * TT, BN = 64 * TC, STAGE = (BM + BN) * TILE_K;
     __shared__ __align__(1024) char ring[TILE_STAGES * STAGE];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int tiles = g.tiles_m * g.tiles_n;
-    const int part = PARTS ? blockIdx.x / tiles : 0, tile = PARTS ? blockIdx.x - part * tiles : blockIdx.x;
-    const int tm = tile % g.tiles_m, tn = tile / g.tiles_m;
+    // An XCD (workgroups are dealt to the eight of them in turn) has neighbouring tiles, in bands of BAND row tiles: what its CUs have at a time
+    // shares panels in its L2 (1100 rows, 4096 x 4096: 49.7 us by rows alone, 40.0; 129, 32 768 x 16 384 174, 163; 8192, 8192 x 8192 the same).
+    constexpr int BAND = 4;
+    const int tiles = g.tiles_m * g.tiles_n, work = (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3);      // (the grid: a multiple of 8)
+    if (work >= tiles * g.parts) return;
+    const int part = PARTS ? work / tiles : 0, tile = PARTS ? work - part * tiles : work;
+    const int band = tile / (BAND * g.tiles_n), in_band = tile - band * BAND * g.tiles_n, height = min(BAND, g.tiles_m - band * BAND);
+    const int tn = in_band / height, tm = band * BAND + in_band - tn * height;
     const int64_t row0 = (int64_t)tm * BM, ch0 = (int64_t)tn * BN;
     const int wt = (wave & 1) * 32 * TT, wc = (wave >> 1) * 32 * TC;
     const int begin = part * g.per_part, stages = min(g.per_part, g.stages - begin);
@@ -560,6 +565,11 @@ __global__ __launch_bounds__(TILE_THREADS) void linear8_tile_kernel(TileWork g)
     }
     if (BM == TILE_THREADS || threadIdx.x < BM) scales_x[threadIdx.x] = split_scale(end_x);
     lds_barrier();
+    Scale by[TC][16];            // of a lane's channels, for all its tokens
+#pragma unroll
+    for (int i = 0; i < TC; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) by[i][e] = scales_w[wc + 32 * i + 8 * (e >> 2) + 4 * (lane >> 5) + (e & 3)];
 #pragma unroll
     for (int j = 0; j < TT; ++j) {
         const Scale a = scales_x[wt + 32 * j + (lane & 31)];
@@ -571,7 +581,7 @@ __global__ __launch_bounds__(TILE_THREADS) void linear8_tile_kernel(TileWork g)
                 float y[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    y[e] = scaled(acc[i][j][4 * q + e], a, scales_w[wc + c + e]);
+                    y[e] = scaled(acc[i][j][4 * q + e], a, by[i][4 * q + e]);
                     if (g.out.bias) y[e] += biases[wc + c + e];
                 }
                 kv_store<4>(own, TYPE, (lane & 31) * (PITCH / SIZE) + c, 4, y);
@@ -725,7 +735,7 @@ hipError_t launch_linear8(const RowCodes &x, const RowCodes &w, int d, const Lin
     const TileWork g = {x.codes, w.codes, x.scales, w.scales, x.n, w.n, row_blocks(d), stages, (int)ceil_div(stages, plan.parts),
                         (int)ceil_div(x.n, (int64_t)plan.rows), (int)ceil_div(w.n, (int64_t)plan.channels), plan.parts, out,
                         static_cast<int *>(workspace)};
-    const dim3 grid((unsigned)(g.tiles_m * g.tiles_n * plan.parts));
+    const dim3 grid((unsigned)round_up((int64_t)g.tiles_m * g.tiles_n * plan.parts, 8));
     if (plan.parts > 1) {
         if (plan.rows == 128) linear8_tile_kernel<2, 2, 0, true><<<grid, TILE_THREADS, 0, st>>>(g);
         else linear8_tile_kernel<1, 1, 0, true><<<grid, TILE_THREADS, 0, st>>>(g);
