@@ -49,13 +49,10 @@ typedef _Float16 v8h __attribute__((ext_vector_type(8)));
 
 constexpr int THREADS = 256, WAVES = 4;
 constexpr float NEG = -INFINITY;
-constexpr float WEIGHT_TOP = 15.0f;  // weights are exp2(t - m + lift): at most 2^15
-// How far scores may pass the maximum before it moves (powers of two), and what weights are lifted by: HEADROOM + LIFT = WEIGHT_TOP.  By 2, fp16
-// holds weights to 2^-37 of the largest; masked calls of bfloat16 have 6 and 2^-33, and the maximum hardly moves after a pair's first
-// tiles: 32 trees on 96 rows a head 161 us by 2, 154 by 6.  Not so for float16, whose error grows with it by a tenth: the largest weight is then
-// not a power of two as a rule.
-__host__ __device__ constexpr float headroom(bool masked, int type) { return masked && type == LPQ_TYPE_BF16 ? 6.0f : 2.0f; }
-__host__ __device__ constexpr float lift(bool masked, int type) { return WEIGHT_TOP - headroom(masked, type); }
+// Not more, also where it would take less time (bfloat16 rows with a mask by 6, so to 2^-33: 32 trees on 96 rows a head 161 us by 2, 154 by 6): what a token
+// sees does not say how exact its weights are.
+constexpr float HEADROOM = 2.0f;     // how far scores may pass the maximum before it moves (powers of two)
+constexpr float LIFT = 13.0f;        // weights are exp2(t - m + LIFT): at most 2^15, and fp16 holds them to 2^-37 of the largest
 constexpr float FAR = 1024.0f;       // maxima beyond it are subtracted from the scores before these are multiplied by their scale
 constexpr float MAXIMUM = 0x1p-48f;  // maxima that go from wave to wave and from part to part are times this: finite for any query and scale
 __device__ __forceinline__ float lag(float m, float top) { return top == NEG ? 1.0f : __builtin_amdgcn_exp2f((m - top) * (1.0f / MAXIMUM)); }
@@ -464,7 +461,6 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, TYPE, std::i
     typedef Tile<DP, PACKED> T;
     constexpr bool WINDOW = std::is_same<CALL, KvWindow>::value, TREE = std::is_same<CALL, KvTree>::value, MASKED = WINDOW || TREE;
     constexpr int TG = T::TG, NS = T::NS, NT = T::NT, TOK = 16 * TG;
-    constexpr float HEADROOM = headroom(MASKED, TYPE), LIFT = lift(MASKED, TYPE);
     constexpr int ND = query_digits(TYPE), NP = TYPE == LPQ_TYPE_F32 ? 2 : 1, RB = PACKED ? DP / 2 : DP;
     // what ND digits hold, less a rounding
     constexpr float QMAX = ND == 4 ? 2139061888.0f : ND == 3 ? 8355600.0f : 32639.0f;
@@ -949,7 +945,6 @@ __host__ __device__ constexpr int rows_blocks_per_cu(int dpad) { return dpad <= 
 template <int DP, bool PACKED, int TYPE>
 __global__ __launch_bounds__(ROWS_THREADS, 2 * rows_blocks_per_cu(DP)) void kv_rows_kernel(KvView kv, KvQueries q, KvWindow a, int row_tiles)
 {
-    constexpr float HEADROOM = headroom(true, TYPE), LIFT = lift(true, TYPE);
     constexpr int NS = DP / 64, NT = DP / 16, RB = PACKED ? DP / 2 : DP, VW = ((PACKED ? NT / 2 : NT) + 3) / 4;
     constexpr int ND = query_digits(TYPE), NP = TYPE == LPQ_TYPE_F32 ? 2 : 1, TILE_ROWS = ROWS_TILE;
     constexpr float QMAX = ND == 4 ? 2139061888.0f : ND == 3 ? 8355600.0f : 32639.0f;
@@ -1331,7 +1326,7 @@ __global__ __launch_bounds__(NT) void kv_join_kernel(KvView kv, KvQueries q, KvA
     kv_store<4>(a.out, q.type, out_row + c0, kv.dim - c0, v);
     if (a.lse && col == 0) {
         const int64_t lat = ((int64_t)b * q.new_tokens + r / q.group) * ((int64_t)kv.heads * q.group) + h * q.group + r % q.group;
-        a.lse[lat] = l == 0.0f ? NEG : (top * (1.0f / MAXIMUM) - lift(MASKED, q.type) + __log2f(l)) * 0.69314718055994531f + a.lse[lat];
+        a.lse[lat] = l == 0.0f ? NEG : (top * (1.0f / MAXIMUM) - LIFT + __log2f(l)) * 0.69314718055994531f + a.lse[lat];
     }
 }
 
