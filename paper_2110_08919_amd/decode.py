@@ -9,7 +9,8 @@ attention over them (or, with --pages 0, over all).  Beside the tokens per secon
 cache's attention is from attention over the unquantised keys and values, and from it over all pages.
 
 With --codes the projections are 8-bit codes as well (a scale for each row and channel), with --rotate queries and keys are turned by their
-positions' angles on the way into the cache, and --window N has a token see the last N positions and the first 4.
+positions' angles on the way into the cache, and --window N has a token see the last N positions and the first 4.  Pages are not selected then: they are
+ranked over a whole conversation, and the window would mask most of those picked.
 """
 from __future__ import annotations
 
@@ -141,7 +142,8 @@ class Decoder:
         return (self._norm(x) @ self.embedding.t().contiguous()).argmax(-1)
 
     def step(self, pages: int, watch=None):
-        """One token for every conversation; pages > 0: attention over that many selected pages of each head."""
+        """One token for every conversation; pages > 0: attention over that many selected pages of each head (without a window only)."""
+        assert not (pages and self.shape.window), "pages are ranked over all tokens: with a window, select none"
         if watch is None:
             self.kept = None                             # this step's keys and values are not kept
         x = self.embedding[self.tokens]
@@ -189,17 +191,21 @@ class Decoder:
 
 
 def main(argv=None):
-    a = argparse.ArgumentParser(description=__doc__.splitlines()[0])
-    a.add_argument("--prompt", type=int, default=4000, help="tokens of the longest prompt")
-    a.add_argument("--conversations", type=int, default=4)
-    a.add_argument("--steps", type=int, default=32)
-    a.add_argument("--pages", type=int, default=16, help="pages a head looks at per token; 0: all")
-    a.add_argument("--packed", action="store_true", help="4-bit codes, two per byte")
-    a.add_argument("--layers", type=int, default=4)
-    a.add_argument("--codes", action="store_true", help="projections on 8-bit codes")
-    a.add_argument("--rotate", action="store_true", help="queries and keys turned by their positions' angles")
-    a.add_argument("--window", type=int, default=0, help="positions a token sees up to its own, and the first 4; 0: all")
-    a = a.parse_args(argv)
+    parser = argparse.ArgumentParser(description=__doc__.splitlines()[0])
+    parser.add_argument("--prompt", type=int, default=4000, help="tokens of the longest prompt")
+    parser.add_argument("--conversations", type=int, default=4)
+    parser.add_argument("--steps", type=int, default=32)
+    parser.add_argument("--pages", type=int, default=None, help="pages a head looks at per token, 16 by default (none with a window); 0: all")
+    parser.add_argument("--packed", action="store_true", help="4-bit codes, two per byte")
+    parser.add_argument("--layers", type=int, default=4)
+    parser.add_argument("--codes", action="store_true", help="projections on 8-bit codes")
+    parser.add_argument("--rotate", action="store_true", help="queries and keys turned by their positions' angles")
+    parser.add_argument("--window", type=int, default=0, help="positions a token sees up to its own, and the first 4; 0: all")
+    a = parser.parse_args(argv)
+    if a.pages and a.window:
+        parser.error("--pages with --window: pages are ranked over all tokens, not those of the window")
+    if a.pages is None:
+        a.pages = 0 if a.window else 16
     shape = Shape(layers=a.layers, rotate=a.rotate, window=a.window)
     g = torch.Generator().manual_seed(1)
     lengths = [max(1, a.prompt * (b + 1) // a.conversations) for b in range(a.conversations)]
