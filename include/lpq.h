@@ -381,11 +381,11 @@ int lpq_kv_attend_masked(const lpq_kv *kv, const void *q_dev, int64_t ldq_seq, i
  * lpq_row_codes_bytes: what n rows take, the last block's rows behind n included (0: out of range).
  * lpq_encode_rows: x_dev [n][d] of `type`, rows ldx elements apart, to codes and scales_dev float [n].  Features from d to the end of the last
  * block are set to 0; rows of it behind n are not touched.
- * lpq_matmul_i8: out[i][c] = (sum_k a[i][k] b[c][k]) * a_scale[i] * b_scale[c] + bias[c] for m rows and n channels, with exact sums, the
- * products with the scales (in this order) and the sum with the bias each rounded to binary32, the result to `type`; no scale makes a
- * product leave binary32's range on the way.  bias_dev float [n] or null; rows of the output ldo elements apart.  Codes are -127 .. 127 as
- * lpq_encode_rows leaves them: features behind d are read and must be 0 in a or in b; what rows behind m or n hold does not matter.  One set of
- * codes can go through several products.
+ * lpq_matmul_i8: out[i][c] = (sum_k a[i][k] b[c][k]) * a_scale[i] * b_scale[c] + bias[c] for m rows and n channels.  Sums are exact in 32 bits; then
+ * each step is rounded to binary32: the sum itself (beyond 2^24), its products with the scales in this order, the sum with the bias; and the result to
+ * `type`.  No scale makes a product leave binary32's range on the way.  bias_dev float [n] or null; rows of the output ldo elements apart.
+ * Codes are -127 .. 127 as lpq_encode_rows leaves them: features behind d are read and must be 0 in a or in b; what rows behind m or n hold does
+ * not matter.  One set of codes can go through several products.
  * lpq_linear8: both for rows x_dev [m][d] of `type`, which the output has too.  Rows x_dev may overlap (ldx 0: one row n times).  A row's results do not depend on the rows beside it.
  * Codes: 256-byte aligned.  Workspace: 256-byte aligned, for the one call (null where 0 bytes are needed); one that
  * was captured into a graph belongs to the graph.  Output and workspace must not overlap the inputs.

@@ -207,7 +207,7 @@ __global__ __launch_bounds__(MANY_THREADS, 4) void encode_many_kernel(const void
 
 // ------------------------------------------------------------------------ products ----
 // A scale as mantissa and exponent: sum * ma * mb stays in binary32's middle range whatever the scales, and the exponents come on last, with one
-// rounding.  Where nothing leaves that range the result is fl(fl(sum sa) sb), bit for bit.
+// rounding.  Where nothing leaves that range the result is fl(fl(fl(sum) sa) sb), bit for bit: a sum beyond 2^24 is rounded before it is scaled.
 struct Scale {
     float m;
     int e;
