@@ -375,6 +375,12 @@ TYPE_F32, TYPE_F16, TYPE_BF16 = 0, 1, 2
 _TYPE = {torch.float32: TYPE_F32, torch.float16: TYPE_F16, torch.bfloat16: TYPE_BF16}
 
 
+def _no_gradient(why: str, *tensors):
+    """Refuses tensors that ask for a gradient which the call would not give."""
+    if torch.is_grad_enabled():
+        assert not any(t is not None and t.requires_grad for t in tensors), f"{why}: use torch.no_grad() or detach()"
+
+
 def _dev_ints(t: torch.Tensor, n: int):
     assert t.is_cuda and t.dtype is torch.int32 and t.dim() == 1 and t.shape[0] == n and t.is_contiguous(), \
         f"need {n} contiguous int32 values on the device"
@@ -447,7 +453,8 @@ class KVCache:
         """write() of keys that are turned by their positions' angles on the way, and the queries q [n, query heads, features] of
         the same rows turned with them (returned; out=q: in place).  cos, sin: float32 [positions, turned features / 2]; features are
         paired with those half the turned ones further, interleaved: with their neighbours.  positions: int32 [n], where a row
-        stands if not at the position it is written to."""
+        stands if not at the position it is written to.  Rows, queries and angles that require a gradient are refused."""
+        _no_gradient("rotated rows have no gradient here", k, v, q, cos, sin)
         nseq, tab = self._table(table)
         n, keys = self._rows(k, k.dtype)
         same, values = self._rows(v, k.dtype)
@@ -460,7 +467,6 @@ class KVCache:
         queries, q_heads = (None, 0, 0), 0
         into = (None, 0, 0)
         if q is not None:
-            assert not (q.requires_grad and torch.is_grad_enabled()), "rotated queries have no gradient here: use torch.no_grad() or q.detach()"
             if out is None:
                 out = q.new_empty(q.shape)
             q_heads, queries = self._query_rows(q, n, k.dtype)
