@@ -542,7 +542,7 @@ class KVCache:
         tokens, new tokens] (or without the first axis, for all sequences), which new tokens each sees beside all the
         tokens ahead of them: drafted tokens, themselves and their ancestors.
         There is no way back through the codes: queries that require a gradient are refused."""
-        assert not (q.requires_grad and torch.is_grad_enabled()), "attention over codes has no gradient: use torch.no_grad() or q.detach()"
+        _no_gradient("attention over codes has no gradient", q)
         nseq, tab = self._table(table)
         new, q_heads, queries = self._queries(q, nseq)
         if out is None:
@@ -622,7 +622,7 @@ class RowCodes:
 def encode_rows(x: torch.Tensor) -> RowCodes:
     """lpq_encode_rows of x [n, d] (float32, float16 or bfloat16): each row's largest magnitude becomes 127.  There is no way back through
     the codes: rows that require a gradient are refused."""
-    assert not (x.requires_grad and torch.is_grad_enabled()), "codes have no gradient: use torch.no_grad() or x.detach()"
+    _no_gradient("codes have no gradient", x)
     n, d, ld = _typed_matrix(x, "rows")
     assert lib().lpq_row_codes_bytes(n, d) > 0 or n == 0, f"rows of 1 to 131072 values, not {d}"
     with torch.cuda.device(x.device):
@@ -639,7 +639,9 @@ def _bias(bias: torch.Tensor, n: int, device):
 
 
 def matmul_i8(a: RowCodes, b: RowCodes, bias: torch.Tensor = None, dtype=torch.bfloat16, out: torch.Tensor = None) -> torch.Tensor:
-    """[rows of a, rows of b] of `dtype`: the products of all rows of a with all rows of b (and bias, one for each row of b)."""
+    """[rows of a, rows of b] of `dtype`: the products of all rows of a with all rows of b (and bias, one for each row of b).  A bias that requires a
+    gradient is refused."""
+    _no_gradient("products of codes have no gradient", bias)
     assert a.d == b.d, f"rows of {a.d} and of {b.d} codes"
     assert a.blocks.device == b.blocks.device, "both on one device"
     if out is None:
@@ -660,7 +662,7 @@ def _scratch(need: int, device):
 
 class Linear8:
     """lpq_linear8: y = x w^T + bias with w [channels, d] kept as 8-bit codes (a scale for each channel) and the rows of x made codes on
-    the way (a scale for each row).  For serving: inputs that require a gradient are refused."""
+    the way (a scale for each row).  For serving: weight and bias are taken as they are now, inputs that require a gradient are refused."""
 
     def __init__(self, weight: torch.Tensor, bias: torch.Tensor = None):
         self.weight = encode_rows(weight.detach())
@@ -673,7 +675,7 @@ class Linear8:
 
     def __call__(self, x: torch.Tensor, out: torch.Tensor = None, workspace: torch.Tensor = None) -> torch.Tensor:
         """x [..., d] of float32, float16 or bfloat16 -> [..., channels] of its type."""
-        assert not (x.requires_grad and torch.is_grad_enabled()), "codes have no gradient: use torch.no_grad() or x.detach()"
+        _no_gradient("codes have no gradient", x)
         assert x.dim() >= 1 and x.shape[-1] == self.d and x.device == self.device, f"need [..., {self.d}] on {self.device}"
         rows = x if x.dim() == 2 else x.reshape(-1, self.d)
         m, _, ldx = _typed_matrix(rows, "rows")

@@ -1,5 +1,6 @@
 """Calls of the decoder layer on codes that would drop a gradient refuse the input that asks for one, before they look at its memory: no device needed."""
 import os
+from types import SimpleNamespace
 
 import pytest
 import torch
@@ -24,3 +25,12 @@ def test_rotated_rows_and_angles(lpq, which):
         cache.write_rotated(first=ints, table=ints[None], **given)
     with torch.no_grad(), pytest.raises(AssertionError, match="device"):      # taken, and then refused for where it lies
         cache.write_rotated(first=ints, table=ints[None], **given)
+
+
+def test_a_bias_of_products(lpq):
+    codes = SimpleNamespace(d=64, n=3, blocks=torch.zeros(1))
+    bias = torch.zeros(3, requires_grad=True)
+    with pytest.raises(AssertionError, match="gradient"):
+        lpq.matmul_i8(codes, codes, bias)
+    with torch.no_grad(), pytest.raises(AssertionError, match="device"):
+        lpq.matmul_i8(codes, codes, bias)
