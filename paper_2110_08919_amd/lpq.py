@@ -11,6 +11,7 @@ import ctypes as C
 import os
 
 import torch
+from torch.autograd import forward_ad
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.environ.get("LPQ_LIBRARY") or os.path.join(_HERE, "liblpq.so")   # LPQ_LIBRARY: another build of the same ABI
@@ -376,9 +377,13 @@ _TYPE = {torch.float32: TYPE_F32, torch.float16: TYPE_F16, torch.bfloat16: TYPE_
 
 
 def _no_gradient(why: str, *tensors):
-    """Refuses tensors that ask for a gradient which the call would not give."""
+    """Refuses tensors that ask for a gradient, or carry a tangent, which the call would not give or pass on."""
     if torch.is_grad_enabled():
-        assert not any(t is not None and t.requires_grad for t in tensors), f"{why}: use torch.no_grad() or detach()"
+        for t in tensors:
+            assert t is None or not t.requires_grad, f"{why}: use torch.no_grad() or detach()"
+    if forward_ad._current_level >= 0:           # within dual_level(), with or without gradients enabled
+        for t in tensors:
+            assert t is None or forward_ad.unpack_dual(t).tangent is None, f"{why}, nor a tangent: use unpack_dual(t).primal"
 
 
 def _dev_ints(t: torch.Tensor, n: int):

@@ -4,6 +4,7 @@ from types import SimpleNamespace
 
 import pytest
 import torch
+from torch.autograd import forward_ad
 
 
 @pytest.fixture(scope="module")
@@ -34,3 +35,25 @@ def test_a_bias_of_products(lpq):
         lpq.matmul_i8(codes, codes, bias)
     with torch.no_grad(), pytest.raises(AssertionError, match="device"):
         lpq.matmul_i8(codes, codes, bias)
+
+
+def test_tangents(lpq):
+    """Forward-mode derivatives are refused too, also where gradients are off: they would be dropped."""
+    ints = torch.zeros(1, dtype=torch.int32)
+    cache, layer = object.__new__(lpq.KVCache), object.__new__(lpq.Linear8)
+    with forward_ad.dual_level():
+        dual = forward_ad.make_dual(torch.zeros(3, 4), torch.ones(3, 4))
+        rows, bias = dual[:1, None], dual[:, 0]
+        codes = SimpleNamespace(d=64, n=3, blocks=torch.zeros(1))
+        plain = torch.zeros(1, 1, 4)
+        calls = [lambda: lpq.encode_rows(dual), lambda: layer(dual), lambda: lpq.matmul_i8(codes, codes, bias),
+                 lambda: cache.attend(dual[None, :1, None], ints, ints[None], window=3),
+                 lambda: cache.write_rotated(rows, plain, ints, ints[None], plain[0, :, :2], plain[0, :, :2]),
+                 lambda: cache.write_rotated(plain, plain, ints, ints[None], plain[0, :, :2], plain[0, :, :2], q=rows)]
+        for call in calls:
+            with pytest.raises(AssertionError, match="tangent"):
+                call()
+            with torch.no_grad(), pytest.raises(AssertionError, match="tangent"):
+                call()
+        with pytest.raises(AssertionError, match="device"):                    # without one: refused for where it lies
+            lpq.encode_rows(torch.zeros(3, 4))
