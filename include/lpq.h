@@ -310,6 +310,8 @@ int lpq_kv_read(const lpq_kv *kv, void *k_dev, int64_t ldk_token, int64_t ldk_he
 /* Queries of the calls below: q_dev [nseq][new_tokens][q_heads][D] of `type`, strides in elements; q_heads a multiple
  * of heads, query heads h G .. h G + G - 1 share key-value head h (G = q_heads / heads).  lengths_dev int32 [nseq]:
  * tokens of each sequence, the new ones included: new token i sees positions <= length - new_tokens + i.
+ * A call takes new_tokens * q_heads <= 65536, nseq * new_tokens * q_heads and nseq * heads <= 2^22, and table_pages * page < 2^31 (else
+ * LPQ_ERANGE); longer prompts go through attention in parts, each with the length up to its end.
  *
  * Which pages can hold large inner products.  Over the R = new_tokens * G rows of a key-value head, in binary32:
  * q' = q s, A = max |q'|, z = rint(q' * (127 / A)) (what is not finite counts as 0; A <= 1e-30: all 0);

@@ -546,6 +546,8 @@ class KVCache:
         window: a token sees the last `window` positions up to its own, and the first `sinks`.  tree: bool [sequences, new
         tokens, new tokens] (or without the first axis, for all sequences), which new tokens each sees beside all the
         tokens ahead of them: drafted tokens, themselves and their ancestors.
+        A call takes up to 65 536 (new token, query head) pairs of a sequence, 2^22 in all: longer prompts go through it in parts,
+        each with the lengths up to its end.
         There is no way back through the codes: queries that require a gradient are refused."""
         _no_gradient("attention over codes has no gradient", q)
         nseq, tab = self._table(table)
