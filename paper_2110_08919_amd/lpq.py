@@ -129,6 +129,10 @@ def _stream_of(t: torch.Tensor) -> int:
     return _raw_stream(t.get_device()) if _raw_stream is not None else torch.cuda.current_stream(t.device).cuda_stream
 
 
+# (torch.cuda.current_device() looks first whether there is one)
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
+
 def _ptr(t):
     return None if t is None else t.data_ptr()
 
@@ -386,9 +390,9 @@ def _no_gradient(why: str, *tensors):
             assert t is None or forward_ad.unpack_dual(t).tangent is None, f"{why}, nor a tangent: use unpack_dual(t).primal"
 
 
-def _dev_ints(t: torch.Tensor, n: int):
-    assert t.is_cuda and t.dtype is torch.int32 and t.dim() == 1 and t.shape[0] == n and t.is_contiguous(), \
-        f"need {n} contiguous int32 values on the device"
+def _dev_ints(t: torch.Tensor, n: int, device: int):
+    assert t.get_device() == device and t.dtype is torch.int32 and t.dim() == 1 and t.shape[0] == n and t.is_contiguous(), \
+        f"need {n} contiguous int32 values on the cache's device"
     return t.data_ptr()
 
 
@@ -398,18 +402,24 @@ class KVCache:
     The quantizers hold the constants of the heads' features one after the other (d = heads * features of a head).
     Storage is three tensors of this object: `k` and `v` [pages, heads, page, row bytes] and the pages' bounds.
     Which pages a sequence has is the caller's to say: `table` int32 [sequences, columns], page numbers in order of
-    position, -1 (or anything outside the pool) where there is none."""
+    position, -1 (or anything outside the pool) where there is none.  Everything that a call is given lies on the cache's device, which is the current one;
+    the quantizers were made there."""
 
     def __init__(self, keys: Quantizer, values: Quantizer, heads: int, page: int, pages: int, packed: bool = False,
                  device="cuda"):
         assert heads >= 1 and keys.d % heads == 0, "d of the quantizers must be a multiple of heads"
         assert torch.device(device).type == "cuda", "the cache lies in device memory"
+        with torch.cuda.device(device):
+            self._create(keys, values, heads, page, pages, packed, device)
+
+    def _create(self, keys, values, heads, page, pages, packed, device):
         row = C.c_int()
         self.heads, self.dim, self.page, self.pages, self.packed = heads, keys.d // heads, page, pages, packed
         _check(lib().lpq_kv_storage_bytes(heads, self.dim, page, pages, 1 if packed else 0, None, None, C.byref(row)))
         shape = (pages, heads, page, row.value // 2 if packed else row.value)
         kind = torch.uint8 if packed else torch.int8
         self.k, self.v = (torch.zeros(shape, dtype=kind, device=device) for _ in range(2))
+        self._at = self.k.get_device()
         self._bounds = torch.zeros((pages, heads, 2, row.value), dtype=torch.int8, device=device)
         torch.cuda.current_stream().synchronize()           # calls on any stream find it cleared
         h = C.c_void_p()
@@ -428,14 +438,15 @@ class KVCache:
         return self._bounds[..., :self.dim]
 
     def _table(self, table: torch.Tensor):
-        assert table.is_cuda and table.dtype is torch.int32 and table.dim() == 2, "need a device table int32 [sequences, columns]"
+        assert _current_device() == self._at, "calls go to the current device: make the cache's the current one"
+        assert table.get_device() == self._at and table.dtype is torch.int32 and table.dim() == 2, "need a device table int32 [sequences, columns]"
         nseq, columns = table.shape
         ld, inner = table.stride()
         assert inner == 1 or columns == 1, "need the columns of the table side by side"
         return nseq, (table.data_ptr(), ld if nseq > 1 else max(ld, columns), columns)
 
     def _rows(self, t: torch.Tensor, dtype):
-        assert t.is_cuda and t.dtype is dtype and t.dim() == 3, f"need device rows of {dtype}"
+        assert t.get_device() == self._at and t.dtype is dtype and t.dim() == 3, f"need device rows of {dtype}"
         n, heads, dim = t.shape
         by_row, by_head, inner = t.stride()
         assert heads == self.heads and dim == self.dim and (inner == 1 or dim == 1), \
@@ -449,8 +460,8 @@ class KVCache:
         n, keys = self._rows(k, k.dtype)
         same, values = self._rows(v, k.dtype)
         assert n == same, "as many values as keys"
-        _check(_lib.lpq_kv_write(self._h, *keys, *values, _TYPE[k.dtype], n, nseq, _dev_ints(first, nseq),
-                                 None if starts is None else _dev_ints(starts, nseq + 1), *tab, _stream_of(table)))
+        _check(_lib.lpq_kv_write(self._h, *keys, *values, _TYPE[k.dtype], n, nseq, _dev_ints(first, nseq, self._at),
+                                 None if starts is None else _dev_ints(starts, nseq + 1, self._at), *tab, _stream_of(table)))
 
     def write_rotated(self, k: torch.Tensor, v: torch.Tensor, first: torch.Tensor, table: torch.Tensor, cos: torch.Tensor, sin: torch.Tensor,
                       starts: torch.Tensor = None, positions: torch.Tensor = None, q: torch.Tensor = None, out: torch.Tensor = None,
@@ -464,11 +475,12 @@ class KVCache:
         n, keys = self._rows(k, k.dtype)
         same, values = self._rows(v, k.dtype)
         assert n == same, "as many values as keys"
-        assert cos.is_cuda and cos.dtype is torch.float32 and cos.dim() == 2 and cos.stride(1) == 1, "need device angles float32 [positions, pairs]"
+        assert cos.get_device() == self._at and cos.dtype is torch.float32 and cos.dim() == 2 and cos.stride(1) == 1, \
+            "need device angles float32 [positions, pairs]"
         count, pairs = cos.shape
         apart = cos.stride(0) if count > 1 else max(cos.stride(0), pairs)
-        assert sin.is_cuda and sin.dtype is torch.float32 and sin.shape == cos.shape and sin.stride(1) == 1 and (count == 1 or sin.stride(0) == apart), \
-            "need sines laid out as the cosines"
+        assert sin.get_device() == self._at and sin.dtype is torch.float32 and sin.shape == cos.shape and sin.stride(1) == 1 \
+            and (count == 1 or sin.stride(0) == apart), "need sines laid out as the cosines"
         queries, q_heads = (None, 0, 0), 0
         into = (None, 0, 0)
         if q is not None:
@@ -477,14 +489,14 @@ class KVCache:
             q_heads, queries = self._query_rows(q, n, k.dtype)
             more, into = self._query_rows(out, n, k.dtype)
             assert more == q_heads, "as many heads in the output"
-        _check(_lib.lpq_kv_write_rotated(self._h, *keys, *values, _TYPE[k.dtype], n, nseq, _dev_ints(first, nseq),
-                                         None if starts is None else _dev_ints(starts, nseq + 1), *tab, cos.data_ptr(), sin.data_ptr(), apart, count,
-                                         2 * pairs, interleaved, None if positions is None else _dev_ints(positions, n), *queries, q_heads, *into,
+        _check(_lib.lpq_kv_write_rotated(self._h, *keys, *values, _TYPE[k.dtype], n, nseq, _dev_ints(first, nseq, self._at),
+                                         None if starts is None else _dev_ints(starts, nseq + 1, self._at), *tab, cos.data_ptr(), sin.data_ptr(), apart, count,
+                                         2 * pairs, interleaved, None if positions is None else _dev_ints(positions, n, self._at), *queries, q_heads, *into,
                                          _stream_of(table)))
         return out
 
     def _query_rows(self, t: torch.Tensor, n: int, dtype):
-        assert t.is_cuda and t.dtype is dtype and t.dim() == 3, f"need device queries of {dtype}"
+        assert t.get_device() == self._at and t.dtype is dtype and t.dim() == 3, f"need device queries of {dtype}"
         rows, heads, dim = t.shape
         by_row, by_head, inner = t.stride()
         assert rows == n and dim == self.dim and (inner == 1 or dim == 1), f"need queries [{n}, query heads, {self.dim}], features side by side"
@@ -503,12 +515,12 @@ class KVCache:
         a, keys = self._rows(k, k.dtype)
         b, values = self._rows(v, k.dtype)
         assert a == n and b == n, f"need {n} rows"
-        _check(_lib.lpq_kv_read(self._h, *keys, *values, _TYPE[k.dtype], n, nseq, _dev_ints(first, nseq),
-                                None if starts is None else _dev_ints(starts, nseq + 1), *tab, _stream_of(table)))
+        _check(_lib.lpq_kv_read(self._h, *keys, *values, _TYPE[k.dtype], n, nseq, _dev_ints(first, nseq, self._at),
+                                None if starts is None else _dev_ints(starts, nseq + 1, self._at), *tab, _stream_of(table)))
         return k, v
 
     def _queries(self, q: torch.Tensor, nseq: int):
-        assert q.is_cuda and q.dtype in _TYPE and q.dim() == 4, "need device queries of float32, float16 or bfloat16"
+        assert q.get_device() == self._at and q.dtype in _TYPE and q.dim() == 4, "need device queries of float32, float16 or bfloat16"
         n, new, heads, dim = q.shape
         by_seq, by_token, by_head, inner = q.stride()
         assert n == nseq and dim == self.dim and (inner == 1 or dim == 1), \
@@ -519,7 +531,7 @@ class KVCache:
     def _workspace(given: torch.Tensor, need: int, device):
         """The workspace to pass: memory of this call's own unless some was given (calls on several streams do not share any)."""
         if given is not None:
-            assert given.is_cuda and given.is_contiguous(), "need a workspace that is one run of device memory"
+            assert given.is_cuda and given.is_contiguous() and given.device == device, "need a workspace that is one run of the device's memory"
         elif need:
             given = torch.empty(need, dtype=torch.uint8, device=device)
         return (given, None, 0) if given is None else (given, given.data_ptr(), given.numel() * given.element_size())
@@ -532,9 +544,9 @@ class KVCache:
         new, q_heads, queries = self._queries(q, nseq)
         if out is None:
             out = torch.empty((nseq, self.heads, n_select), dtype=torch.int32, device=q.device)
-        assert out.is_cuda and out.dtype is torch.int32 and out.is_contiguous() and out.shape == (nseq, self.heads, n_select)
+        assert out.get_device() == self._at and out.dtype is torch.int32 and out.is_contiguous() and out.shape == (nseq, self.heads, n_select)
         workspace, ws, size = self._workspace(workspace, _lib.lpq_kv_select_workspace_bytes(self._h, nseq, tab[2]), q.device)
-        _check(_lib.lpq_kv_select(self._h, *queries, _TYPE[q.dtype], nseq, new, q_heads, _dev_ints(lengths, nseq), *tab,
+        _check(_lib.lpq_kv_select(self._h, *queries, _TYPE[q.dtype], nseq, new, q_heads, _dev_ints(lengths, nseq, self._at), *tab,
                                   n_select, keep_first, keep_last, out.data_ptr(), ws, size, _stream_of(q)))
         return out
 
@@ -562,7 +574,7 @@ class KVCache:
         n_select = 0
         if pages is not None:
             n_select = pages.shape[-1]
-            assert pages.is_cuda and pages.dtype is torch.int32 and pages.is_contiguous() and pages.shape == (nseq, self.heads, n_select) \
+            assert pages.get_device() == self._at and pages.dtype is torch.int32 and pages.is_contiguous() and pages.shape == (nseq, self.heads, n_select) \
                 and n_select > 0, "need contiguous int32 pages [sequences, heads, pages], at least one of them"
         if window is not None or sinks or tree is not None:
             return self._attend_masked(q, queries, nseq, new, q_heads, lengths, tab, pages, n_select, scale, out, outputs, lse, workspace,
@@ -570,7 +582,7 @@ class KVCache:
         workspace, ws, size = self._workspace(
             workspace, _lib.lpq_kv_attend_workspace_bytes(self._h, nseq, new, q_heads, tab[2], n_select), q.device)
         _check(_lib.lpq_kv_attend(self._h, *queries, _TYPE[q.dtype], nseq, new, q_heads,
-                                  self.dim ** -0.5 if scale is None else scale, _dev_ints(lengths, nseq), *tab, _ptr(pages), n_select,
+                                  self.dim ** -0.5 if scale is None else scale, _dev_ints(lengths, nseq, self._at), *tab, _ptr(pages), n_select,
                                   *outputs, _ptr(lse), ws, size, _stream_of(q)))
         return (out, lse) if return_lse else out
 
@@ -580,14 +592,14 @@ class KVCache:
         assert 0 <= sinks < 2 ** 31, "sinks are counted from 0"
         mask, by_seq, by_token = None, 0, 0
         if tree is not None:
-            assert tree.is_cuda and tree.dtype is torch.bool and tree.shape in ((nseq, new, new), (new, new)) and (tree.stride(-1) == 1 or new == 1), \
-                f"need a device tree bool [{nseq}, {new}, {new}], the last axis contiguous"
+            assert tree.get_device() == self._at and tree.dtype is torch.bool and tree.shape in ((nseq, new, new), (new, new)) \
+                and (tree.stride(-1) == 1 or new == 1), f"need a device tree bool [{nseq}, {new}, {new}], the last axis contiguous"
             mask, by_seq, by_token = tree.data_ptr(), tree.stride(0) if tree.dim() == 3 else 0, tree.stride(-2)
         width = 0 if window is None else min(window, 2 ** 40)
         workspace, ws, size = self._workspace(
             workspace, _lib.lpq_kv_attend_masked_workspace_bytes(self._h, nseq, new, q_heads, tab[2], n_select, width, sinks, mask is not None), q.device)
         _check(_lib.lpq_kv_attend_masked(self._h, *queries, _TYPE[q.dtype], nseq, new, q_heads, self.dim ** -0.5 if scale is None else scale,
-                                         _dev_ints(lengths, nseq), *tab, _ptr(pages), n_select, width, sinks, mask, by_seq, by_token, *outputs,
+                                         _dev_ints(lengths, nseq, self._at), *tab, _ptr(pages), n_select, width, sinks, mask, by_seq, by_token, *outputs,
                                          _ptr(lse), ws, size, _stream_of(q)))
         return out if lse is None else (out, lse)
 

@@ -17,8 +17,10 @@ def lpq():
 
 
 @pytest.mark.parametrize("which", ["k", "v", "q", "cos", "sin"])
-def test_rotated_rows_and_angles(lpq, which):
+def test_rotated_rows_and_angles(lpq, which, monkeypatch):
+    monkeypatch.setattr(lpq, "_current_device", lambda: 0)
     cache = object.__new__(lpq.KVCache)
+    cache._at = 0
     given = {name: torch.zeros(1, 1, 4) for name in ("k", "v", "q")} | {name: torch.ones(1, 2) for name in ("cos", "sin")}
     given[which].requires_grad_()
     ints = torch.zeros(1, dtype=torch.int32)
