@@ -287,11 +287,13 @@ int lpq_kv_write(const lpq_kv *kv, const void *k_dev, int64_t ldk_token, int64_t
  * and the keys encoded from that, without a rounding to their type between.  A row's position is the one that it is written to, or
  * positions_dev[row] (int32 [n], null: none given), as for drafted tokens that share a depth in a tree.
  * q_dev null, or n rows [n][q_heads][D] numbered as the keys, of the same type: out_dev receives them turned, rounded to
- * the type; q_heads a multiple of heads.  out_dev may be q_dev with its strides (turned in place); else the two must not overlap.
+ * the type; q_heads a multiple of heads.  out_dev may be q_dev with its strides (turned in place); else the two must not overlap, and out_dev
+ * never overlaps the keys, the values or the angles.
  * Rows at positions below 0 and rows of no sequence are not turned (queries come out as they are; keys as in lpq_kv_write); at positions beyond the table's
  * the turned features are NaN (which a key's code holds as 0).
  * Errors as lpq_kv_write; LPQ_EINVAL: rotated odd, below 2 or above D, angles < 1, ld_angles < rotated / 2, queries without an
- * output, q_heads not a multiple of heads, strides of the output that overlap; LPQ_ERANGE: angles >= 2^31, q_heads > 65536. */
+ * output, q_heads not a multiple of heads, strides of the output that overlap, an output that begins where the keys or the values do, or where the
+ * queries do with other strides; LPQ_ERANGE: angles >= 2^31, q_heads > 65536. */
 int lpq_kv_write_rotated(const lpq_kv *kv, const void *k_dev, int64_t ldk_token, int64_t ldk_head, const void *v_dev,
                          int64_t ldv_token, int64_t ldv_head, int type, int64_t n, int64_t nseq,
                          const int32_t *first_dev, const int32_t *starts_dev, const int32_t *table_dev, int64_t ld_table,

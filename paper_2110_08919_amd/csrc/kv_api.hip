@@ -216,6 +216,10 @@ extern "C" int lpq_kv_write_rotated(const lpq_kv *kv, const void *k_dev, int64_t
         }
         if (!disjoint(dim, {{{strides[1][0], n}, {strides[1][1], q_heads}, {0, 1}}}))
             return kv_fail(LPQ_EINVAL, "strides %lld, %lld of the output overlap", (long long)ldo_token, (long long)ldo_head);
+        // keys and values are read beside queries that are written
+        if (out_dev == k_dev || out_dev == v_dev) return kv_fail(LPQ_EINVAL, "turned queries in the place of keys or values");
+        if (out_dev == q_dev && (strides[0][0] != strides[1][0] || strides[0][1] != strides[1][1]))
+            return kv_fail(LPQ_EINVAL, "queries turned in place with other strides");
         a.q = {const_cast<void *>(q_dev), strides[0][0], strides[0][1], type};
         a.out = {out_dev, strides[1][0], strides[1][1], type};
         a.q_heads = q_heads;

@@ -467,7 +467,7 @@ class KVCache:
                       starts: torch.Tensor = None, positions: torch.Tensor = None, q: torch.Tensor = None, out: torch.Tensor = None,
                       interleaved: bool = False):
         """write() of keys that are turned by their positions' angles on the way, and the queries q [n, query heads, features] of
-        the same rows turned with them (returned; out=q: in place).  cos, sin: float32 [positions, turned features / 2]; features are
+        the same rows turned with them (returned; out=q: in place; out must not overlap k, v or the angles).  cos, sin: float32 [positions, turned features / 2]; features are
         paired with those half the turned ones further, interleaved: with their neighbours.  positions: int32 [n], where a row
         stands if not at the position it is written to.  Rows, queries and angles that require a gradient are refused."""
         _no_gradient("rotated rows have no gradient here", k, v, q, cos, sin)
