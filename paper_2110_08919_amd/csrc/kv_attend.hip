@@ -932,11 +932,13 @@ __global__ __launch_bounds__(THREADS, blocks_per_cu(DP, PACKED, RT, TYPE, std::i
 // codes are fetched, unpacked and made fp16 once for 128 rows; two buffers take turns, with one barrier to a tile, and the next tile's codes are under
 // way in registers meanwhile.  No row is another wave's concern: nothing is joined, and what a workgroup costs before its first tile and
 // behind its last, 9 us there, is shared by eight times the rows.
-// us, kv_attend_kernel and this one: 4 sequences of up to 9000 tokens, windows of 600 for 6000 rows a head, 4 heads of 96 on 4-bit codes, float16 113, 67; 8 of
-// 128 on 8-bit codes, bfloat16 265, 146, windows of 4000 1114, 532; 2800 float32 rows, windows of 1000, heads of 128 224, 149, of 256 575, 277; 128
-// sequences, 48 rows, windows of 1000 141, 102.  Where its workgroups do not fill the chip it loses: 32 sequences of 96 rows, windows of 2000, 87, 89,
-// 720 float32 rows on one head of 192 25, 41.  Bound by the vector pipe: of 64 tokens a row tile has 16 scores a lane, each joined from its digits,
-// compared, scaled, raised and rounded.
+// us, kv_attend_kernel and this one: 4 sequences of up to 9000 tokens, windows of 600 for 6000 rows a head, 4 heads of 96 on 4-bit codes, float16 113, 70; 8 of
+// 128 on 8-bit codes, bfloat16 265, 144, windows of 4000 1114, 515; 2800 float32 rows, windows of 1000, heads of 128 224, 150, of 256 575, 271; 128
+// sequences, 48 rows, windows of 1000 141, 103.  Where its workgroups do not fill the chip it loses: 32 sequences of 96 rows, windows of 2000, 87, 89,
+// 720 float32 rows on one head of 192 25, 41.  Bound by the chain of a wave, which goes from scores over maximum, exponentials and roundings to sums with
+// nothing of the next tokens beside it, and by how the last workgroups fill the chip: the first call's 752 stand on 512 places, so that 2.8 of 4 waves
+// are on a SIMD on average, the vector pipe is busy 61 % of the time (16 scores a lane of 64 tokens, each joined from its digits, compared, scaled,
+// raised and rounded) and the matrix pipe 23 %.
 constexpr int ROWS_TOKENS = 64, ROWS_WAVES = 8, ROWS_THREADS = 64 * ROWS_WAVES, ROWS_TILE = 16 * ROWS_WAVES;
 __host__ __device__ constexpr int rows_digits(int type, int dpad) { return query_digits(type) * 8 * (dpad + 16); }      // bytes, of 8 rows
 __host__ __device__ constexpr int rows_stage(int dpad) { return ROWS_TOKENS * dpad * 3; }

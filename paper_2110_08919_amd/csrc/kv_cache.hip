@@ -14,7 +14,9 @@
 // Turned on the way, with four query heads to a key head: one row of 8 heads of 128, bfloat16: 6.6 us; 320 float32 rows of 2 x 80, 64 of them turned, and
 // 12 query heads: 12.4; 26 244 float16 rows of 6 x 100 to packed codes, 52 turned in pairs of neighbours, and 18 query heads: 113 where a copy of
 // as many bytes takes 57 (vector instructions for 58: Eq. 1, the turns, pieces of odd units; as they are, loads and instructions of a
-// workgroup follow each other); 23 140 bfloat16 rows of 8 x 128 and 32 query heads: 157 where a copy takes 108.
+// workgroup follow each other); 23 140 bfloat16 rows of 8 x 128 and 32 query heads: 158 where a copy takes 108 (1.5 waves to a SIMD, as the
+// registers allow, 60 % of their time spent waiting, the vector pipe busy 31 %: keys have angles and the other features of their pairs loaded for 8
+// features at a time, and share the queries' registers).
 #include <algorithm>
 #include <type_traits>
 

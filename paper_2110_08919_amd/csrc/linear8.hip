@@ -5,9 +5,10 @@
 //
 // Measured with the rows' codes, bfloat16 unless said otherwise, weights not in a cache: 1 row, 4096 x 4096 5.8 us (4.3 where the weights are in the
 // memory-side cache), 32 768 x 16 384 91 us, 5.9 TB/s; 48 float16 rows, 11 111 x 4100 19.1; 64 rows, 16 384 x 8192 36; 128 rows, 32 768 x 16 384
-// 124; 1024 rows, 4096 x 4096 34; 8192 rows, 8192 x 8192 513, of these 43 for the codes (4.7 TB/s, as a copy of memory) and 470 for the product,
-// 2.34 POP/s, where a register-resident loop of the instruction sustains 3.46 on random bytes.  What is left there: a stage takes 0.81 us, 0.68
-// without its copies (0.62 at that loop's rate), and 10 us go before a tile's first stage and behind its last.
+// 116 to 124; 129, 256, 512, 1024, 2048 rows, 4096 x 4096 18.5, 21.3, 24.2, 30 to 34, 48; 8192 rows, 8192 x 8192 499 to 513, of these 45 for the codes
+// (4.5 TB/s, as a copy of memory) and 452 for the product, 2.43 POP/s, where a register-resident loop of the instruction sustains 3.46 on random
+// bytes.  What is left there: a stage takes 0.81 us, 0.68 without its copies (0.62 at that loop's rate), and 10 us go before a tile's first stage
+// and behind its last.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -407,8 +408,10 @@ __global__ __launch_bounds__(STREAM_THREADS, stream_waves_per_simd(MT, CT)) void
 // Tiles.  The workgroup's four waves stand 2 x 2; a wave has TC x TT tiles of 32 channels x 32 tokens (v_mfma_i32_32x32x32_i8, channels as rows of
 // the result, so that a lane holds 4 neighbouring channels of a token).  Stages of 64 features of all the workgroup's channels and tokens come
 // into a ring in LDS by asynchronous copies of 16 bytes a lane, a block at a time, three stages ahead; the operands of the next half of a
-// stage are read from there while the matrix instructions of this half run.  Bound by the matrix pipe and the power it draws (1.9 GHz): 32 instructions of
-// 32 cycles to a stage and wave, 64 KB read from LDS and 32 KB copied into it a workgroup, of 128 bytes a cycle.
+// stage are read from there while the matrix instructions of this half run.  Bound by issue and by LDS: its 128 KB (256 x 256) leave one wave to a SIMD, so
+// that nothing runs where a wave waits for the barrier, for operands or for its copies to be taken in.  8192 x 8192 x 8192: the matrix pipe is busy 59 %
+// of the time, at 2.0 GHz: 32 instructions of 32 cycles of the 1600 that a stage takes, beside 64 KB read from LDS and 32 KB copied into it a
+// workgroup, of 128 bytes a cycle.
 constexpr int TILE_THREADS = 256, TILE_K = 64, TILE_STAGES = 4;
 
 struct TileWork {
@@ -651,11 +654,12 @@ hipError_t launch_encode_rows(const void *x, int64_t ldx, int type, int64_t n, i
 }
 
 // What takes the shortest time by these estimates, in microseconds beside what all have in common (measured over 33 to 8192 rows, 1024 to 32 768
-// channels and 1024 to 16 384 features, within a fifth; k: workgroups to a CU).  The weights come at 4.5 TB/s at best.  Few rows: what a workgroup
-// reads at 60 GB/s; of tiles of 16 channels as many as leave one generation of workgroups (48 rows, 11 111 x 4100: 1, 2, 3, 4 tiles 23.7, 22.8,
-// 19.1, 20.4 us; 64 rows, 16 384 x 8192: 48, 42.8, 46.6, 36.1).  Tiles: a stage takes 0.21 us (64 x 64), 0.33 us (128 x 128) and 0.83 us (256 x
-// 256) alone on its CU, and more together with others.  Parts cost a launch and 0.42 us for a MB of sums (128 rows, 1024 x 16 384: tiles of 64 in 1, 2, 4, 8
-// parts 59.6, 37.5, 25.4, 21.1 us, few rows' way 40.5).
+// channels and 1024 to 16 384 features, within a fifth; k: workgroups to a CU).  None is below the weights at 4.5 TB/s, about the best that more than 32
+// rows had them at (128 rows, 32 768 x 16 384: 4.3 to 4.6; up to 32 rows, which need no estimate, 5.9); of estimates that stand there the first looked at
+// stays: few rows' way, then small tiles, then few parts.  Few rows: what a workgroup reads at 60 GB/s; of tiles of 16 channels as many as leave one
+// generation of workgroups (48 rows, 11 111 x 4100: 1, 2, 3, 4 tiles 23.7, 22.8, 19.1, 20.4 us; 64 rows, 16 384 x 8192: 48, 42.8, 46.6, 36.1).  Tiles:
+// a stage takes 0.21 us (64 x 64), 0.33 us (128 x 128) and 0.83 us (256 x 256) alone on its CU, and more together with others.  Parts cost a launch
+// and 0.42 us for a MB of sums (128 rows, 1024 x 16 384: tiles of 64 in 1, 2, 4, 8 parts 59.6, 37.5, 25.4, 21.1 us, few rows' way 40.5).
 Linear8Plan linear8_plan(int64_t m, int64_t n, int d)
 {
     const double stages = (double)ceil_div(d, TILE_K);
